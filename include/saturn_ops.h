@@ -121,12 +121,83 @@ sat_status sat_op_attention_bwd(const void* q, const void* k, const void* v, int
                                 int64_t lddv, int32_t B, int32_t H, int32_t S, int32_t dh,
                                 int32_t causal, float scale, void* stream);
 
+/* Attention inside packed sequences, forward and backward: rows of several
+ * sequences follow each other in one buffer without padding between them.
+ *   rows     cu: device int32 [n_seq + 1], not decreasing; rows cu[s] ..
+ *            cu[s + 1] - 1 of every row array are sequence s (a length may be
+ *            0).  T rows per array, 0 <= T <= 2^29.  Rows outside all sequences are
+ *            not read and keep what they hold in every output.  cu is read on the
+ *            device only, so a captured call takes the lengths of the
+ *            replay; values outside [0, T] are taken as the nearer of the two.
+ *   heads    H query heads, Hkv K / V heads, Hkv a divisor of H; query head h
+ *            reads K / V head h / (H / Hkv).  dh: a multiple of 8 up to 256
+ *            (64, 80, 128 and 256 have kernels of their width, others run in the
+ *            next wider one).  Element (row t, head h, dim j) at ptr[t * ld + h * dh + j].
+ *   mask     query i and key j of one sequence: j <= i when causal, and |i - j| <
+ *            window when window > 0 (0: none).  Every query sees itself.
+ *   values   o = softmax(scale q k^T) v as bf16, lse [H, T] fp32 the natural-log
+ *            log-sum-exp; gradients of q, k, v as bf16, dk and dv summed in fp32 over
+ *            the query heads that share them.  A row of a sequence that holds NaN
+ *            or infinities may spoil other rows of that sequence, none of another.
+ *            The same inputs give the same bits on every call.
+ * q, k, v, o and dout are 16-byte aligned with leading dimensions that are
+ * multiples of 8 and below 2^22, dq, dk, dv 8-byte aligned with multiples of 4;
+ * scale > 0.  Outputs overlap no input and no other output.  The backward reads the
+ * forward's o and lse; ws is fp32 scratch of ws_elems elements, at least
+ * what sat_op_attention_packed_bwd_ws says for the same sizes (it may grow
+ * with H, Hkv, dh, T and n_seq only); calls that may overlap need a ws each.  The forward does
+ * not read dout and what stands behind it.
+ * Errors: SAT_EINVAL for null pointers (T > 0), sizes, alignment, or a ws that is too small. */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t ldq, ldk, ldv;
+  void* o;
+  int64_t ldo;
+  float* lse;
+  const int32_t* cu;
+  int32_t n_seq, T, H, Hkv, dh, causal, window;
+  float scale;
+  const void* dout;
+  int64_t lddo;
+  void* dq;
+  void* dk;
+  void* dv;
+  int64_t lddq, lddk, lddv;
+  float* ws;
+  int64_t ws_elems;
+} sat_attn_packed_desc;
+sat_status sat_op_attention_packed_fwd(const sat_attn_packed_desc* d, void* stream);
+sat_status sat_op_attention_packed_bwd(const sat_attn_packed_desc* d, void* stream);
+/* fp32 elements of ws for these sizes (only n_seq, T, H, Hkv and dh are read). */
+sat_status sat_op_attention_packed_bwd_ws(const sat_attn_packed_desc* d, int64_t* elems);
+
 /* Rotary on interleaved pairs of the first rd dims of every q and k head, in
  * place; qk bf16 [B*S, ld] with q at column 0 and k at column H*dh.
  * inverse = 1 applies the transpose rotation (backward).  ld and dh even, qk
  * 4-byte aligned (SAT_EINVAL otherwise). */
 sat_status sat_op_rotary(void* qk, int64_t ld, int32_t B, int32_t S, int32_t H, int32_t dh,
                          int32_t rd, int32_t inverse, void* stream);
+
+/* Rotary positions with one to four axes (for instance time, height, width) on
+ * rows x [T, ldx] of H heads of dh dims, head h at column h * dh, written to y [T, ldy].
+ * pos: int32 [T, ldp], one position per row and axis, any sign.  Axis a turns
+ * pairs[a] >= 0 consecutive pairs, half = sum of pairs <= dh / 2 and <= 128 of
+ * them in all, the first 2 half dims of every head: pair i is dims (2 i, 2 i + 1)
+ * when interleaved, else (i, i + half).  Its angle is pos * base^(-i / half), or,
+ * with own_freqs, pos * base^(-j / pairs[a]) with j its place among its axis' pairs; angles are
+ * formed in 64 bits, cos and sin rounded to fp32.  inverse = 1 applies the
+ * transpose (backward).  y == x (with ldy == ldx): in place, the other dims stay; else
+ * the heads' other dims are copied, and y must not overlap x.  Columns behind
+ * the heads are not touched.  f32: x and y are fp32, else bf16.  dh even, x and y
+ * aligned to their elements (16-byte aligned rows are fastest).
+ * Errors: SAT_EINVAL for null pointers (T > 0), sizes and alignment. */
+sat_status sat_op_rotary_axes(const void* x, int64_t ldx, void* y, int64_t ldy, int32_t f32,
+                              const int32_t* pos, int64_t ldp, int32_t n_axes,
+                              const int32_t* pairs, int32_t T, int32_t H, int32_t dh, double base,
+                              int32_t interleaved, int32_t own_freqs, int32_t inverse,
+                              void* stream);
 
 /* Softmax cross-entropy forward + backward over fp32 logits z [N, ldz]:
  * row_loss fp32 [N] (0 for label -1), dz bf16 [N, lddz] = (softmax - onehot)
@@ -140,6 +211,48 @@ sat_status sat_op_cross_entropy(const float* z, int64_t ldz, const int32_t* labe
 sat_status sat_op_adamw(float* p, const float* g, float* m, float* v, void* shadow, int64_t n,
                         double lr, double beta1, double beta2, double eps, double wd, int64_t t,
                         void* stream);
+
+/* The same step over `count` tensors in few launches, moments in 32 or in 8 bits
+ * (state_bits).  The table t is host memory, read during the call only.  Each
+ * entry: n >= 0 fp32 values p, their gradient g (bf16 when grad_bf16, else fp32), moments m
+ * and v, the tensor's weight decay, a bf16 shadow that is refreshed (may be
+ * NULL); no array that is written overlaps another of the table.
+ *   32 bits: m, v fp32 [n]; with an fp32 gradient every value is bitwise that of
+ *            sat_op_adamw.
+ *   8 bits:  m, v uint8 [n], m_exp, v_exp uint8 [ceil(n / 256)], all zero before the
+ *            first step.  The 256 elements of a block share the factor 2^(exp - 127).  m is a sign
+ *            (bit 7) and a 7-bit, the root of v an 8-bit magnitude c, (1 + f / F) 2^(e - 15)
+ *            with c = F e + f, F = 8 for m and 16 for the root, and 0 for c = 0.  The update takes m
+ *            and v as they were formed in fp32; what is kept is rounded up or down at random
+ *            with the mean right, by a hash of (seed, t, place in the table, element): the
+ *            same call gives the same bits, and each step of a run should have its own
+ *            seed or t.  A root over 0 is kept as no less than the least code, 2^-15 of its
+ *            block's largest at most; an m under that is kept as 0.  A gradient that is not
+ *            finite spoils p and the moments of its block.
+ * Arrays are aligned to their elements (16 bytes for all is fastest).  Step t >= 1,
+ * as constants: a captured call repeats the same lr and t.
+ * Errors: SAT_EINVAL for null pointers, sizes, state_bits and constants. */
+typedef struct {
+  float* p;
+  const void* g;
+  void* m;
+  void* v;
+  uint8_t* m_exp;
+  uint8_t* v_exp;
+  void* shadow;
+  int64_t n;
+  double weight_decay;
+} sat_adamw_tensor;
+sat_status sat_op_adamw_multi(const sat_adamw_tensor* t, int32_t count, int32_t state_bits,
+                              int32_t grad_bf16, double lr, double beta1, double beta2,
+                              double eps, int64_t step, uint64_t seed, void* stream);
+/* The values that 8-bit moments stand for, m and v of every tensor to m_out[k] and
+ * v_out[k] (host arrays of device pointers to n values), fp32 (exact) or, with out_bf16,
+ * bf16 (m exact, v rounded once): to store 32-bit moments, or to look at them.  Of the
+ * table, m, v, m_exp, v_exp and n are read.  Errors: SAT_EINVAL. */
+sat_status sat_op_adamw_multi_state(const sat_adamw_tensor* t, int32_t count,
+                                    void* const* m_out, void* const* v_out, int32_t out_bf16,
+                                    void* stream);
 
 /* Token embedding forward h[t] = wte[tok[t]] (+ wpe[t % S]) and its
  * deterministic backward dwte[v] = sum over t with tok[t] == v of dh[t] in

@@ -58,6 +58,28 @@ class sat_gemm_desc(C.Structure):
     ]
 
 
+class sat_attn_packed_desc(C.Structure):
+    _fields_ = [
+        ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+        ("ldq", C.c_int64), ("ldk", C.c_int64), ("ldv", C.c_int64),
+        ("o", C.c_void_p), ("ldo", C.c_int64), ("lse", C.c_void_p), ("cu", C.c_void_p),
+        ("n_seq", C.c_int32), ("T", C.c_int32), ("H", C.c_int32), ("Hkv", C.c_int32),
+        ("dh", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32), ("scale", C.c_float),
+        ("dout", C.c_void_p), ("lddo", C.c_int64),
+        ("dq", C.c_void_p), ("dk", C.c_void_p), ("dv", C.c_void_p),
+        ("lddq", C.c_int64), ("lddk", C.c_int64), ("lddv", C.c_int64),
+        ("ws", C.c_void_p), ("ws_elems", C.c_int64),
+    ]
+
+
+class sat_adamw_tensor(C.Structure):
+    _fields_ = [
+        ("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+        ("m_exp", C.c_void_p), ("v_exp", C.c_void_p), ("shadow", C.c_void_p),
+        ("n", C.c_int64), ("weight_decay", C.c_double),
+    ]
+
+
 class sat_profile_result(C.Structure):
     _fields_ = [
         ("struct_size", C.c_uint32), ("steps", C.c_int32),
@@ -105,6 +127,15 @@ SIGNATURES = {
     "sat_op_attention_bwd": (C.c_int, [_VP, _VP, _VP, _I64, _I64, _I64, _VP, _I64, _VP, _VP, _I64, _VP,
                                        _VP, _VP, _VP, _I64, _I64, _I64, _I32, _I32, _I32, _I32, _I32,
                                        _F32, _VP]),
+    "sat_op_attention_packed_fwd": (C.c_int, [C.POINTER(sat_attn_packed_desc), _VP]),
+    "sat_op_attention_packed_bwd": (C.c_int, [C.POINTER(sat_attn_packed_desc), _VP]),
+    "sat_op_attention_packed_bwd_ws": (C.c_int, [C.POINTER(sat_attn_packed_desc), C.POINTER(_I64)]),
+    "sat_op_rotary_axes": (C.c_int, [_VP, _I64, _VP, _I64, _I32, _VP, _I64, _I32, C.POINTER(_I32), _I32, _I32,
+                                     _I32, C.c_double, _I32, _I32, _I32, _VP]),
+    "sat_op_adamw_multi": (C.c_int, [C.POINTER(sat_adamw_tensor), _I32, _I32, _I32, C.c_double, C.c_double,
+                                     C.c_double, C.c_double, _I64, C.c_uint64, _VP]),
+    "sat_op_adamw_multi_state": (C.c_int, [C.POINTER(sat_adamw_tensor), _I32, C.POINTER(_VP), C.POINTER(_VP),
+                                           _I32, _VP]),
     "sat_op_rotary": (C.c_int, [_VP, _I64, _I32, _I32, _I32, _I32, _I32, _I32, _VP]),
     "sat_op_cross_entropy": (C.c_int, [_VP, _I64, _VP, _I32, _I32, _VP, _VP, _I64, _VP, _VP]),
     "sat_op_adamw": (C.c_int, [_VP, _VP, _VP, _VP, _VP, _I64, C.c_double, C.c_double, C.c_double,

@@ -21,6 +21,13 @@
 //    more than 8, so the probabilities exp2(x - m) stay below 2^8 and the
 //    128 accumulator rescales are skipped on almost every block.  The result
 //    is exact: O and l always share the same m.
+//
+// Every kernel also runs over packed sequences (AttnPackedArgs: rows of one sequence in place of one
+// batch row, query heads that share K / V heads, a window; PAD: heads of 136 to 248
+// dims with zeros behind them).  The batch form's arithmetic does not change with it.
+#include <type_traits>
+
+#include "attn_packed.h"
 #include "common.h"
 #include "kernels.h"
 
@@ -65,16 +72,16 @@ __device__ __forceinline__ int acc_row(int r, int g) { return 8 * (r >> 2) + 4 *
 // Copies of one 64-row block (K or V) of this (batch, head): 32 instructions
 // of 1 KB (two 512-byte rows each), eight per wave; rows >= nvalid read zero.
 // SWZ selects the row-fragment (0) or transposed-read (1) chunk swizzle.
-template <int SWZ>
+template <int SWZ, bool PAD>
 __device__ __forceinline__ void copy_block(__amdgpu_buffer_rsrc_t rs, long ld, int nvalid,
-                                           bf16* dst, int wave) {
+                                           bf16* dst, int wave, int dh) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int j = 4 * i + wave;
     const int row = 2 * j + (lane >> 5);
     const int c = (lane & 31) ^ (SWZ ? swz_tr(row) : swz_row(row));
-    const uint32_t o = row < nvalid ? (uint32_t)(((long)row * ld + 8 * c) * 2) : OOB;
+    const uint32_t o = row < nvalid && (!PAD || 8 * c < dh) ? (uint32_t)(((long)row * ld + 8 * c) * 2) : OOB;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, lds(dst + j * 512), 16, o, 0, 0, 0);
   }
 }
@@ -119,8 +126,10 @@ struct FwdState {
 constexpr int PF_K = 3;  // k-steps (two MFMAs each) of K fragments in flight
 constexpr int PF_V = 3;  // MFMAs of V^T fragments in flight
 
+// Keys [low, lim) of this lane's query are valid, both relative to the block's first key.
+template <bool LOW>
 __device__ __forceinline__ void fwd_block(FwdState& st, const bf16* Ks, const bf16* Vs, float sc,
-                                          int kv0, int q, int S, int causal, int g, bool mask) {
+                                          int low, int lim, int g, bool mask) {
   floatx16 s0 = zero16(), s1 = zero16();
   // K fragment of k-step c, tile t (keys kv0 + 32 t ..): k-steps 8..15 sit 16 chunks further
   auto kread = [&](int c, int t) -> bf16x8 {
@@ -143,13 +152,14 @@ __device__ __forceinline__ void fwd_block(FwdState& st, const bf16* Ks, const bf
     __builtin_amdgcn_sched_barrier(0);
   }
   if (mask) {
-    // keys past the end, or (causal) past the query, score -inf; lim = first key excluded
-    const int lim = min(S, causal ? q + 1 : S) - kv0 - 4 * g;
+    // keys past the end, or (causal) past the query, score -inf
+    lim -= 4 * g;
+    low -= 4 * g;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int kr = 8 * (r >> 2) + (r & 3);  // key - kv0 - 4 g in the first tile
-      s0[r] = kr < lim ? s0[r] : -INFINITY;
-      s1[r] = kr + 32 < lim ? s1[r] : -INFINITY;
+      s0[r] = kr < lim && (!LOW || kr >= low) ? s0[r] : -INFINITY;
+      s1[r] = kr + 32 < lim && (!LOW || kr + 32 >= low) ? s1[r] : -INFINITY;
     }
   }
   // the scale is positive, so the largest scaled score is the scaled largest score
@@ -200,25 +210,47 @@ __device__ __forceinline__ void fwd_block(FwdState& st, const bf16* Ks, const bf
   }
 }
 
-__global__ __launch_bounds__(NT, 1) void attn256_fwd_kernel(AttnArgs a) {
+template <class A>
+constexpr bool kPacked = !std::is_same_v<A, AttnArgs> && !std::is_same_v<A, AttnBwdArgs>;
+
+template <class A, bool PAD>
+__global__ __launch_bounds__(NT, 1) void attn256_fwd_kernel(A a) {
+  constexpr bool PK = kPacked<A>;
   __shared__ __attribute__((aligned(1024))) bf16 smem[2 * 2 * TILE];  // 2 stages x (K, V)
-  const int S = a.S;
-  const int nqb = (S + QPB - 1) / QPB;
-  // one-dimensional grid, query blocks outermost: with a causal mask every
-  // (batch, head)'s heaviest block is dispatched before any lighter one
-  const int BH = a.B * a.H;
-  const int xb = (int)blockIdx.x / BH, bh = (int)blockIdx.x % BH;
-  const int qb = a.causal ? (nqb - 1 - xb) : xb;
-  const int b = bh / a.H, h = bh % a.H;
+  int S, qb, h, kvh, dh = DH;  // K / V head kvh; first row and its lse from here on
+  long row0, lrow;
+  if constexpr (PK) {
+    dh = a.dh;
+    const int G = a.H / a.Hkv;
+    int tile, part, s0, blk;
+    if (!packed_item(a, G, tile, kvh, part)) return;
+    if (!find_rows(a, tile, QPB, s0, S, blk)) return;
+    qb = a.causal ? (S + QPB - 1) / QPB - 1 - blk : blk;
+    h = kvh * G + part;
+    row0 = s0;
+    lrow = (long)h * a.T + s0;
+  } else {
+    S = a.S;
+    const int nqb = (S + QPB - 1) / QPB;
+    // one-dimensional grid, query blocks outermost: with a causal mask every
+    // (batch, head)'s heaviest block is dispatched before any lighter one
+    const int BH = a.B * a.H;
+    const int xb = (int)blockIdx.x / BH, bh = (int)blockIdx.x % BH;
+    qb = a.causal ? (nqb - 1 - xb) : xb;
+    const int b = bh / a.H;
+    h = kvh = bh % a.H;
+    row0 = (long)b * S;
+    lrow = ((long)b * a.H + h) * S;
+  }
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5;
   const int q0 = qb * QPB;
   const int wq0 = q0 + wave * WQ;
   const int q = wq0 + (lane & 31);
-  const bf16* Qb = a.q + (long)b * S * a.ldq + (long)h * DH;
-  const bf16* Kb = a.k + (long)b * S * a.ldk + (long)h * DH;
-  const bf16* Vb = a.v + (long)b * S * a.ldv + (long)h * DH;
+  const bf16* Qb = a.q + row0 * a.ldq + (long)h * dh;
+  const bf16* Kb = a.k + row0 * a.ldk + (long)kvh * dh;
+  const bf16* Vb = a.v + row0 * a.ldv + (long)kvh * dh;
 
   FwdState st;
   {
@@ -227,7 +259,8 @@ __global__ __launch_bounds__(NT, 1) void attn256_fwd_kernel(AttnArgs a) {
     const uint32_t qo = wq0 + qr < S ? (uint32_t)(((long)qr * a.ldq + 8 * g) * 2) : OOB;
 #pragma unroll
     for (int c = 0; c < DH / 16; ++c)
-      st.qf[c] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rq, qo, 32 * c, 0));
+      st.qf[c] = __builtin_bit_cast(
+          bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rq, !PAD || 16 * c + 8 * g < dh ? qo : OOB, 32 * c, 0));
   }
 #pragma unroll
   for (int t = 0; t < DH / 32; ++t) st.o[t] = zero16();
@@ -249,45 +282,60 @@ __global__ __launch_bounds__(NT, 1) void attn256_fwd_kernel(AttnArgs a) {
     st.vofs[ot] = key * DH + 8 * (c ^ swz_tr(key)) + 4 * (ll & 1);
   }
   const float sc = a.scale * LOG2E;
-  const int kv_end = a.causal ? min(S, q0 + QPB) : S;
-  const int nblk = (kv_end + KB - 1) / KB;
+  // blocks [jb, je); keys that some query of the wave sees [wlo, whi), all of them see [flo, fhi), this
+  // lane's does [lo, hi)
+  int jb = 0, je, wlo = 0, whi, flo = 0, fhi, lo = 0, hi;
+  if constexpr (PK) {
+    jb = key_lo(a, q0) / KB;
+    je = (key_hi(a, q0 + QPB - 1, S) + KB - 1) / KB;
+    wlo = key_lo(a, wq0);
+    whi = wq0 < S ? key_hi(a, wq0 + WQ - 1, S) : 0;
+    flo = key_lo(a, wq0 + WQ - 1);
+    fhi = key_hi(a, wq0, S);
+    lo = key_lo(a, q);
+    hi = key_hi(a, q, S);
+  } else {
+    je = ((a.causal ? min(S, q0 + QPB) : S) + KB - 1) / KB;
+    whi = a.causal ? wq0 + WQ : S;
+    fhi = a.causal ? min(S, wq0 + 1) : S;
+    hi = min(S, a.causal ? q + 1 : S);
+  }
 
-  // prologue: block 0 in stage 0
-  copy_block<0>(rows_rsrc(Kb, 0, a.ldk), a.ldk, S, smem, wave);
-  copy_block<1>(rows_rsrc(Vb, 0, a.ldv), a.ldv, S, smem + TILE, wave);
+  auto copy = [&](int j) {
+    bf16* st = smem + (j & 1) * 2 * TILE;
+    copy_block<0, PAD>(rows_rsrc(Kb, j * KB, a.ldk), a.ldk, S - j * KB, st, wave, dh);
+    copy_block<1, PAD>(rows_rsrc(Vb, j * KB, a.ldv), a.ldv, S - j * KB, st + TILE, wave, dh);
+  };
+  // prologue: the first block
+  copy(jb);
   wait_vm_lgkm0<0>();
   cta_barrier();
 
-  for (int j = 0; j < nblk; ++j) {
+  for (int j = jb; j < je; ++j) {
     const int kv0 = j * KB;
     const bf16* Ks = smem + (j & 1) * 2 * TILE;
-    bf16* nxt = smem + ((j + 1) & 1) * 2 * TILE;
-    if (j + 1 < nblk) {
-      copy_block<0>(rows_rsrc(Kb, kv0 + KB, a.ldk), a.ldk, S - kv0 - KB, nxt, wave);
-      copy_block<1>(rows_rsrc(Vb, kv0 + KB, a.ldv), a.ldv, S - kv0 - KB, nxt + TILE, wave);
-    }
-    if (!(a.causal && kv0 > wq0 + WQ - 1)) {
-      const bool mask = kv0 + KB > S || (a.causal && kv0 + KB - 1 > wq0);
-      fwd_block(st, Ks, Ks + TILE, sc, kv0, q, S, a.causal, g, mask);
-    }
-    if (j + 1 < nblk) {
+    if (j + 1 < je) copy(j + 1);
+    if (kv0 < whi && (!PK || kv0 + KB > wlo))
+      fwd_block<PK>(st, Ks, Ks + TILE, sc, lo - kv0, hi - kv0, g, kv0 + KB > fhi || (PK && kv0 < flo));
+    if (j + 1 < je) {
       wait_vm_lgkm0<0>();
       cta_barrier();
     }
   }
   if (q < S) {
     const float inv = (st.l > 0.f) ? 1.f / st.l : 0.f;
-    bf16* Ob = a.o + ((long)b * S + q) * a.ldo + (long)h * DH;
+    bf16* Ob = a.o + (row0 + q) * a.ldo + (long)h * dh;
 #pragma unroll
     for (int ot = 0; ot < DH / 32; ++ot)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
+        if (PAD && 32 * ot + acc_row(4 * r4, g) >= dh) continue;
         bf16x4 y;
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = f2bf(st.o[ot][4 * r4 + e] * inv);
         *reinterpret_cast<bf16x4*>(Ob + 32 * ot + acc_row(4 * r4, g)) = y;
       }
-    if (g == 0) a.lse[((long)b * a.H + h) * S + q] = (st.m + log2f(st.l)) * LN2;
+    if (g == 0) a.lse[lrow + q] = (st.m + log2f(st.l)) * LN2;
   }
 }
 
@@ -320,15 +368,16 @@ constexpr int PF_RQ = 1;  // dQ: row-fragment reads in flight (S^T, dP^T product
 __device__ __forceinline__ int swz_dual(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
 
 // 32 rows of 512 bytes: 16 copy instructions, two per wave of eight.
+template <bool PAD>
 __device__ __forceinline__ void copy_rows32(__amdgpu_buffer_rsrc_t rs, long ld, int nvalid, bf16* dst,
-                                            int wave) {
+                                            int wave, int dh) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int j = 8 * i + wave;
     const int row = 2 * j + (lane >> 5);
     const int c = (lane & 31) ^ swz_dual(row);
-    const uint32_t o = row < nvalid ? (uint32_t)(((long)row * ld + 8 * c) * 2) : OOB;
+    const uint32_t o = row < nvalid && (!PAD || 8 * c < dh) ? (uint32_t)(((long)row * ld + 8 * c) * 2) : OOB;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, lds(dst + j * 512), 16, o, 0, 0, 0);
   }
 }
@@ -339,30 +388,49 @@ __device__ __forceinline__ bf16x8 row_frag(const bf16* tile, int r, int c, int g
   return *reinterpret_cast<const bf16x8*>(tile + r * DH + 8 * ((2 * c + g) ^ swz_dual(r)));
 }
 
-__global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(AttnBwdArgs a) {
+// Over packed sequences the blocks of all query heads that read this K / V head follow each other.
+template <class A, bool PAD>
+__global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(A a) {
+  constexpr bool PK = kPacked<A>;
   constexpr int SMEM = 2 * STG_B + 4 * 64 * 16 * 2 + 8 * (DH / 16 - NRF) * 64 * 8;
   static_assert(SMEM * 2 <= 163840, "LDS budget");
   __shared__ __attribute__((aligned(1024))) bf16 smem[SMEM];
   float* xbuf = reinterpret_cast<float*>(smem + 2 * STG_B);  // P exchange: [pair][16][64 lanes]
   // resident fragments NRF.. of every wave: [wave][fragment][lane], 16 bytes each
   bf16* rfs = smem + 2 * STG_B + 4 * 64 * 16 * 2;
-  const int S = a.f.S;
-  // one-dimensional grid, key blocks outermost: with a causal mask the
-  // first key blocks see the most queries and are dispatched first
-  const int BH = a.f.B * a.f.H;
-  const int bh = (int)blockIdx.x % BH, b = bh / a.f.H, h = bh % a.f.H;
+  int S, k0, kvh, heads = 1, dh = DH;  // query heads that read K / V head kvh
+  long row0, lrow, lhead = 0;  // lse of row0 for the first head, and from head to head
+  if constexpr (PK) {
+    dh = a.f.dh;
+    heads = a.f.H / a.f.Hkv;
+    int tile, part, s0, blk;
+    if (!packed_item(a.f, 1, tile, kvh, part)) return;
+    if (!find_rows(a.f, tile, KPW, s0, S, blk)) return;
+    k0 = blk * KPW;
+    row0 = s0;
+    lhead = a.f.T;
+    lrow = (long)kvh * heads * lhead + s0;
+  } else {
+    S = a.f.S;
+    // one-dimensional grid, key blocks outermost: with a causal mask the
+    // first key blocks see the most queries and are dispatched first
+    const int BH = a.f.B * a.f.H;
+    const int bh = (int)blockIdx.x % BH, b = bh / a.f.H;
+    kvh = bh % a.f.H;
+    k0 = ((int)blockIdx.x / BH) * KPW;
+    row0 = (long)b * S;
+    lrow = ((long)b * a.f.H + kvh) * S;
+  }
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5;
   const int pair = wave & 3, role = wave >> 2;
-  const int k0 = ((int)blockIdx.x / BH) * KPW;
   const int kmin = k0 + pair * 32;
   const int key = kmin + (lane & 31);
-  const long hs = ((long)b * a.f.H + h) * S;
-  const bf16* Qb = a.f.q + (long)b * S * a.f.ldq + (long)h * DH;
-  const bf16* Kb = a.f.k + (long)b * S * a.f.ldk + (long)h * DH;
-  const bf16* Vb = a.f.v + (long)b * S * a.f.ldv + (long)h * DH;
-  const bf16* dOb = a.dout + (long)b * S * a.lddo + (long)h * DH;
+  const bf16* Qb = a.f.q + row0 * a.f.ldq + (long)kvh * heads * dh;
+  const bf16* Kb = a.f.k + row0 * a.f.ldk + (long)kvh * dh;
+  const bf16* Vb = a.f.v + row0 * a.f.ldv + (long)kvh * dh;
+  const bf16* dOb = a.dout + row0 * a.lddo + (long)kvh * heads * dh;
   const float sc = a.f.scale * LOG2E;
 
   // resident operand: K (role A) or V (role B) of this lane's key, dims 16 c + 8 g .. + 7
@@ -375,11 +443,12 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(AttnBwdArgs a)
     const uint32_t ko = key < S ? (uint32_t)(((long)(lane & 31) * ld + 8 * g) * 2) : OOB;
 #pragma unroll
     for (int c = 0; c < NRF; ++c)
-      rf[c] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rk, ko, 32 * c, 0));
+      rf[c] = __builtin_bit_cast(
+          bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rk, !PAD || 16 * c + 8 * g < dh ? ko : OOB, 32 * c, 0));
 #pragma unroll
     for (int c = NRF; c < DH / 16; ++c)
-      *reinterpret_cast<bf16x8*>(rfw + (c - NRF) * 512) =
-          __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rk, ko, 32 * c, 0));
+      *reinterpret_cast<bf16x8*>(rfw + (c - NRF) * 512) = __builtin_bit_cast(
+          bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rk, !PAD || 16 * c + 8 * g < dh ? ko : OOB, 32 * c, 0));
   }
   floatx16 acc[DH / 32];  // dV^T (role A) or dK^T (role B): dims 32 ot + acc_row(r, g), key = lane
 #pragma unroll
@@ -395,22 +464,38 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(AttnBwdArgs a)
     tofs[ot] = r * DH + 8 * (c ^ swz_dual(r)) + 4 * (ll & 1);
   }
 
-  const int q_start = a.f.causal ? k0 : 0;
-  const int nqb = (S - q_start + BQ - 1) / BQ;
+  // queries [q_start, q_end); those that some key of the wave sees [wlo, whi), this lane's [lo, hi)
+  int q_start, q_end, wlo, whi, lo, hi;
+  if constexpr (PK) {
+    q_start = query_lo(a.f, k0);
+    q_end = query_hi(a.f, k0 + KPW - 1, S);
+    wlo = query_lo(a.f, kmin);
+    whi = query_hi(a.f, kmin + 31, S);
+    lo = query_lo(a.f, key);
+    hi = query_hi(a.f, key, S);
+  } else {
+    q_start = a.f.causal ? k0 : 0;
+    q_end = whi = hi = S;
+    wlo = a.f.causal ? kmin : 0;
+    lo = a.f.causal ? key : 0;
+  }
+  const int nqb = (q_end - q_start + BQ - 1) / BQ, total = nqb * heads;  // step i nqb + j: block j of head i
   float* xw = xbuf + pair * 16 * 64;
   float lsd = 0.f;  // wave 0: lse2 (lanes 0..31) or delta (lanes 32..63) of the next block
 
   auto stage_ptr = [&](int j) { return smem + (j & 1) * STG_B; };
-  auto fetch = [&](int j) {  // copies of block j; wave 0 also loads its lse / delta
-    const int qs = q_start + j * BQ;
+  auto fetch = [&](int j) {  // copies of step j; wave 0 also loads its lse / delta
+    const int i = PK ? j / nqb : 0;
+    const int qs = q_start + (j - i * nqb) * BQ;
     bf16* st = stage_ptr(j);
-    copy_rows32(rows_rsrc(Qb, qs, a.f.ldq), a.f.ldq, S - qs, st, wave);
-    copy_rows32(rows_rsrc(dOb, qs, a.lddo), a.lddo, S - qs, st + QT, wave);
+    copy_rows32<PAD>(rows_rsrc(Qb + (long)i * dh, qs, a.f.ldq), a.f.ldq, S - qs, st, wave, dh);
+    copy_rows32<PAD>(rows_rsrc(dOb + (long)i * dh, qs, a.lddo), a.lddo, S - qs, st + QT, wave, dh);
     if (wave == 0) {
       // the raw value: scaling it here would make the wave wait for the
       // copies just issued (one vmcnt counts loads in issue order)
       const int qi = qs + (lane & 31);
-      lsd = qi < S ? (g ? a.delta[hs + qi] : a.f.lse[hs + qi]) : 0.f;
+      const long at = lrow + i * lhead + qi;
+      lsd = qi < S ? (g ? a.delta[at] : a.f.lse[at]) : 0.f;
     }
   };
   auto publish = [&](int j) {  // wave 0 stores lse2 / delta of block j (after its loads landed)
@@ -423,13 +508,13 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(AttnBwdArgs a)
   wait_vm_lgkm0<0>();
   cta_barrier();
 
-  for (int j = 0; j < nqb; ++j) {
-    const int qs0 = q_start + j * BQ;
+  for (int j = 0; j < total; ++j) {
+    const int qs0 = q_start + (PK ? j % nqb : j) * BQ;
     const bf16* st = stage_ptr(j);
     const bf16* Qs = st;
     const bf16* dOs = st + QT;
     const float* lsd_s = reinterpret_cast<const float*>(st + 2 * QT);
-    const bool active = !(a.f.causal && qs0 + BQ - 1 < kmin);
+    const bool active = qs0 + BQ > wlo && (!PK || qs0 < whi);
     // S = Q K^T (role A) or dP = dO V^T (role B): rows = queries, column = key
     floatx16 x = zero16();
     if (active) {
@@ -453,12 +538,12 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(AttnBwdArgs a)
     // The next block's copies go out after this block's resident-operand
     // products (issued before them, the kernel alone ran 1.5 % faster but
     // the step, where it shares the chip, no faster).
-    if (j + 1 < nqb) fetch(j + 1);
+    if (j + 1 < total) fetch(j + 1);
     if (active) {
       if (role == 0) {
         // P = exp2(S log2e - lse2); zero for queries past S and (causal) keys past the query
-        const int lim_q = S - qs0 - 4 * g;            // rows r with acc_row < lim_q are valid
-        const int lim_k = key - qs0 - 4 * g;          // causal: need acc_row >= key - qs0
+        const int lim_q = hi - qs0 - 4 * g;  // rows r with lim_k <= acc_row - 4 g < lim_q are valid
+        const int lim_k = lo - qs0 - 4 * g;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const floatx4 l4 = *reinterpret_cast<const floatx4*>(lsd_s + 8 * i + 4 * g);
@@ -466,7 +551,7 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(AttnBwdArgs a)
           for (int e = 0; e < 4; ++e) {
             const int rr = 8 * i + e;  // acc_row - 4 g
             float pr = __builtin_amdgcn_exp2f(x[4 * i + e] * sc - l4[e]);
-            const bool ok = (rr < lim_q) & ((a.f.causal == 0) | (rr >= lim_k));
+            const bool ok = (rr < lim_q) & (rr >= lim_k);
             pr = ok ? pr : 0.f;
             x[4 * i + e] = pr;
             xw[(4 * i + e) * 64 + lane] = pr;
@@ -513,7 +598,7 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(AttnBwdArgs a)
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (j + 1 < nqb) {
+    if (j + 1 < total) {
       wait_vm_lgkm0<0>();
       publish(j + 1);
       wait_vm_lgkm0<0>();
@@ -521,13 +606,14 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(AttnBwdArgs a)
     }
   }
   if (key < S) {
-    bf16* out = role ? a.dk + ((long)b * S + key) * a.lddk + (long)h * DH
-                     : a.dv + ((long)b * S + key) * a.lddv + (long)h * DH;
+    bf16* out = role ? a.dk + (row0 + key) * a.lddk + (long)kvh * dh
+                     : a.dv + (row0 + key) * a.lddv + (long)kvh * dh;
     const float f = role ? a.f.scale : 1.f;
 #pragma unroll
     for (int ot = 0; ot < DH / 32; ++ot)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
+        if (PAD && 32 * ot + acc_row(4 * r4, g) >= dh) continue;
         bf16x4 y;
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = f2bf(acc[ot][4 * r4 + e] * f);
@@ -559,17 +645,36 @@ constexpr int STG_Q = 2 * QT;  // K rows, V rows of a 32-key block
 constexpr int NSTG_Q = 4;      // K / V stages
 constexpr int XB = 4 * 16 * 64;  // floats of one P^T exchange buffer (4 pairs)
 
-__global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(AttnBwdArgs a) {
+template <class A, bool PAD>
+__global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(A a) {
+  constexpr bool PK = kPacked<A>;
   static_assert((NSTG_Q * STG_Q + 2 * XB * 2) * 2 <= 163840, "LDS budget");
   __shared__ __attribute__((aligned(1024))) bf16 smem[NSTG_Q * STG_Q + 2 * XB * 2];
   float* xbuf = reinterpret_cast<float*>(smem + NSTG_Q * STG_Q);
-  const int S = a.f.S;
-  const int nqb = (S + QPW - 1) / QPW;
-  // one-dimensional grid, query blocks outermost, heaviest first
-  const int BH = a.f.B * a.f.H;
-  const int xb = (int)blockIdx.x / BH, bh = (int)blockIdx.x % BH;
-  const int qb = a.f.causal ? (nqb - 1 - xb) : xb;
-  const int b = bh / a.f.H, h = bh % a.f.H;
+  int S, qb, h, kvh, dh = DH;
+  long row0, hs;
+  if constexpr (PK) {
+    dh = a.f.dh;
+    const int G = a.f.H / a.f.Hkv;
+    int tile, part, s0, blk;
+    if (!packed_item(a.f, G, tile, kvh, part)) return;
+    if (!find_rows(a.f, tile, QPW, s0, S, blk)) return;
+    qb = a.f.causal ? (S + QPW - 1) / QPW - 1 - blk : blk;
+    h = kvh * G + part;
+    row0 = s0;
+    hs = (long)h * a.f.T + s0;
+  } else {
+    S = a.f.S;
+    const int nqb = (S + QPW - 1) / QPW;
+    // one-dimensional grid, query blocks outermost, heaviest first
+    const int BH = a.f.B * a.f.H;
+    const int xb = (int)blockIdx.x / BH, bh = (int)blockIdx.x % BH;
+    qb = a.f.causal ? (nqb - 1 - xb) : xb;
+    const int b = bh / a.f.H;
+    h = kvh = bh % a.f.H;
+    row0 = (long)b * S;
+    hs = ((long)b * a.f.H + h) * S;
+  }
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5;
@@ -577,11 +682,10 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(AttnBwdArgs a) {
   const int q0 = qb * QPW;
   const int pq0 = q0 + pair * 32;
   const int q = pq0 + (lane & 31);
-  const long hs = ((long)b * a.f.H + h) * S;
-  const bf16* Qb = a.f.q + (long)b * S * a.f.ldq + (long)h * DH;
-  const bf16* Kb = a.f.k + (long)b * S * a.f.ldk + (long)h * DH;
-  const bf16* Vb = a.f.v + (long)b * S * a.f.ldv + (long)h * DH;
-  const bf16* dOb = a.dout + (long)b * S * a.lddo + (long)h * DH;
+  const bf16* Qb = a.f.q + row0 * a.f.ldq + (long)h * dh;
+  const bf16* Kb = a.f.k + row0 * a.f.ldk + (long)kvh * dh;
+  const bf16* Vb = a.f.v + row0 * a.f.ldv + (long)kvh * dh;
+  const bf16* dOb = a.dout + row0 * a.lddo + (long)h * dh;
   const float sc = a.f.scale * LOG2E;
 
   bf16x8 rf[DH / 16];  // Q (role A) or dO (role B) of this lane's query
@@ -592,7 +696,8 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(AttnBwdArgs a) {
     const uint32_t qo = q < S ? (uint32_t)(((long)(lane & 31) * ld + 8 * g) * 2) : OOB;
 #pragma unroll
     for (int c = 0; c < DH / 16; ++c)
-      rf[c] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rq, qo, 32 * c, 0));
+      rf[c] = __builtin_bit_cast(
+          bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rq, !PAD || 16 * c + 8 * g < dh ? qo : OOB, 32 * c, 0));
   }
   // role A: lse2 of this lane's query; role B: delta = rowsum(dO * O), from
   // the two halves of the row (lanes l and l + 32), also stored for the dK / dV
@@ -601,12 +706,13 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(AttnBwdArgs a) {
   if (role == 0) {
     lsd = q < S ? a.f.lse[hs + q] * LOG2E : 0.f;
   } else {
-    const __amdgpu_buffer_rsrc_t ro = rows_rsrc(a.f.o + (long)b * S * a.f.ldo + (long)h * DH, pq0, a.f.ldo);
+    const __amdgpu_buffer_rsrc_t ro = rows_rsrc(a.f.o + row0 * a.f.ldo + (long)h * dh, pq0, a.f.ldo);
     const uint32_t oo = q < S ? (uint32_t)(((long)(lane & 31) * a.f.ldo + 8 * g) * 2) : OOB;
     float acc = 0.f;
 #pragma unroll
     for (int c = 0; c < DH / 16; ++c) {
-      const bf16x8 ov = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(ro, oo, 32 * c, 0));
+      const bf16x8 ov = __builtin_bit_cast(
+          bf16x8, __builtin_amdgcn_raw_buffer_load_b128(ro, !PAD || 16 * c + 8 * g < dh ? oo : OOB, 32 * c, 0));
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc = __builtin_fmaf(bf2f(rf[c][e]), bf2f(ov[e]), acc);
     }
@@ -625,34 +731,46 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(AttnBwdArgs a) {
     tofs[ot] = r * DH + 8 * (c ^ swz_dual(r)) + 4 * (ll & 1);
   }
 
-  const int kv_end = a.f.causal ? min(S, q0 + QPW) : S;
-  const int nkb = (kv_end + BQ - 1) / BQ;
+  // blocks [jb, je); keys that some query of the pair sees [wlo, whi), this lane's [lo, hi)
+  int jb = 0, je, wlo = 0, whi, lo = 0, hi;
+  if constexpr (PK) {
+    jb = key_lo(a.f, q0) / BQ;
+    je = (key_hi(a.f, q0 + QPW - 1, S) + BQ - 1) / BQ;
+    wlo = key_lo(a.f, pq0);
+    whi = pq0 < S ? key_hi(a.f, pq0 + 31, S) : 0;
+    lo = key_lo(a.f, q);
+    hi = key_hi(a.f, q, S);
+  } else {
+    je = ((a.f.causal ? min(S, q0 + QPW) : S) + BQ - 1) / BQ;
+    whi = a.f.causal ? pq0 + 32 : S;
+    hi = min(S, a.f.causal ? q + 1 : S);
+  }
   auto stage_ptr = [&](int j) { return smem + (j % NSTG_Q) * STG_Q; };
   // four copy instructions per wave per block
   auto fetch = [&](int j) {
     const int kv = j * BQ;
     bf16* st = stage_ptr(j);
-    copy_rows32(rows_rsrc(Kb, kv, a.f.ldk), a.f.ldk, S - kv, st, wave);
-    copy_rows32(rows_rsrc(Vb, kv, a.f.ldv), a.f.ldv, S - kv, st + QT, wave);
+    copy_rows32<PAD>(rows_rsrc(Kb, kv, a.f.ldk), a.f.ldk, S - kv, st, wave, dh);
+    copy_rows32<PAD>(rows_rsrc(Vb, kv, a.f.ldv), a.f.ldv, S - kv, st + QT, wave, dh);
   };
 
-  fetch(0);
-  if (nkb > 1) {
-    fetch(1);
-    wait_vm_lgkm0<4>();  // block 0 resident, block 1 may stay in flight
+  fetch(jb);
+  if (je - jb > 1) {
+    fetch(jb + 1);
+    wait_vm_lgkm0<4>();  // the first block resident, the second may stay in flight
   } else {
     wait_vm_lgkm0<0>();
   }
   cta_barrier();
 
-  for (int j = 0; j < nkb; ++j) {
+  for (int j = jb; j < je; ++j) {
     const int kv0 = j * BQ;
     const bf16* Ks = stage_ptr(j);
     const bf16* Vs = Ks + QT;
     float* xw = xbuf + (j & 1) * XB + pair * 16 * 64;
-    const bool more2 = j + 2 < nkb;
+    const bool more2 = j + 2 < je;
     if (more2) fetch(j + 2);
-    const bool active = !(a.f.causal && kv0 > pq0 + 31);
+    const bool active = kv0 < whi && (!PK || kv0 + BQ > wlo);
     floatx16 x = zero16();
     if (active) {
       const bf16* rows = role ? Vs : Ks;
@@ -666,13 +784,13 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(AttnBwdArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       }
       if (role == 0) {
-        // P^T = exp2(S^T log2e - lse2); zero for keys past S or (causal) past the query
-        const int lim = min(S, a.f.causal ? q + 1 : S) - kv0 - 4 * g;  // keys with acc_row < lim valid
+        // P^T = exp2(S^T log2e - lse2); zero for keys that the query does not see
+        const int lim = hi - kv0 - 4 * g, low = lo - kv0 - 4 * g;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int kr = 8 * (r >> 2) + (r & 3);  // acc_row - 4 g
           float pr = __builtin_amdgcn_exp2f(x[r] * sc - lsd);
-          pr = kr < lim ? pr : 0.f;
+          pr = kr < lim && (!PK || kr >= low) ? pr : 0.f;
           xw[r * 64 + lane] = pr;
         }
       }
@@ -702,11 +820,12 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(AttnBwdArgs a) {
     }
   }
   if (role == 1 && q < S) {
-    bf16* out = a.dq + ((long)b * S + q) * a.lddq + (long)h * DH;
+    bf16* out = a.dq + (row0 + q) * a.lddq + (long)h * dh;
 #pragma unroll
     for (int ot = 0; ot < DH / 32; ++ot)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
+        if (PAD && 32 * ot + acc_row(4 * r4, g) >= dh) continue;
         bf16x4 y;
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = f2bf(acc[ot][4 * r4 + e] * a.f.scale);
@@ -736,18 +855,40 @@ bool attn256_bwd_eligible(const AttnBwdArgs& a) {
 
 hipError_t launch_attn256_bwd_dkdv(const AttnBwdArgs& a, hipStream_t s) {
   dim3 grid((unsigned)(((a.f.S + KPW - 1) / KPW) * a.f.B * a.f.H));
-  hipLaunchKernelGGL(attn256_bwd_dkdv_kernel, grid, dim3(NT8), 0, s, a);
+  hipLaunchKernelGGL((attn256_bwd_dkdv_kernel<AttnBwdArgs, false>), grid, dim3(NT8), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_attn256_bwd_dq(const AttnBwdArgs& a, hipStream_t s) {
   dim3 grid((unsigned)(((a.f.S + QPW - 1) / QPW) * a.f.B * a.f.H));
-  hipLaunchKernelGGL(attn256_bwd_dq_kernel, grid, dim3(NT8), 0, s, a);
+  hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnBwdArgs, false>), grid, dim3(NT8), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_attn256_fwd(const AttnArgs& a, hipStream_t s) {
   dim3 grid((unsigned)(((a.S + QPB - 1) / QPB) * a.B * a.H));
-  hipLaunchKernelGGL(attn256_fwd_kernel, grid, dim3(NT), 0, s, a);
+  hipLaunchKernelGGL((attn256_fwd_kernel<AttnArgs, false>), grid, dim3(NT), 0, s, a);
+  return hipGetLastError();
+}
+
+// Packed sequences: 128-row blocks of one sequence.
+hipError_t launch_attn256_packed_fwd(const AttnPackedArgs& args, hipStream_t s) {
+  AttnPackedArgs a = args;
+  const dim3 grid(packed_grid(a, QPB, a.H / a.Hkv));
+  if (a.dh == DH) hipLaunchKernelGGL((attn256_fwd_kernel<AttnPackedArgs, false>), grid, dim3(NT), 0, s, a);
+  else hipLaunchKernelGGL((attn256_fwd_kernel<AttnPackedArgs, true>), grid, dim3(NT), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_attn256_packed_bwd(const AttnPackedBwdArgs& args, hipStream_t s) {
+  AttnPackedBwdArgs a = args;
+  const dim3 qgrid(packed_grid(a.f, QPW, a.f.H / a.f.Hkv));
+  if (a.f.dh == DH) hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnPackedBwdArgs, false>), qgrid, dim3(NT8), 0, s, a);
+  else hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnPackedBwdArgs, true>), qgrid, dim3(NT8), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const dim3 kgrid(packed_grid(a.f, KPW, 1));
+  if (a.f.dh == DH) hipLaunchKernelGGL((attn256_bwd_dkdv_kernel<AttnPackedBwdArgs, false>), kgrid, dim3(NT8), 0, s, a);
+  else hipLaunchKernelGGL((attn256_bwd_dkdv_kernel<AttnPackedBwdArgs, true>), kgrid, dim3(NT8), 0, s, a);
   return hipGetLastError();
 }

@@ -217,6 +217,37 @@ bool attn_small_bwd_eligible(const AttnBwdArgs& a);
 hipError_t launch_attn_small_fwd(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_small_bwd(const AttnBwdArgs& a, hipStream_t s);
 
+// Attention inside packed sequences (attn_packed.hip; heads over 128 wide: attn256.hip).  Rows
+// cu[s] .. cu[s + 1] - 1 are sequence s; H query heads on Hkv K / V heads, dh a multiple of 8.
+struct AttnPackedArgs {
+  const bf16* q;     // q(t, h, :) = q[t * ldq + h * dh]
+  const bf16* k;     // k(t, h / (H / Hkv), :)
+  const bf16* v;
+  long ldq, ldk, ldv;
+  bf16* o;
+  long ldo;
+  float* lse;        // [H, T] log-sum-exp of the scaled scores (natural log)
+  const int32_t* cu; // device, n_seq + 1
+  int n_seq, T, H, Hkv, dh;
+  int causal, window;  // window: 1 .. 2^30 (no window)
+  float scale;
+  int ntile, run;      // set by the launchers: numbered blocks, blocks of a unit (attn_packed.h)
+};
+struct AttnPackedBwdArgs {
+  AttnPackedArgs f;
+  const bf16* dout;
+  long lddo;
+  float* delta;      // [H, T] rowsum(dO * O)
+  bf16* dq;
+  bf16* dk;
+  bf16* dv;
+  long lddq, lddk, lddv;
+};
+hipError_t launch_attn_packed_fwd(const AttnPackedArgs& a, hipStream_t s);
+hipError_t launch_attn_packed_bwd(const AttnPackedBwdArgs& a, hipStream_t s);
+hipError_t launch_attn256_packed_fwd(const AttnPackedArgs& a, hipStream_t s);
+hipError_t launch_attn256_packed_bwd(const AttnPackedBwdArgs& a, hipStream_t s);
+
 // ---------------------------------------------------------------- elementwise
 // GPT-J rotary on interleaved pairs of the first rd dims of every q and k head,
 // in place on the bf16 [T, ld] buffer (q at column 0, k at column d).  cs: the
@@ -226,6 +257,21 @@ hipError_t launch_rotary(bf16* qk, long ld, int B, int S, int H, int dh, int rd,
                          hipStream_t s, const float2* cs = nullptr);
 // cs[pos * (rd / 2) + i] = (cos, sin) of pos * 10000^(-2i/rd), pos < S.
 hipError_t launch_rope_table(float2* cs, int S, int rd, hipStream_t s);
+// Rotary positions with several axes on rows [T, ld] of H heads, fp32 or bf16 (rotary_axes.hip):
+// pair i turns by pos[t ldp + axis[i]] * freq[i] turns.  x == y (and ldx == ldy): in place;
+// otherwise the heads' other elements are copied too.  The last six are set by the launcher.
+struct RotaryAxes {
+  const void* x;
+  void* y;
+  const int32_t* pos;
+  long ldx, ldy, ldp;
+  int T, H, dh, half, inverse;  // half: pairs of a head, at most 128
+  int rows_wg, items, head_items;
+  uint32_t inv_items, inv_head_items, inv_half;
+  double freq[128];
+  uint8_t axis[128];
+};
+hipError_t launch_rotary_axes(const RotaryAxes& a, bool f32, bool inter, hipStream_t s);
 // h0[t, :] = wte[tok[t], :] (+ wpe[t % S, :])
 hipError_t launch_embed_fwd(const int32_t* tok, const float* wte, const float* wpe, float* h,
                             int T, int S, int d, int V, hipStream_t s);
@@ -269,6 +315,38 @@ hipError_t launch_synth_images(float* img, long n, int32_t* y, int B, int classe
 AdamWConsts adamw_consts(double lr, double beta1, double beta2, double eps, double wd, long t);
 hipError_t launch_adamw(float* p, const float* g, float* m, float* v, bf16* shadow, long n,
                         const AdamWConsts& c, hipStream_t s);
+// One AdamW step over many tensors (adamw_multi.hip).  A launch takes up to kAdamWEntries
+// tensors, entry k's chunks are workgroups first[k] .. first[k + 1] - 1 (adamw_chunks(n) each).
+// vec: every array of the entry is aligned for four elements at once.
+struct AdamWEntry {
+  float* p;
+  const void* g;       // fp32 or bf16
+  void* m;             // fp32, or uint8 codes
+  void* v;
+  uint8_t* m_exp;      // one exponent for each 256 codes
+  uint8_t* v_exp;
+  union {
+    bf16* shadow;      // step; may be null
+    void* m_out;       // state: fp32 or bf16
+  };
+  void* v_out;
+  long n;
+  float lr_wd;
+  uint32_t key;
+  int vec;
+};
+constexpr int kAdamWEntries = 40;  // of 88 bytes: kernel arguments below 4 KB
+struct AdamWMulti {
+  AdamWConsts c;
+  int count;
+  int first[kAdamWEntries];
+  AdamWEntry t[kAdamWEntries];
+};
+static_assert(sizeof(AdamWMulti) <= 4096, "kernel arguments");
+long adamw_chunks(long n);
+hipError_t launch_adamw_multi(const AdamWMulti& a, int chunks, int bits, bool grad_bf16, hipStream_t s);
+// The values of 8-bit moments to m_out and v_out.
+hipError_t launch_adamw_state(const AdamWMulti& a, int chunks, bool out_bf16, hipStream_t s);
 // One piece of the trainable parameters for the segmented AdamW below.
 // Flat segment (toff < 0): n = rows elements at off.  Matrix segment: the
 // [rows, cols] row-major matrix at off, updated in 64 x 64 tiles whose bf16

@@ -250,3 +250,159 @@ def maxpool_bwd(dy, arg, N, H, W, C):
     dx = torch.empty(N * H * W, C, device=dy.device, dtype=torch.float32)
     _lib.call("sat_op_maxpool_bwd", _p(dy), _p(arg), N, H, W, C, _p(dx), _stream())
     return dx
+
+
+# ---------------------------------------------------------------- packed rows
+
+def _here(t, dtype, name):
+    """t: a tensor of `dtype` on the current device (the calls run on its current stream)."""
+    _need(t, dtype, name)
+    if t is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _rows_of(t, dtype, name, rows, cols):
+    """Leading dimension of a matrix of at least `rows` rows and `cols` columns, columns contiguous."""
+    _here(t, dtype, name)
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < cols or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: expected [{rows}, >= {cols}] with contiguous rows, got {tuple(t.shape)} "
+                         f"strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window):
+    T = q.shape[0]
+    bf = torch.bfloat16
+    d = _lib.sat_attn_packed_desc(
+        q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), o=o.data_ptr(), lse=lse.data_ptr(), cu=cu.data_ptr(),
+        ldq=_rows_of(q, bf, "q", T, H * dh), ldk=_rows_of(k, bf, "k", T, Hkv * dh),
+        ldv=_rows_of(v, bf, "v", T, Hkv * dh), ldo=_rows_of(o, bf, "o", T, H * dh),
+        n_seq=cu.numel() - 1, T=T, H=H, Hkv=Hkv, dh=dh, causal=int(causal), window=window, scale=scale)
+    _here(lse, torch.float32, "lse")
+    _here(cu, torch.int32, "cu")
+    if cu.dim() != 1 or cu.numel() < 1 or not cu.is_contiguous():
+        raise ValueError("cu: expected a contiguous vector of n_seq + 1 row numbers")
+    if tuple(lse.shape) != (H, T) or not lse.is_contiguous():
+        raise ValueError(f"lse: expected a contiguous [{H}, {T}], got {tuple(lse.shape)}")
+    return d
+
+
+def attention_packed_fwd(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, *, window=0):
+    """Attention inside packed sequences: rows cu[s] .. cu[s + 1] - 1 of q, o [T, >= H dh] and
+    k, v [T, >= Hkv dh] (bf16, views of a wider buffer allowed) are sequence s; lse fp32 [H, T].
+    See saturn_ops.h for the masks."""
+    d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window)
+    _lib.call("sat_op_attention_packed_fwd", C.byref(d), _stream())
+
+
+def attention_packed_bwd(q, k, v, o, lse, cu, dout, dq, dk, dv, H, Hkv, dh, causal, scale, *, window=0):
+    """Its backward from dout [T, >= H dh] and the forward's o and lse; writes dq, dk, dv.
+    The workspace comes from torch's allocator, on the current stream."""
+    d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window)
+    bf = torch.bfloat16
+    for n, t, w in (("dout", dout, H), ("dq", dq, H), ("dk", dk, Hkv), ("dv", dv, Hkv)):
+        setattr(d, n, t.data_ptr())
+        setattr(d, "lddo" if n == "dout" else "ld" + n, _rows_of(t, bf, n, d.T, w * dh))
+    need = C.c_int64()
+    _lib.call("sat_op_attention_packed_bwd_ws", C.byref(d), C.byref(need))
+    ws = torch.empty(max(1, need.value), device=q.device, dtype=torch.float32)
+    d.ws, d.ws_elems = ws.data_ptr(), ws.numel()
+    _lib.call("sat_op_attention_packed_bwd", C.byref(d), _stream())
+
+
+def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=True, own_freqs=False, inverse=False):
+    """Rotary positions with len(pairs) axes on the H heads of x [T, >= H dh] (bf16 or fp32), axis a
+    turning pairs[a] pairs of every head by pos[:, a] (int32 [T, axes]); in place, or into `out`.
+    See saturn_ops.h.  Returns the rotated tensor."""
+    f32 = x.dtype == torch.float32
+    dt = torch.float32 if f32 else torch.bfloat16
+    T = x.shape[0]
+    y = x if out is None else out
+    ldx, ldy = _rows_of(x, dt, "x", T, H * dh), _rows_of(y, dt, "out", T, H * dh)
+    ldp = _rows_of(pos, torch.int32, "pos", T, len(pairs))
+    n = (C.c_int32 * len(pairs))(*pairs)
+    _lib.call("sat_op_rotary_axes", _p(x), ldx, _p(y), ldy, int(f32), _p(pos), ldp, len(pairs), n, T, H, dh,
+              float(base), int(interleaved), int(own_freqs), int(inverse), _stream())
+    return y
+
+
+class AdamWTensors:
+    """The tensors of adamw_multi: parameters (fp32), gradients (all fp32 or all bf16), moments
+    (all fp32, or all uint8 with m_exp and v_exp, one uint8 for each 256 elements of a tensor), bf16
+    shadows (optional) and weight decay (a number, or one per tensor).  Holds the tensors."""
+
+    def __init__(self, params, grads, m, v, *, shadows=None, weight_decay=0.0, m_exp=None, v_exp=None):
+        n = len(params)
+        if any(len(x) != n for x in (grads, m, v)):
+            raise ValueError("one of everything for each parameter")
+        self.bits = 8 if n and m[0].dtype == torch.uint8 else 32
+        self.grad_bf16 = bool(n) and grads[0].dtype == torch.bfloat16
+        st = torch.uint8 if self.bits == 8 else torch.float32
+        decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        lists = dict(params=params, grads=grads, m=m, v=v)
+        if shadows is not None:
+            lists["shadows"] = shadows
+        if self.bits == 8:
+            if m_exp is None or v_exp is None:
+                raise ValueError("8-bit moments need m_exp and v_exp")
+            lists.update(m_exp=m_exp, v_exp=v_exp)
+        elif m_exp is not None or v_exp is not None:
+            raise ValueError("m_exp and v_exp belong to 8-bit moments")
+        if any(len(x) != n for x in lists.values()) or len(decay) != n:
+            raise ValueError("one of everything for each parameter")
+        dtypes = dict(params=torch.float32, grads=torch.bfloat16 if self.grad_bf16 else torch.float32, m=st, v=st,
+                      shadows=torch.bfloat16, m_exp=torch.uint8, v_exp=torch.uint8)
+        written, read = [], []
+        for name, ts in lists.items():
+            for i, t in enumerate(ts):
+                _here(t, dtypes[name], f"{name}[{i}]")
+                want = params[i].numel() if not name.endswith("_exp") else -(-params[i].numel() // 256)
+                if not t.is_contiguous() or t.numel() != want:
+                    raise ValueError(f"{name}[{i}]: expected {want} contiguous elements, got {tuple(t.shape)}")
+                if want:
+                    (read if name == "grads" else written).append(
+                        (t.data_ptr(), t.data_ptr() + want * t.element_size(), f"{name}[{i}]", name != "grads"))
+        end, last = 0, None
+        for a, b, what, w in sorted(written + read):
+            if a < end and (w or last[1]):
+                raise ValueError(f"{what} overlaps {last[0]}")
+            if b > end:
+                end, last = b, (what, w)
+        self.tensors = lists
+        self.table = (_lib.sat_adamw_tensor * n)()
+        for i, e in enumerate(self.table):
+            e.p, e.g, e.m, e.v = (lists[x][i].data_ptr() for x in ("params", "grads", "m", "v"))
+            e.shadow = None if shadows is None else shadows[i].data_ptr()
+            if self.bits == 8:
+                e.m_exp, e.v_exp = m_exp[i].data_ptr(), v_exp[i].data_ptr()
+            e.n, e.weight_decay = params[i].numel(), decay[i]
+
+
+def adamw_multi(tensors, lr, beta1, beta2, eps, t, *, seed=0):
+    """One AdamW step t (>= 1) on all of `tensors` (AdamWTensors); seed: of the rounding of 8-bit moments."""
+    _on_device(tensors)
+    _lib.call("sat_op_adamw_multi", tensors.table, len(tensors.table), tensors.bits, int(tensors.grad_bf16),
+              float(lr), float(beta1), float(beta2), float(eps), t, seed & 0xFFFFFFFFFFFFFFFF, _stream())
+
+
+def adamw_multi_state(tensors, m_out, v_out):
+    """The values of 8-bit moments, to one contiguous tensor per parameter in each list (all fp32 or all bf16)."""
+    _on_device(tensors)
+    if tensors.bits != 8:
+        raise ValueError("adamw_multi_state: the moments are fp32 already")
+    n = len(tensors.table)
+    if len(m_out) != n or len(v_out) != n:
+        raise ValueError("adamw_multi_state: one output of each kind for each parameter")
+    dt = torch.bfloat16 if n and m_out[0].dtype == torch.bfloat16 else torch.float32
+    for i in range(n):
+        for name, t in (("m_out", m_out[i]), ("v_out", v_out[i])):
+            _here(t, dt, f"{name}[{i}]")
+            if not t.is_contiguous() or t.numel() != tensors.table[i].n:
+                raise ValueError(f"{name}[{i}]: expected {tensors.table[i].n} contiguous elements, got {tuple(t.shape)}")
+    ms, vs = ((C.c_void_p * n)(*[t.data_ptr() for t in ts]) for ts in (m_out, v_out))
+    _lib.call("sat_op_adamw_multi_state", tensors.table, n, ms, vs, int(dt == torch.bfloat16), _stream())
+
+
+def _on_device(tensors):
+    for t in tensors.tensors["params"][:1]:
+        _here(t, torch.float32, "params[0]")

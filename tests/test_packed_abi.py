@@ -1,0 +1,165 @@
+"""Host-side checks of the operators on packed rows that need no GPU: refusals of the C entry
+points before any launch, workspace sizes, the reference's gradients against differences."""
+
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import packed_ref as R
+
+
+def _L():
+    from paper_2309_01226_amd import _lib
+    return _lib
+
+
+def _desc(**kw):
+    d = dict(q=1 << 20, k=1 << 20, v=1 << 20, ldq=512, ldk=256, ldv=256, o=1 << 20, ldo=512, lse=1 << 20, cu=1 << 20,
+             n_seq=3, T=100, H=8, Hkv=4, dh=64, causal=1, window=0, scale=0.125, dout=1 << 20, lddo=512, dq=1 << 20,
+             dk=1 << 20, dv=1 << 20, lddq=512, lddk=256, lddv=256, ws=1 << 20, ws_elems=1 << 40)
+    d.update(kw)
+    return _L().sat_attn_packed_desc(**d)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(lse=None), dict(cu=None),
+    dict(q=(1 << 20) + 8), dict(v=(1 << 20) + 2), dict(o=(1 << 20) + 8), dict(lse=(1 << 20) + 2), dict(cu=(1 << 20) + 1),
+    dict(ldq=504), dict(ldk=248), dict(ldv=260), dict(ldo=516), dict(ldq=1 << 22),
+    dict(T=-1), dict(T=(1 << 29) + 1), dict(n_seq=-1), dict(H=6), dict(Hkv=0), dict(H=0), dict(Hkv=-4),
+    dict(dh=0), dict(dh=60), dict(dh=264), dict(window=-1), dict(scale=0.0), dict(scale=-1.0),
+    dict(scale=math.nan), dict(scale=math.inf), dict(T=1 << 29, H=1 << 16, Hkv=1 << 16, dh=8, ldq=1 << 20),
+])
+def test_attention_refusals(bad):
+    L = _L()
+    d = _desc(**bad)
+    for f in (L.lib().sat_op_attention_packed_fwd, L.lib().sat_op_attention_packed_bwd):
+        assert f(C.byref(d), None) == L.SAT_EINVAL
+        assert "attention_packed" in L.last_error()
+
+
+@pytest.mark.parametrize("bad", [
+    dict(dout=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(ws=None), dict(ws_elems=799), dict(lddo=504),
+    dict(lddo=516), dict(dout=(1 << 20) + 8), dict(dq=(1 << 20) + 4), dict(lddq=508), dict(lddk=255), dict(lddv=252),
+    dict(ws=(1 << 20) + 2), dict(lddo=1 << 22),
+])
+def test_attention_backward_refusals(bad):
+    L = _L()
+    d = _desc(**bad)
+    assert L.lib().sat_op_attention_packed_bwd(C.byref(d), None) == L.SAT_EINVAL
+    assert L.last_error()
+
+
+def test_attention_null_descriptor_and_ws():
+    L = _L()
+    assert L.lib().sat_op_attention_packed_fwd(None, None) == L.SAT_EINVAL
+    assert L.lib().sat_op_attention_packed_bwd(None, None) == L.SAT_EINVAL
+    n = C.c_int64()
+    assert L.lib().sat_op_attention_packed_bwd_ws(None, C.byref(n)) == L.SAT_EINVAL
+    assert L.lib().sat_op_attention_packed_bwd_ws(C.byref(_desc()), None) == L.SAT_EINVAL
+    # sizes alone are read
+    d = L.sat_attn_packed_desc(n_seq=3, T=100, H=8, Hkv=4, dh=64)
+    assert L.lib().sat_op_attention_packed_bwd_ws(C.byref(d), C.byref(n)) == 0 and n.value >= 800
+
+
+def _rotary(**kw):
+    a = dict(x=1 << 20, ldx=320, y=1 << 20, ldy=320, f32=0, pos=1 << 20, ldp=2, n_axes=2, pairs=(16, 16), T=9, H=4, dh=80,
+             base=1e4, interleaved=1, own_freqs=0, inverse=0)
+    a.update(kw)
+    p = a["pairs"]
+    a["pairs"] = None if p is None else (C.c_int32 * max(1, len(p)))(*p)
+    return _L().lib().sat_op_rotary_axes(*a.values(), None)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(x=None), dict(y=None), dict(pos=None), dict(pairs=None), dict(n_axes=0), dict(n_axes=5, pairs=(1,) * 5, ldp=5),
+    dict(pairs=(41, 0)), dict(pairs=(0, 0)), dict(pairs=(-1, 9)), dict(pairs=(20, 21)), dict(T=-1), dict(H=0), dict(dh=81, ldx=400, ldy=400),
+    dict(ldx=319), dict(ldy=319, y=1 << 24), dict(ldp=1), dict(ldy=328), dict(x=(1 << 20) + 1), dict(f32=1, x=(1 << 20) + 2),
+    dict(pos=(1 << 20) + 2), dict(base=0.0), dict(base=-1.0), dict(base=math.inf), dict(base=math.nan),
+    dict(pairs=(129, 0), dh=512, ldx=2048, ldy=2048),
+])
+def test_rotary_refusals(bad):
+    assert _rotary(**bad) == _L().SAT_EINVAL
+    assert "rotary_axes" in _L().last_error()
+
+
+def _adamw(bits=32, bf=0, lr=1e-3, b1=0.9, b2=0.999, eps=1e-8, t=1, count=None, **kw):
+    L = _L()
+    e = dict(p=1 << 20, g=1 << 20, m=1 << 20, v=1 << 20, m_exp=1 << 20, v_exp=1 << 20, shadow=None, n=10, weight_decay=0.0)
+    e.update(kw)
+    tab = (L.sat_adamw_tensor * 1)(L.sat_adamw_tensor(**e))
+    return L.lib().sat_op_adamw_multi(tab, 1 if count is None else count, bits, bf, lr, b1, b2, eps, t, 0, None)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(bits=16), dict(t=0), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(b2=math.nan), dict(eps=-1.0), dict(lr=math.inf),
+    dict(count=-1), dict(p=None), dict(g=None), dict(m=None), dict(v=None), dict(bits=8, m_exp=None), dict(bits=8, v_exp=None),
+    dict(n=-1), dict(n=(1 << 42) + 1), dict(p=(1 << 20) + 2), dict(g=(1 << 20) + 2), dict(bf=1, g=(1 << 20) + 1),
+    dict(m=(1 << 20) + 1), dict(v=(1 << 20) + 2), dict(shadow=(1 << 20) + 1),
+])
+def test_adamw_refusals(bad):
+    assert _adamw(**bad) == _L().SAT_EINVAL
+    assert "adamw_multi" in _L().last_error()
+
+
+def test_adamw_empty_tables():
+    L = _L()
+    assert L.lib().sat_op_adamw_multi(None, 0, 32, 0, 1e-3, 0.9, 0.999, 1e-8, 1, 0, None) == 0
+    assert L.lib().sat_op_adamw_multi(None, 1, 32, 0, 1e-3, 0.9, 0.999, 1e-8, 1, 0, None) == L.SAT_EINVAL
+    assert _adamw(n=0, p=None, g=None) == 0  # an empty tensor needs nothing
+    one = (C.c_void_p * 1)(None)
+    tab = (L.sat_adamw_tensor * 1)(L.sat_adamw_tensor(m=1 << 20, v=1 << 20, m_exp=1 << 20, v_exp=1 << 20, n=4))
+    assert L.lib().sat_op_adamw_multi_state(tab, 1, one, one, 0, None) == L.SAT_EINVAL
+    assert L.lib().sat_op_adamw_multi_state(tab, 1, None, one, 0, None) == L.SAT_EINVAL
+    odd = (C.c_void_p * 1)((1 << 20) + 1)
+    assert L.lib().sat_op_adamw_multi_state(tab, 1, odd, odd, 1, None) == L.SAT_EINVAL
+    assert L.lib().sat_op_adamw_multi_state(None, 0, None, None, 0, None) == 0
+
+
+def test_python_entry_points_refuse_host_tensors():
+    from paper_2309_01226_amd import ops
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    with pytest.raises(TypeError):
+        ops.rotary_axes(x, torch.zeros(4, 1, dtype=torch.int32), 1, 64, (32,))
+    with pytest.raises(TypeError):
+        ops.attention_packed_fwd(x, x, x, x, torch.zeros(1, 4), torch.zeros(2, dtype=torch.int32), 1, 1, 64, True, 0.125)
+    p = [torch.zeros(8)]
+    with pytest.raises(TypeError):
+        ops.AdamWTensors(p, p, p, p)
+    with pytest.raises(ValueError):
+        ops.AdamWTensors(p, p, [torch.zeros(8, dtype=torch.uint8)], [torch.zeros(8, dtype=torch.uint8)])
+
+
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 3), (False, 2)])
+def test_reference_gradients_against_differences(causal, window):
+    """The formulas that the kernels are held to, against central differences of the forward."""
+    g = torch.Generator().manual_seed(3)
+    H, Hkv, dh, cu = 4, 2, 8, [1, 1, 6, 7, 12]
+    q, k, v, do = (torch.randn(13, n * dh, generator=g, dtype=torch.float64) for n in (H, Hkv, Hkv, H))
+    out, _ = R.attention(q, k, v, cu, H, Hkv, dh, causal, 0.3, window, do)
+    step = 1e-5
+    for name, x in (("dq", q), ("dk", k), ("dv", v)):
+        d = torch.randn(x.shape, generator=g, dtype=torch.float64)
+        f = []
+        for s in (step, -step):
+            a = dict(q=q, k=k, v=v)
+            a[name[1]] = x + s * d
+            f.append(float((R.attention(**a, cu=cu, H=H, Hkv=Hkv, dh=dh, causal=causal, scale=0.3, window=window)[0]["o"] * do).sum()))
+        want = float((out[name] * d).sum())
+        # the difference is off by step^2 times a third derivative, and by rounding / step: 1e-8 at most here
+        assert abs((f[0] - f[1]) / (2 * step) - want) < 1e-7 * max(1.0, abs(want))
+
+
+def test_reference_rotary_is_orthogonal_and_inverse():
+    rng = np.random.default_rng(0)
+    x = rng.normal(size=(7, 40))
+    pos = rng.integers(-50, 1 << 20, size=(7, 3))
+    for inter in (True, False):
+        for own in (True, False):
+            y = R.rotary(x, pos, 2, 20, (3, 0, 5), interleaved=inter, own_freqs=own)
+            assert np.allclose(np.linalg.norm(y, axis=1), np.linalg.norm(x, axis=1))
+            back = R.rotary(y, pos, 2, 20, (3, 0, 5), interleaved=inter, own_freqs=own, inverse=True)
+            assert np.allclose(back, x)
+            assert np.array_equal(y[:, 16:20], x[:, 16:20])
