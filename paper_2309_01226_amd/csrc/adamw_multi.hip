@@ -21,7 +21,7 @@
 //
 // Bound by HBM: 30 bytes per element with 32-bit moments and an fp32 gradient (28
 // without the bf16 copy), 18 with 8-bit ones, 16 with a bf16 gradient also.  A
-// workgroup takes 4096 consecutive elements of one tensor, found from the launch's table
+// workgroup takes 4096 (1024 where the table is small) consecutive elements of one tensor, found from the launch's table
 // of tensors in the kernel arguments (nothing is copied to the device, so the
 // call needs no workspace and can be captured); a wave takes whole blocks, four
 // consecutive elements per lane, and has the loads of all its blocks in flight first.
@@ -31,9 +31,8 @@
 
 namespace {
 
-constexpr int CHUNK = 4096;   // elements of a workgroup
-constexpr int NB = 4;         // 256-element blocks of a wave
 typedef uint8_t u8x4 __attribute__((ext_vector_type(4)));
+typedef uint8_t u8x8 __attribute__((ext_vector_type(8)));
 
 // The tensor of the launch whose chunks include workgroup `wg`: every lane looks at one entry.
 __device__ __forceinline__ int entry_of(const int* first, int count, int wg) {
@@ -42,35 +41,43 @@ __device__ __forceinline__ int entry_of(const int* first, int count, int wg) {
   return __builtin_amdgcn_readfirstlane((int)__popcll(__builtin_amdgcn_ballot_w64(at)) - 1);
 }
 
-template <class V, class T>
-__device__ __forceinline__ void load4(const T* p, long i, long n, bool vec, T (&x)[4]) {
-  if (vec && i + 4 <= n) {
+// N elements from i on.  FULL: all below n and aligned; otherwise one by one.
+template <bool FULL, class V, class T, int N>
+__device__ __forceinline__ void load(const T* p, long i, long n, T (&x)[N]) {
+  if constexpr (FULL) {
     const V v = __builtin_nontemporal_load(reinterpret_cast<const V*>(p + i));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = v[e];
+    for (int e = 0; e < N; ++e) x[e] = v[e];
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = i + e < n ? p[i + e] : T(0);
+    for (int e = 0; e < N; ++e) x[e] = i + e < n ? p[i + e] : T(0);
   }
 }
-template <class V, class T>
-__device__ __forceinline__ void store4(T* p, long i, long n, bool vec, const T (&x)[4]) {
-  if (vec && i + 4 <= n) {
+template <bool FULL, class V, class T, int N>
+__device__ __forceinline__ void store(T* p, long i, long n, const T (&x)[N]) {
+  if constexpr (FULL) {
     V v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = x[e];
+    for (int e = 0; e < N; ++e) v[e] = x[e];
     __builtin_nontemporal_store(v, reinterpret_cast<V*>(p + i));
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < N; ++e)
       if (i + e < n) p[i + e] = x[e];
   }
 }
 
+// Maximum over the wave, on the vector unit: lanes 1 and 2 away, 4 and 8 around the row of 16, then
+// the rows and halves.
 __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, SAT_WAVE));
-  return v;
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 15, 15, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 15, 15, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 15, 15, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 15, 15, true));
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(r[0], r[1]);
+  const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(h[0], h[1]);
 }
 
 // Exponent byte of a block whose largest magnitude has the bits `top`: the power of two
@@ -98,93 +105,92 @@ template <>
 struct Vec4<float> { using type = floatx4; };
 template <>
 struct Vec4<bf16> { using type = bf16x4; };
+template <class O>
+struct Vec8;
+template <>
+struct Vec8<float> { typedef float type __attribute__((ext_vector_type(8))); };
+template <>
+struct Vec8<bf16> { using type = bf16x8; };
 
-template <class G>
-__global__ __launch_bounds__(256) void adamw_multi32_kernel(AdamWMulti a) {
-  const int k = entry_of(a.first, a.count, blockIdx.x);
-  const AdamWEntry& t = a.t[k];
-  AdamWConsts c = a.c;
-  c.lr_wd = t.lr_wd;
-  const long n = t.n, base = (long)((int)blockIdx.x - a.first[k]) * CHUNK + 4 * threadIdx.x;
-  const bool vec = t.vec;
-  const G* g = (const G*)t.g;
+// A wave's NB runs of 256 elements from `b0` (in runs) on.
+template <class G, int NB, bool FULL>
+__device__ __forceinline__ void step32(const AdamWEntry& t, const AdamWConsts& c, long b0) {
+  using GV = typename Vec4<G>::type;
+  const long n = t.n, i0 = b0 * 256 + 4 * (threadIdx.x & 63);
   float* m = (float*)t.m;
   float* v = (float*)t.v;
   float pp[NB][4], mm[NB][4], vv[NB][4];
   G gg[NB][4];
 #pragma unroll
   for (int u = 0; u < NB; ++u) {
-    const long i = base + u * 1024;
-    load4<floatx4>((const float*)t.p, i, n, vec, pp[u]);
-    load4<typename Vec4<G>::type>(g, i, n, vec, gg[u]);
-    load4<floatx4>((const float*)m, i, n, vec, mm[u]);
-    load4<floatx4>((const float*)v, i, n, vec, vv[u]);
+    load<FULL, floatx4>((const float*)t.p, i0 + u * 256, n, pp[u]);
+    load<FULL, GV>((const G*)t.g, i0 + u * 256, n, gg[u]);
+    load<FULL, floatx4>((const float*)m, i0 + u * 256, n, mm[u]);
+    load<FULL, floatx4>((const float*)v, i0 + u * 256, n, vv[u]);
   }
 #pragma unroll
   for (int u = 0; u < NB; ++u) {
-    const long i = base + u * 1024;
+    const long i = i0 + u * 256;
     bf16 sh[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       adamw_one(pp[u][e], (float)gg[u][e], mm[u][e], vv[u][e], c);
       sh[e] = f2bf(pp[u][e]);
     }
-    store4<floatx4>(t.p, i, n, vec, pp[u]);
-    store4<floatx4>(m, i, n, vec, mm[u]);
-    store4<floatx4>(v, i, n, vec, vv[u]);
-    if (t.shadow != nullptr) store4<bf16x4>(t.shadow, i, n, vec, sh);
+    store<FULL, floatx4>(t.p, i, n, pp[u]);
+    store<FULL, floatx4>(m, i, n, mm[u]);
+    store<FULL, floatx4>(v, i, n, vv[u]);
+    if (t.shadow != nullptr) store<FULL, bf16x4>(t.shadow, i, n, sh);
   }
 }
 
-template <class G>
-__global__ __launch_bounds__(256) void adamw_multi8_kernel(AdamWMulti a) {
-  const int k = entry_of(a.first, a.count, blockIdx.x);
-  const AdamWEntry& t = a.t[k];
-  AdamWConsts c = a.c;
-  c.lr_wd = t.lr_wd;
+// A wave's NB blocks from b0 on.
+template <class G, int NB, bool FULL>
+__device__ __forceinline__ void step8(const AdamWEntry& t, const AdamWConsts& c, long b0) {
+  using GV = typename Vec4<G>::type;
   const int lane = threadIdx.x & 63;
-  const long n = t.n;
-  const long b0 = (long)((int)blockIdx.x - a.first[k]) * (CHUNK / 256) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NB;
-  const bool vec = t.vec;
-  const G* g = (const G*)t.g;
+  const long n = t.n, i0 = b0 * 256 + 4 * lane;
   uint8_t* m = (uint8_t*)t.m;
   uint8_t* v = (uint8_t*)t.v;
+  const float ibc = 1.f / c.bc2s;
   float pp[NB][4];
   G gg[NB][4];
   uint8_t mc[NB][4], vc[NB][4];
   int me[NB], ve[NB];
 #pragma unroll
   for (int u = 0; u < NB; ++u) {
-    const long i = (b0 + u) * 256 + 4 * lane;
-    load4<floatx4>((const float*)t.p, i, n, vec, pp[u]);
-    load4<typename Vec4<G>::type>(g, i, n, vec, gg[u]);
-    load4<u8x4>((const uint8_t*)m, i, n, vec, mc[u]);
-    load4<u8x4>((const uint8_t*)v, i, n, vec, vc[u]);
-    const bool live = (b0 + u) * 256 < n;
+    const bool live = FULL || (b0 + u) * 256 < n;
     me[u] = live ? t.m_exp[b0 + u] : 0;
     ve[u] = live ? t.v_exp[b0 + u] : 0;
+    load<FULL, u8x4>((const uint8_t*)m, i0 + u * 256, n, mc[u]);
+    load<FULL, u8x4>((const uint8_t*)v, i0 + u * 256, n, vc[u]);
+    load<FULL, GV>((const G*)t.g, i0 + u * 256, n, gg[u]);
+    load<FULL, floatx4>((const float*)t.p, i0 + u * 256, n, pp[u]);
   }
 #pragma unroll
   for (int u = 0; u < NB; ++u) {
-    if ((b0 + u) * 256 >= n) break;
-    const long i = (b0 + u) * 256 + 4 * lane;
+    if (!FULL && (b0 + u) * 256 >= n) break;
+    const long i = i0 + u * 256;
     float mm[4], rr[4];
     bf16 sh[4];
     uint32_t mtop = 0, rtop = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
 #pragma clang fp contract(off)
-      mm[e] = decode_m(mc[u][e], me[u]);
+      const float g = (float)gg[u][e];
       const float r = decode<4>(vc[u][e], ve[u]);
-      float vv = r * r;
-      adamw_one(pp[u][e], (float)gg[u][e], mm[e], vv, c);
-      rr[e] = sqrtf(vv);
-      sh[e] = f2bf(pp[u][e]);
+      mm[e] = c.b1 * decode_m(mc[u][e], me[u]) + c.omb1 * g;
+      rr[e] = __builtin_amdgcn_sqrtf(c.b2 * (r * r) + c.omb2 * g * g);
+      float p = pp[u][e];
+      p = p - c.lr_wd * p;
+      p = p - c.step * mm[e] * __builtin_amdgcn_rcpf(rr[e] * ibc + c.eps);
+      pp[u][e] = p;
+      sh[e] = f2bf(p);
       mtop = max(mtop, __float_as_uint(mm[e]) & 0x7FFFFFFFu);
       rtop = max(rtop, __float_as_uint(rr[e]));
     }
-    store4<floatx4>(t.p, i, n, vec, pp[u]);
-    if (t.shadow != nullptr) store4<bf16x4>(t.shadow, i, n, vec, sh);
+    store<FULL, floatx4>(t.p, i, n, pp[u]);
+    if (t.shadow != nullptr) store<FULL, bf16x4>(t.shadow, i, n, sh);
     const int em = block_exp<3>(wave_umax(mtop)), er = block_exp<4>(wave_umax(rtop));
     const uint32_t h0 = ((uint32_t)i + t.key) * 0x9E3779B1u;
 #pragma unroll
@@ -198,8 +204,8 @@ __global__ __launch_bounds__(256) void adamw_multi8_kernel(AdamWMulti a) {
       mc[u][e] = (uint8_t)(qm | (int)(mb >> 31) << 7);
       vc[u][e] = (uint8_t)(rr[e] > 0.f ? qr : 0);
     }
-    store4<u8x4>(m, i, n, vec, mc[u]);
-    store4<u8x4>(v, i, n, vec, vc[u]);
+    store<FULL, u8x4>(m, i, n, mc[u]);
+    store<FULL, u8x4>(v, i, n, vc[u]);
     if (lane == 0) {
       t.m_exp[b0 + u] = (uint8_t)em;
       t.v_exp[b0 + u] = (uint8_t)er;
@@ -207,57 +213,85 @@ __global__ __launch_bounds__(256) void adamw_multi8_kernel(AdamWMulti a) {
   }
 }
 
-// The values that 8-bit moments stand for: m and v = r^2 (both exact in fp32; m also in bf16).
-template <class O>
-__global__ __launch_bounds__(256) void adamw_state_kernel(AdamWMulti a) {
+template <class G, int BITS, int NB>
+__global__ __launch_bounds__(256) void adamw_multi_kernel(AdamWMulti a) {
   const int k = entry_of(a.first, a.count, blockIdx.x);
   const AdamWEntry& t = a.t[k];
+  AdamWConsts c = a.c;
+  c.lr_wd = t.lr_wd;
+  const long b0 = ((long)((int)blockIdx.x - a.first[k]) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * NB;
+  const bool full = t.vec && (b0 + NB) * 256 <= t.n;
+  if constexpr (BITS == 32) {
+    if (full) step32<G, NB, true>(t, c, b0);
+    else step32<G, NB, false>(t, c, b0);
+  } else {
+    if (full) step8<G, NB, true>(t, c, b0);
+    else step8<G, NB, false>(t, c, b0);
+  }
+}
+
+// The values that 8-bit moments stand for: m and v = r^2 (both exact in fp32; m also in bf16).  A
+// lane takes eight elements, so that a wave's bf16 values are stored 16 bytes at a time.
+template <class O, int NB, bool FULL>
+__device__ __forceinline__ void values(const AdamWEntry& t, long b0) {
+  using OV = typename Vec8<O>::type;
   const int lane = threadIdx.x & 63;
-  const long n = t.n;
-  const long b0 = (long)((int)blockIdx.x - a.first[k]) * (CHUNK / 256) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * NB;
-  const bool vec = t.vec;
-  uint8_t mc[NB][4], vc[NB][4];
-  int me[NB], ve[NB];
+  const long n = t.n, i0 = b0 * 256 + 8 * lane;
+  constexpr int R = NB / 2;  // rounds of two blocks
+  uint8_t mc[R][8], vc[R][8];
+  int me[R], ve[R];
 #pragma unroll
-  for (int u = 0; u < NB; ++u) {
-    const long i = (b0 + u) * 256 + 4 * lane;
-    load4<u8x4>((const uint8_t*)t.m, i, n, vec, mc[u]);
-    load4<u8x4>((const uint8_t*)t.v, i, n, vec, vc[u]);
-    const bool live = (b0 + u) * 256 < n;
-    me[u] = live ? t.m_exp[b0 + u] : 0;
-    ve[u] = live ? t.v_exp[b0 + u] : 0;
+  for (int u = 0; u < R; ++u) {
+    const long b = b0 + 2 * u + (lane >> 5);
+    const bool live = FULL || b * 256 < n;
+    me[u] = live ? t.m_exp[b] : 0;
+    ve[u] = live ? t.v_exp[b] : 0;
+    load<FULL, u8x8>((const uint8_t*)t.m, i0 + u * 512, n, mc[u]);
+    load<FULL, u8x8>((const uint8_t*)t.v, i0 + u * 512, n, vc[u]);
   }
 #pragma unroll
-  for (int u = 0; u < NB; ++u) {
-    const long i = (b0 + u) * 256 + 4 * lane;
-    O mo[4], vo[4];
+  for (int u = 0; u < R; ++u) {
+    O mo[8], vo[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < 8; ++e) {
       const float r = decode<4>(vc[u][e], ve[u]);
       mo[e] = (O)decode_m(mc[u][e], me[u]);
       vo[e] = (O)(r * r);
     }
-    store4<typename Vec4<O>::type>((O*)t.m_out, i, n, vec, mo);
-    store4<typename Vec4<O>::type>((O*)t.v_out, i, n, vec, vo);
+    store<FULL, OV>((O*)t.m_out, i0 + u * 512, n, mo);
+    store<FULL, OV>((O*)t.v_out, i0 + u * 512, n, vo);
   }
+}
+
+template <class O, int NB>
+__global__ __launch_bounds__(256) void adamw_state_kernel(AdamWMulti a) {
+  const int k = entry_of(a.first, a.count, blockIdx.x);
+  const AdamWEntry& t = a.t[k];
+  const long b0 = ((long)((int)blockIdx.x - a.first[k]) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * NB;
+  if (t.vec && (b0 + NB) * 256 <= t.n) values<O, NB, true>(t, b0);
+  else values<O, NB, false>(t, b0);
 }
 
 }  // namespace
 
-long adamw_chunks(long n) { return (n + CHUNK - 1) / CHUNK; }
+template <class G, int BITS>
+static void step(const AdamWMulti& a, dim3 grid, int chunk, hipStream_t s) {
+  if (chunk == kAdamWMultiChunk) hipLaunchKernelGGL((adamw_multi_kernel<G, BITS, 4>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((adamw_multi_kernel<G, BITS, 1>), grid, dim3(256), 0, s, a);
+}
 
-hipError_t launch_adamw_multi(const AdamWMulti& a, int chunks, int bits, bool grad_bf16, hipStream_t s) {
-  const dim3 grid((unsigned)chunks), block(256);
-  if (bits == 32 && grad_bf16) hipLaunchKernelGGL(adamw_multi32_kernel<bf16>, grid, block, 0, s, a);
-  else if (bits == 32) hipLaunchKernelGGL(adamw_multi32_kernel<float>, grid, block, 0, s, a);
-  else if (grad_bf16) hipLaunchKernelGGL(adamw_multi8_kernel<bf16>, grid, block, 0, s, a);
-  else hipLaunchKernelGGL(adamw_multi8_kernel<float>, grid, block, 0, s, a);
+hipError_t launch_adamw_multi(const AdamWMulti& a, int chunks, int chunk, int bits, bool grad_bf16, hipStream_t s) {
+  const dim3 grid((unsigned)chunks);
+  if (bits == 32 && grad_bf16) step<bf16, 32>(a, grid, chunk, s);
+  else if (bits == 32) step<float, 32>(a, grid, chunk, s);
+  else if (grad_bf16) step<bf16, 8>(a, grid, chunk, s);
+  else step<float, 8>(a, grid, chunk, s);
   return hipGetLastError();
 }
 
 hipError_t launch_adamw_state(const AdamWMulti& a, int chunks, bool out_bf16, hipStream_t s) {
-  const dim3 grid((unsigned)chunks), block(256);
-  if (out_bf16) hipLaunchKernelGGL(adamw_state_kernel<bf16>, grid, block, 0, s, a);
-  else hipLaunchKernelGGL(adamw_state_kernel<float>, grid, block, 0, s, a);
+  const dim3 grid((unsigned)chunks);
+  if (out_bf16) hipLaunchKernelGGL((adamw_state_kernel<bf16, 4>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((adamw_state_kernel<float, 4>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }

@@ -316,7 +316,7 @@ AdamWConsts adamw_consts(double lr, double beta1, double beta2, double eps, doub
 hipError_t launch_adamw(float* p, const float* g, float* m, float* v, bf16* shadow, long n,
                         const AdamWConsts& c, hipStream_t s);
 // One AdamW step over many tensors (adamw_multi.hip).  A launch takes up to kAdamWEntries
-// tensors, entry k's chunks are workgroups first[k] .. first[k + 1] - 1 (adamw_chunks(n) each).
+// tensors, entry k's chunks are workgroups first[k] .. first[k + 1] - 1.
 // vec: every array of the entry is aligned for four elements at once.
 struct AdamWEntry {
   float* p;
@@ -343,9 +343,10 @@ struct AdamWMulti {
   AdamWEntry t[kAdamWEntries];
 };
 static_assert(sizeof(AdamWMulti) <= 4096, "kernel arguments");
-long adamw_chunks(long n);
-hipError_t launch_adamw_multi(const AdamWMulti& a, int chunks, int bits, bool grad_bf16, hipStream_t s);
-// The values of 8-bit moments to m_out and v_out.
+// Elements of a workgroup, and of one where the whole table has too few for 1024 workgroups.
+constexpr int kAdamWMultiChunk = 4096, kAdamWMultiSmall = 1024;
+hipError_t launch_adamw_multi(const AdamWMulti& a, int chunks, int chunk, int bits, bool grad_bf16, hipStream_t s);
+// The values of 8-bit moments to m_out and v_out; chunks of kAdamWMultiChunk.
 hipError_t launch_adamw_state(const AdamWMulti& a, int chunks, bool out_bf16, hipStream_t s);
 // One piece of the trainable parameters for the segmented AdamW below.
 // Flat segment (toff < 0): n = rows elements at off.  Matrix segment: the

@@ -148,14 +148,15 @@ static uint32_t dither_key(uint64_t seed, int64_t t, int j) {
 
 // Fills launches of up to kAdamWEntries tensors and hands each to `go` (chunks, arguments).
 template <class Fill, class Go>
-static hipError_t over_tensors(const sat_adamw_tensor* t, int32_t count, const AdamWConsts& c, Fill fill, Go go) {
+static hipError_t over_tensors(const sat_adamw_tensor* t, int32_t count, int chunk, const AdamWConsts& c, Fill fill,
+                               Go go) {
   AdamWMulti a;
   a.c = c;
   a.count = 0;
   int64_t chunks = 0;
   for (int k = 0; k < count; ++k) {
     if (t[k].n == 0) continue;
-    const int64_t more = adamw_chunks(t[k].n);
+    const int64_t more = (t[k].n + chunk - 1) / chunk;
     if (a.count == kAdamWEntries || chunks + more > 0x7FFFFFFF) {
       const hipError_t e = go(a, (int)chunks);
       if (e != hipSuccess) return e;
@@ -182,18 +183,21 @@ extern "C" sat_status sat_op_adamw_multi(const sat_adamw_tensor* t, int32_t coun
   SAT_CHECK_ARG(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1 && eps >= 0 && isfinite(lr),
                 "%s: betas must be in [0, 1), eps >= 0 and lr finite", fn);
   const uintptr_t ga = grad_bf16 ? 2 : 4, sa = state_bits == 8 ? 1 : 4;
+  int64_t total = 0;
   for (int k = 0; k < count; ++k) {
     const sat_adamw_tensor& e = t[k];
     SAT_CHECK_ARG(e.n >= 0 && e.n <= kMaxN, "%s: tensor %d has n=%ld", fn, k, (long)e.n);
     if (e.n == 0) continue;
+    total += e.n;
     SAT_CHECK_ARG(e.p && e.g && e.m && e.v && (state_bits == 32 || (e.m_exp && e.v_exp)), "%s: tensor %d: null pointer",
                   fn, k);
     SAT_CHECK_ARG(aligned(e.p, 4) && aligned(e.g, ga) && aligned(e.m, sa) && aligned(e.v, sa) && aligned(e.shadow, 2),
                   "%s: tensor %d: arrays must be aligned to their elements", fn, k);
   }
   const AdamWConsts c = adamw_consts(lr, beta1, beta2, eps, 0.0, step);
+  const int chunk = total < 1024LL * kAdamWMultiChunk ? kAdamWMultiSmall : kAdamWMultiChunk;
   SAT_HIP(over_tensors(
-      t, count, c,
+      t, count, chunk, c,
       [&](int k, AdamWEntry& o) {
         const sat_adamw_tensor& e = t[k];
         o.p = e.p; o.g = e.g; o.m = e.m; o.v = e.v; o.m_exp = e.m_exp; o.v_exp = e.v_exp;
@@ -206,7 +210,7 @@ extern "C" sat_status sat_op_adamw_multi(const sat_adamw_tensor* t, int32_t coun
                 aligned(e.shadow, 8);
       },
       [&](const AdamWMulti& a, int chunks) {
-        return launch_adamw_multi(a, chunks, state_bits, grad_bf16 != 0, S(stream));
+        return launch_adamw_multi(a, chunks, chunk, state_bits, grad_bf16 != 0, S(stream));
       }));
   return SAT_OK;
 }
@@ -227,14 +231,14 @@ extern "C" sat_status sat_op_adamw_multi_state(const sat_adamw_tensor* t, int32_
   AdamWConsts none;
   memset(&none, 0, sizeof none);
   SAT_HIP(over_tensors(
-      t, count, none,
+      t, count, kAdamWMultiChunk, none,
       [&](int k, AdamWEntry& o) {
         const sat_adamw_tensor& e = t[k];
         memset(&o, 0, sizeof o);
         o.m = e.m; o.v = e.v; o.m_exp = e.m_exp; o.v_exp = e.v_exp;
         o.m_out = m_out[k]; o.v_out = v_out[k];
         o.n = e.n;
-        o.vec = aligned(e.m, 4) && aligned(e.v, 4) && aligned(m_out[k], 4 * oa) && aligned(v_out[k], 4 * oa);
+        o.vec = aligned(e.m, 8) && aligned(e.v, 8) && aligned(m_out[k], 8 * oa) && aligned(v_out[k], 8 * oa);
       },
       [&](const AdamWMulti& a, int chunks) { return launch_adamw_state(a, chunks, out_bf16 != 0, S(stream)); }));
   return SAT_OK;
