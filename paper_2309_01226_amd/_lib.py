@@ -186,4 +186,4 @@ def check(status):
 
 def call(name, *args):
     """Call a sat_* function that returns a status; raise on failure."""
-    return check(getattr(lib(), name)(*args))
+    return check(getattr(_lib or lib(), name)(*args))

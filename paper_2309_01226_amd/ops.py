@@ -20,7 +20,8 @@ def _ptr(t):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    """The current stream's handle (without the torch.cuda.Stream object, which takes 3 us to make)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _need(t, dtype, name):
@@ -254,60 +255,71 @@ def maxpool_bwd(dy, arg, N, H, W, C):
 
 # ---------------------------------------------------------------- packed rows
 
-def _here(t, dtype, name):
-    """t: a tensor of `dtype` on the current device (the calls run on its current stream)."""
-    _need(t, dtype, name)
-    if t is not None and t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+def _here(t, dtype, name, dev):
+    """t: a tensor of `dtype` on the current device `dev` (the calls run on its current stream)."""
+    if not t.is_cuda or t.dtype != dtype:
+        _need(t, dtype, name)
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{dev}")
 
 
-def _rows_of(t, dtype, name, rows, cols):
+def _device(t, name):
+    """The current device, for a call on `t`, which has to be on some GPU."""
+    if not t.is_cuda:
+        raise TypeError(f"{name}: expected a CUDA tensor, got {t.device}")
+    return torch.cuda.current_device()
+
+
+def _rows_of(t, dtype, name, rows, cols, dev):
     """Leading dimension of a matrix of at least `rows` rows and `cols` columns, columns contiguous."""
-    _here(t, dtype, name)
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < cols or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: expected [{rows}, >= {cols}] with contiguous rows, got {tuple(t.shape)} "
-                         f"strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    _here(t, dtype, name, dev)
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] < rows or shape[1] < cols or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name}: expected [{rows}, >= {cols}] with contiguous rows, got {tuple(shape)} "
+                         f"strides {stride}")
+    return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
 
 
-def _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window):
+def _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev):
     T = q.shape[0]
-    bf = torch.bfloat16
-    d = _lib.sat_attn_packed_desc(
-        q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), o=o.data_ptr(), lse=lse.data_ptr(), cu=cu.data_ptr(),
-        ldq=_rows_of(q, bf, "q", T, H * dh), ldk=_rows_of(k, bf, "k", T, Hkv * dh),
-        ldv=_rows_of(v, bf, "v", T, Hkv * dh), ldo=_rows_of(o, bf, "o", T, H * dh),
-        n_seq=cu.numel() - 1, T=T, H=H, Hkv=Hkv, dh=dh, causal=int(causal), window=window, scale=scale)
-    _here(lse, torch.float32, "lse")
-    _here(cu, torch.int32, "cu")
-    if cu.dim() != 1 or cu.numel() < 1 or not cu.is_contiguous():
+    bf, wq, wk = torch.bfloat16, H * dh, Hkv * dh
+    _here(lse, torch.float32, "lse", dev)
+    _here(cu, torch.int32, "cu", dev)
+    n = cu.shape
+    if len(n) != 1 or n[0] < 1 or not cu.is_contiguous():
         raise ValueError("cu: expected a contiguous vector of n_seq + 1 row numbers")
     if tuple(lse.shape) != (H, T) or not lse.is_contiguous():
         raise ValueError(f"lse: expected a contiguous [{H}, {T}], got {tuple(lse.shape)}")
-    return d
+    # in the order of the C struct
+    return _lib.sat_attn_packed_desc(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), _rows_of(q, bf, "q", T, wq, dev), _rows_of(k, bf, "k", T, wk, dev),
+        _rows_of(v, bf, "v", T, wk, dev), o.data_ptr(), _rows_of(o, bf, "o", T, wq, dev), lse.data_ptr(), cu.data_ptr(),
+        n[0] - 1, T, H, Hkv, dh, bool(causal), window, scale)
 
 
 def attention_packed_fwd(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, *, window=0):
     """Attention inside packed sequences: rows cu[s] .. cu[s + 1] - 1 of q, o [T, >= H dh] and
     k, v [T, >= Hkv dh] (bf16, views of a wider buffer allowed) are sequence s; lse fp32 [H, T].
     See saturn_ops.h for the masks."""
-    d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window)
-    _lib.call("sat_op_attention_packed_fwd", C.byref(d), _stream())
+    d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, _device(q, "q"))
+    _lib.call("sat_op_attention_packed_fwd", d, _stream())
 
 
 def attention_packed_bwd(q, k, v, o, lse, cu, dout, dq, dk, dv, H, Hkv, dh, causal, scale, *, window=0):
     """Its backward from dout [T, >= H dh] and the forward's o and lse; writes dq, dk, dv.
     The workspace comes from torch's allocator, on the current stream."""
-    d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window)
-    bf = torch.bfloat16
-    for n, t, w in (("dout", dout, H), ("dq", dq, H), ("dk", dk, Hkv), ("dv", dv, Hkv)):
-        setattr(d, n, t.data_ptr())
-        setattr(d, "lddo" if n == "dout" else "ld" + n, _rows_of(t, bf, n, d.T, w * dh))
+    dev = _device(q, "q")
+    d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev)
+    bf, T, wq, wk = torch.bfloat16, d.T, H * dh, Hkv * dh
+    d.dout, d.lddo = dout.data_ptr(), _rows_of(dout, bf, "dout", T, wq, dev)
+    d.dq, d.lddq = dq.data_ptr(), _rows_of(dq, bf, "dq", T, wq, dev)
+    d.dk, d.lddk = dk.data_ptr(), _rows_of(dk, bf, "dk", T, wk, dev)
+    d.dv, d.lddv = dv.data_ptr(), _rows_of(dv, bf, "dv", T, wk, dev)
     need = C.c_int64()
-    _lib.call("sat_op_attention_packed_bwd_ws", C.byref(d), C.byref(need))
+    _lib.call("sat_op_attention_packed_bwd_ws", d, need)
     ws = torch.empty(max(1, need.value), device=q.device, dtype=torch.float32)
-    d.ws, d.ws_elems = ws.data_ptr(), ws.numel()
-    _lib.call("sat_op_attention_packed_bwd", C.byref(d), _stream())
+    d.ws, d.ws_elems = ws.data_ptr(), need.value
+    _lib.call("sat_op_attention_packed_bwd", d, _stream())
 
 
 def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=True, own_freqs=False, inverse=False):
@@ -316,13 +328,13 @@ def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=Tru
     See saturn_ops.h.  Returns the rotated tensor."""
     f32 = x.dtype == torch.float32
     dt = torch.float32 if f32 else torch.bfloat16
-    T = x.shape[0]
+    T, A, dev = x.shape[0], len(pairs), _device(x, "x")
     y = x if out is None else out
-    ldx, ldy = _rows_of(x, dt, "x", T, H * dh), _rows_of(y, dt, "out", T, H * dh)
-    ldp = _rows_of(pos, torch.int32, "pos", T, len(pairs))
-    n = (C.c_int32 * len(pairs))(*pairs)
-    _lib.call("sat_op_rotary_axes", _p(x), ldx, _p(y), ldy, int(f32), _p(pos), ldp, len(pairs), n, T, H, dh,
-              float(base), int(interleaved), int(own_freqs), int(inverse), _stream())
+    ldx = _rows_of(x, dt, "x", T, H * dh, dev)
+    ldy = ldx if out is None else _rows_of(out, dt, "out", T, H * dh, dev)
+    ldp = _rows_of(pos, torch.int32, "pos", T, A, dev)
+    _lib.call("sat_op_rotary_axes", x.data_ptr(), ldx, y.data_ptr(), ldy, f32, pos.data_ptr(), ldp, A,
+              (C.c_int32 * A)(*pairs), T, H, dh, base, interleaved, own_freqs, inverse, _stream())
     return y
 
 
@@ -352,10 +364,10 @@ class AdamWTensors:
             raise ValueError("one of everything for each parameter")
         dtypes = dict(params=torch.float32, grads=torch.bfloat16 if self.grad_bf16 else torch.float32, m=st, v=st,
                       shadows=torch.bfloat16, m_exp=torch.uint8, v_exp=torch.uint8)
-        written, read = [], []
+        written, read, dev = [], [], _device(params[0], "params[0]") if n else None
         for name, ts in lists.items():
             for i, t in enumerate(ts):
-                _here(t, dtypes[name], f"{name}[{i}]")
+                _here(t, dtypes[name], f"{name}[{i}]", dev)
                 want = params[i].numel() if not name.endswith("_exp") else -(-params[i].numel() // 256)
                 if not t.is_contiguous() or t.numel() != want:
                     raise ValueError(f"{name}[{i}]: expected {want} contiguous elements, got {tuple(t.shape)}")
@@ -368,7 +380,7 @@ class AdamWTensors:
                 raise ValueError(f"{what} overlaps {last[0]}")
             if b > end:
                 end, last = b, (what, w)
-        self.tensors = lists
+        self.tensors, self.device = lists, dev
         self.table = (_lib.sat_adamw_tensor * n)()
         for i, e in enumerate(self.table):
             e.p, e.g, e.m, e.v = (lists[x][i].data_ptr() for x in ("params", "grads", "m", "v"))
@@ -381,8 +393,8 @@ class AdamWTensors:
 def adamw_multi(tensors, lr, beta1, beta2, eps, t, *, seed=0):
     """One AdamW step t (>= 1) on all of `tensors` (AdamWTensors); seed: of the rounding of 8-bit moments."""
     _on_device(tensors)
-    _lib.call("sat_op_adamw_multi", tensors.table, len(tensors.table), tensors.bits, int(tensors.grad_bf16),
-              float(lr), float(beta1), float(beta2), float(eps), t, seed & 0xFFFFFFFFFFFFFFFF, _stream())
+    _lib.call("sat_op_adamw_multi", tensors.table, len(tensors.table), tensors.bits, tensors.grad_bf16, lr, beta1, beta2,
+              eps, t, seed & 0xFFFFFFFFFFFFFFFF, _stream())
 
 
 def adamw_multi_state(tensors, m_out, v_out):
@@ -394,15 +406,16 @@ def adamw_multi_state(tensors, m_out, v_out):
     if len(m_out) != n or len(v_out) != n:
         raise ValueError("adamw_multi_state: one output of each kind for each parameter")
     dt = torch.bfloat16 if n and m_out[0].dtype == torch.bfloat16 else torch.float32
-    for i in range(n):
-        for name, t in (("m_out", m_out[i]), ("v_out", v_out[i])):
-            _here(t, dt, f"{name}[{i}]")
-            if not t.is_contiguous() or t.numel() != tensors.table[i].n:
-                raise ValueError(f"{name}[{i}]: expected {tensors.table[i].n} contiguous elements, got {tuple(t.shape)}")
+    want = [e.n for e in tensors.table]
+    for name, ts in (("m_out", m_out), ("v_out", v_out)):
+        for i, t in enumerate(ts):
+            _here(t, dt, f"{name}[{i}]", tensors.device)
+            if not t.is_contiguous() or t.numel() != want[i]:
+                raise ValueError(f"{name}[{i}]: expected {want[i]} contiguous elements, got {tuple(t.shape)}")
     ms, vs = ((C.c_void_p * n)(*[t.data_ptr() for t in ts]) for ts in (m_out, v_out))
-    _lib.call("sat_op_adamw_multi_state", tensors.table, n, ms, vs, int(dt == torch.bfloat16), _stream())
+    _lib.call("sat_op_adamw_multi_state", tensors.table, n, ms, vs, dt == torch.bfloat16, _stream())
 
 
 def _on_device(tensors):
-    for t in tensors.tensors["params"][:1]:
-        _here(t, torch.float32, "params[0]")
+    if tensors.device not in (None, torch.cuda.current_device()):
+        raise ValueError(f"params: on cuda:{tensors.device}, but the current device is cuda:{torch.cuda.current_device()}")
