@@ -28,10 +28,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_fwd_kernel(AttnPackedA
   constexpr int TILE = KB * DH, WGR = NW * WR;
   __shared__ __attribute__((aligned(1024))) bf16 smem[2 * 2 * TILE];  // 2 stages x (K, V)
   const int G = a.H / a.Hkv;
-  int tile, kvh, part, s0, S, blk;
+  int tile, kvh, part, s0, S, qb;
   if (!packed_item(a, G, tile, kvh, part)) return;
-  if (!find_rows(a, tile, WGR, s0, S, blk)) return;
-  const int qb = a.causal ? (S + WGR - 1) / WGR - 1 - blk : blk;  // causal: heaviest first
+  if (!find_rows(a, tile, WGR, a.causal, s0, S, qb)) return;
   const int h = kvh * G + part;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -102,10 +101,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
   __shared__ __attribute__((aligned(1024))) bf16 smem[2 * 2 * TILE];  // 2 stages x (K, V)
   const AttnPackedArgs& a = ba.f;
   const int G = a.H / a.Hkv;
-  int tile, kvh, part, s0, S, blk;
+  int tile, kvh, part, s0, S, qb;
   if (!packed_item(a, G, tile, kvh, part)) return;
-  if (!find_rows(a, tile, WGR, s0, S, blk)) return;
-  const int qb = a.causal ? (S + WGR - 1) / WGR - 1 - blk : blk;
+  if (!find_rows(a, tile, WGR, a.causal, s0, S, qb)) return;
   const int h = kvh * G + part;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -191,11 +189,12 @@ __global__ __launch_bounds__(64 * NW, DH == 128 ? 1 : 2) void attn_packed_dkdv_k
   const int G = a.H / a.Hkv;
   int tile, kvh, part, s0, S, blk;
   if (!packed_item(a, 1, tile, kvh, part)) return;
-  if (!find_rows(a, tile, WGR, s0, S, blk)) return;
+  if (!find_rows(a, tile, WGR, a.causal, s0, S, blk)) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5;
-  const int k0 = blk * WGR;  // causal: the first keys see the most queries
+  // causal: the first keys see the most queries, so the places count from the end
+  const int k0 = (a.causal ? (S + WGR - 1) / WGR - 1 - blk : blk) * WGR;
   const int kmin = k0 + wave * WR;
   const int key = kmin + (lane & 31);
   const float sc = a.scale * LOG2E;

@@ -231,7 +231,8 @@ struct AttnPackedArgs {
   int n_seq, T, H, Hkv, dh;
   int causal, window;  // window: 1 .. 2^30 (no window)
   float scale;
-  int ntile, run;      // set by the launchers: numbered blocks, blocks of a unit (attn_packed.h)
+  // set by the launchers (attn_packed.h): blocks, parts that a K / V head's blocks are dealt to, blocks of a part
+  int ntile, parts, run;
 };
 struct AttnPackedBwdArgs {
   AttnPackedArgs f;

@@ -23,8 +23,8 @@ static sat_status packed_sizes(const sat_attn_packed_desc* d, const char* fn) {
                 "%s: H=%d must be a positive multiple of Hkv=%d", fn, d->H, d->Hkv);
   SAT_CHECK_ARG(d->dh >= 8 && d->dh <= 256 && d->dh % 8 == 0,
                 "%s: head dim %d must be a multiple of 8 up to 256", fn, d->dh);
-  // workgroups of the smallest blocks (64 rows), in units of up to 16 blocks
-  SAT_CHECK_ARG(((int64_t)d->T / 64 + d->n_seq + 256) * d->H < (1LL << 31), "%s: too many rows x heads", fn);
+  // workgroups of the smallest blocks (64 rows), a whole number of them for each of up to 8 parts
+  SAT_CHECK_ARG(((int64_t)d->T / 64 + d->n_seq + 8) * d->H < (1LL << 31), "%s: too many rows x heads", fn);
   return SAT_OK;
 }
 
@@ -50,7 +50,7 @@ static sat_status packed_args(const sat_attn_packed_desc* d, AttnPackedArgs* out
   a.causal = d->causal != 0;
   a.window = d->window == 0 || d->window > (1 << 30) ? 1 << 30 : d->window;
   a.scale = d->scale;
-  a.ntile = a.run = 0;
+  a.ntile = a.parts = a.run = 0;
   return SAT_OK;
 }
 
