@@ -42,82 +42,94 @@ __device__ __forceinline__ int nth_bit(uint64_t mask, int n) {
 // start.  False: no such block.  16384 rows of 32 documents, 16 heads of 64, causal, dK / dV: 148 us in the
 // order of the rows, 131 by work.
 constexpr int kSortedSeqs = 256;
+// Of `C` sequences a lane: block counts nb, sequences s .. e.
+template <int C>
+__device__ __forceinline__ bool sorted_block(const AttnPackedArgs& a, int rank, int R, bool by_place, int& s0, int& S,
+                                             int& blk) {
+  const int lane = threadIdx.x & 63;
+  int s[C], e[C], nb[C], most = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int i = min(lane + 64 * c, a.n_seq - 1);
+    s[c] = row_at(a, i);
+    e[c] = row_at(a, i + 1);
+    nb[c] = lane + 64 * c < a.n_seq ? (max(e[c], s[c]) - s[c] + R - 1) / R : 0;
+    most = max(most, nb[c]);
+  }
+  auto beyond = [&](int x) {
+    int n = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) n += by_place ? max(0, nb[c] - x) : nb[c] > x ? nb[c] : 0;
+    return wave_all(n, [](int p, int q) { return p + q; });
+  };
+  int lo = 0, hi = wave_all(most, [](int p, int q) { return max(p, q); }), at_hi = 0;
+  if (rank >= beyond(0)) return false;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1, n = beyond(mid);
+    if (n > rank) {
+      lo = mid;
+    } else {
+      hi = mid;
+      at_hi = n;
+    }
+  }
+  int k = rank - at_hi;  // among the blocks of level lo
+  const int of = by_place ? 1 : lo + 1;
+  int seq = by_place ? k : k / of;
+  blk = by_place ? lo : k - seq * of;
+  s0 = S = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const uint64_t on = __builtin_amdgcn_ballot_w64(by_place ? nb[c] > lo : nb[c] == lo + 1);
+    const int n = (int)__popcll(on);
+    if (seq >= 0 && seq < n) {
+      const int i = nth_bit(on, seq);
+      s0 = __builtin_amdgcn_readlane(s[c], i);
+      S = __builtin_amdgcn_readlane(e[c], i) - s0;
+    }
+    seq -= n;  // below 0 from there on
+  }
+  return true;
+}
+
 __device__ __forceinline__ bool find_rows(const AttnPackedArgs& a, int rank, int R, bool by_place, int& s0, int& S, int& blk) {
   const int lane = threadIdx.x & 63;
-  if (a.n_seq <= kSortedSeqs) {
-    int nb[4], most = 0;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int i = lane + 64 * c;
-      nb[c] = 0;
-      if (i < a.n_seq) {
-        const int s = row_at(a, i);
-        nb[c] = (max(row_at(a, i + 1), s) - s + R - 1) / R;
-      }
-      most = max(most, nb[c]);
-    }
-    auto beyond = [&](int x) {
-      int n = 0;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) n += by_place ? max(0, nb[c] - x) : nb[c] > x ? nb[c] : 0;
-      return wave_all(n, [](int p, int q) { return p + q; });
-    };
-    int lo = 0, hi = wave_all(most, [](int p, int q) { return max(p, q); }), at_hi = 0;
-    if (rank >= beyond(0)) return false;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1, n = beyond(mid);
-      if (n > rank) {
-        lo = mid;
-      } else {
-        hi = mid;
-        at_hi = n;
-      }
-    }
-    int k = rank - at_hi;  // among the blocks of level lo
-    const int of = by_place ? 1 : lo + 1;
-    int seq = k / of;
-    blk = by_place ? lo : k - seq * of;
-    int i = 0;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const uint64_t on = __builtin_amdgcn_ballot_w64(by_place ? nb[c] > lo : nb[c] == lo + 1);
-      const int n = (int)__popcll(on);
-      if (seq >= 0 && seq < n) i = 64 * c + nth_bit(on, seq);
-      seq -= n;  // below 0 from there on
-    }
-    i = __builtin_amdgcn_readfirstlane(i);
-    s0 = row_at(a, i);
-    S = max(row_at(a, i + 1), s0) - s0;
-    return true;
-  }
-  int lo = 0, hi = a.n_seq;
+  if (a.n_seq <= kSortedSeqs)
+    return a.n_seq <= 64 ? sorted_block<1>(a, rank, R, by_place, s0, S, blk)
+                         : sorted_block<4>(a, rank, R, by_place, s0, S, blk);
+  int lo = 0, hi = a.n_seq, s, e;
   for (;;) {
     const int step = (hi - lo + 63) >> 6;
-    const int i = lo + lane * step;
-    const bool at = i < hi && row_at(a, i < hi ? i : lo) / R + i <= rank;
+    const int i = min(lo + lane * step, a.n_seq - 1);
+    s = row_at(a, i);
+    e = row_at(a, i + 1);
+    const bool at = lo + lane * step < hi && s / R + i <= rank;
     const int n = (int)__popcll(__builtin_amdgcn_ballot_w64(at));
     if (n == 0) return false;
+    if (step <= 1) {
+      s0 = __builtin_amdgcn_readlane(s, n - 1);
+      S = __builtin_amdgcn_readlane(e, n - 1) - s0;
+      blk = rank - (s0 / R + lo + n - 1);
+      return blk >= 0 && blk * R < S;
+    }
     lo += (n - 1) * step;
     hi = min(hi, lo + step);
-    if (step <= 1) break;
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  s0 = row_at(a, lo);
-  S = max(row_at(a, lo + 1), s0) - s0;
-  blk = rank - (s0 / R + lo);
-  return blk >= 0 && blk * R < S;
 }
 
 // The workgroup's block number and head.  Workgroups are dealt round-robin over the 8 XCDs, each
-// with its own L2.  An XCD takes one K / V head at a time, all its blocks or, where the heads are no
-// multiple of 8, every parts-th, each for all `per` query heads (or head parts) that read it: the head's K
-// and V come from HBM into one L2 (parts of them), and the XCDs have the same work.
+// with its own L2.  Each K / V head's blocks belong to one XCD or, where the heads are no multiple of 8, every
+// parts-th of them: its K and V come from HBM into one L2 (parts of them), and the XCDs have the same work.
+// An XCD takes the blocks in their order, each for all its heads and the `per` query heads (or head parts) on
+// them: a long block that starts late ends late, since three workgroups share a CU's time.
 __device__ __forceinline__ bool packed_item(const AttnPackedArgs& a, int per, int& rank, int& kv, int& part) {
-  const int id = blockIdx.x, slot = id >> 3, each = a.run * per;
-  const int unit = slot / each * 8 + (id & 7), w = slot % each;
-  kv = unit % a.Hkv;
-  rank = w / per * a.parts + unit / a.Hkv;
+  const int id = blockIdx.x, slot = id >> 3;
+  const int units = a.Hkv * a.parts >> 3;  // of an XCD
+  const int block = slot / (units * per), w = slot - block * units * per;
+  const int unit = w / per * 8 + (id & 7);
   part = w % per;
+  kv = unit % a.Hkv;
+  rank = block * a.parts + unit / a.Hkv;
   return rank < a.ntile;
 }
 
