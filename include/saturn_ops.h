@@ -143,10 +143,12 @@ sat_status sat_op_attention_bwd(const void* q, const void* k, const void* v, int
  * q, k, v, o and dout are 16-byte aligned with leading dimensions that are
  * multiples of 8 and below 2^22, dq, dk, dv 8-byte aligned with multiples of 4;
  * scale > 0.  Outputs overlap no input and no other output.  The backward reads the
- * forward's o and lse; ws is fp32 scratch of ws_elems elements, at least
- * what sat_op_attention_packed_bwd_ws says for the same sizes (it may grow
- * with H, Hkv, dh, T and n_seq only); calls that may overlap need a ws each.  The forward does
- * not read dout and what stands behind it.
+ * forward's o and lse.  ws: fp32 scratch of ws_elems elements, 16-byte aligned.  The
+ * forward uses it where few blocks of queries meet many keys, whose work is then split and joined,
+ * and may have none (NULL); the backward needs at least H T (rounded up to 4) and
+ * splits with more.  The _ws calls say how much each takes at most for the same sizes and
+ * mask; results with and without differ by the order of sums only.  Calls that may overlap need a
+ * ws each.  The forward reads nothing else from dout on.
  * Errors: SAT_EINVAL for null pointers (T > 0), sizes, alignment, or a ws that is too small. */
 typedef struct {
   const void* q;
@@ -170,7 +172,8 @@ typedef struct {
 } sat_attn_packed_desc;
 sat_status sat_op_attention_packed_fwd(const sat_attn_packed_desc* d, void* stream);
 sat_status sat_op_attention_packed_bwd(const sat_attn_packed_desc* d, void* stream);
-/* fp32 elements of ws for these sizes (only n_seq, T, H, Hkv and dh are read). */
+/* fp32 elements of ws for these sizes (n_seq, T, H, Hkv, dh, causal and window are read). */
+sat_status sat_op_attention_packed_fwd_ws(const sat_attn_packed_desc* d, int64_t* elems);
 sat_status sat_op_attention_packed_bwd_ws(const sat_attn_packed_desc* d, int64_t* elems);
 
 /* Rotary on interleaved pairs of the first rd dims of every q and k head, in

@@ -129,6 +129,7 @@ SIGNATURES = {
                                        _F32, _VP]),
     "sat_op_attention_packed_fwd": (C.c_int, [C.POINTER(sat_attn_packed_desc), _VP]),
     "sat_op_attention_packed_bwd": (C.c_int, [C.POINTER(sat_attn_packed_desc), _VP]),
+    "sat_op_attention_packed_fwd_ws": (C.c_int, [C.POINTER(sat_attn_packed_desc), C.POINTER(_I64)]),
     "sat_op_attention_packed_bwd_ws": (C.c_int, [C.POINTER(sat_attn_packed_desc), C.POINTER(_I64)]),
     "sat_op_rotary_axes": (C.c_int, [_VP, _I64, _VP, _I64, _I32, _VP, _I64, _I32, C.POINTER(_I32), _I32, _I32,
                                      _I32, C.c_double, _I32, _I32, _I32, _VP]),

@@ -144,10 +144,9 @@ __device__ __forceinline__ int query_hi(const AttnPackedArgs& a, int k, int S) {
 }  // namespace
 
 // Launch shape for blocks of R rows and `per` workgroups on each block and K / V head: sets
-// a.ntile, a.parts and a.run, returns the workgroups.
+// a.ntile and a.parts, returns the workgroups.
 inline unsigned packed_grid(AttnPackedArgs& a, int R, int per) {
   a.ntile = a.T / R + a.n_seq;
   a.parts = a.Hkv % 8 == 0 ? 1 : a.Hkv % 4 == 0 ? 2 : a.Hkv % 2 == 0 ? 4 : 8;
-  a.run = sat_cdiv(a.ntile, a.parts);
-  return (unsigned)((long)a.Hkv * a.parts * a.run * per);
+  return (unsigned)((long)a.Hkv * a.parts * sat_cdiv(a.ntile, a.parts) * per);
 }

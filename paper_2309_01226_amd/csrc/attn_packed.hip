@@ -9,6 +9,8 @@
 // p is recomputed from lse in the backward.  Products take bf16 operands (p and dS rounded to
 // nearest, at most 2^-8 of the value) and sum in fp32, as do the softmax's statistics, delta and the
 // sums over heads; the results are rounded once.  No atomics: every result has one order of sums.
+// Where the blocks are too few for the chip a block's steps are split among workgroups, whose fp32 partial
+// results a second kernel joins in their order.
 //
 // A workgroup is 2 or 4 waves of 32 rows of one sequence and head; blocks of 64 rows of the
 // other operand stream through LDS (attn_tile.h).  Only blocks that some row's mask
@@ -22,6 +24,39 @@
 
 namespace {
 
+// Part sp of `split` of a block's steps [j0, j1).
+__device__ __forceinline__ void part_of(int sp, int split, int& j0, int& j1) {
+  const int n = j1 - j0, b = j0;
+  j0 = b + (int)((long)sp * n / split);
+  j1 = b + (int)((long)(sp + 1) * n / split);
+}
+
+// Partial results of a part: a wave's accumulators, 64 lanes side by side, at `at` (a part's place in the
+// scratch) + its own share of `regs` registers.
+__device__ __forceinline__ float* wave_share(float* ws, long at, int NW, int regs, int wave) {
+  return ws + ((at * NW + wave) * regs) * 64 + (threadIdx.x & 63) * 4;
+}
+template <int OT>
+__device__ __forceinline__ void put_acc(float* p, const floatx16 (&acc)[OT]) {
+#pragma unroll
+  for (int t = 0; t < OT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<floatx4*>(p + (4 * t + i) * 256) =
+          floatx4{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
+}
+template <int OT>
+__device__ __forceinline__ void add_acc(const float* p, float f, floatx16 (&acc)[OT]) {
+#pragma unroll
+  for (int t = 0; t < OT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const floatx4 x = *reinterpret_cast<const floatx4*>(p + (4 * t + i) * 256);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[t][4 * i + e] = __builtin_fmaf(x[e], f, acc[t][4 * i + e]);
+    }
+}
+
 template <int DH, int NW, bool PAD>
 __global__ __launch_bounds__(64 * NW, 2) void attn_packed_fwd_kernel(AttnPackedArgs a) {
   using C = Cfg<DH>;
@@ -29,9 +64,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_fwd_kernel(AttnPackedA
   __shared__ __attribute__((aligned(1024))) bf16 smem[2 * 2 * TILE];  // 2 stages x (K, V)
   const int G = a.H / a.Hkv;
   int tile, kvh, part, s0, S, qb;
-  if (!packed_item(a, G, tile, kvh, part)) return;
+  if (!packed_item(a, G * a.split, tile, kvh, part)) return;
   if (!find_rows(a, tile, WGR, a.causal, s0, S, qb)) return;
-  const int h = kvh * G + part;
+  const int sp = part % a.split, h = kvh * G + part / a.split;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5;
@@ -51,7 +86,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_fwd_kernel(AttnPackedA
   const float sc = a.scale * LOG2E;
   // blocks of the workgroup [jb, je), those that every query of the wave sees whole [j1, j2),
   // keys that some query of the wave sees [wlo, whi), those of this lane's [lo, hi)
-  const int jb = key_lo(a, q0) / KB, je = (key_hi(a, q0 + WGR - 1, S) + KB - 1) / KB;
+  int jb = key_lo(a, q0) / KB, je = (key_hi(a, q0 + WGR - 1, S) + KB - 1) / KB;
+  part_of(sp, a.split, jb, je);
   const bool idle = wq0 >= S;
   const int wlo = key_lo(a, wq0), whi = idle ? 0 : key_hi(a, wq0 + WR - 1, S);
   const int lo = key_lo(a, q), hi = key_hi(a, q, S);
@@ -72,7 +108,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_fwd_kernel(AttnPackedA
     wait_vm_lgkm0<0>();
     cta_barrier();
   };
-  copy(jb);
+  if (jb < je) copy(jb);  // a part may be empty
   wait_vm_lgkm0<0>();
   cta_barrier();
   int j = jb;
@@ -86,10 +122,47 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_fwd_kernel(AttnPackedA
   }
   for (; j < je; ++j) masked(j);
   st.l = halves_sum(st.l);
+  if (a.split > 1) {
+    float* p = wave_share(a.ws, ((long)tile * a.H + h) * a.split + sp, NW, 16 * C::OT + 4, wave);
+    put_acc<C::OT>(p, st.o);
+    *reinterpret_cast<floatx2*>(p + 16 * C::OT * 64) = floatx2{st.m, st.l};
+    return;
+  }
   if (q < S) {
     const float inv = (st.l > 0.f) ? 1.f / st.l : 0.f;
     store_rowT<DH, PAD>(a.o + (long)(s0 + q) * a.ldo + (long)h * a.dh, st.o, inv, g, a.dh);
     if (g == 0) a.lse[(long)h * a.T + s0 + q] = (st.m + log2f(st.l)) * LN2;
+  }
+}
+
+// Joins the parts of a split forward: each part's o and l under the common maximum.
+template <int DH, int NW, bool PAD>
+__global__ __launch_bounds__(64 * NW) void attn_packed_join_kernel(AttnPackedArgs a) {
+  using C = Cfg<DH>;
+  constexpr int WGR = NW * WR;
+  const int G = a.H / a.Hkv;
+  int tile, kvh, part, s0, S, qb;
+  if (!packed_item(a, G, tile, kvh, part)) return;
+  if (!find_rows(a, tile, WGR, a.causal, s0, S, qb)) return;
+  const int h = kvh * G + part, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int q = qb * WGR + wave * WR + (lane & 31);
+  const long at = ((long)tile * a.H + h) * a.split;
+  auto share = [&](int sp) { return wave_share(a.ws, at + sp, NW, 16 * C::OT + 4, wave); };
+  float m = -INFINITY, l = 0.f;
+  for (int sp = 0; sp < a.split; ++sp) m = fmaxf(m, share(sp)[16 * C::OT * 64]);
+  floatx16 o[C::OT];
+#pragma unroll
+  for (int t = 0; t < C::OT; ++t) o[t] = zero16();
+  for (int sp = 0; sp < a.split; ++sp) {
+    const floatx2 ml = *reinterpret_cast<const floatx2*>(share(sp) + 16 * C::OT * 64);
+    // a part without keys for this query: nothing.  A NaN l stays.
+    const float f = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m);
+    l = __builtin_fmaf(ml[1], f, l);
+    add_acc<C::OT>(share(sp), f, o);
+  }
+  if (q < S) {
+    store_rowT<DH, PAD>(a.o + (long)(s0 + q) * a.ldo + (long)h * a.dh, o, (l > 0.f) ? 1.f / l : 0.f, lane >> 5, a.dh);
+    if (lane < 32) a.lse[(long)h * a.T + s0 + q] = (m + log2f(l)) * LN2;
   }
 }
 
@@ -102,9 +175,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
   const AttnPackedArgs& a = ba.f;
   const int G = a.H / a.Hkv;
   int tile, kvh, part, s0, S, qb;
-  if (!packed_item(a, G, tile, kvh, part)) return;
+  if (!packed_item(a, G * a.split, tile, kvh, part)) return;
   if (!find_rows(a, tile, WGR, a.causal, s0, S, qb)) return;
-  const int h = kvh * G + part;
+  const int sp = part % a.split, h = kvh * G + part / a.split;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5;
@@ -127,13 +200,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc = __builtin_fmaf(bf2f(st.of[c][e]), bf2f(ov[c][e]), acc);
     st.dlt = halves_sum(acc);
-    if (g == 0 && q < S) ba.delta[hs + q] = st.dlt;
+    if (g == 0 && q < S && sp == 0) ba.delta[hs + q] = st.dlt;
   }
 #pragma unroll
   for (int t = 0; t < C::OT; ++t) st.dq[t] = zero16();
   TileOfs<DH, KB> to;
   to.init(lane);
-  const int jb = key_lo(a, q0) / KB, je = (key_hi(a, q0 + WGR - 1, S) + KB - 1) / KB;  // as in the forward
+  int jb = key_lo(a, q0) / KB, je = (key_hi(a, q0 + WGR - 1, S) + KB - 1) / KB;  // as in the forward
+  part_of(sp, a.split, jb, je);
   const bool idle = wq0 >= S;
   const int wlo = key_lo(a, wq0), whi = idle ? 0 : key_hi(a, wq0 + WR - 1, S);
   const int lo = key_lo(a, q), hi = key_hi(a, q, S);
@@ -157,7 +231,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
     wait_vm_lgkm0<0>();
     cta_barrier();
   };
-  copy(jb);
+  if (jb < je) copy(jb);  // a part may be empty
   wait_vm_lgkm0<0>();
   cta_barrier();
   int j = jb;
@@ -174,7 +248,35 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
     cta_barrier();
   }
   for (; j < je; ++j) masked(j);
-  if (q < S) store_rowT<DH, PAD>(ba.dq + (long)(s0 + q) * ba.lddq + (long)h * a.dh, st.dq, a.scale, g, a.dh);
+  if (a.split > 1) put_acc<C::OT>(wave_share(a.ws, ((long)tile * a.H + h) * a.split + sp, NW, 16 * C::OT, wave), st.dq);
+  else if (q < S) store_rowT<DH, PAD>(ba.dq + (long)(s0 + q) * ba.lddq + (long)h * a.dh, st.dq, a.scale, g, a.dh);
+}
+
+// Adds the parts of a split dQ (KV: of a split dK / dV) in their order.
+template <int DH, int NW, bool PAD, bool KV>
+__global__ __launch_bounds__(64 * NW) void attn_packed_add_kernel(AttnPackedBwdArgs ba) {
+  using C = Cfg<DH>;
+  constexpr int WGR = NW * WR, N = KV ? 2 : 1;
+  const AttnPackedArgs& a = ba.f;
+  const int per = KV ? 1 : a.H / a.Hkv;
+  int tile, kvh, part, s0, S, blk;
+  if (!packed_item(a, per, tile, kvh, part)) return;
+  if (!find_rows(a, tile, WGR, a.causal, s0, S, blk)) return;
+  if (KV && a.causal) blk = (S + WGR - 1) / WGR - 1 - blk;
+  const int h = kvh * per + part, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = blk * WGR + wave * WR + (lane & 31);
+  const long at = ((long)tile * (KV ? a.Hkv : a.H) + h) * a.split;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    floatx16 acc[C::OT];
+#pragma unroll
+    for (int t = 0; t < C::OT; ++t) acc[t] = zero16();
+    for (int sp = 0; sp < a.split; ++sp)
+      add_acc<C::OT>(wave_share(a.ws, at + sp, NW, N * 16 * C::OT, wave) + i * 16 * C::OT * 64, 1.f, acc);
+    bf16* out = KV ? (i ? ba.dv + (long)(s0 + row) * ba.lddv : ba.dk + (long)(s0 + row) * ba.lddk)
+                   : ba.dq + (long)(s0 + row) * ba.lddq;
+    if (row < S) store_rowT<DH, PAD>(out + (long)h * a.dh, acc, i ? 1.f : a.scale, lane >> 5, a.dh);
+  }
 }
 
 // dK and dV of one K / V head: the blocks of Q and dO of all its query heads in turn.
@@ -188,7 +290,7 @@ __global__ __launch_bounds__(64 * NW, DH == 128 ? 1 : 2) void attn_packed_dkdv_k
   const AttnPackedArgs& a = ba.f;
   const int G = a.H / a.Hkv;
   int tile, kvh, part, s0, S, blk;
-  if (!packed_item(a, 1, tile, kvh, part)) return;
+  if (!packed_item(a, a.split, tile, kvh, part)) return;
   if (!find_rows(a, tile, WGR, a.causal, s0, S, blk)) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -212,7 +314,8 @@ __global__ __launch_bounds__(64 * NW, DH == 128 ? 1 : 2) void attn_packed_dkdv_k
 
   const int q_start = query_lo(a, k0);
   const int nqb = (query_hi(a, k0 + WGR - 1, S) - q_start + BQ - 1) / BQ;
-  const int total = nqb * G;  // block j of head kvh G + i is step i nqb + j
+  int first = 0, total = nqb * G;  // block j of head kvh G + i is step i nqb + j
+  part_of(part, a.split, first, total);
   float lsd = 0.f;            // wave 0: lse of the next block's query `lane`; wave 1: its delta
 
   auto stage = [&](int it) { return smem + (it & 1) * STG; };
@@ -258,9 +361,11 @@ __global__ __launch_bounds__(64 * NW, DH == 128 ? 1 : 2) void attn_packed_dkdv_k
     next(it);
   };
 
-  fetch(0);
-  wait_vm_lgkm0<0>();
-  publish(0);
+  if (first < total) {
+    fetch(first);
+    wait_vm_lgkm0<0>();
+    publish(first);
+  }
   wait_vm_lgkm0<0>();
   cta_barrier();
 
@@ -268,11 +373,11 @@ __global__ __launch_bounds__(64 * NW, DH == 128 ? 1 : 2) void attn_packed_dkdv_k
   // variants would copy the accumulators)
   const int j1 = min(max((query_lo(a, kmin + WR - 1) - q_start + BQ - 1) / BQ, 0), nqb);
   const int j2 = idle ? j1 : min(max((query_hi(a, kmin, S) - q_start) / BQ, j1), nqb);
-  for (int i = 0; i < G; ++i) {
-    const int i0 = i * nqb;
-    int j = 0;
-    for (; j < j1; ++j) masked(i0 + j, j);
-    for (; j < j2; ++j) {
+  for (int it = first; it < total;) {  // head by head
+    const int i0 = it / nqb * nqb, end = min(total - i0, nqb);
+    int j = it - i0;
+    for (; j < min(j1, end); ++j) masked(i0 + j, j);
+    for (; j < min(j2, end); ++j) {
       const bf16* Qs = stage(i0 + j);
       const float* l2s = reinterpret_cast<const float*>(Qs + 2 * QT);
       if (i0 + j + 1 < total) fetch(i0 + j + 1);
@@ -283,7 +388,14 @@ __global__ __launch_bounds__(64 * NW, DH == 128 ? 1 : 2) void attn_packed_dkdv_k
       }
       next(i0 + j);
     }
-    for (; j < nqb; ++j) masked(i0 + j, j);
+    for (; j < end; ++j) masked(i0 + j, j);
+    it = i0 + end;
+  }
+  if (a.split > 1) {
+    float* p = wave_share(a.ws, ((long)tile * a.Hkv + kvh) * a.split + part, NW, 2 * 16 * C::OT, wave);
+    put_acc<C::OT>(p, st.dk);
+    put_acc<C::OT>(p + 16 * C::OT * 64, st.dv);
+    return;
   }
   if (key < S) {
     store_rowT<DH, PAD>(ba.dk + (long)(s0 + key) * ba.lddk + (long)kvh * a.dh, st.dk, a.scale, g, a.dh);
@@ -291,38 +403,90 @@ __global__ __launch_bounds__(64 * NW, DH == 128 ? 1 : 2) void attn_packed_dkdv_k
   }
 }
 
-// Waves (of 32 rows) per workgroup: four share the staged blocks; two where that leaves CUs
-// idle or where the sequences are mostly too short for four (the idle waves wait).
-int packed_waves(const AttnPackedArgs& a, int per) {
+// Launch shape of one kernel: waves per workgroup, parts of a block's work, scratch.
+struct Plan {
+  int nw, split;
+  long ws;
+};
+enum Pass { FWD, DQ, DKDV };
+
+// Waves (of 32 rows): four share the staged blocks; two where that leaves CUs idle or where the
+// sequences are mostly too short for four (the idle waves wait).
+// Parts: a block's steps (64 keys; of dK / dV, 64 queries of each head) are split where all blocks together would
+// not keep the CUs busy, and where a causal mask without a window makes the longest block the
+// last to end: twice the mean for one sequence, more for sequences of several lengths.  The price is the
+// partial results' way through memory, so that a part keeps at least 8 steps of an average block where
+// CUs are idle, else 32.
+Plan plan(const AttnPackedArgs& a, Pass pass) {
+  const int G = a.H / a.Hkv, per = pass == DKDV ? 1 : G;
   const long rows = a.T / std::max(1, a.n_seq);
-  if ((long)(a.T / 128 + 1) * a.Hkv * per < 192 || rows < 96) return 2;
-  return 4;
+  Plan p;
+  p.nw = (long)(a.T / 128 + 1) * a.Hkv * per < 192 || rows < (pass == FWD ? 96 : 160) ? 2 : 4;
+  const int dh = a.dh <= 64 ? 64 : a.dh <= 80 ? 80 : 128, R = p.nw * WR;
+  const bool tail = a.causal && a.window >= a.T;
+  const long items = (a.T / R + 1) * (long)a.Hkv * per;
+  const long slots = 256L * (4 / p.nw) * (pass == DKDV ? (dh == 128 ? 1 : 2) : dh == 64 ? 3 : 2);
+  const long want = (pass == DKDV && tail ? 4 : 1) * slots;
+  const long steps = std::min(rows, 2L * a.window) / KB * (pass == DKDV ? G : 1) / (a.causal ? 2 : 1);
+  p.split = 1;
+  while (p.split < 16 && items * p.split < want && steps / (2 * p.split) >= (items * p.split < slots ? 8 : 32))
+    p.split *= 2;
+  const int regs = pass == FWD ? 16 * ((dh + 31) / 32) + 4 : (pass == DKDV ? 32 : 16) * ((dh + 31) / 32);
+  p.ws = p.split == 1 ? 0 : (a.T / R + a.n_seq) * (long)a.Hkv * per * p.split * p.nw * regs * 64;
+  return p;
 }
+// The plan that the scratch allows.
+Plan plan_in(const AttnPackedArgs& a, Pass pass) {
+  Plan p = plan(a, pass);
+  if (p.ws > a.ws_elems) p.split = 1;
+  return p;
+}
+
+// Launches the two-wave or the four-wave instance of a kernel.
+#define PACKED_LAUNCH(NW_, GRID, ...)                                                                        \
+  do {                                                                                                       \
+    if ((NW_) == 2) hipLaunchKernelGGL((__VA_ARGS__(2)), GRID, dim3(128), 0, s, a);                          \
+    else hipLaunchKernelGGL((__VA_ARGS__(4)), GRID, dim3(256), 0, s, a);                                     \
+    const hipError_t e_ = hipGetLastError();                                                                 \
+    if (e_ != hipSuccess) return e_;                                                                         \
+  } while (0)
 
 template <int DH, bool PAD>
 hipError_t fwd(AttnPackedArgs a, hipStream_t s) {
-  const int per = a.H / a.Hkv, nw = packed_waves(a, per);
-  const dim3 grid(packed_grid(a, nw * WR, per));
-  if (nw == 2) hipLaunchKernelGGL((attn_packed_fwd_kernel<DH, 2, PAD>), grid, dim3(128), 0, s, a);
-  else hipLaunchKernelGGL((attn_packed_fwd_kernel<DH, 4, PAD>), grid, dim3(256), 0, s, a);
-  return hipGetLastError();
+#define FWD_K(NW) attn_packed_fwd_kernel<DH, NW, PAD>
+#define JOIN_K(NW) attn_packed_join_kernel<DH, NW, PAD>
+  const int per = a.H / a.Hkv;
+  const Plan p = plan_in(a, FWD);
+  a.split = p.split;
+  PACKED_LAUNCH(p.nw, dim3(packed_grid(a, p.nw * WR, per * p.split)), FWD_K);
+  if (p.split > 1) PACKED_LAUNCH(p.nw, dim3(packed_grid(a, p.nw * WR, per)), JOIN_K);
+  return hipSuccess;
 }
 
 template <int DH, bool PAD>
 hipError_t bwd(AttnPackedBwdArgs a, hipStream_t s) {
-  const int per = a.f.H / a.f.Hkv, nq = packed_waves(a.f, per), nk = packed_waves(a.f, 1);
-  const dim3 qgrid(packed_grid(a.f, nq * WR, per));
-  if (nq == 2) hipLaunchKernelGGL((attn_packed_dq_kernel<DH, 2, PAD>), qgrid, dim3(128), 0, s, a);
-  else hipLaunchKernelGGL((attn_packed_dq_kernel<DH, 4, PAD>), qgrid, dim3(256), 0, s, a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const dim3 kgrid(packed_grid(a.f, nk * WR, 1));
-  if (nk == 2) hipLaunchKernelGGL((attn_packed_dkdv_kernel<DH, 2, PAD>), kgrid, dim3(128), 0, s, a);
-  else hipLaunchKernelGGL((attn_packed_dkdv_kernel<DH, 4, PAD>), kgrid, dim3(256), 0, s, a);
-  return hipGetLastError();
+#define DQ_K(NW) attn_packed_dq_kernel<DH, NW, PAD>
+#define ADDQ_K(NW) attn_packed_add_kernel<DH, NW, PAD, false>
+#define DKDV_K(NW) attn_packed_dkdv_kernel<DH, NW, PAD>
+#define ADDKV_K(NW) attn_packed_add_kernel<DH, NW, PAD, true>
+  const int per = a.f.H / a.f.Hkv;
+  Plan p = plan_in(a.f, DQ);
+  a.f.split = p.split;
+  PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, per * p.split)), DQ_K);
+  if (p.split > 1) PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, per)), ADDQ_K);
+  p = plan_in(a.f, DKDV);
+  a.f.split = p.split;
+  PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, p.split)), DKDV_K);
+  if (p.split > 1) PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, 1)), ADDKV_K);
+  return hipSuccess;
 }
 
 }  // namespace
+
+long attn_packed_ws(const AttnPackedArgs& a, bool backward) {
+  if (a.T == 0 || a.n_seq == 0 || a.dh > 128) return 0;
+  return backward ? std::max(plan(a, DQ).ws, plan(a, DKDV).ws) : plan(a, FWD).ws;
+}
 
 hipError_t launch_attn_packed_fwd(const AttnPackedArgs& a, hipStream_t s) {
   if (a.T == 0 || a.n_seq == 0) return hipSuccess;

@@ -231,8 +231,12 @@ struct AttnPackedArgs {
   int n_seq, T, H, Hkv, dh;
   int causal, window;  // window: 1 .. 2^30 (no window)
   float scale;
-  // set by the launchers (attn_packed.h): blocks, parts that a K / V head's blocks are dealt to, blocks of a part
-  int ntile, parts, run;
+  // scratch of ws_elems fp32 elements, may be null: partial results where a block's work is split
+  float* ws;
+  long ws_elems;
+  // set by the launchers (attn_packed.h): blocks, parts that a K / V head's blocks are dealt to, parts of a
+  // block's work
+  int ntile, parts, split;
 };
 struct AttnPackedBwdArgs {
   AttnPackedArgs f;
@@ -244,6 +248,8 @@ struct AttnPackedBwdArgs {
   bf16* dv;
   long lddq, lddk, lddv;
 };
+// fp32 elements of scratch that let the forward, or the backward's dQ and dK / dV, split (0: they would not).
+long attn_packed_ws(const AttnPackedArgs& a, bool backward);
 hipError_t launch_attn_packed_fwd(const AttnPackedArgs& a, hipStream_t s);
 hipError_t launch_attn_packed_bwd(const AttnPackedBwdArgs& a, hipStream_t s);
 hipError_t launch_attn256_packed_fwd(const AttnPackedArgs& a, hipStream_t s);

@@ -50,7 +50,9 @@ static sat_status packed_args(const sat_attn_packed_desc* d, AttnPackedArgs* out
   a.causal = d->causal != 0;
   a.window = d->window == 0 || d->window > (1 << 30) ? 1 << 30 : d->window;
   a.scale = d->scale;
-  a.ntile = a.parts = a.run = 0;
+  a.ws = nullptr;
+  a.ws_elems = 0;
+  a.ntile = a.parts = a.split = 0;
   return SAT_OK;
 }
 
@@ -58,15 +60,39 @@ extern "C" sat_status sat_op_attention_packed_fwd(const sat_attn_packed_desc* d,
   AttnPackedArgs a;
   sat_status st = packed_args(d, &a, "attention_packed_fwd");
   if (st != SAT_OK) return st;
+  SAT_CHECK_ARG(d->ws_elems >= 0 && aligned(d->ws, 16), "attention_packed_fwd: ws must be 16-byte aligned");
+  a.ws = d->ws;
+  a.ws_elems = d->ws ? d->ws_elems : 0;
   SAT_HIP(launch_attn_packed_fwd(a, S(stream)));
   return SAT_OK;
 }
+
+// The part of the arguments that the workspaces depend on.
+static AttnPackedArgs shape_of(const sat_attn_packed_desc* d) {
+  AttnPackedArgs a;
+  memset(&a, 0, sizeof a);
+  a.n_seq = d->n_seq; a.T = d->T; a.H = d->H; a.Hkv = d->Hkv; a.dh = d->dh;
+  a.causal = d->causal != 0;
+  a.window = d->window <= 0 || d->window > (1 << 30) ? 1 << 30 : d->window;
+  return a;
+}
+
+extern "C" sat_status sat_op_attention_packed_fwd_ws(const sat_attn_packed_desc* d, int64_t* elems) {
+  SAT_CHECK_ARG(elems != nullptr, "attention_packed_fwd_ws: null pointer");
+  sat_status st = packed_sizes(d, "attention_packed_fwd_ws");
+  if (st != SAT_OK) return st;
+  *elems = attn_packed_ws(shape_of(d), false);
+  return SAT_OK;
+}
+
+// delta, rounded up so that what follows is aligned.
+static int64_t delta_elems(const sat_attn_packed_desc* d) { return ((int64_t)d->H * d->T + 3) / 4 * 4; }
 
 extern "C" sat_status sat_op_attention_packed_bwd_ws(const sat_attn_packed_desc* d, int64_t* elems) {
   SAT_CHECK_ARG(elems != nullptr, "attention_packed_bwd_ws: null pointer");
   sat_status st = packed_sizes(d, "attention_packed_bwd_ws");
   if (st != SAT_OK) return st;
-  *elems = (int64_t)d->H * d->T;  // delta
+  *elems = delta_elems(d) + attn_packed_ws(shape_of(d), true);
   return SAT_OK;
 }
 
@@ -83,13 +109,13 @@ extern "C" sat_status sat_op_attention_packed_bwd(const sat_attn_packed_desc* d,
   SAT_CHECK_ARG(d->lddq % 4 == 0 && d->lddk % 4 == 0 && d->lddv % 4 == 0 && aligned(d->dq, 8) && aligned(d->dk, 8) &&
                     aligned(d->dv, 8),
                 "%s: dq, dk, dv must be 8-byte aligned with leading dimensions %% 4 == 0", fn);
-  int64_t need = 0;
-  st = sat_op_attention_packed_bwd_ws(d, &need);
-  if (st != SAT_OK) return st;
-  SAT_CHECK_ARG(d->ws_elems >= need && aligned(d->ws, 4), "%s: ws of %ld elements, %ld needed", fn, (long)d->ws_elems,
-                (long)need);
+  const int64_t need = delta_elems(d);
+  SAT_CHECK_ARG(d->ws_elems >= need && aligned(d->ws, 16),
+                "%s: ws of %ld elements, at least %ld needed, 16-byte aligned", fn, (long)d->ws_elems, (long)need);
   a.dout = (const bf16*)d->dout; a.lddo = d->lddo;
   a.delta = d->ws;
+  a.f.ws = d->ws + need;
+  a.f.ws_elems = d->ws_elems - need;
   a.dq = (bf16*)d->dq; a.dk = (bf16*)d->dk; a.dv = (bf16*)d->dv;
   a.lddq = d->lddq; a.lddk = d->lddk; a.lddv = d->lddv;
   SAT_HIP(launch_attn_packed_bwd(a, S(stream)));

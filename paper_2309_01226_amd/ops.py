@@ -298,16 +298,20 @@ def _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev):
 
 
 def attention_packed_fwd(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, *, window=0):
-    """Attention inside packed sequences: rows cu[s] .. cu[s + 1] - 1 of q, o [T, >= H dh] and
+    """Attention inside packed sequences (workspaces come from torch's allocator, on the current stream): rows cu[s] .. cu[s + 1] - 1 of q, o [T, >= H dh] and
     k, v [T, >= Hkv dh] (bf16, views of a wider buffer allowed) are sequence s; lse fp32 [H, T].
     See saturn_ops.h for the masks."""
     d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, _device(q, "q"))
+    need = C.c_int64()
+    _lib.call("sat_op_attention_packed_fwd_ws", d, need)
+    if need.value:
+        ws = torch.empty(need.value, device=q.device, dtype=torch.float32)
+        d.ws, d.ws_elems = ws.data_ptr(), need.value
     _lib.call("sat_op_attention_packed_fwd", d, _stream())
 
 
 def attention_packed_bwd(q, k, v, o, lse, cu, dout, dq, dk, dv, H, Hkv, dh, causal, scale, *, window=0):
-    """Its backward from dout [T, >= H dh] and the forward's o and lse; writes dq, dk, dv.
-    The workspace comes from torch's allocator, on the current stream."""
+    """Its backward from dout [T, >= H dh] and the forward's o and lse; writes dq, dk, dv."""
     dev = _device(q, "q")
     d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev)
     bf, T, wq, wk = torch.bfloat16, d.T, H * dh, Hkv * dh
