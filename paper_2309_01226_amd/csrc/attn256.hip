@@ -224,7 +224,7 @@ __global__ __launch_bounds__(NT, 1) void attn256_fwd_kernel(A a) {
     const int G = a.H / a.Hkv;
     int tile, part, s0;
     if (!packed_item(a, G, tile, kvh, part)) return;
-    if (!find_rows(a, tile, QPB, a.causal, s0, S, qb)) return;
+    if (!find_rows(a, tile, QPB, s0, S, qb)) return;
     h = kvh * G + part;
     row0 = s0;
     lrow = (long)h * a.T + s0;
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(A a) {
     heads = a.f.H / a.f.Hkv;
     int tile, part, s0, blk;
     if (!packed_item(a.f, 1, tile, kvh, part)) return;
-    if (!find_rows(a.f, tile, KPW, a.f.causal, s0, S, blk)) return;
+    if (!find_rows(a.f, tile, KPW, s0, S, blk)) return;
     // causal: the first keys see the most queries, so the places count from the end
     k0 = (a.f.causal ? (S + KPW - 1) / KPW - 1 - blk : blk) * KPW;
     row0 = s0;
@@ -658,7 +658,7 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(A a) {
     const int G = a.f.H / a.f.Hkv;
     int tile, part, s0;
     if (!packed_item(a.f, G, tile, kvh, part)) return;
-    if (!find_rows(a.f, tile, QPW, a.f.causal, s0, S, qb)) return;
+    if (!find_rows(a.f, tile, QPW, s0, S, qb)) return;
     h = kvh * G + part;
     row0 = s0;
     hs = (long)h * a.f.T + s0;

@@ -31,21 +31,24 @@ __device__ __forceinline__ int nth_bit(uint64_t mask, int n) {
 }
 
 // Block number `rank` (R rows each) of all sequences, in the order of their work, the longest first, so
-// that the last blocks to end are short ones.  Nothing is sorted: with nb sequence blocks
-// held by the lanes, causal blocks have the work of their place b, and sum max(0, nb - x)
-// of them a place of x or more; without a mask those of one sequence are alike, and sum [nb > x]
-// nb are in sequences of more than x.  A bisection over x finds the level that holds the rank,
-// bit counts the sequence on it.  Beyond 256 sequences (four a lane) the blocks are short on average and are
+// that the last blocks to end are short ones.  Nothing is sorted: nb is a sequence's number of blocks,
+// held by the lanes.  By place: causal blocks have the work of their place b in the sequence, and sum
+// max(0, nb - x) of them a place of x or more.  By sequence: sum [nb > x] nb blocks are in
+// sequences of more than x, each sequence's own in a row.  A bisection over x finds the level
+// that holds the rank, bit counts the sequence on it.  Causal blocks go by place where sequences are long
+// (1024 rows on average; 256 with 64-wide heads, whose K and V are smallest), by sequence where they are short and what
+// counts is that a sequence's K and V are read once: 4 x 4096 rows, 16 heads of 64, forward 158 against 174
+// us; 24 documents in 8192 rows, 12 heads of 64, 24.3 against 26.5; 32 documents of 64 to 2048 rows, 80-wide, 155 by
+// place, 123 by sequence; dK / dV of 128-wide heads, one workgroup on a CU, always by place (50 images:
+// backward 263 against 283).  Beyond 256 sequences (four a lane) the blocks are short on average and are
 // numbered from first(i) = cu[i] / R + i instead, which leaves each sequence at least as many numbers as it
 // has blocks.  Row numbers are held to [0, T], so no row outside the buffers is touched whatever
-// cu holds.  blk counts from the end of the sequence whose blocks have most work (`by_place`), else from its
-// start.  False: no such block.  16384 rows of 32 documents, 16 heads of 64, causal, dK / dV: 148 us in the
-// order of the rows, 131 by work.
+// cu holds.  blk counts the places in the order of causal work (a query block's own place; a key block's
+// from the end of its sequence).  False: no such block.
 constexpr int kSortedSeqs = 256;
-// Of `C` sequences a lane: block counts nb, sequences s .. e.
+// C sequences a lane.
 template <int C>
-__device__ __forceinline__ bool sorted_block(const AttnPackedArgs& a, int rank, int R, bool by_place, int& s0, int& S,
-                                             int& blk) {
+__device__ __forceinline__ bool sorted_block(const AttnPackedArgs& a, int rank, int R, int& s0, int& S, int& blk) {
   const int lane = threadIdx.x & 63;
   int s[C], e[C], nb[C], most = 0;
 #pragma unroll
@@ -59,7 +62,7 @@ __device__ __forceinline__ bool sorted_block(const AttnPackedArgs& a, int rank, 
   auto beyond = [&](int x) {
     int n = 0;
 #pragma unroll
-    for (int c = 0; c < C; ++c) n += by_place ? max(0, nb[c] - x) : nb[c] > x ? nb[c] : 0;
+    for (int c = 0; c < C; ++c) n += a.by_place ? max(0, nb[c] - x) : nb[c] > x ? nb[c] : 0;
     return wave_all(n, [](int p, int q) { return p + q; });
   };
   int lo = 0, hi = wave_all(most, [](int p, int q) { return max(p, q); }), at_hi = 0;
@@ -74,13 +77,13 @@ __device__ __forceinline__ bool sorted_block(const AttnPackedArgs& a, int rank, 
     }
   }
   int k = rank - at_hi;  // among the blocks of level lo
-  const int of = by_place ? 1 : lo + 1;
-  int seq = by_place ? k : k / of;
-  blk = by_place ? lo : k - seq * of;
+  const int of = a.by_place ? 1 : lo + 1;
+  int seq = a.by_place ? k : k / of;
+  blk = a.by_place ? lo : a.causal ? lo - (k - seq * of) : k - seq * of;
   s0 = S = 0;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const uint64_t on = __builtin_amdgcn_ballot_w64(by_place ? nb[c] > lo : nb[c] == lo + 1);
+    const uint64_t on = __builtin_amdgcn_ballot_w64(a.by_place ? nb[c] > lo : nb[c] == lo + 1);
     const int n = (int)__popcll(on);
     if (seq >= 0 && seq < n) {
       const int i = nth_bit(on, seq);
@@ -92,11 +95,10 @@ __device__ __forceinline__ bool sorted_block(const AttnPackedArgs& a, int rank, 
   return true;
 }
 
-__device__ __forceinline__ bool find_rows(const AttnPackedArgs& a, int rank, int R, bool by_place, int& s0, int& S, int& blk) {
+__device__ __forceinline__ bool find_rows(const AttnPackedArgs& a, int rank, int R, int& s0, int& S, int& blk) {
   const int lane = threadIdx.x & 63;
   if (a.n_seq <= kSortedSeqs)
-    return a.n_seq <= 64 ? sorted_block<1>(a, rank, R, by_place, s0, S, blk)
-                         : sorted_block<4>(a, rank, R, by_place, s0, S, blk);
+    return a.n_seq <= 64 ? sorted_block<1>(a, rank, R, s0, S, blk) : sorted_block<4>(a, rank, R, s0, S, blk);
   int lo = 0, hi = a.n_seq, s, e;
   for (;;) {
     const int step = (hi - lo + 63) >> 6;
@@ -144,9 +146,10 @@ __device__ __forceinline__ int query_hi(const AttnPackedArgs& a, int k, int S) {
 }  // namespace
 
 // Launch shape for blocks of R rows and `per` workgroups on each block and K / V head: sets
-// a.ntile and a.parts, returns the workgroups.
-inline unsigned packed_grid(AttnPackedArgs& a, int R, int per) {
+// a.ntile, a.parts and a.by_place, returns the workgroups.
+inline unsigned packed_grid(AttnPackedArgs& a, int R, int per, bool always_by_place = false) {
   a.ntile = a.T / R + a.n_seq;
+  a.by_place = a.causal && (always_by_place || a.T >= (a.dh <= 64 ? 256L : 1024L) * a.n_seq);
   a.parts = a.Hkv % 8 == 0 ? 1 : a.Hkv % 4 == 0 ? 2 : a.Hkv % 2 == 0 ? 4 : 8;
   return (unsigned)((long)a.Hkv * a.parts * sat_cdiv(a.ntile, a.parts) * per);
 }

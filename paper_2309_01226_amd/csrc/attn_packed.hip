@@ -18,6 +18,7 @@
 // every sequence, read as zeros and are never written.  Heads narrower than 64, 80 or 128
 // dims run in the next wider kernel with zeros behind them; 256-wide ones are in attn256.hip.
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_packed.h"
 #include "attn_tile.h"
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_fwd_kernel(AttnPackedA
   const int G = a.H / a.Hkv;
   int tile, kvh, part, s0, S, qb;
   if (!packed_item(a, G * a.split, tile, kvh, part)) return;
-  if (!find_rows(a, tile, WGR, a.causal, s0, S, qb)) return;
+  if (!find_rows(a, tile, WGR, s0, S, qb)) return;
   const int sp = part % a.split, h = kvh * G + part / a.split;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -143,7 +144,7 @@ __global__ __launch_bounds__(64 * NW) void attn_packed_join_kernel(AttnPackedArg
   const int G = a.H / a.Hkv;
   int tile, kvh, part, s0, S, qb;
   if (!packed_item(a, G, tile, kvh, part)) return;
-  if (!find_rows(a, tile, WGR, a.causal, s0, S, qb)) return;
+  if (!find_rows(a, tile, WGR, s0, S, qb)) return;
   const int h = kvh * G + part, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int q = qb * WGR + wave * WR + (lane & 31);
   const long at = ((long)tile * a.H + h) * a.split;
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
   const int G = a.H / a.Hkv;
   int tile, kvh, part, s0, S, qb;
   if (!packed_item(a, G * a.split, tile, kvh, part)) return;
-  if (!find_rows(a, tile, WGR, a.causal, s0, S, qb)) return;
+  if (!find_rows(a, tile, WGR, s0, S, qb)) return;
   const int sp = part % a.split, h = kvh * G + part / a.split;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -261,7 +262,7 @@ __global__ __launch_bounds__(64 * NW) void attn_packed_add_kernel(AttnPackedBwdA
   const int per = KV ? 1 : a.H / a.Hkv;
   int tile, kvh, part, s0, S, blk;
   if (!packed_item(a, per, tile, kvh, part)) return;
-  if (!find_rows(a, tile, WGR, a.causal, s0, S, blk)) return;
+  if (!find_rows(a, tile, WGR, s0, S, blk)) return;
   if (KV && a.causal) blk = (S + WGR - 1) / WGR - 1 - blk;
   const int h = kvh * per + part, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = blk * WGR + wave * WR + (lane & 31);
@@ -279,9 +280,10 @@ __global__ __launch_bounds__(64 * NW) void attn_packed_add_kernel(AttnPackedBwdA
   }
 }
 
-// dK and dV of one K / V head: the blocks of Q and dO of all its query heads in turn.
+// ================================================================ dK and dV
+// dK and dV of one K / V head, 64- and 80-wide: the blocks of Q and dO of all its query heads in turn.
 template <int DH, int NW, bool PAD>
-__global__ __launch_bounds__(64 * NW, DH == 128 ? 1 : 2) void attn_packed_dkdv_kernel(AttnPackedBwdArgs ba) {
+__global__ __launch_bounds__(64 * NW, 2) void attn_packed_dkdv_kernel(AttnPackedBwdArgs ba) {
   using C = Cfg<DH>;
   constexpr int BQ = KB, WGR = NW * WR;
   constexpr int QT = BQ * DH;
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(64 * NW, DH == 128 ? 1 : 2) void attn_packed_dkdv_k
   const int G = a.H / a.Hkv;
   int tile, kvh, part, s0, S, blk;
   if (!packed_item(a, a.split, tile, kvh, part)) return;
-  if (!find_rows(a, tile, WGR, a.causal, s0, S, blk)) return;
+  if (!find_rows(a, tile, WGR, s0, S, blk)) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 5;
@@ -384,12 +386,226 @@ __global__ __launch_bounds__(64 * NW, DH == 128 ? 1 : 2) void attn_packed_dkdv_k
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         dkdv_sub<DH, false>(st, to, Qs, Qs + QT, l2s, l2s + BQ, u, g, sc, 0, 0);
-        if (DH != 128) __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_sched_barrier(0);
       }
       next(i0 + j);
     }
     for (; j < end; ++j) masked(i0 + j, j);
     it = i0 + end;
+  }
+  if (a.split > 1) {
+    float* p = wave_share(a.ws, ((long)tile * a.Hkv + kvh) * a.split + part, NW, 2 * 16 * C::OT, wave);
+    put_acc<C::OT>(p, st.dk);
+    put_acc<C::OT>(p + 16 * C::OT * 64, st.dv);
+    return;
+  }
+  if (key < S) {
+    store_rowT<DH, PAD>(ba.dk + (long)(s0 + key) * ba.lddk + (long)kvh * a.dh, st.dk, a.scale, g, a.dh);
+    store_rowT<DH, PAD>(ba.dv + (long)(s0 + key) * ba.lddv + (long)kvh * a.dh, st.dv, 1.f, g, a.dh);
+  }
+}
+
+// 128-wide heads.  A wave owns 32 keys and takes 32 queries (a slot) at a time: S = Q K^T and dP = dO V^T with
+// queries as rows (lane = key), P = exp2(S scale log2e - lse2), dS = P (dP - delta), then dV^T += dO^T P and
+// dK^T += Q^T dS.  Its 256 registers of operands and accumulators leave room for one wave on a SIMD, which
+// has to keep the matrix cores busy alone: the products S and dP of the next slot are issued between the
+// exponentials of the current one, and their subtractions between the products dV and dK, in an order
+// that scheduling barriers pin.  4 x 4096 rows, 16 heads, no mask: 1055 us against 1140 with the step that
+// the narrower heads take, whose two waves on a SIMD fill each other's gaps (64: 580 against 570).
+struct Slot {
+  float t[16], u[16];  // S scale log2e - lse2 and dP - delta
+};
+
+// NEXT: the slot of rows Qn, dOn, half un of a block, with its lse2 ln and delta dn, into `nx`.  CUR: `cur`, of
+// rows Qc, dOc, half uc, into dV and dK.
+template <bool NEXT, bool CUR>
+__device__ __forceinline__ void dkdv_step(DkvState<128>& st, const TileOfs<128, KB>& to, const Slot& cur, Slot& nx, const bf16* Qn,
+                                          const float* ln, int un, const bf16* Qc, int uc, int g, float sc) {
+  constexpr int KS = Cfg<128>::KS, OT = Cfg<128>::OT, QT = KB * 128;
+  constexpr int PFR = 3, PFT = 3;  // k-steps, pairs of transposed fragments in flight
+  bf16x8 qr[PFR + 1], dr[PFR + 1], qt[PFT + 1], dt[PFT + 1], pb[2], db[2];
+  floatx16 x, y;
+  auto rows = [&](int c) {
+    qr[c % (PFR + 1)] = to.row(Qn, un, c);
+    dr[c % (PFR + 1)] = to.row(Qn + QT, un, c);
+  };
+  auto cols = [&](int i) {
+    dt[i % (PFT + 1)] = to.trans(Qc + QT, 2 * uc + i / OT, i % OT);
+    qt[i % (PFT + 1)] = to.trans(Qc, 2 * uc + i / OT, i % OT);
+  };
+  if constexpr (NEXT) {
+#pragma unroll
+    for (int c = 0; c < PFR; ++c) rows(c);
+    x = zero16();
+    y = zero16();
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int c = 0; c < KS; ++c) {
+    if constexpr (NEXT) {
+      if (c + PFR < KS) rows(c + PFR);
+      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qr[c % (PFR + 1)], st.kf[c], x, 0, 0, 0);
+      y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dr[c % (PFR + 1)], st.vf[c], y, 0, 0, 0);
+    }
+    if constexpr (CUR) {
+      if (c >= KS - PFT) cols(c - (KS - PFT));
+#pragma unroll
+      for (int r = 16 * c / KS; r < 16 * (c + 1) / KS; ++r) {
+        const float pr = __builtin_amdgcn_exp2f(cur.t[r]);
+        pb[r >> 3][r & 7] = f2bf(pr);
+        db[r >> 3][r & 7] = f2bf(pr * cur.u[r]);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  floatx4 l4[4], d4[4];
+  if constexpr (NEXT) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      l4[i] = *reinterpret_cast<const floatx4*>(ln + 32 * un + 8 * i + 4 * g);
+      d4[i] = *reinterpret_cast<const floatx4*>(ln + KB + 32 * un + 8 * i + 4 * g);
+    }
+  }
+  constexpr int NP = 2 * OT;  // pairs of products; one goes ahead of the first look at x and y
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    if constexpr (CUR) {
+      const int hh = i / OT, ot = i % OT;
+      if (i + PFT < NP) cols(i + PFT);
+      st.dv[ot] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dt[i % (PFT + 1)], pb[hh], st.dv[ot], 0, 0, 0);
+      st.dk[ot] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qt[i % (PFT + 1)], db[hh], st.dk[ot], 0, 0, 0);
+    }
+    if constexpr (NEXT) {
+      if (i >= 1) {
+#pragma unroll
+        for (int r = 16 * (i - 1) / (NP - 1); r < 16 * i / (NP - 1); ++r) {
+          nx.t[r] = __builtin_fmaf(x[r], sc, -l4[r >> 2][r & 3]);
+          nx.u[r] = y[r] - d4[r >> 2][r & 3];
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+template <bool PAD>
+__global__ __launch_bounds__(256, 1) void attn_packed_dkdv128_kernel(AttnPackedBwdArgs ba) {
+  constexpr int DH = 128, NW = 4;
+  using C = Cfg<DH>;
+  constexpr int BQ = KB, WGR = NW * WR, NS = 3;  // stages: a block, the next, whose first slot is begun with it, and one on its way
+  constexpr int QT = BQ * DH;
+  constexpr int STG = 2 * QT + 2 * 2 * BQ;  // Q, dO, lse2[64], delta[64]
+  __shared__ __attribute__((aligned(1024))) bf16 smem[NS * STG];
+  const AttnPackedArgs& a = ba.f;
+  const int G = a.H / a.Hkv;
+  int tile, kvh, part, s0, S, blk;
+  if (!packed_item(a, a.split, tile, kvh, part)) return;
+  if (!find_rows(a, tile, WGR, s0, S, blk)) return;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 5;
+  // causal: the first keys see the most queries, so the places count from the end
+  const int k0 = (a.causal ? (S + WGR - 1) / WGR - 1 - blk : blk) * WGR;
+  const int kmin = k0 + wave * WR;
+  const int key = kmin + (lane & 31);
+  const float sc = a.scale * LOG2E;
+
+  DkvState<DH> st;
+  load_rows<DH, PAD>(a.k + (long)s0 * a.ldk + (long)kvh * a.dh, a.ldk, kmin, S - kmin, lane, st.kf, a.dh);
+  load_rows<DH, PAD>(a.v + (long)s0 * a.ldv + (long)kvh * a.dh, a.ldv, kmin, S - kmin, lane, st.vf, a.dh);
+#pragma unroll
+  for (int t = 0; t < C::OT; ++t) {
+    st.dk[t] = zero16();
+    st.dv[t] = zero16();
+  }
+  TileOfs<DH, BQ> to;
+  to.init(lane);
+
+  const int q_start = query_lo(a, k0);
+  const int nqb = (query_hi(a, k0 + WGR - 1, S) - q_start + BQ - 1) / BQ;
+  int first = 0, total = nqb * G;  // block j of head kvh G + i is step i nqb + j
+  part_of(part, a.split, first, total);
+  float lsd = 0.f;            // wave 0: lse of the next block's query `lane`; wave 1: its delta
+
+  auto stage = [&](int it) { return smem + it % NS * STG; };
+  auto fetch = [&](int it) {
+    if (it >= total) return;
+    const int i = it / nqb, qs = q_start + (it - i * nqb) * BQ;
+    const int h = kvh * G + i;
+    bf16* sj = stage(it);
+    copy_tile<DH, BQ, NW, PAD>(rows_rsrc(a.q + (long)(s0 + qs) * a.ldq + (long)h * a.dh, 0), a.ldq, S - qs, sj, wave, a.dh);
+    copy_tile<DH, BQ, NW, PAD>(rows_rsrc(ba.dout + (long)(s0 + qs) * ba.lddo + (long)h * a.dh, 0), ba.lddo, S - qs, sj + QT,
+                               wave, a.dh);
+    if (wave < 2) {
+      const int qi = qs + lane;
+      const long at = (long)h * a.T + s0 + qi;
+      lsd = qi < S ? (wave ? ba.delta[at] : a.lse[at]) : 0.f;
+    }
+  };
+  auto publish = [&](int it) {
+    if (wave < 2) reinterpret_cast<float*>(stage(it) + 2 * QT)[wave * BQ + lane] = wave ? lsd : lsd * LOG2E;
+  };
+  // before block `it`: the next one lands too, and the one after it is fetched over the block before
+  // `it`, which every wave has left
+  auto middle = [&](int it) {
+    wait_vm_lgkm0<0>();
+    if (it + 1 < total) publish(it + 1);
+    wait_vm_lgkm0<0>();
+    cta_barrier();
+    fetch(it + 2);
+  };
+  const bool idle = kmin >= S;
+  // queries that some key of the wave sees [wlo, whi), those of this lane's key [lo, hi)
+  const int wlo = query_lo(a, kmin), whi = idle ? wlo : query_hi(a, kmin + WR - 1, S);
+  const int lo = query_lo(a, key), hi = query_hi(a, key, S);
+  // blocks of a head that hold a valid pair for this wave
+  const int ja = max(wlo - q_start, 0) / BQ, jb = idle ? 0 : (whi - q_start + BQ - 1) / BQ;
+  // queries that all keys of the wave see
+  const int flo = query_lo(a, kmin + WR - 1), fhi = query_hi(a, kmin, S);
+
+  fetch(first);
+  wait_vm_lgkm0<0>();
+  if (first < total) publish(first);
+  wait_vm_lgkm0<0>();
+  cta_barrier();
+  fetch(first + 1);
+
+  auto lse2 = [&](const bf16* st_) { return reinterpret_cast<const float*>(st_ + 2 * QT); };
+  // blocks of a head whose pairs are all valid for this wave
+  const int fa = (max(flo - q_start, 0) + BQ - 1) / BQ, fb = (fhi - q_start) / BQ;
+  Slot A, B;
+  int it = first, i0 = 0;
+  // one block: its two slots, and the products of the next block's first one, which go unused behind
+  // this wave's last block
+  auto block = [&](auto whole) {
+    middle(it);
+    const bf16* Qc = stage(it);
+    const bf16* Qn = stage(it + 1);
+    auto mask = [&](Slot& p, int u) {  // exp2 makes closed pairs 0
+      const int qs = q_start + (it - i0) * BQ + 32 * u + 4 * g;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int q = qs + 8 * (r >> 2) + (r & 3);
+        p.t[r] = q >= lo && q < hi ? p.t[r] : -INFINITY;
+      }
+    };
+    if (!decltype(whole)::value) mask(A, 0);
+    dkdv_step<true, true>(st, to, A, B, Qc, lse2(Qc), 1, Qc, 0, g, sc);
+    if (!decltype(whole)::value) mask(B, 1);
+    dkdv_step<true, true>(st, to, B, A, Qn, lse2(Qn), 0, Qc, 1, g, sc);
+    ++it;
+  };
+  while (it < total) {  // head by head: its blocks before this wave's, this wave's, those behind
+    i0 = it / nqb * nqb;
+    const int end = min(total, i0 + nqb);
+    const int from = min(max(it, i0 + ja), end), until = min(max(from, i0 + jb), end);
+    for (; it < from; ++it) middle(it);
+    if (it < until) dkdv_step<true, false>(st, to, B, A, stage(it), lse2(stage(it)), 0, stage(it), 0, g, sc);
+    const int w0 = min(max(it, i0 + fa), until), w1 = min(max(w0, i0 + fb), until);
+    while (it < w0) block(std::false_type{});
+    while (it < w1) block(std::true_type{});
+    while (it < until) block(std::false_type{});
+    for (; it < end; ++it) middle(it);
   }
   if (a.split > 1) {
     float* p = wave_share(a.ws, ((long)tile * a.Hkv + kvh) * a.split + part, NW, 2 * 16 * C::OT, wave);
@@ -421,8 +637,10 @@ Plan plan(const AttnPackedArgs& a, Pass pass) {
   const int G = a.H / a.Hkv, per = pass == DKDV ? 1 : G;
   const long rows = a.T / std::max(1, a.n_seq);
   Plan p;
+  const int dh = a.dh <= 64 ? 64 : a.dh <= 80 ? 80 : 128;
   p.nw = (long)(a.T / 128 + 1) * a.Hkv * per < 192 || rows < (pass == FWD ? 96 : 160) ? 2 : 4;
-  const int dh = a.dh <= 64 ? 64 : a.dh <= 80 ? 80 : 128, R = p.nw * WR;
+  if (dh == 128 && pass == DKDV) p.nw = 4;
+  const int R = p.nw * WR;
   const bool tail = a.causal && a.window >= a.T;
   const long items = (a.T / R + 1) * (long)a.Hkv * per;
   const long slots = 256L * (4 / p.nw) * (pass == DKDV ? (dh == 128 ? 1 : 2) : dh == 64 ? 3 : 2);
@@ -476,8 +694,15 @@ hipError_t bwd(AttnPackedBwdArgs a, hipStream_t s) {
   if (p.split > 1) PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, per)), ADDQ_K);
   p = plan_in(a.f, DKDV);
   a.f.split = p.split;
-  PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, p.split)), DKDV_K);
-  if (p.split > 1) PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, 1)), ADDKV_K);
+  const dim3 grid(packed_grid(a.f, p.nw * WR, p.split, DH == 128));
+  if constexpr (DH == 128) {
+    hipLaunchKernelGGL(attn_packed_dkdv128_kernel<PAD>, grid, dim3(256), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  } else {
+    PACKED_LAUNCH(p.nw, grid, DKDV_K);
+  }
+  if (p.split > 1) PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, 1, DH == 128)), ADDKV_K);
   return hipSuccess;
 }
 

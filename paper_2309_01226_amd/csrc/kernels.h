@@ -235,8 +235,8 @@ struct AttnPackedArgs {
   float* ws;
   long ws_elems;
   // set by the launchers (attn_packed.h): blocks, parts that a K / V head's blocks are dealt to, parts of a
-  // block's work
-  int ntile, parts, split;
+  // block's work, order of the blocks
+  int ntile, parts, split, by_place;
 };
 struct AttnPackedBwdArgs {
   AttnPackedArgs f;

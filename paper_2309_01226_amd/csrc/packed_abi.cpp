@@ -52,7 +52,7 @@ static sat_status packed_args(const sat_attn_packed_desc* d, AttnPackedArgs* out
   a.scale = d->scale;
   a.ws = nullptr;
   a.ws_elems = 0;
-  a.ntile = a.parts = a.split = 0;
+  a.ntile = a.parts = a.split = a.by_place = 0;
   return SAT_OK;
 }
 
