@@ -34,7 +34,7 @@ __device__ __forceinline__ int nth_bit(uint64_t mask, int n) {
 // that the last blocks to end are short ones.  Nothing is sorted: nb is a sequence's number of blocks,
 // held by the lanes.  By place: causal blocks have the work of their place b in the sequence, and sum
 // max(0, nb - x) of them a place of x or more.  By sequence: sum [nb > x] nb blocks are in
-// sequences of more than x, each sequence's own in a row.  A bisection over x finds the level
+// sequences of more than x, each sequence's own in a row.  A walk or a bisection over x finds the level
 // that holds the rank, bit counts the sequence on it.  Causal blocks go by place where sequences are long
 // (1024 rows on average; 256 with 64-wide heads, whose K and V are smallest), by sequence where they are short and what
 // counts is that a sequence's K and V are read once: 4 x 4096 rows, 16 heads of 64, forward 158 against 174
@@ -46,59 +46,89 @@ __device__ __forceinline__ int nth_bit(uint64_t mask, int n) {
 // cu holds.  blk counts the places in the order of causal work (a query block's own place; a key block's
 // from the end of its sequence).  False: no such block.
 constexpr int kSortedSeqs = 256;
-// C sequences a lane.
+// C sequences a lane: first rows, rows and blocks, and the most blocks of one.
 template <int C>
-__device__ __forceinline__ bool sorted_block(const AttnPackedArgs& a, int rank, int R, int& s0, int& S, int& blk) {
-  const int lane = threadIdx.x & 63;
-  int s[C], e[C], nb[C], most = 0;
+struct SeqLanes {
+  int s[C], len[C], nb[C], most;
+  __device__ __forceinline__ void load(const AttnPackedArgs& a, int R) {
+    most = 0;
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int i = min(lane + 64 * c, a.n_seq - 1);
-    s[c] = row_at(a, i);
-    e[c] = row_at(a, i + 1);
-    nb[c] = lane + 64 * c < a.n_seq ? (max(e[c], s[c]) - s[c] + R - 1) / R : 0;
-    most = max(most, nb[c]);
+    for (int c = 0; c < C; ++c) {
+      const int i = (threadIdx.x & 63) + 64 * c, j = min(i, a.n_seq - 1);
+      s[c] = row_at(a, j);
+      len[c] = max(row_at(a, j + 1), s[c]) - s[c];
+      nb[c] = i < a.n_seq ? (len[c] + R - 1) / R : 0;
+      most = max(most, nb[c]);
+    }
+    most = wave_all(most, [](int p, int q) { return max(p, q); });
   }
-  auto beyond = [&](int x) {
-    int n = 0;
+  __device__ __forceinline__ bool find(const AttnPackedArgs& a, int rank, int& s0, int& S, int& blk) const {
+    // blocks on level x, and on the levels from x on
+    auto level = [&](int x) {
+      int n = 0;
 #pragma unroll
-    for (int c = 0; c < C; ++c) n += a.by_place ? max(0, nb[c] - x) : nb[c] > x ? nb[c] : 0;
-    return wave_all(n, [](int p, int q) { return p + q; });
-  };
-  int lo = 0, hi = wave_all(most, [](int p, int q) { return max(p, q); }), at_hi = 0;
-  if (rank >= beyond(0)) return false;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1, n = beyond(mid);
-    if (n > rank) {
-      lo = mid;
+      for (int c = 0; c < C; ++c) n += (int)__popcll(__builtin_amdgcn_ballot_w64(a.by_place ? nb[c] > x : nb[c] == x + 1));
+      return a.by_place ? n : n * (x + 1);
+    };
+    auto from = [&](int x) {
+      int n = 0;
+#pragma unroll
+      for (int c = 0; c < C; ++c) n += a.by_place ? max(0, nb[c] - x) : nb[c] > x ? nb[c] : 0;
+      return wave_all(n, [](int p, int q) { return p + q; });
+    };
+    int lo, above = 0;  // the rank's level, blocks on the levels above it
+    if (most <= 16) {   // level by level: a compare and a bit count each
+      for (lo = most - 1; lo >= 0; --lo) {
+        const int n = level(lo);
+        if (above + n > rank) break;
+        above += n;
+      }
+      if (lo < 0) return false;
     } else {
-      hi = mid;
-      at_hi = n;
+      if (rank >= from(0)) return false;
+      lo = 0;
+      for (int hi = most; hi - lo > 1;) {
+        const int mid = (lo + hi) >> 1, n = from(mid);
+        if (n > rank) {
+          lo = mid;
+        } else {
+          hi = mid;
+          above = n;
+        }
+      }
     }
-  }
-  int k = rank - at_hi;  // among the blocks of level lo
-  const int of = a.by_place ? 1 : lo + 1;
-  int seq = a.by_place ? k : k / of;
-  blk = a.by_place ? lo : a.causal ? lo - (k - seq * of) : k - seq * of;
-  s0 = S = 0;
+    const int k = rank - above;  // among the blocks of the level
+    const int of = a.by_place ? 1 : lo + 1;
+    int seq = a.by_place ? k : k / of;
+    blk = a.by_place ? lo : a.causal ? lo - (k - seq * of) : k - seq * of;
+    s0 = S = 0;
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const uint64_t on = __builtin_amdgcn_ballot_w64(a.by_place ? nb[c] > lo : nb[c] == lo + 1);
-    const int n = (int)__popcll(on);
-    if (seq >= 0 && seq < n) {
-      const int i = nth_bit(on, seq);
-      s0 = __builtin_amdgcn_readlane(s[c], i);
-      S = __builtin_amdgcn_readlane(e[c], i) - s0;
+    for (int c = 0; c < C; ++c) {
+      const uint64_t on = __builtin_amdgcn_ballot_w64(a.by_place ? nb[c] > lo : nb[c] == lo + 1);
+      const int n = (int)__popcll(on);
+      if (seq >= 0 && seq < n) {
+        const int i = nth_bit(on, seq);
+        s0 = __builtin_amdgcn_readlane(s[c], i);
+        S = __builtin_amdgcn_readlane(len[c], i);
+      }
+      seq -= n;  // below 0 from there on
     }
-    seq -= n;  // below 0 from there on
+    return true;
   }
-  return true;
-}
+};
 
 __device__ __forceinline__ bool find_rows(const AttnPackedArgs& a, int rank, int R, int& s0, int& S, int& blk) {
   const int lane = threadIdx.x & 63;
-  if (a.n_seq <= kSortedSeqs)
-    return a.n_seq <= 64 ? sorted_block<1>(a, rank, R, s0, S, blk) : sorted_block<4>(a, rank, R, s0, S, blk);
+  if (a.n_seq <= 64) {
+    SeqLanes<1> q;
+    q.load(a, R);
+    return q.find(a, rank, s0, S, blk);
+  }
+  if (a.n_seq <= kSortedSeqs) {
+    SeqLanes<4> q;
+    q.load(a, R);
+    return q.find(a, rank, s0, S, blk);
+  }
   int lo = 0, hi = a.n_seq, s, e;
   for (;;) {
     const int step = (hi - lo + 63) >> 6;
