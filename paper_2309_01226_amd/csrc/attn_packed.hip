@@ -168,6 +168,10 @@ __global__ __launch_bounds__(64 * NW) void attn_packed_join_kernel(AttnPackedArg
 }
 
 // dQ, and delta for the dK / dV kernel, which runs after it.
+// delta = rowsum(dO * O) comes from the rounded O, which is off by 2^-8 of it where a query sees few keys and
+// O is as large as V.  The same sum over the keys, sum P dP, has no such error: it is formed beside dQ (a
+// multiply-add per pair) for the dK / dV kernel and, where all keys of the workgroup fit the two stages, in a pass
+// of its own before dQ.  Gradients of 24 rows: 0.27 % -> 0.24 % off, of which 0.17 % is the results' rounding.
 template <int DH, int NW, bool PAD>
 __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBwdArgs ba) {
   using C = Cfg<DH>;
@@ -201,8 +205,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc = __builtin_fmaf(bf2f(st.of[c][e]), bf2f(ov[c][e]), acc);
     st.dlt = halves_sum(acc);
-    if (g == 0 && q < S && sp == 0) ba.delta[hs + q] = st.dlt;
   }
+  st.pd = 0.f;
 #pragma unroll
   for (int t = 0; t < C::OT; ++t) st.dq[t] = zero16();
   TileOfs<DH, KB> to;
@@ -220,35 +224,54 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
     copy_tile<DH, KB, NW, PAD>(rows_rsrc(Kb, (long)j * KB * a.ldk * 2), a.ldk, S - j * KB, dst, wave, a.dh);
     copy_tile<DH, KB, NW, PAD>(rows_rsrc(Vb, (long)j * KB * a.ldv * 2), a.ldv, S - j * KB, dst + TILE, wave, a.dh);
   };
-  auto masked = [&](int j) {
+  // the pairs of block j that the mask leaves
+  auto masked = [&](int j, auto sum, auto dq) {
     const bf16* Ks = smem + (j & 1) * 2 * TILE;
-    if (j + 1 < je) copy(j + 1);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int kv = j * KB + 32 * u;
       if (kv < whi && kv + 32 > wlo)
-        dq_sub<DH, true, true>(st, to, Ks, Ks + TILE, u, sc, hi - kv - 4 * g, lo - kv - 4 * g);
+        dq_sub<DH, true, true, decltype(sum)::value, decltype(dq)::value>(st, to, Ks, Ks + TILE, u, sc, hi - kv - 4 * g,
+                                                                        lo - kv - 4 * g);
     }
-    wait_vm_lgkm0<0>();
-    cta_barrier();
   };
+  using Yes = std::true_type;
+  using No = std::false_type;
   if (jb < je) copy(jb);  // a part may be empty
-  wait_vm_lgkm0<0>();
-  cta_barrier();
-  int j = jb;
-  for (; j < j1; ++j) masked(j);
-  for (; j < j2; ++j) {
-    const bf16* Ks = smem + (j & 1) * 2 * TILE;
-    if (j + 1 < je) copy(j + 1);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      dq_sub<DH, false>(st, to, Ks, Ks + TILE, u, sc, 0);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+  if (je - jb <= 2 && a.split == 1) {
+    if (je - jb == 2) copy(jb + 1);
     wait_vm_lgkm0<0>();
     cta_barrier();
+    for (int j = jb; j < je; ++j) masked(j, Yes(), No());
+    st.dlt = halves_sum(st.pd);
+    if (g == 0 && q < S) ba.delta[hs + q] = st.dlt;
+    for (int j = jb; j < je; ++j) masked(j, No(), Yes());
+  } else {
+    auto step = [&](int j) {
+      if (j + 1 < je) copy(j + 1);
+      masked(j, Yes(), Yes());
+      wait_vm_lgkm0<0>();
+      cta_barrier();
+    };
+    wait_vm_lgkm0<0>();
+    cta_barrier();
+    int j = jb;
+    for (; j < j1; ++j) step(j);
+    for (; j < j2; ++j) {
+      const bf16* Ks = smem + (j & 1) * 2 * TILE;
+      if (j + 1 < je) copy(j + 1);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        dq_sub<DH, false, false, true>(st, to, Ks, Ks + TILE, u, sc, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      wait_vm_lgkm0<0>();
+      cta_barrier();
+    }
+    for (; j < je; ++j) step(j);
+    const float sum = halves_sum(st.pd);  // a part has a part of it only
+    if (g == 0 && q < S && sp == 0) ba.delta[hs + q] = a.split > 1 ? st.dlt : sum;
   }
-  for (; j < je; ++j) masked(j);
   if (a.split > 1) put_acc<C::OT>(wave_share(a.ws, ((long)tile * a.H + h) * a.split + sp, NW, 16 * C::OT, wave), st.dq);
   else if (q < S) store_rowT<DH, PAD>(ba.dq + (long)(s0 + q) * ba.lddq + (long)h * a.dh, st.dq, a.scale, g, a.dh);
 }

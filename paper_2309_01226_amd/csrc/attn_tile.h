@@ -366,11 +366,12 @@ struct DqState {
   bf16x8 qf[Cfg<DH>::KS], of[Cfg<DH>::KS];
   floatx16 dq[Cfg<DH>::OT];
   float nl2, dlt;  // -lse * log2 e and delta of this lane's query
+  float pd;        // sum of P dP over this lane's keys (where it is taken)
 };
 
 // Sub-tile u (32 keys) of a staged block.  MASK: keys with acc_row - 4 g < lim_rel (LOW: and
-// >= low_rel) are valid.
-template <int DH, bool MASK, bool LOW = false>
+// >= low_rel) are valid.  SUM: also adds P dP to st.pd; DQ: adds to dQ.
+template <int DH, bool MASK, bool LOW = false, bool SUM = false, bool DQ = true>
 __device__ __forceinline__ void dq_sub(DqState<DH>& st, const TileOfs<DH, KB>& to, const bf16* Ks,
                                        const bf16* Vs, int u, float sc, int lim_rel, int low_rel = 0) {
   using C = Cfg<DH>;
@@ -391,10 +392,12 @@ __device__ __forceinline__ void dq_sub(DqState<DH>& st, const TileOfs<DH, KB>& t
     }
   }
   bf16x8 kt[2][C::OT];
+  if constexpr (DQ) {
 #pragma unroll
-  for (int hh = 0; hh < 2; ++hh)
+    for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-    for (int ot = 0; ot < C::OT; ++ot) kt[hh][ot] = to.trans(Ks, 2 * u + hh, ot);
+      for (int ot = 0; ot < C::OT; ++ot) kt[hh][ot] = to.trans(Ks, 2 * u + hh, ot);
+  }
   __builtin_amdgcn_sched_barrier(0);
   bf16x8 db[2];
 #pragma unroll
@@ -404,13 +407,16 @@ __device__ __forceinline__ void dq_sub(DqState<DH>& st, const TileOfs<DH, KB>& t
       const int kr = 8 * (r >> 2) + (r & 3);
       pr = kr < lim_rel && (!LOW || kr >= low_rel) ? pr : 0.f;
     }
-    db[r >> 3][r & 7] = f2bf(pr * (y[r] - st.dlt));
+    if (SUM) st.pd = __builtin_fmaf(pr, y[r], st.pd);
+    if (DQ) db[r >> 3][r & 7] = f2bf(pr * (y[r] - st.dlt));
   }
+  if constexpr (DQ) {
 #pragma unroll
-  for (int hh = 0; hh < 2; ++hh)
+    for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-    for (int ot = 0; ot < C::OT; ++ot)
-      st.dq[ot] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kt[hh][ot], db[hh], st.dq[ot], 0, 0, 0);
+      for (int ot = 0; ot < C::OT; ++ot)
+        st.dq[ot] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kt[hh][ot], db[hh], st.dq[ot], 0, 0, 0);
+  }
 }
 
 bool ok16(const void* p, long ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0; }

@@ -6,6 +6,7 @@ the stream; every element of every output is computed by the HIP kernels.
 """
 
 import ctypes as C
+import functools
 
 import torch
 
@@ -257,9 +258,8 @@ def maxpool_bwd(dy, arg, N, H, W, C):
 
 def _here(t, dtype, name, dev):
     """t: a tensor of `dtype` on the current device `dev` (the calls run on its current stream)."""
-    if not t.is_cuda or t.dtype != dtype:
+    if t.dtype is not dtype or t.get_device() != dev:
         _need(t, dtype, name)
-    if t.get_device() != dev:
         raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{dev}")
 
 
@@ -272,57 +272,64 @@ def _device(t, name):
 
 def _rows_of(t, dtype, name, rows, cols, dev):
     """Leading dimension of a matrix of at least `rows` rows and `cols` columns, columns contiguous."""
-    _here(t, dtype, name, dev)
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or shape[0] < rows or shape[1] < cols or (stride[1] != 1 and shape[1] > 1):
-        raise ValueError(f"{name}: expected [{rows}, >= {cols}] with contiguous rows, got {tuple(shape)} "
-                         f"strides {stride}")
-    return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
+    if t.dtype is not dtype or t.get_device() != dev:
+        _here(t, dtype, name, dev)
+    shape = t.shape
+    if len(shape) == 2:
+        r, c = shape
+        ld, one = t.stride()
+        if r >= rows and c >= cols and (one == 1 or c < 2):
+            return ld if r > 1 else max(ld, c)
+    raise ValueError(f"{name}: expected [{rows}, >= {cols}] with contiguous rows, got {tuple(shape)} strides {t.stride()}")
 
 
-def _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev):
+def _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev, more=()):
     T = q.shape[0]
     bf, wq, wk = torch.bfloat16, H * dh, Hkv * dh
     _here(lse, torch.float32, "lse", dev)
     _here(cu, torch.int32, "cu", dev)
-    n = cu.shape
-    if len(n) != 1 or n[0] < 1 or not cu.is_contiguous():
+    n = cu.numel()
+    if cu.dim() != 1 or n < 1 or not cu.is_contiguous():
         raise ValueError("cu: expected a contiguous vector of n_seq + 1 row numbers")
-    if tuple(lse.shape) != (H, T) or not lse.is_contiguous():
+    if lse.shape != (H, T) or not lse.is_contiguous():
         raise ValueError(f"lse: expected a contiguous [{H}, {T}], got {tuple(lse.shape)}")
     # in the order of the C struct
     return _lib.sat_attn_packed_desc(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), _rows_of(q, bf, "q", T, wq, dev), _rows_of(k, bf, "k", T, wk, dev),
         _rows_of(v, bf, "v", T, wk, dev), o.data_ptr(), _rows_of(o, bf, "o", T, wq, dev), lse.data_ptr(), cu.data_ptr(),
-        n[0] - 1, T, H, Hkv, dh, bool(causal), window, scale)
+        n - 1, T, H, Hkv, dh, bool(causal), window, scale, *more)
+
+
+@functools.lru_cache(maxsize=256)
+def _packed_ws(call, n_seq, T, H, Hkv, dh, causal, window):
+    """fp32 elements of scratch of the forward ("fwd") or the backward ("bwd") for these sizes."""
+    d = _lib.sat_attn_packed_desc(n_seq=n_seq, T=T, H=H, Hkv=Hkv, dh=dh, causal=causal, window=window)
+    need = C.c_int64()
+    _lib.call(f"sat_op_attention_packed_{call}_ws", d, need)
+    return need.value
 
 
 def attention_packed_fwd(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, *, window=0):
-    """Attention inside packed sequences (workspaces come from torch's allocator, on the current stream): rows cu[s] .. cu[s + 1] - 1 of q, o [T, >= H dh] and
-    k, v [T, >= Hkv dh] (bf16, views of a wider buffer allowed) are sequence s; lse fp32 [H, T].
-    See saturn_ops.h for the masks."""
+    """Attention inside packed sequences: rows cu[s] .. cu[s + 1] - 1 of q, o [T, >= H dh] and k, v
+    [T, >= Hkv dh] (bf16, views of a wider buffer allowed) are sequence s; lse fp32 [H, T].  See
+    saturn_ops.h for the masks.  Workspaces come from torch's allocator, on the current stream."""
     d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, _device(q, "q"))
-    need = C.c_int64()
-    _lib.call("sat_op_attention_packed_fwd_ws", d, need)
-    if need.value:
-        ws = torch.empty(need.value, device=q.device, dtype=torch.float32)
-        d.ws, d.ws_elems = ws.data_ptr(), need.value
+    need = _packed_ws("fwd", d.n_seq, d.T, H, Hkv, dh, bool(causal), window)
+    if need:
+        ws = torch.empty(need, device=q.device, dtype=torch.float32)
+        d.ws, d.ws_elems = ws.data_ptr(), need
     _lib.call("sat_op_attention_packed_fwd", d, _stream())
 
 
 def attention_packed_bwd(q, k, v, o, lse, cu, dout, dq, dk, dv, H, Hkv, dh, causal, scale, *, window=0):
     """Its backward from dout [T, >= H dh] and the forward's o and lse; writes dq, dk, dv."""
-    dev = _device(q, "q")
-    d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev)
-    bf, T, wq, wk = torch.bfloat16, d.T, H * dh, Hkv * dh
-    d.dout, d.lddo = dout.data_ptr(), _rows_of(dout, bf, "dout", T, wq, dev)
-    d.dq, d.lddq = dq.data_ptr(), _rows_of(dq, bf, "dq", T, wq, dev)
-    d.dk, d.lddk = dk.data_ptr(), _rows_of(dk, bf, "dk", T, wk, dev)
-    d.dv, d.lddv = dv.data_ptr(), _rows_of(dv, bf, "dv", T, wk, dev)
-    need = C.c_int64()
-    _lib.call("sat_op_attention_packed_bwd_ws", d, need)
-    ws = torch.empty(max(1, need.value), device=q.device, dtype=torch.float32)
-    d.ws, d.ws_elems = ws.data_ptr(), need.value
+    dev, T, bf, wq, wk = _device(q, "q"), q.shape[0], torch.bfloat16, H * dh, Hkv * dh
+    need = _packed_ws("bwd", cu.numel() - 1, T, H, Hkv, dh, bool(causal), window)
+    ws = torch.empty(max(1, need), device=q.device, dtype=torch.float32)
+    d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev, (
+        dout.data_ptr(), _rows_of(dout, bf, "dout", T, wq, dev), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+        _rows_of(dq, bf, "dq", T, wq, dev), _rows_of(dk, bf, "dk", T, wk, dev), _rows_of(dv, bf, "dv", T, wk, dev),
+        ws.data_ptr(), need))
     _lib.call("sat_op_attention_packed_bwd", d, _stream())
 
 
@@ -368,30 +375,32 @@ class AdamWTensors:
             raise ValueError("one of everything for each parameter")
         dtypes = dict(params=torch.float32, grads=torch.bfloat16 if self.grad_bf16 else torch.float32, m=st, v=st,
                       shadows=torch.bfloat16, m_exp=torch.uint8, v_exp=torch.uint8)
-        written, read, dev = [], [], _device(params[0], "params[0]") if n else None
+        dev = _device(params[0], "params[0]") if n else None
+        sizes = [t.numel() for t in params]
+        eighth = [-(-k // 256) for k in sizes]
+        spans, ptrs = [], {}
         for name, ts in lists.items():
+            dtype, written, want = dtypes[name], name != "grads", eighth if name.endswith("_exp") else sizes
+            ptrs[name] = [t.data_ptr() for t in ts]
             for i, t in enumerate(ts):
-                _here(t, dtypes[name], f"{name}[{i}]", dev)
-                want = params[i].numel() if not name.endswith("_exp") else -(-params[i].numel() // 256)
-                if not t.is_contiguous() or t.numel() != want:
-                    raise ValueError(f"{name}[{i}]: expected {want} contiguous elements, got {tuple(t.shape)}")
-                if want:
-                    (read if name == "grads" else written).append(
-                        (t.data_ptr(), t.data_ptr() + want * t.element_size(), f"{name}[{i}]", name != "grads"))
+                if t.dtype is not dtype or t.get_device() != dev:
+                    _here(t, dtype, f"{name}[{i}]", dev)
+                if not t.is_contiguous() or t.numel() != want[i]:
+                    raise ValueError(f"{name}[{i}]: expected {want[i]} contiguous elements, got {tuple(t.shape)}")
+            size = dtype.itemsize
+            spans += [(p, p + k * size, written, name, i) for i, (p, k) in enumerate(zip(ptrs[name], want)) if k]
         end, last = 0, None
-        for a, b, what, w in sorted(written + read):
-            if a < end and (w or last[1]):
-                raise ValueError(f"{what} overlaps {last[0]}")
-            if b > end:
-                end, last = b, (what, w)
+        for span in sorted(spans):
+            if span[0] < end and (span[2] or last[2]):
+                raise ValueError("{}[{}] overlaps {}[{}]".format(*span[3:], *last[3:]))
+            if span[1] > end:
+                end, last = span[1], span
         self.tensors, self.device = lists, dev
         self.table = (_lib.sat_adamw_tensor * n)()
-        for i, e in enumerate(self.table):
-            e.p, e.g, e.m, e.v = (lists[x][i].data_ptr() for x in ("params", "grads", "m", "v"))
-            e.shadow = None if shadows is None else shadows[i].data_ptr()
-            if self.bits == 8:
-                e.m_exp, e.v_exp = m_exp[i].data_ptr(), v_exp[i].data_ptr()
-            e.n, e.weight_decay = params[i].numel(), decay[i]
+        none = [None] * n
+        columns = [ptrs.get(x, none) for x in ("params", "grads", "m", "v", "m_exp", "v_exp", "shadows")]
+        for i, row in enumerate(zip(*columns, sizes, decay)):
+            self.table[i] = row
 
 
 def adamw_multi(tensors, lr, beta1, beta2, eps, t, *, seed=0):
