@@ -151,12 +151,23 @@ extern "C" sat_status sat_op_rotary_axes(const void* x, int64_t ldx, void* y, in
   a.x = x; a.y = y; a.pos = pos;
   a.ldx = ldx; a.ldy = ldy; a.ldp = ldp;
   a.T = T; a.H = H; a.dh = dh; a.half = half; a.inverse = inverse != 0;
+  // turns per position of pair j of n: base^(-j / n) / (2 pi), as the product of two powers (a power
+  // for each pair would take longer than the launch)
   const double turn = 6.283185307179586476925286766559;
-  for (int ax = 0, i = 0; ax < n_axes; ++ax)
+  double fine[8], coarse[16];
+  auto powers = [&](int n) {
+    for (int k = 0; k < 8 && k < n; ++k) fine[k] = pow(base, -(double)k / n);
+    for (int k = 0; 8 * k < n; ++k) coarse[k] = pow(base, -8.0 * k / n) / turn;
+  };
+  if (!own_freqs) powers(half);
+  for (int ax = 0, i = 0; ax < n_axes; ++ax) {
+    if (own_freqs && pairs[ax]) powers(pairs[ax]);
     for (int j = 0; j < pairs[ax]; ++j, ++i) {
+      const int k = own_freqs ? j : i;
       a.axis[i] = (uint8_t)ax;
-      a.freq[i] = pow(base, own_freqs ? -(double)j / pairs[ax] : -(double)i / half) / turn;
+      a.freq[i] = fine[k & 7] * coarse[k >> 3];
     }
+  }
   SAT_HIP(launch_rotary_axes(a, f32 != 0, interleaved != 0, S(stream)));
   return SAT_OK;
 }
