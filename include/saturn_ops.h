@@ -125,7 +125,8 @@ sat_status sat_op_attention_bwd(const void* q, const void* k, const void* v, int
  * sequences follow each other in one buffer without padding between them.
  *   rows     cu: device int32 [n_seq + 1], not decreasing; rows cu[s] ..
  *            cu[s + 1] - 1 of every row array are sequence s (a length may be
- *            0).  T rows per array, 0 <= T <= 2^29.  Rows outside all sequences are
+ *            0).  T rows per array, 0 <= T <= 2^29, (T / 64 + 2 n_seq + 16) H below
+ *            2^25.  Rows outside all sequences are
  *            not read and keep what they hold in every output.  cu is read on the
  *            device only, so a captured call takes the lengths of the
  *            replay; values outside [0, T] are taken as the nearer of the two.
@@ -193,8 +194,8 @@ sat_status sat_op_rotary(void* qk, int64_t ld, int32_t B, int32_t S, int32_t H, 
  * formed in 64 bits, cos and sin rounded to fp32.  inverse = 1 applies the
  * transpose (backward).  y == x (with ldy == ldx): in place, the other dims stay; else
  * the heads' other dims are copied, and y must not overlap x.  Columns behind
- * the heads are not touched.  f32: x and y are fp32, else bf16.  dh even, x and y
- * aligned to their elements (16-byte aligned rows are fastest).
+ * the heads are not touched.  f32: x and y are fp32, else bf16.  dh even, H dh^2 below
+ * 2^32, T below 2^24, x and y aligned to their elements (16-byte aligned rows are fastest).
  * Errors: SAT_EINVAL for null pointers (T > 0), sizes and alignment. */
 sat_status sat_op_rotary_axes(const void* x, int64_t ldx, void* y, int64_t ldy, int32_t f32,
                               const int32_t* pos, int64_t ldp, int32_t n_axes,
@@ -217,7 +218,7 @@ sat_status sat_op_adamw(float* p, const float* g, float* m, float* v, void* shad
 
 /* The same step over `count` tensors in few launches, moments in 32 or in 8 bits
  * (state_bits).  The table t is host memory, read during the call only.  Each
- * entry: n >= 0 fp32 values p, their gradient g (bf16 when grad_bf16, else fp32), moments m
+ * entry: 0 <= n <= 2^35 fp32 values p, their gradient g (bf16 when grad_bf16, else fp32), moments m
  * and v, the tensor's weight decay, a bf16 shadow that is refreshed (may be
  * NULL); no array that is written overlaps another of the table.
  *   32 bits: m, v fp32 [n]; with an fp32 gradient every value is bitwise that of

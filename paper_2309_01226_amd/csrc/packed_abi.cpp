@@ -11,6 +11,8 @@
 static inline hipStream_t S(void* s) { return reinterpret_cast<hipStream_t>(s); }
 static bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+static constexpr int64_t kMaxGroups = 1 << 24;  // of 256 threads: a launch has fewer than 2^32
+
 // ---------------------------------------------------------------- attention
 
 static constexpr int64_t kMaxLd = 1 << 22;  // a block's rows stay within 32-bit buffer offsets
@@ -23,8 +25,9 @@ static sat_status packed_sizes(const sat_attn_packed_desc* d, const char* fn) {
                 "%s: H=%d must be a positive multiple of Hkv=%d", fn, d->H, d->Hkv);
   SAT_CHECK_ARG(d->dh >= 8 && d->dh <= 256 && d->dh % 8 == 0,
                 "%s: head dim %d must be a multiple of 8 up to 256", fn, d->dh);
-  // workgroups of the smallest blocks (64 rows), a whole number of them for each of up to 8 parts
-  SAT_CHECK_ARG(((int64_t)d->T / 64 + d->n_seq + 8) * d->H < (1LL << 31), "%s: too many rows x heads", fn);
+  // workgroups, a whole number of them for each of up to 8 parts: blocks of 64 rows have 128 threads, of
+  // 128 rows 256, and a launch fewer than 2^32 threads
+  SAT_CHECK_ARG(((int64_t)d->T / 64 + 2 * ((int64_t)d->n_seq + 8)) * d->H < (1LL << 25), "%s: too many rows x heads", fn);
   return SAT_OK;
 }
 
@@ -131,8 +134,9 @@ extern "C" sat_status sat_op_rotary_axes(const void* x, int64_t ldx, void* y, in
   const char* fn = "rotary_axes";
   SAT_CHECK_ARG(pairs && (T == 0 || (x && y && pos)), "%s: null pointer", fn);
   SAT_CHECK_ARG(n_axes >= 1 && n_axes <= 4, "%s: %d axes, 1 to 4 are possible", fn, n_axes);
-  SAT_CHECK_ARG(T >= 0 && H >= 1 && H <= (1 << 16) && dh >= 2 && dh % 2 == 0 && dh <= (1 << 12),
+  SAT_CHECK_ARG(T >= 0 && T < kMaxGroups && H >= 1 && H <= (1 << 16) && dh >= 2 && dh % 2 == 0 && dh <= (1 << 12),
                 "%s: bad sizes T=%d H=%d dh=%d (dh must be even)", fn, T, H, dh);
+  SAT_CHECK_ARG((int64_t)H * dh * dh < (1LL << 32), "%s: %d heads of %d dims are too wide", fn, H, dh);
   int half = 0;
   for (int a = 0; a < n_axes; ++a) {
     SAT_CHECK_ARG(pairs[a] >= 0 && pairs[a] <= 128, "%s: axis %d has %d pairs", fn, a, pairs[a]);
@@ -194,7 +198,7 @@ static hipError_t over_tensors(const sat_adamw_tensor* t, int32_t count, int chu
   for (int k = 0; k < count; ++k) {
     if (t[k].n == 0) continue;
     const int64_t more = (t[k].n + chunk - 1) / chunk;
-    if (a.count == kAdamWEntries || chunks + more > 0x7FFFFFFF) {
+    if (a.count == kAdamWEntries || chunks + more >= kMaxGroups) {
       const hipError_t e = go(a, (int)chunks);
       if (e != hipSuccess) return e;
       a.count = 0;
@@ -208,7 +212,7 @@ static hipError_t over_tensors(const sat_adamw_tensor* t, int32_t count, int chu
   return a.count ? go(a, (int)chunks) : hipSuccess;
 }
 
-static constexpr int64_t kMaxN = 1LL << 42;
+static constexpr int64_t kMaxN = 1LL << 35;  // one tensor's chunks fit a launch
 
 extern "C" sat_status sat_op_adamw_multi(const sat_adamw_tensor* t, int32_t count, int32_t state_bits,
                                          int32_t grad_bf16, double lr, double beta1, double beta2, double eps,

@@ -57,7 +57,7 @@ __device__ __forceinline__ void st(T* p, const T (&x)[V]) {
   }
 }
 
-// x / d for inv = 2^32 / d + 1 (0 for d = 1): exact while x d < 2^32.
+// x / d for inv = 2^32 / d + 1 (0 for d = 1): exact while x d < 2^32 (of a row, x < H dh and d <= dh).
 __device__ __forceinline__ int div_by(int x, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)x, inv) : x; }
 
 // V: elements of one load.  INTER: pairs (2 i, 2 i + 1), V of them = V / 2 pairs per

@@ -291,6 +291,8 @@ def _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev, mo
     n = cu.numel()
     if cu.dim() != 1 or n < 1 or not cu.is_contiguous():
         raise ValueError("cu: expected a contiguous vector of n_seq + 1 row numbers")
+    if not 0 <= window < 1 << 31:  # ctypes would cut it
+        raise ValueError(f"window: {window}")
     if lse.shape != (H, T) or not lse.is_contiguous():
         raise ValueError(f"lse: expected a contiguous [{H}, {T}], got {tuple(lse.shape)}")
     # in the order of the C struct
@@ -344,6 +346,8 @@ def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=Tru
     ldx = _rows_of(x, dt, "x", T, H * dh, dev)
     ldy = ldx if out is None else _rows_of(out, dt, "out", T, H * dh, dev)
     ldp = _rows_of(pos, torch.int32, "pos", T, A, dev)
+    if max(pairs, default=0) > 128:  # ctypes would cut it
+        raise ValueError(f"pairs: {pairs}")
     _lib.call("sat_op_rotary_axes", x.data_ptr(), ldx, y.data_ptr(), ldy, f32, pos.data_ptr(), ldp, A,
               (C.c_int32 * A)(*pairs), T, H, dh, base, interleaved, own_freqs, inverse, _stream())
     return y

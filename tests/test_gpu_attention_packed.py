@@ -318,3 +318,11 @@ def test_python_checks():
     for b in bad:
         with pytest.raises((TypeError, ValueError)):
             fwd(**b)
+
+
+@pytest.mark.parametrize("window", [-1, 1 << 31, (1 << 32) + 5])
+def test_windows_that_are_refused(window):
+    from paper_2309_01226_amd import ops
+    s = _make([10], 2, 1, 64)
+    with pytest.raises(ValueError):
+        ops.attention_packed_fwd(s["q"], s["k"], s["v"], s["o"], s["lse"], s["cu"], 2, 1, 64, True, 0.1, window=window)

@@ -155,3 +155,29 @@ def test_python_checks():
                      ((x, pos, 2, 64, (32,)), dict(out=x.bfloat16()))):
         with pytest.raises((TypeError, ValueError)):
             ops.rotary_axes(*args, **kw)
+
+
+def test_pair_counts_that_are_refused():
+    from paper_2309_01226_amd import ops
+    x, pos = torch.randn(6, 128, device="cuda"), torch.zeros(6, 1, dtype=torch.int32, device="cuda")
+    for n in ((1 << 32) + 16, 129, 33, -1):
+        with pytest.raises((ValueError, RuntimeError)):
+            ops.rotary_axes(x, pos, 2, 64, (n,))
+
+
+def test_widest_rows():
+    """H dh^2 just under 2^32, one element at a time: the last heads' items are the largest numbers divided."""
+    T, H, dh = 2, 4094, 1024
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn(T, H * dh, generator=g).to(torch.bfloat16)
+    pos = torch.tensor([[3], [-70000]], dtype=torch.int32)
+    from paper_2309_01226_amd import ops
+    buf = torch.zeros(T, H * dh + 1, device="cuda", dtype=torch.bfloat16)[:, 1:]  # 2-byte aligned
+    ops.rotary_axes(x.cuda(), pos.cuda(), H, dh, (3,), out=buf, interleaved=False)
+    want = torch.as_tensor(R.rotary(x.double().numpy(), pos.numpy(), H, dh, (3,), interleaved=False))
+    got = buf.double().cpu()
+    # (2^-22 + 2^-23) (|u| + |w|) as above, and one rounding of the result
+    tol = 2.0 ** -8 * want.abs() + 2.0 ** -20 * x.double().abs().max()
+    assert bool(((got - want).abs() <= tol).all())
+    rest = got.view(T, H, dh)[:, :, 6:]
+    assert torch.equal(rest, x.double().view(T, H, dh)[:, :, 6:])

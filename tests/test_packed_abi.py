@@ -163,3 +163,34 @@ def test_reference_rotary_is_orthogonal_and_inverse():
             back = R.rotary(y, pos, 2, 20, (3, 0, 5), interleaved=inter, own_freqs=own, inverse=True)
             assert np.allclose(back, x)
             assert np.array_equal(y[:, 16:20], x[:, 16:20])
+
+
+@pytest.mark.parametrize("bad", [dict(H=64, Hkv=64, n_seq=1 << 18, ldq=4096), dict(T=1 << 26, H=32, Hkv=32, dh=8)])
+def test_attention_refuses_more_threads_than_a_launch_has(bad):
+    d = _desc(**{**bad, "ldk": 4096, "ldv": 4096, "ldo": 4096, "lddo": 4096, "lddq": 4096, "lddk": 4096, "lddv": 4096})
+    L = _L()
+    for f in (L.lib().sat_op_attention_packed_fwd, L.lib().sat_op_attention_packed_bwd):
+        assert f(C.byref(d), None) == L.SAT_EINVAL
+        assert "too many" in L.last_error()
+
+
+@pytest.mark.parametrize("bad", [
+    dict(T=1 << 24), dict(H=257, dh=4096, ldx=1 << 21, ldy=1 << 21), dict(H=1 << 16, dh=256, ldx=1 << 24, ldy=1 << 24),
+])
+def test_rotary_refuses_rows_that_its_division_does_not_hold(bad):
+    assert _rotary(**bad) == _L().SAT_EINVAL
+    assert "rotary_axes" in _L().last_error()
+
+
+def test_rotary_division_is_exact_within_the_limits():
+    """The kernel's x / d by a product with 2^32 / d + 1: items of one row, d of them to a head, H d^2 < 2^32."""
+    for d in [2, 3, 7, 31, 40, 127, 255, 1000, 2999, 4095, 4096]:
+        heads = min(1 << 16, ((1 << 32) - 1) // (d * d))
+        inv = (1 << 32) // d + 1
+        x = np.unique(np.concatenate([np.arange(0, heads * d, max(1, heads * d // 100003)), d * np.arange(1, heads) - 1,
+                                      d * np.arange(heads), [heads * d - 1]])).astype(np.uint64)
+        assert np.array_equal((x * np.uint64(inv)) >> np.uint64(32), x // np.uint64(d)), d
+
+
+def test_adamw_refuses_more_than_a_launch_takes():
+    assert _adamw(n=(1 << 35) + 1) == _L().SAT_EINVAL
