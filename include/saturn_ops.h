@@ -126,7 +126,7 @@ sat_status sat_op_attention_bwd(const void* q, const void* k, const void* v, int
  *   rows     cu: device int32 [n_seq + 1], not decreasing; rows cu[s] ..
  *            cu[s + 1] - 1 of every row array are sequence s (a length may be
  *            0).  T rows per array, 0 <= T <= 2^29, (T / 64 + 2 n_seq + 16) H below
- *            2^25.  Rows outside all sequences are
+ *            2^24.  Rows outside all sequences are
  *            not read and keep what they hold in every output.  cu is read on the
  *            device only, so a captured call takes the lengths of the
  *            replay; values outside [0, T] are taken as the nearer of the two.

@@ -26,8 +26,8 @@ static sat_status packed_sizes(const sat_attn_packed_desc* d, const char* fn) {
   SAT_CHECK_ARG(d->dh >= 8 && d->dh <= 256 && d->dh % 8 == 0,
                 "%s: head dim %d must be a multiple of 8 up to 256", fn, d->dh);
   // workgroups, a whole number of them for each of up to 8 parts: blocks of 64 rows have 128 threads, of
-  // 128 rows 256, and a launch fewer than 2^32 threads
-  SAT_CHECK_ARG(((int64_t)d->T / 64 + 2 * ((int64_t)d->n_seq + 8)) * d->H < (1LL << 25), "%s: too many rows x heads", fn);
+  // 128 rows up to 512, and a launch fewer than 2^32 threads
+  SAT_CHECK_ARG(((int64_t)d->T / 64 + 2 * ((int64_t)d->n_seq + 8)) * d->H < (1LL << 24), "%s: too many rows x heads", fn);
   return SAT_OK;
 }
 
