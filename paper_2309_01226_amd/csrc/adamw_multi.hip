@@ -21,10 +21,15 @@
 //
 // Bound by HBM: 30 bytes per element with 32-bit moments and an fp32 gradient (28
 // without the bf16 copy), 18 with 8-bit ones, 16 with a bf16 gradient also.  A
-// workgroup takes 4096 (1024 where the table is small) consecutive elements of one tensor, found from the launch's table
-// of tensors in the kernel arguments (nothing is copied to the device, so the
-// call needs no workspace and can be captured); a wave takes whole blocks, four
-// consecutive elements per lane, and has the loads of all its blocks in flight first.
+// workgroup takes consecutive elements of one tensor, found from the launch's table of tensors in the
+// kernel arguments (nothing is copied to the device, so the call needs no workspace and can be
+// captured); a wave takes whole blocks, four consecutive elements per lane, and has the loads of all its blocks
+// in flight first.  4096 elements a workgroup; 1024 where the whole table would give 256 CUs fewer than four
+// workgroups each: 0.17 M elements 9.0 -> 4.2 us, large tables the same within 1 %.  Whole aligned runs take a
+// straight-line path (8 bits: 1891 -> 1197 us), the others go element by element.
+// 160 M values with 32-bit moments: 4.79 GB in 807 us, 5.9 TB/s; 444 M with 8-bit ones: 7.1 GB in 1197 us, 5.9;
+// reading their values back as bf16, 6 bytes each: 500 us, 5.3.  (A copy of 4 GiB moves 4.7 TB/s; the
+// reads and writes here bypass the caches.)
 #include "adamw_math.h"
 #include "common.h"
 #include "kernels.h"

@@ -11,7 +11,10 @@
 // Bound by HBM for many heads: read and write of every rotated element (and, into
 // another buffer, of the others).  cos and sin of a row serve all its heads: a
 // workgroup takes up to 16 rows, starts the loads of its elements, forms the rows'
-// cos and sin in LDS meanwhile, then rotates.
+// cos and sin in LDS meanwhile, then rotates.  32749 rows of 20 heads of 128, bf16 in place: 335 MB
+// in 74 us, 4.5 TB/s; 5003 rows of 32 fp32 heads of 256, half of the pairs rotated, into another
+// buffer: 328 MB in 69 us, 4.7 TB/s (a copy of 4 GiB: 4.7).  257 rows of 32 heads of 80: 4.1 us, of which about
+// 3 are a launch that does nothing; the call's host side is 4 us more.
 #include <algorithm>
 
 #include "common.h"
