@@ -22,7 +22,7 @@
 // instructions a pair against 4 dh flop), 128-wide ones by the matrix cores at the clock that the power limit
 // leaves (the large matrix product: 1.4 PFLOP/s).  Forward, dQ, dK / dV of
 //   32 documents of 16 to 2048 rows in 16384, 16 heads of 64, causal       77, 100, 131 us (forward 450 TFLOP/s)
-//   64 images of 65 to 577 rows in 16448, 16 heads of 80, no mask          77, 102, 123 us
+//   64 images of 65 to 577 rows in 16448, 16 heads of 80, no mask          72, 102, 123 us
 //   4 documents in 16001 rows, 16 heads of 128 on 4 K / V heads, causal    290, 390, 650 us (forward 1.0 PFLOP/s; the
 //     backward executes 7 products for the 5 counted: 1.0 PFLOP/s executed)
 #include <algorithm>
@@ -66,8 +66,11 @@ __device__ __forceinline__ void add_acc(const float* p, float f, floatx16 (&acc)
     }
 }
 
+// 80-wide heads of four waves are held to the registers of three waves on a SIMD (one value spilled before the
+// loop): 50 images, 16 heads, 61.4 -> 56.5 us; 4 x 4096 rows causal 246 -> 235.  64-wide ones have three anyway, and
+// four would spill in the loop (30 -> 35 us on 16 short documents).
 template <int DH, int NW, bool PAD>
-__global__ __launch_bounds__(64 * NW, 2) void attn_packed_fwd_kernel(AttnPackedArgs a) {
+__global__ __launch_bounds__(64 * NW, DH == 80 && NW == 4 ? 3 : 2) void attn_packed_fwd_kernel(AttnPackedArgs a) {
   using C = Cfg<DH>;
   constexpr int TILE = KB * DH, WGR = NW * WR;
   __shared__ __attribute__((aligned(1024))) bf16 smem[2 * 2 * TILE];  // 2 stages x (K, V)
@@ -675,7 +678,7 @@ Plan plan(const AttnPackedArgs& a, Pass pass) {
   const int R = p.nw * WR;
   const bool tail = a.causal && a.window >= a.T;
   const long items = (a.T / R + 1) * (long)a.Hkv * per;
-  const long slots = 256L * (4 / p.nw) * (pass == DKDV ? (dh == 128 ? 1 : 2) : dh == 64 ? 3 : 2);
+  const long slots = 256L * (4 / p.nw) * (pass == DKDV ? (dh == 128 ? 1 : 2) : dh == 64 || (dh == 80 && pass == FWD) ? 3 : 2);
   const long want = (pass == DKDV && tail ? 4 : 1) * slots;
   const long steps = std::min(rows, 2L * a.window) / KB * (pass == DKDV ? G : 1) / (a.causal ? 2 : 1);
   p.split = 1;
