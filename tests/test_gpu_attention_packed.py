@@ -326,3 +326,54 @@ def test_windows_that_are_refused(window):
     s = _make([10], 2, 1, 64)
     with pytest.raises(ValueError):
         ops.attention_packed_fwd(s["q"], s["k"], s["v"], s["o"], s["lse"], s["cu"], 2, 1, 64, True, 0.1, window=window)
+
+
+@pytest.mark.parametrize("dh,H,Hkv", [(64, 4, 1), (128, 4, 1), (256, 2, 1)])
+def test_two_streams_at_once(dh, H, Hkv):
+    """Calls that overlap have scratch of their own; long sequences of few heads are the ones that use it."""
+    sets = [_make([2500 + i, 33], H, Hkv, dh, seed=i) for i in range(2)]
+    for s in sets:
+        _run(s, True, 0, 0.1)
+    torch.cuda.synchronize()
+    names = ("o", "lse", "dq", "dk", "dv")
+    alone = [{n: s[n].clone() for n in names} for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(4):
+        for s in sets:
+            for n in names:
+                s[n].fill_(0)
+        torch.cuda.synchronize()
+        for s, side in zip(sets, streams):
+            with torch.cuda.stream(side):
+                for _ in range(2):
+                    _run(s, True, 0, 0.1)
+        torch.cuda.synchronize()
+        for s, want in zip(sets, alone):
+            for n in names:
+                assert torch.equal(s[n], want[n]), n
+
+
+def test_two_captured_graphs_at_once():
+    sets = [_make([2500 + i, 33], 4, 1, 64, seed=i) for i in range(2)]
+    for s in sets:
+        _run(s, True, 0, 0.1)
+    torch.cuda.synchronize()
+    names = ("o", "lse", "dq", "dk", "dv")
+    alone = [{n: s[n].clone() for n in names} for s in sets]
+    graphs = [torch.cuda.CUDAGraph() for _ in sets]
+    for s, g in zip(sets, graphs):
+        with torch.cuda.graph(g):
+            _run(s, True, 0, 0.1)
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(3):
+        for s in sets:
+            for n in names:
+                s[n].fill_(0)
+        torch.cuda.synchronize()
+        for g, side in zip(graphs, streams):
+            with torch.cuda.stream(side):
+                g.replay()
+        torch.cuda.synchronize()
+        for s, want in zip(sets, alone):
+            for n in names:
+                assert torch.equal(s[n], want[n]), n

@@ -181,3 +181,19 @@ def test_widest_rows():
     assert bool(((got - want).abs() <= tol).all())
     rest = got.view(T, H, dh)[:, :, 6:]
     assert torch.equal(rest, x.double().view(T, H, dh)[:, :, 6:])
+
+
+@pytest.mark.parametrize("inplace", [True, False])
+def test_offsets_past_32_bits(inplace):
+    from paper_2309_01226_amd import ops
+    flush("rotary far rows", inplace)
+    ld, T, H, dh = (1 << 22) + 8, 1030, 2, 64
+    big = torch.empty(T * ld, device="cuda", dtype=torch.bfloat16)
+    x = big.as_strided((T, H * dh), (ld, 1))
+    out = None if inplace else big.as_strided((T, H * dh), (ld, 1), 1 << 21)
+    a = torch.randn(T, H * dh, device="cuda").to(torch.bfloat16)
+    x.copy_(a)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    got = ops.rotary_axes(x, pos, H, dh, (32,), out=out)
+    near = ops.rotary_axes(a.clone(), pos, H, dh, (32,))
+    assert torch.equal(got, near)
