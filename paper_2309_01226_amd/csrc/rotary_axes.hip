@@ -12,10 +12,11 @@
 // another buffer, of the others).  cos and sin of a row serve all its heads: a
 // workgroup takes up to 16 rows, starts the loads of its elements, forms the rows'
 // cos and sin in LDS meanwhile, then rotates.  32749 rows of 20 heads of 128, bf16 in place: 335 MB
-// in 74 us, 4.5 TB/s; 5003 rows of 32 fp32 heads of 256, half of the pairs rotated, into another
-// buffer: 328 MB in 69 us, 4.7 TB/s (a copy of 4 GiB: 4.7).  257 rows of 32 heads of 80: 4.1 us, of which about
+// in 58 us, 5.8 TB/s; 5003 rows of 32 fp32 heads of 256, a quarter of the dims rotated, into another
+// buffer: 328 MB in 57 us, 5.7 TB/s (a copy of 4 GiB: 4.7).  257 rows of 32 heads of 80: 4.1 us, of which about
 // 3 are a launch that does nothing; the call's host side is 4 us more.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -23,7 +24,7 @@
 namespace {
 
 constexpr int NT = 256;
-constexpr int U = 4;        // items of a thread in flight
+constexpr int U = 2;        // items of a thread in flight (168 MB in place: 66.7 us, four 74.0, of streams 57.9 and 62.2)
 constexpr int MAX_CS = 2048;  // (cos, sin) pairs in LDS: rows of a workgroup x pairs
 
 template <class T, int V>
@@ -31,10 +32,12 @@ struct Item {
   T a[V], b[V];  // pairs apart: first and second halves; interleaved: a only
 };
 
-template <class T, int V>
+// STREAM: past the caches.
+template <bool STREAM, class T, int V>
 __device__ __forceinline__ void ld(const T* p, T (&x)[V]) {
   if constexpr (V * sizeof(T) == 16) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+    const u32x4* q = reinterpret_cast<const u32x4*>(p);
+    const u32x4 w = STREAM ? __builtin_nontemporal_load(q) : *q;
     __builtin_memcpy(x, &w, 16);
   } else if constexpr (V * sizeof(T) == 8 && V > 2) {
     const u32x2 w = *reinterpret_cast<const u32x2*>(p);
@@ -44,12 +47,14 @@ __device__ __forceinline__ void ld(const T* p, T (&x)[V]) {
     for (int e = 0; e < V; ++e) x[e] = p[e];
   }
 }
-template <class T, int V>
+template <bool STREAM, class T, int V>
 __device__ __forceinline__ void st(T* p, const T (&x)[V]) {
   if constexpr (V * sizeof(T) == 16) {
     u32x4 w;
     __builtin_memcpy(&w, x, 16);
-    *reinterpret_cast<u32x4*>(p) = w;
+    u32x4* q = reinterpret_cast<u32x4*>(p);
+    if (STREAM) __builtin_nontemporal_store(w, q);
+    else *q = w;
   } else if constexpr (V * sizeof(T) == 8 && V > 2) {
     u32x2 w;
     __builtin_memcpy(&w, x, 8);
@@ -66,7 +71,7 @@ __device__ __forceinline__ int div_by(int x, uint32_t inv) { return inv ? (int)_
 // V: elements of one load.  INTER: pairs (2 i, 2 i + 1), V of them = V / 2 pairs per
 // item; otherwise an item is V pairs, V elements of each half.  Items of a row: for each head its
 // rotated items, then (copy) its unrotated ones, V elements each.
-template <class T, int V, bool INTER>
+template <class T, int V, bool INTER, bool STREAM>
 __global__ __launch_bounds__(NT) void rotary_axes_kernel(RotaryAxes a) {
   __shared__ float2 cs[MAX_CS];
   const int t0 = blockIdx.x * a.rows_wg;
@@ -94,8 +99,8 @@ __global__ __launch_bounds__(NT) void rotary_axes_kernel(RotaryAxes a) {
     int row, off, pair;
     place(i, row, off, pair);
     const T* p = x + (long)row * a.ldx + off;
-    ld<T, V>(p, it.a);
-    if (!INTER && pair >= 0) ld<T, V>(p + half, it.b);
+    ld<STREAM, T, V>(p, it.a);
+    if (!INTER && pair >= 0) ld<STREAM, T, V>(p + half, it.b);
   };
   auto rotate = [&](int i, Item<T, V>& it) {
     int row, off, pair;
@@ -119,10 +124,10 @@ __global__ __launch_bounds__(NT) void rotary_axes_kernel(RotaryAxes a) {
           it.a[e] = (T)(u * c - w * s);
           it.b[e] = (T)(u * s + w * c);
         }
-        st<T, V>(p + half, it.b);
+        st<STREAM, T, V>(p + half, it.b);
       }
     }
-    st<T, V>(p, it.a);
+    st<STREAM, T, V>(p, it.a);
   };
 
   Item<T, V> it[U];
@@ -166,13 +171,21 @@ hipError_t launch(RotaryAxes a, bool inter, bool copy, hipStream_t s) {
   a.inv_head_items = inv_of(a.head_items);
   a.inv_half = inv_of(a.half);
   const dim3 grid((unsigned)sat_cdiv(a.T, rows));
+  // What does not stay in the last-level cache (256 MB) for the next operator goes past the caches: 2 x 168 MB 57.9
+  // us against 66.7, 2 x 96 MB from memory 34.2 against 39.5 (from the cache 33.5 against 31.5); 2 x 64 MB
+  // would be 24.1 against 22.0.
+  const bool stream = V * sizeof(T) == 16 && (double)a.T * a.H * (copy ? 2 * a.dh : 2 * a.half) * sizeof(T) >= 80e6;
+  auto go = [&](auto inter_, auto stream_) {
+    hipLaunchKernelGGL((rotary_axes_kernel<T, V, decltype(inter_)::value, decltype(stream_)::value>), grid, dim3(NT), 0, s, a);
+    return hipGetLastError();
+  };
+  using Yes = std::true_type;
+  using No = std::false_type;
+  if constexpr (V * sizeof(T) == 16)
+    if (stream) return inter ? go(Yes(), Yes()) : go(No(), Yes());
   if constexpr (V > 1)
-    if (inter) {
-      hipLaunchKernelGGL((rotary_axes_kernel<T, V, true>), grid, dim3(NT), 0, s, a);
-      return hipGetLastError();
-    }
-  hipLaunchKernelGGL((rotary_axes_kernel<T, V, false>), grid, dim3(NT), 0, s, a);
-  return hipGetLastError();
+    if (inter) return go(Yes(), No());
+  return go(No(), No());
 }
 
 }  // namespace

@@ -197,3 +197,19 @@ def test_offsets_past_32_bits(inplace):
     got = ops.rotary_axes(x, pos, H, dh, (32,), out=out)
     near = ops.rotary_axes(a.clone(), pos, H, dh, (32,))
     assert torch.equal(got, near)
+
+
+@pytest.mark.parametrize("inter", [True, False])
+@pytest.mark.parametrize("dt,T", [(torch.bfloat16, 11003), (torch.float32, 5503)])
+@pytest.mark.parametrize("inplace", [True, False])
+def test_large_calls_as_their_parts(inplace, dt, T, inter):
+    """Past 80 MB the rows bypass the caches: the same bits as calls on fewer rows."""
+    from paper_2309_01226_amd import ops
+    flush("rotary large", inplace, dt, T, inter)
+    H, dh = 30, 128
+    x = torch.randn(T, H * dh, device="cuda").to(dt)
+    pos = torch.randint(-99, 999, (T, 2), device="cuda", dtype=torch.int32)
+    kw = dict(interleaved=inter, inverse=True)
+    want = torch.cat([ops.rotary_axes(a.clone(), p, H, dh, (24, 40), **kw) for a, p in zip(x.split(1999), pos.split(1999))])
+    got = ops.rotary_axes(x, pos, H, dh, (24, 40), out=None if inplace else torch.empty_like(x), **kw)
+    assert torch.equal(got, want)
