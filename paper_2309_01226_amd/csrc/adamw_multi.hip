@@ -25,7 +25,9 @@
 // kernel arguments (nothing is copied to the device, so the call needs no workspace and can be
 // captured); a wave takes whole blocks, four consecutive elements per lane, and has the loads of all its blocks
 // in flight first.  4096 elements a workgroup; 1024 where the whole table would give 256 CUs fewer than four
-// workgroups each: 0.17 M elements 9.0 -> 4.2 us, large tables the same within 1 %.  Whole aligned runs take a
+// workgroups each: 0.17 M elements 9.0 -> 4.2 us, large tables the same within 1 %.  Such a table (up to 126 MB)
+// stays in the last-level cache from step to step, a larger one goes past the caches: 2 M elements 8.1 us, past them
+// 10.5; 4 M 19.8 and 21.3; 160 M with 32-bit moments 883 us through the caches, 799 past them.  Whole aligned runs take a
 // straight-line path (8 bits: 1891 -> 1197 us), the others go element by element.
 // 160 M values with 32-bit moments: 4.79 GB in 807 us, 5.9 TB/s; 444 M with 8-bit ones: 7.1 GB in 1197 us, 5.9;
 // reading their values back as bf16, 6 bytes each: 500 us, 5.3.  (A copy of 4 GiB moves 4.7 TB/s; the
@@ -46,11 +48,12 @@ __device__ __forceinline__ int entry_of(const int* first, int count, int wg) {
   return __builtin_amdgcn_readfirstlane((int)__popcll(__builtin_amdgcn_ballot_w64(at)) - 1);
 }
 
-// N elements from i on.  FULL: all below n and aligned; otherwise one by one.
-template <bool FULL, class V, class T, int N>
+// N elements from i on.  FULL: all below n and aligned; otherwise one by one.  STREAM: past the caches.
+template <bool FULL, class V, bool STREAM, class T, int N>
 __device__ __forceinline__ void load(const T* p, long i, long n, T (&x)[N]) {
   if constexpr (FULL) {
-    const V v = __builtin_nontemporal_load(reinterpret_cast<const V*>(p + i));
+    const V* q = reinterpret_cast<const V*>(p + i);
+    const V v = STREAM ? __builtin_nontemporal_load(q) : *q;
 #pragma unroll
     for (int e = 0; e < N; ++e) x[e] = v[e];
   } else {
@@ -58,13 +61,15 @@ __device__ __forceinline__ void load(const T* p, long i, long n, T (&x)[N]) {
     for (int e = 0; e < N; ++e) x[e] = i + e < n ? p[i + e] : T(0);
   }
 }
-template <bool FULL, class V, class T, int N>
+template <bool FULL, class V, bool STREAM, class T, int N>
 __device__ __forceinline__ void store(T* p, long i, long n, const T (&x)[N]) {
   if constexpr (FULL) {
     V v;
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = x[e];
-    __builtin_nontemporal_store(v, reinterpret_cast<V*>(p + i));
+    V* q = reinterpret_cast<V*>(p + i);
+    if (STREAM) __builtin_nontemporal_store(v, q);
+    else *q = v;
   } else {
 #pragma unroll
     for (int e = 0; e < N; ++e)
@@ -120,6 +125,7 @@ struct Vec8<bf16> { using type = bf16x8; };
 // A wave's NB runs of 256 elements from `b0` (in runs) on.
 template <class G, int NB, bool FULL>
 __device__ __forceinline__ void step32(const AdamWEntry& t, const AdamWConsts& c, long b0) {
+  constexpr bool STREAM = NB > 1;
   using GV = typename Vec4<G>::type;
   const long n = t.n, i0 = b0 * 256 + 4 * (threadIdx.x & 63);
   float* m = (float*)t.m;
@@ -128,10 +134,10 @@ __device__ __forceinline__ void step32(const AdamWEntry& t, const AdamWConsts& c
   G gg[NB][4];
 #pragma unroll
   for (int u = 0; u < NB; ++u) {
-    load<FULL, floatx4>((const float*)t.p, i0 + u * 256, n, pp[u]);
-    load<FULL, GV>((const G*)t.g, i0 + u * 256, n, gg[u]);
-    load<FULL, floatx4>((const float*)m, i0 + u * 256, n, mm[u]);
-    load<FULL, floatx4>((const float*)v, i0 + u * 256, n, vv[u]);
+    load<FULL, floatx4, STREAM>((const float*)t.p, i0 + u * 256, n, pp[u]);
+    load<FULL, GV, STREAM>((const G*)t.g, i0 + u * 256, n, gg[u]);
+    load<FULL, floatx4, STREAM>((const float*)m, i0 + u * 256, n, mm[u]);
+    load<FULL, floatx4, STREAM>((const float*)v, i0 + u * 256, n, vv[u]);
   }
 #pragma unroll
   for (int u = 0; u < NB; ++u) {
@@ -142,16 +148,17 @@ __device__ __forceinline__ void step32(const AdamWEntry& t, const AdamWConsts& c
       adamw_one(pp[u][e], (float)gg[u][e], mm[u][e], vv[u][e], c);
       sh[e] = f2bf(pp[u][e]);
     }
-    store<FULL, floatx4>(t.p, i, n, pp[u]);
-    store<FULL, floatx4>(m, i, n, mm[u]);
-    store<FULL, floatx4>(v, i, n, vv[u]);
-    if (t.shadow != nullptr) store<FULL, bf16x4>(t.shadow, i, n, sh);
+    store<FULL, floatx4, STREAM>(t.p, i, n, pp[u]);
+    store<FULL, floatx4, STREAM>(m, i, n, mm[u]);
+    store<FULL, floatx4, STREAM>(v, i, n, vv[u]);
+    if (t.shadow != nullptr) store<FULL, bf16x4, STREAM>(t.shadow, i, n, sh);
   }
 }
 
 // A wave's NB blocks from b0 on.
 template <class G, int NB, bool FULL>
 __device__ __forceinline__ void step8(const AdamWEntry& t, const AdamWConsts& c, long b0) {
+  constexpr bool STREAM = NB > 1;
   using GV = typename Vec4<G>::type;
   const int lane = threadIdx.x & 63;
   const long n = t.n, i0 = b0 * 256 + 4 * lane;
@@ -167,10 +174,10 @@ __device__ __forceinline__ void step8(const AdamWEntry& t, const AdamWConsts& c,
     const bool live = FULL || (b0 + u) * 256 < n;
     me[u] = live ? t.m_exp[b0 + u] : 0;
     ve[u] = live ? t.v_exp[b0 + u] : 0;
-    load<FULL, u8x4>((const uint8_t*)m, i0 + u * 256, n, mc[u]);
-    load<FULL, u8x4>((const uint8_t*)v, i0 + u * 256, n, vc[u]);
-    load<FULL, GV>((const G*)t.g, i0 + u * 256, n, gg[u]);
-    load<FULL, floatx4>((const float*)t.p, i0 + u * 256, n, pp[u]);
+    load<FULL, u8x4, STREAM>((const uint8_t*)m, i0 + u * 256, n, mc[u]);
+    load<FULL, u8x4, STREAM>((const uint8_t*)v, i0 + u * 256, n, vc[u]);
+    load<FULL, GV, STREAM>((const G*)t.g, i0 + u * 256, n, gg[u]);
+    load<FULL, floatx4, STREAM>((const float*)t.p, i0 + u * 256, n, pp[u]);
   }
 #pragma unroll
   for (int u = 0; u < NB; ++u) {
@@ -194,8 +201,8 @@ __device__ __forceinline__ void step8(const AdamWEntry& t, const AdamWConsts& c,
       mtop = max(mtop, __float_as_uint(mm[e]) & 0x7FFFFFFFu);
       rtop = max(rtop, __float_as_uint(rr[e]));
     }
-    store<FULL, floatx4>(t.p, i, n, pp[u]);
-    if (t.shadow != nullptr) store<FULL, bf16x4>(t.shadow, i, n, sh);
+    store<FULL, floatx4, STREAM>(t.p, i, n, pp[u]);
+    if (t.shadow != nullptr) store<FULL, bf16x4, STREAM>(t.shadow, i, n, sh);
     const int em = block_exp<3>(wave_umax(mtop)), er = block_exp<4>(wave_umax(rtop));
     const uint32_t h0 = ((uint32_t)i + t.key) * 0x9E3779B1u;
 #pragma unroll
@@ -209,8 +216,8 @@ __device__ __forceinline__ void step8(const AdamWEntry& t, const AdamWConsts& c,
       mc[u][e] = (uint8_t)(qm | (int)(mb >> 31) << 7);
       vc[u][e] = (uint8_t)(rr[e] > 0.f ? qr : 0);
     }
-    store<FULL, u8x4>(m, i, n, mc[u]);
-    store<FULL, u8x4>(v, i, n, vc[u]);
+    store<FULL, u8x4, STREAM>(m, i, n, mc[u]);
+    store<FULL, u8x4, STREAM>(v, i, n, vc[u]);
     if (lane == 0) {
       t.m_exp[b0 + u] = (uint8_t)em;
       t.v_exp[b0 + u] = (uint8_t)er;
@@ -251,8 +258,8 @@ __device__ __forceinline__ void values(const AdamWEntry& t, long b0) {
     const bool live = FULL || b * 256 < n;
     me[u] = live ? t.m_exp[b] : 0;
     ve[u] = live ? t.v_exp[b] : 0;
-    load<FULL, u8x8>((const uint8_t*)t.m, i0 + u * 512, n, mc[u]);
-    load<FULL, u8x8>((const uint8_t*)t.v, i0 + u * 512, n, vc[u]);
+    load<FULL, u8x8, true>((const uint8_t*)t.m, i0 + u * 512, n, mc[u]);
+    load<FULL, u8x8, true>((const uint8_t*)t.v, i0 + u * 512, n, vc[u]);
   }
 #pragma unroll
   for (int u = 0; u < R; ++u) {
@@ -263,8 +270,8 @@ __device__ __forceinline__ void values(const AdamWEntry& t, long b0) {
       mo[e] = (O)decode_m(mc[u][e], me[u]);
       vo[e] = (O)(r * r);
     }
-    store<FULL, OV>((O*)t.m_out, i0 + u * 512, n, mo);
-    store<FULL, OV>((O*)t.v_out, i0 + u * 512, n, vo);
+    store<FULL, OV, true>((O*)t.m_out, i0 + u * 512, n, mo);
+    store<FULL, OV, true>((O*)t.v_out, i0 + u * 512, n, vo);
   }
 }
 
