@@ -30,7 +30,7 @@
 // 10.5; 4 M 19.8 and 21.3; 160 M with 32-bit moments 883 us through the caches, 799 past them.  Whole aligned runs take a
 // straight-line path (8 bits: 1891 -> 1197 us), the others go element by element.
 // 160 M values with 32-bit moments: 4.79 GB in 807 us, 5.9 TB/s; 444 M with 8-bit ones: 7.1 GB in 1197 us, 5.9;
-// reading their values back as bf16, 6 bytes each: 500 us, 5.3.  (A copy of 4 GiB moves 4.7 TB/s; the
+// reading the values of 466 M back as bf16, 6 bytes each: 470 us, 5.9.  (A copy of 4 GiB moves 4.7 TB/s; the
 // reads and writes here bypass the caches.)
 #include "adamw_math.h"
 #include "common.h"
@@ -115,12 +115,13 @@ template <>
 struct Vec4<float> { using type = floatx4; };
 template <>
 struct Vec4<bf16> { using type = bf16x4; };
+// Of 16 bytes of values, and their codes.
 template <class O>
-struct Vec8;
+struct Store;
 template <>
-struct Vec8<float> { typedef float type __attribute__((ext_vector_type(8))); };
+struct Store<float> { using type = floatx4; using codes = u8x4; };
 template <>
-struct Vec8<bf16> { using type = bf16x8; };
+struct Store<bf16> { using type = bf16x8; using codes = u8x8; };
 
 // A wave's NB runs of 256 elements from `b0` (in runs) on.
 template <class G, int NB, bool FULL>
@@ -243,35 +244,37 @@ __global__ __launch_bounds__(256) void adamw_multi_kernel(AdamWMulti a) {
 }
 
 // The values that 8-bit moments stand for: m and v = r^2 (both exact in fp32; m also in bf16).  A
-// lane takes eight elements, so that a wave's bf16 values are stored 16 bytes at a time.
+// lane takes as many elements as fill a store of 16 bytes, so that a wave's stores are whole lines (fp32, 210 M
+// elements: eight a lane 450 us, four 377).
 template <class O, int NB, bool FULL>
 __device__ __forceinline__ void values(const AdamWEntry& t, long b0) {
-  using OV = typename Vec8<O>::type;
+  using OV = typename Store<O>::type;
+  using CV = typename Store<O>::codes;
+  constexpr int E = 16 / sizeof(O), R = NB * 4 / E;  // elements of a lane, rounds of a wave
   const int lane = threadIdx.x & 63;
-  const long n = t.n, i0 = b0 * 256 + 8 * lane;
-  constexpr int R = NB / 2;  // rounds of two blocks
-  uint8_t mc[R][8], vc[R][8];
+  const long n = t.n, i0 = b0 * 256 + E * lane;
+  uint8_t mc[R][E], vc[R][E];
   int me[R], ve[R];
 #pragma unroll
   for (int u = 0; u < R; ++u) {
-    const long b = b0 + 2 * u + (lane >> 5);
+    const long b = (i0 + u * 64 * E) >> 8;
     const bool live = FULL || b * 256 < n;
     me[u] = live ? t.m_exp[b] : 0;
     ve[u] = live ? t.v_exp[b] : 0;
-    load<FULL, u8x8, true>((const uint8_t*)t.m, i0 + u * 512, n, mc[u]);
-    load<FULL, u8x8, true>((const uint8_t*)t.v, i0 + u * 512, n, vc[u]);
+    load<FULL, CV, true>((const uint8_t*)t.m, i0 + u * 64 * E, n, mc[u]);
+    load<FULL, CV, true>((const uint8_t*)t.v, i0 + u * 64 * E, n, vc[u]);
   }
 #pragma unroll
   for (int u = 0; u < R; ++u) {
-    O mo[8], vo[8];
+    O mo[E], vo[E];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < E; ++e) {
       const float r = decode<4>(vc[u][e], ve[u]);
       mo[e] = (O)decode_m(mc[u][e], me[u]);
       vo[e] = (O)(r * r);
     }
-    store<FULL, OV, true>((O*)t.m_out, i0 + u * 512, n, mo);
-    store<FULL, OV, true>((O*)t.v_out, i0 + u * 512, n, vo);
+    store<FULL, OV, true>((O*)t.m_out, i0 + u * 64 * E, n, mo);
+    store<FULL, OV, true>((O*)t.v_out, i0 + u * 64 * E, n, vo);
   }
 }
 

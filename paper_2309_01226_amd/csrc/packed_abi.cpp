@@ -279,7 +279,7 @@ extern "C" sat_status sat_op_adamw_multi_state(const sat_adamw_tensor* t, int32_
         o.m = e.m; o.v = e.v; o.m_exp = e.m_exp; o.v_exp = e.v_exp;
         o.m_out = m_out[k]; o.v_out = v_out[k];
         o.n = e.n;
-        o.vec = aligned(e.m, 8) && aligned(e.v, 8) && aligned(m_out[k], 8 * oa) && aligned(v_out[k], 8 * oa);
+        o.vec = aligned(e.m, 16 / oa) && aligned(e.v, 16 / oa) && aligned(m_out[k], 16) && aligned(v_out[k], 16);
       },
       [&](const AdamWMulti& a, int chunks) { return launch_adamw_state(a, chunks, out_bf16 != 0, S(stream)); }));
   return SAT_OK;
