@@ -24,7 +24,8 @@
 //
 // Every kernel also runs over packed sequences (AttnPackedArgs: rows of one sequence in place of one
 // batch row, query heads that share K / V heads, a window; PAD: heads of 136 to 248
-// dims with zeros behind them).  The batch form's arithmetic does not change with it.
+// dims with zeros behind them).  Few blocks are split among workgroups there, as in attn_packed.hip: 8192 rows,
+// one head, causal: forward 248 -> 80 us, backward 865 -> 263.  The batch form's arithmetic does not change with it.
 #include <type_traits>
 
 #include "attn_packed.h"
@@ -210,6 +211,8 @@ __device__ __forceinline__ void fwd_block(FwdState& st, const bf16* Ks, const bf
   }
 }
 
+constexpr int FWD_REGS = DH / 2 + 4;  // of a lane's part in the scratch: O, then m and l
+
 template <class A>
 constexpr bool kPacked = !std::is_same_v<A, AttnArgs> && !std::is_same_v<A, AttnBwdArgs>;
 
@@ -218,14 +221,17 @@ __global__ __launch_bounds__(NT, 1) void attn256_fwd_kernel(A a) {
   constexpr bool PK = kPacked<A>;
   __shared__ __attribute__((aligned(1024))) bf16 smem[2 * 2 * TILE];  // 2 stages x (K, V)
   int S, qb, h, kvh, dh = DH;  // K / V head kvh; first row and its lse from here on
-  long row0, lrow;
+  int sp = 0;                  // part of the block's keys, and its place in the scratch
+  long row0, lrow, at = 0;
   if constexpr (PK) {
     dh = a.dh;
     const int G = a.H / a.Hkv;
     int tile, part, s0;
-    if (!packed_item(a, G, tile, kvh, part)) return;
+    if (!packed_item(a, G * a.split, tile, kvh, part)) return;
     if (!find_rows(a, tile, QPB, s0, S, qb)) return;
-    h = kvh * G + part;
+    h = kvh * G + part / a.split;
+    sp = part % a.split;
+    at = ((long)tile * a.H + h) * a.split + sp;
     row0 = s0;
     lrow = (long)h * a.T + s0;
   } else {
@@ -287,6 +293,7 @@ __global__ __launch_bounds__(NT, 1) void attn256_fwd_kernel(A a) {
   if constexpr (PK) {
     jb = key_lo(a, q0) / KB;
     je = (key_hi(a, q0 + QPB - 1, S) + KB - 1) / KB;
+    part_of(sp, a.split, jb, je);
     wlo = key_lo(a, wq0);
     whi = wq0 < S ? key_hi(a, wq0 + WQ - 1, S) : 0;
     flo = key_lo(a, wq0 + WQ - 1);
@@ -305,8 +312,8 @@ __global__ __launch_bounds__(NT, 1) void attn256_fwd_kernel(A a) {
     copy_block<0, PAD>(rows_rsrc(Kb, j * KB, a.ldk), a.ldk, S - j * KB, st, wave, dh);
     copy_block<1, PAD>(rows_rsrc(Vb, j * KB, a.ldv), a.ldv, S - j * KB, st + TILE, wave, dh);
   };
-  // prologue: the first block
-  copy(jb);
+  // prologue: the first block (a part may have none)
+  if (!PK || jb < je) copy(jb);
   wait_vm_lgkm0<0>();
   cta_barrier();
 
@@ -319,6 +326,14 @@ __global__ __launch_bounds__(NT, 1) void attn256_fwd_kernel(A a) {
     if (j + 1 < je) {
       wait_vm_lgkm0<0>();
       cta_barrier();
+    }
+  }
+  if constexpr (PK) {
+    if (a.split > 1) {
+      float* p = wave_share(a.ws, at, 4, FWD_REGS, wave);
+      put_acc(p, st.o);
+      *reinterpret_cast<floatx2*>(p + (DH / 2) * 64) = floatx2{st.m, st.l};
+      return;
     }
   }
   if (q < S) {
@@ -399,11 +414,14 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(A a) {
   bf16* rfs = smem + 2 * STG_B + 4 * 64 * 16 * 2;
   int S, k0, kvh, heads = 1, dh = DH;  // query heads that read K / V head kvh
   long row0, lrow, lhead = 0;  // lse of row0 for the first head, and from head to head
+  int sp = 0;                  // part of the block's steps, and its place in the scratch
+  long at = 0;
   if constexpr (PK) {
     dh = a.f.dh;
     heads = a.f.H / a.f.Hkv;
-    int tile, part, s0, blk;
-    if (!packed_item(a.f, 1, tile, kvh, part)) return;
+    int tile, s0, blk;
+    if (!packed_item(a.f, a.f.split, tile, kvh, sp)) return;
+    at = ((long)tile * a.f.Hkv + kvh) * a.f.split + sp;
     if (!find_rows(a.f, tile, KPW, s0, S, blk)) return;
     // causal: the first keys see the most queries, so the places count from the end
     k0 = (a.f.causal ? (S + KPW - 1) / KPW - 1 - blk : blk) * KPW;
@@ -479,7 +497,9 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(A a) {
     wlo = a.f.causal ? kmin : 0;
     lo = a.f.causal ? key : 0;
   }
-  const int nqb = (q_end - q_start + BQ - 1) / BQ, total = nqb * heads;  // step i nqb + j: block j of head i
+  const int nqb = (q_end - q_start + BQ - 1) / BQ;
+  int first = 0, total = nqb * heads;  // step i nqb + j: block j of head i
+  if constexpr (PK) part_of(sp, a.f.split, first, total);
   float* xw = xbuf + pair * 16 * 64;
   float lsd = 0.f;  // wave 0: lse2 (lanes 0..31) or delta (lanes 32..63) of the next block
 
@@ -502,13 +522,15 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(A a) {
     if (wave == 0) reinterpret_cast<float*>(stage_ptr(j) + 2 * QT)[lane] = g ? lsd : lsd * LOG2E;
   };
 
-  fetch(0);
-  wait_vm_lgkm0<0>();
-  publish(0);
+  if (!PK || first < total) {  // a part may have no step
+    fetch(first);
+    wait_vm_lgkm0<0>();
+    publish(first);
+  }
   wait_vm_lgkm0<0>();
   cta_barrier();
 
-  for (int j = 0; j < total; ++j) {
+  for (int j = first; j < total; ++j) {
     const int qs0 = q_start + (PK ? j % nqb : j) * BQ;
     const bf16* st = stage_ptr(j);
     const bf16* Qs = st;
@@ -605,6 +627,12 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dkdv_kernel(A a) {
       cta_barrier();
     }
   }
+  if constexpr (PK) {
+    if (a.f.split > 1) {
+      put_acc(wave_share(a.f.ws, at, 4, DH, pair) + (role ? 0 : DH / 2 * 64), acc);
+      return;
+    }
+  }
   if (key < S) {
     bf16* out = role ? a.dk + (row0 + key) * a.lddk + (long)kvh * dh
                      : a.dv + (row0 + key) * a.lddv + (long)kvh * dh;
@@ -645,21 +673,24 @@ constexpr int STG_Q = 2 * QT;  // K rows, V rows of a 32-key block
 constexpr int NSTG_Q = 4;      // K / V stages
 constexpr int XB = 4 * 16 * 64;  // floats of one P^T exchange buffer (4 pairs)
 
-template <class A, bool PAD>
+template <class A, bool PAD, bool SPLIT>  // SPLIT: a.split > 1, of packed sequences (one spilled value, which costs the others 1.5 %)
 __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(A a) {
   constexpr bool PK = kPacked<A>;
   static_assert((NSTG_Q * STG_Q + 2 * XB * 2) * 2 <= 163840, "LDS budget");
   __shared__ __attribute__((aligned(1024))) bf16 smem[NSTG_Q * STG_Q + 2 * XB * 2];
   float* xbuf = reinterpret_cast<float*>(smem + NSTG_Q * STG_Q);
   int S, qb, h, kvh, dh = DH;
+  int sp = 0;  // part of the block's keys
   long row0, hs;
   if constexpr (PK) {
     dh = a.f.dh;
     const int G = a.f.H / a.f.Hkv;
     int tile, part, s0;
-    if (!packed_item(a.f, G, tile, kvh, part)) return;
+    const int split = SPLIT ? a.f.split : 1;
+    if (!packed_item(a.f, G * split, tile, kvh, part)) return;
     if (!find_rows(a.f, tile, QPW, s0, S, qb)) return;
-    h = kvh * G + part;
+    h = kvh * G + part / split;
+    sp = part % split;
     row0 = s0;
     hs = (long)h * a.f.T + s0;
   } else {
@@ -716,7 +747,7 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(A a) {
       for (int e = 0; e < 8; ++e) acc = __builtin_fmaf(bf2f(rf[c][e]), bf2f(ov[e]), acc);
     }
     lsd = halves_sum(acc);
-    if (g == 0 && q < S) a.delta[hs + q] = lsd;
+    if (g == 0 && q < S && sp == 0) a.delta[hs + q] = lsd;
   }
   floatx16 acc[DH / 32];  // dQ^T (role B): dims 32 ot + acc_row(r, g), query = lane
 #pragma unroll
@@ -735,6 +766,7 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(A a) {
   if constexpr (PK) {
     jb = key_lo(a.f, q0) / BQ;
     je = (key_hi(a.f, q0 + QPW - 1, S) + BQ - 1) / BQ;
+    if (SPLIT) part_of(sp, a.f.split, jb, je);
     wlo = key_lo(a.f, pq0);
     whi = pq0 < S ? key_hi(a.f, pq0 + 31, S) : 0;
     lo = key_lo(a.f, q);
@@ -753,7 +785,7 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(A a) {
     copy_rows32<PAD>(rows_rsrc(Vb, kv, a.f.ldv), a.f.ldv, S - kv, st + QT, wave, dh);
   };
 
-  fetch(jb);
+  if (!SPLIT || jb < je) fetch(jb);  // a part may have no block
   if (je - jb > 1) {
     fetch(jb + 1);
     wait_vm_lgkm0<4>();  // the first block resident, the second may stay in flight
@@ -818,6 +850,12 @@ __global__ __launch_bounds__(NT8, 1) void attn256_bwd_dq_kernel(A a) {
         acc[i & 7] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tread(i), xb[i >> 3], acc[i & 7], 0, 0, 0);
     }
   }
+  if constexpr (SPLIT) {
+    int tile, kv, part;  // again: kept over the loop they spill
+    packed_item(a.f, a.f.H / a.f.Hkv * a.f.split, tile, kv, part);
+    if (role == 1) put_acc(wave_share(a.f.ws, ((long)tile * a.f.H + h) * a.f.split + sp, 4, DH / 2, pair), acc);
+    return;
+  }
   if (role == 1 && q < S) {
     bf16* out = a.dq + (row0 + q) * a.lddq + (long)h * dh;
 #pragma unroll
@@ -860,7 +898,7 @@ hipError_t launch_attn256_bwd_dkdv(const AttnBwdArgs& a, hipStream_t s) {
 
 hipError_t launch_attn256_bwd_dq(const AttnBwdArgs& a, hipStream_t s) {
   dim3 grid((unsigned)(((a.f.S + QPW - 1) / QPW) * a.f.B * a.f.H));
-  hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnBwdArgs, false>), grid, dim3(NT8), 0, s, a);
+  hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnBwdArgs, false, false>), grid, dim3(NT8), 0, s, a);
   return hipGetLastError();
 }
 
@@ -871,23 +909,32 @@ hipError_t launch_attn256_fwd(const AttnArgs& a, hipStream_t s) {
 }
 
 // Packed sequences: 128-row blocks of one sequence.
-hipError_t launch_attn256_packed_fwd(const AttnPackedArgs& args, hipStream_t s) {
+hipError_t launch_attn256_packed_fwd(const AttnPackedArgs& args, int split, hipStream_t s) {
   AttnPackedArgs a = args;
-  const dim3 grid(packed_grid(a, QPB, a.H / a.Hkv));
+  a.split = split;
+  const dim3 grid(packed_grid(a, QPB, a.H / a.Hkv * split));
   if (a.dh == DH) hipLaunchKernelGGL((attn256_fwd_kernel<AttnPackedArgs, false>), grid, dim3(NT), 0, s, a);
   else hipLaunchKernelGGL((attn256_fwd_kernel<AttnPackedArgs, true>), grid, dim3(NT), 0, s, a);
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess && split > 1 ? launch_attn_packed_join(a, 4, s) : e;
 }
 
-hipError_t launch_attn256_packed_bwd(const AttnPackedBwdArgs& args, hipStream_t s) {
-  AttnPackedBwdArgs a = args;
-  const dim3 qgrid(packed_grid(a.f, QPW, a.f.H / a.f.Hkv));
-  if (a.f.dh == DH) hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnPackedBwdArgs, false>), qgrid, dim3(NT8), 0, s, a);
-  else hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnPackedBwdArgs, true>), qgrid, dim3(NT8), 0, s, a);
-  const hipError_t e = hipGetLastError();
+template <bool PAD>
+static hipError_t packed_bwd(AttnPackedBwdArgs a, int qsplit, int ksplit, hipStream_t s) {
+  a.f.split = qsplit;
+  const dim3 qgrid(packed_grid(a.f, QPW, a.f.H / a.f.Hkv * qsplit));
+  if (qsplit > 1) hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnPackedBwdArgs, PAD, true>), qgrid, dim3(NT8), 0, s, a);
+  else hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnPackedBwdArgs, PAD, false>), qgrid, dim3(NT8), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && qsplit > 1) e = launch_attn_packed_add(a, 4, false, false, s);
   if (e != hipSuccess) return e;
-  const dim3 kgrid(packed_grid(a.f, KPW, 1));
-  if (a.f.dh == DH) hipLaunchKernelGGL((attn256_bwd_dkdv_kernel<AttnPackedBwdArgs, false>), kgrid, dim3(NT8), 0, s, a);
-  else hipLaunchKernelGGL((attn256_bwd_dkdv_kernel<AttnPackedBwdArgs, true>), kgrid, dim3(NT8), 0, s, a);
-  return hipGetLastError();
+  a.f.split = ksplit;
+  const dim3 kgrid(packed_grid(a.f, KPW, ksplit));
+  hipLaunchKernelGGL((attn256_bwd_dkdv_kernel<AttnPackedBwdArgs, PAD>), kgrid, dim3(NT8), 0, s, a);
+  e = hipGetLastError();
+  return e == hipSuccess && ksplit > 1 ? launch_attn_packed_add(a, 4, true, false, s) : e;
+}
+
+hipError_t launch_attn256_packed_bwd(const AttnPackedBwdArgs& a, int qsplit, int ksplit, hipStream_t s) {
+  return a.f.dh == DH ? packed_bwd<false>(a, qsplit, ksplit, s) : packed_bwd<true>(a, qsplit, ksplit, s);
 }

@@ -173,6 +173,40 @@ __device__ __forceinline__ int key_hi(const AttnPackedArgs& a, int q, int S) {
 __device__ __forceinline__ int query_lo(const AttnPackedArgs& a, int k) { return a.causal ? k : max(0, k - a.window + 1); }
 __device__ __forceinline__ int query_hi(const AttnPackedArgs& a, int k, int S) { return min(S, k + a.window); }
 
+// Part sp of `split` of a block's steps [j0, j1).
+__device__ __forceinline__ void part_of(int sp, int split, int& j0, int& j1) {
+  const int n = j1 - j0, b = j0;
+  j0 = b + (int)((long)sp * n / split);
+  j1 = b + (int)((long)(sp + 1) * n / split);
+}
+
+// Partial results of a part: a wave's accumulators, 64 lanes side by side, at `at` (a part's place in the
+// scratch) + its own share of `regs` registers.
+__device__ __forceinline__ float* wave_share(float* ws, long at, int NW, int regs, int wave) {
+  return ws + ((at * NW + wave) * regs) * 64 + (threadIdx.x & 63) * 4;
+}
+template <int OT>
+__device__ __forceinline__ void put_acc(float* p, const floatx16 (&acc)[OT]) {
+#pragma unroll
+  for (int t = 0; t < OT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<floatx4*>(p + (4 * t + i) * 256) =
+          floatx4{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
+}
+// Tile t of a transposed accumulator set (32 head dims, column = this lane's row) times f to out[0 .. dh).
+__device__ __forceinline__ void store_tile(bf16* out, const floatx4 (&acc)[4], int t, float f, int g, int dh) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int col = 32 * t + 8 * i + 4 * g;
+    if (col >= dh) continue;
+    bf16x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = f2bf(acc[i][e] * f);
+    *reinterpret_cast<bf16x4*>(out + col) = y;
+  }
+}
+
 }  // namespace
 
 // Launch shape for blocks of R rows and `per` workgroups on each block and K / V head: sets

@@ -33,39 +33,6 @@
 
 namespace {
 
-// Part sp of `split` of a block's steps [j0, j1).
-__device__ __forceinline__ void part_of(int sp, int split, int& j0, int& j1) {
-  const int n = j1 - j0, b = j0;
-  j0 = b + (int)((long)sp * n / split);
-  j1 = b + (int)((long)(sp + 1) * n / split);
-}
-
-// Partial results of a part: a wave's accumulators, 64 lanes side by side, at `at` (a part's place in the
-// scratch) + its own share of `regs` registers.
-__device__ __forceinline__ float* wave_share(float* ws, long at, int NW, int regs, int wave) {
-  return ws + ((at * NW + wave) * regs) * 64 + (threadIdx.x & 63) * 4;
-}
-template <int OT>
-__device__ __forceinline__ void put_acc(float* p, const floatx16 (&acc)[OT]) {
-#pragma unroll
-  for (int t = 0; t < OT; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<floatx4*>(p + (4 * t + i) * 256) =
-          floatx4{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
-}
-template <int OT>
-__device__ __forceinline__ void add_acc(const float* p, float f, floatx16 (&acc)[OT]) {
-#pragma unroll
-  for (int t = 0; t < OT; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const floatx4 x = *reinterpret_cast<const floatx4*>(p + (4 * t + i) * 256);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[t][4 * i + e] = __builtin_fmaf(x[e], f, acc[t][4 * i + e]);
-    }
-}
-
 // 80-wide heads of four waves are held to the registers of three waves on a SIMD (one value spilled before the
 // loop): 50 images, 16 heads, 61.4 -> 56.5 us; 4 x 4096 rows causal 246 -> 235.  64-wide ones have three anyway, and
 // four would spill in the loop (30 -> 35 us on 16 short documents).
@@ -144,37 +111,6 @@ __global__ __launch_bounds__(64 * NW, DH == 80 && NW == 4 ? 3 : 2) void attn_pac
     const float inv = (st.l > 0.f) ? 1.f / st.l : 0.f;
     store_rowT<DH, PAD>(a.o + (long)(s0 + q) * a.ldo + (long)h * a.dh, st.o, inv, g, a.dh);
     if (g == 0) a.lse[(long)h * a.T + s0 + q] = (st.m + log2f(st.l)) * LN2;
-  }
-}
-
-// Joins the parts of a split forward: each part's o and l under the common maximum.
-template <int DH, int NW, bool PAD>
-__global__ __launch_bounds__(64 * NW) void attn_packed_join_kernel(AttnPackedArgs a) {
-  using C = Cfg<DH>;
-  constexpr int WGR = NW * WR;
-  const int G = a.H / a.Hkv;
-  int tile, kvh, part, s0, S, qb;
-  if (!packed_item(a, G, tile, kvh, part)) return;
-  if (!find_rows(a, tile, WGR, s0, S, qb)) return;
-  const int h = kvh * G + part, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q = qb * WGR + wave * WR + (lane & 31);
-  const long at = ((long)tile * a.H + h) * a.split;
-  auto share = [&](int sp) { return wave_share(a.ws, at + sp, NW, 16 * C::OT + 4, wave); };
-  float m = -INFINITY, l = 0.f;
-  for (int sp = 0; sp < a.split; ++sp) m = fmaxf(m, share(sp)[16 * C::OT * 64]);
-  floatx16 o[C::OT];
-#pragma unroll
-  for (int t = 0; t < C::OT; ++t) o[t] = zero16();
-  for (int sp = 0; sp < a.split; ++sp) {
-    const floatx2 ml = *reinterpret_cast<const floatx2*>(share(sp) + 16 * C::OT * 64);
-    // a part without keys for this query: nothing.  A NaN l stays.
-    const float f = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m);
-    l = __builtin_fmaf(ml[1], f, l);
-    add_acc<C::OT>(share(sp), f, o);
-  }
-  if (q < S) {
-    store_rowT<DH, PAD>(a.o + (long)(s0 + q) * a.ldo + (long)h * a.dh, o, (l > 0.f) ? 1.f / l : 0.f, lane >> 5, a.dh);
-    if (lane < 32) a.lse[(long)h * a.T + s0 + q] = (m + log2f(l)) * LN2;
   }
 }
 
@@ -285,33 +221,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
   }
   if (a.split > 1) put_acc<C::OT>(wave_share(a.ws, ((long)tile * a.H + h) * a.split + sp, NW, 16 * C::OT, wave), st.dq);
   else if (q < S) store_rowT<DH, PAD>(ba.dq + (long)(s0 + q) * ba.lddq + (long)h * a.dh, st.dq, a.scale, g, a.dh);
-}
-
-// Adds the parts of a split dQ (KV: of a split dK / dV) in their order.
-template <int DH, int NW, bool PAD, bool KV>
-__global__ __launch_bounds__(64 * NW) void attn_packed_add_kernel(AttnPackedBwdArgs ba) {
-  using C = Cfg<DH>;
-  constexpr int WGR = NW * WR, N = KV ? 2 : 1;
-  const AttnPackedArgs& a = ba.f;
-  const int per = KV ? 1 : a.H / a.Hkv;
-  int tile, kvh, part, s0, S, blk;
-  if (!packed_item(a, per, tile, kvh, part)) return;
-  if (!find_rows(a, tile, WGR, s0, S, blk)) return;
-  if (KV && a.causal) blk = (S + WGR - 1) / WGR - 1 - blk;
-  const int h = kvh * per + part, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = blk * WGR + wave * WR + (lane & 31);
-  const long at = ((long)tile * (KV ? a.Hkv : a.H) + h) * a.split;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    floatx16 acc[C::OT];
-#pragma unroll
-    for (int t = 0; t < C::OT; ++t) acc[t] = zero16();
-    for (int sp = 0; sp < a.split; ++sp)
-      add_acc<C::OT>(wave_share(a.ws, at + sp, NW, N * 16 * C::OT, wave) + i * 16 * C::OT * 64, 1.f, acc);
-    bf16* out = KV ? (i ? ba.dv + (long)(s0 + row) * ba.lddv : ba.dk + (long)(s0 + row) * ba.lddk)
-                   : ba.dq + (long)(s0 + row) * ba.lddq;
-    if (row < S) store_rowT<DH, PAD>(out + (long)h * a.dh, acc, i ? 1.f : a.scale, lane >> 5, a.dh);
-  }
 }
 
 // ================================================================ dK and dV
@@ -653,6 +562,79 @@ __global__ __launch_bounds__(256, 1) void attn_packed_dkdv128_kernel(AttnPackedB
   }
 }
 
+// ================================================================ parts
+// A workgroup joins 32 dims of a block: a lane's values of all parts are independent loads, so that the time is one
+// way to memory and not one for each part (one wave for all dims took 106 us for dK and dV of 2048 rows of 80 in 16
+// parts, this 6).  ot: 32-dim tiles of the kernel's head in the scratch, of which the first (dh + 31) / 32 are taken.
+
+// O and lse of a split forward: each part's o and l under the common maximum.
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void attn_packed_join_kernel(AttnPackedArgs a, int ot) {
+  const int G = a.H / a.Hkv, nt = (a.dh + 31) / 32;
+  int tile, kvh, part, s0, S, qb;
+  if (!packed_item(a, G * nt, tile, kvh, part)) return;
+  if (!find_rows(a, tile, NW * WR, s0, S, qb)) return;
+  const int h = kvh * G + part / nt, t = part % nt;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int q = qb * NW * WR + wave * WR + (lane & 31);
+  const int regs = 16 * ot + 4;
+  const long step = (long)NW * regs * 64;  // from part to part
+  const float* p = wave_share(a.ws, ((long)tile * a.H + h) * a.split, NW, regs, wave);
+  const float* ml = p + 16 * ot * 64;
+  p += 16 * t * 64;
+  float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+  for (int sp = 0; sp < a.split; ++sp) m = fmaxf(m, ml[sp * step]);
+  floatx4 o[4] = {};
+#pragma unroll 4
+  for (int sp = 0; sp < a.split; ++sp) {
+    const floatx2 x = *reinterpret_cast<const floatx2*>(ml + sp * step);
+    // a part without keys for this query: nothing.  A NaN l stays.
+    const float f = x[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[0] - m);
+    l = __builtin_fmaf(x[1], f, l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const floatx4 y = *reinterpret_cast<const floatx4*>(p + sp * step + i * 256);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][e] = __builtin_fmaf(y[e], f, o[i][e]);
+    }
+  }
+  if (q < S) {
+    store_tile(a.o + (long)(s0 + q) * a.ldo + (long)h * a.dh, o, t, (l > 0.f) ? 1.f / l : 0.f, lane >> 5, a.dh);
+    if (t == 0 && lane < 32) a.lse[(long)h * a.T + s0 + q] = (m + log2f(l)) * LN2;
+  }
+}
+
+// dQ, or (KV) dK and dV, of split blocks: the parts' sum in their order.
+template <int NW, bool KV>
+__global__ __launch_bounds__(64 * NW) void attn_packed_add_kernel(AttnPackedBwdArgs ba, int ot) {
+  const AttnPackedArgs& a = ba.f;
+  const int G = a.H / a.Hkv, nt = (a.dh + 31) / 32;
+  int tile, kvh, part, s0, S, blk;
+  if (!packed_item(a, (KV ? 2 : G) * nt, tile, kvh, part)) return;
+  if (!find_rows(a, tile, NW * WR, s0, S, blk)) return;
+  if (KV && a.causal) blk = (S + NW * WR - 1) / (NW * WR) - 1 - blk;
+  const int t = part % nt, which = part / nt, h = KV ? kvh : kvh * G + which;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = blk * NW * WR + wave * WR + (lane & 31);
+  const int regs = (KV ? 2 : 1) * 16 * ot;
+  const long step = (long)NW * regs * 64;  // from part to part
+  const float* p = wave_share(a.ws, ((long)tile * (KV ? a.Hkv : a.H) + h) * a.split, NW, regs, wave) +
+                   16 * ((KV ? which * ot : 0) + t) * 64;
+  floatx4 acc[4] = {};
+#pragma unroll 4
+  for (int sp = 0; sp < a.split; ++sp)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const floatx4 x = *reinterpret_cast<const floatx4*>(p + sp * step + i * 256);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][e] += x[e];
+    }
+  bf16* out = !KV ? ba.dq + (long)(s0 + row) * ba.lddq
+              : which ? ba.dv + (long)(s0 + row) * ba.lddv : ba.dk + (long)(s0 + row) * ba.lddk;
+  if (row < S) store_tile(out + (long)h * a.dh, acc, t, KV && which ? 1.f : a.scale, lane >> 5, a.dh);
+}
+
 // Launch shape of one kernel: waves per workgroup, parts of a block's work, scratch.
 struct Plan {
   int nw, split;
@@ -660,30 +642,42 @@ struct Plan {
 };
 enum Pass { FWD, DQ, DKDV };
 
+// Width of the kernel that heads of dh dims run in.
+int width(int dh) { return dh <= 64 ? 64 : dh <= 80 ? 80 : dh <= 128 ? 128 : 256; }
+
 // Waves (of 32 rows): four share the staged blocks; two where that leaves CUs idle or where the
 // sequences are mostly too short for four (the idle waves wait).
-// Parts: a block's steps (64 keys; of dK / dV, 64 queries of each head) are split where all blocks together would
-// not keep the CUs busy, and where a causal mask without a window makes the longest block the
-// last to end: twice the mean for one sequence, more for sequences of several lengths.  The price is the
-// partial results' way through memory, so that a part keeps at least 8 steps of an average block where
-// CUs are idle, else 32.  4 documents in 15992 rows, 16 heads of 64 on 4, causal: backward 929 us without parts, 675
-// with; heads of 128: 1508 and 1315.
+// Parts: a block's steps (64 keys; of dK / dV, 64 queries of each head) are split among as many workgroups as
+// the CUs hold beside the other blocks': blocks of equal work (no causal mask, or a window) in one round of
+// them at most, since a second one would be as long; of the unequal ones of a causal mask, to the nearest round,
+// where a CU holds one workgroup to the next.  A part keeps at least 4 steps of an average block, of dK / dV (two
+// products more a step) and of 256-wide dQ 2, and the parts save at least what the join's launch takes, 8 steps of a 64-wide
+// forward (8 documents in 12000 rows, 4 heads: 24 us without, 29 with).  A causal mask without a window also makes
+// the longest block of dK / dV the last to end, twice the mean for one sequence, more for several lengths: up
+// to four rounds, of 32 steps at least.  Microseconds without parts and with: 4 documents in 15992 rows, 16 heads of
+// 64 on 4, backward 929, 663; one of 2048 rows, 4 heads of 128, causal, forward 54, 23; 8192 rows, one head of 256,
+// forward and backward 1113, 343; two documents in 1000 rows, 8 heads of 64 on 2, backward 76, 34.
 Plan plan(const AttnPackedArgs& a, Pass pass) {
   const int G = a.H / a.Hkv, per = pass == DKDV ? 1 : G;
   const long rows = a.T / std::max(1, a.n_seq);
   Plan p;
-  const int dh = a.dh <= 64 ? 64 : a.dh <= 80 ? 80 : 128;
+  const int dh = width(a.dh);
   p.nw = (long)(a.T / 128 + 1) * a.Hkv * per < 192 || rows < (pass == FWD ? 96 : 160) ? 2 : 4;
-  if (dh == 128 && pass == DKDV) p.nw = 4;
+  if (dh == 256 || (dh == 128 && pass == DKDV)) p.nw = 4;  // 256: 128 rows, in the backward by eight waves
   const int R = p.nw * WR;
   const bool tail = a.causal && a.window >= a.T;
   const long items = (a.T / R + 1) * (long)a.Hkv * per;
-  const long slots = 256L * (4 / p.nw) * (pass == DKDV ? (dh == 128 ? 1 : 2) : dh == 64 || (dh == 80 && pass == FWD) ? 3 : 2);
-  const long want = (pass == DKDV && tail ? 4 : 1) * slots;
+  const long slots = 256L * (4 / p.nw) *
+                     (dh == 256 || (dh == 128 && pass == DKDV)            ? 1
+                      : pass != DKDV && (dh == 64 || (dh == 80 && pass == FWD)) ? 3
+                                                                           : 2);
   const long steps = std::min(rows, 2L * a.window) / KB * (pass == DKDV ? G : 1) / (a.causal ? 2 : 1);
-  p.split = 1;
-  while (p.split < 16 && items * p.split < want && steps / (2 * p.split) >= (items * p.split < slots ? 8 : 32))
-    p.split *= 2;
+  const long least = pass == DKDV || (dh == 256 && pass == DQ) ? 2 : 4;
+  const long spare = !tail ? 0 : slots == 256 ? items - 1 : items / 2;  // to the round below, above, the nearest
+  p.split = (int)std::min(16L, std::max(1L, std::min((slots + spare) / items, steps / least)));
+  const long products = pass == FWD ? 2 : pass == DQ ? 3 : 4;  // of a step
+  if (steps * (p.split - 1) * products * dh < 1024 * p.split) p.split = 1;
+  if (pass == DKDV && tail) p.split = (int)std::min(16L, std::max((long)p.split, std::min(4 * slots / items, steps / 32)));
   const int regs = pass == FWD ? 16 * ((dh + 31) / 32) + 4 : (pass == DKDV ? 32 : 16) * ((dh + 31) / 32);
   p.ws = p.split == 1 ? 0 : (a.T / R + a.n_seq) * (long)a.Hkv * per * p.split * p.nw * regs * 64;
   return p;
@@ -707,26 +701,25 @@ Plan plan_in(const AttnPackedArgs& a, Pass pass) {
 template <int DH, bool PAD>
 hipError_t fwd(AttnPackedArgs a, hipStream_t s) {
 #define FWD_K(NW) attn_packed_fwd_kernel<DH, NW, PAD>
-#define JOIN_K(NW) attn_packed_join_kernel<DH, NW, PAD>
   const int per = a.H / a.Hkv;
   const Plan p = plan_in(a, FWD);
   a.split = p.split;
   PACKED_LAUNCH(p.nw, dim3(packed_grid(a, p.nw * WR, per * p.split)), FWD_K);
-  if (p.split > 1) PACKED_LAUNCH(p.nw, dim3(packed_grid(a, p.nw * WR, per)), JOIN_K);
-  return hipSuccess;
+  return p.split > 1 ? launch_attn_packed_join(a, p.nw, s) : hipSuccess;
 }
 
 template <int DH, bool PAD>
 hipError_t bwd(AttnPackedBwdArgs a, hipStream_t s) {
 #define DQ_K(NW) attn_packed_dq_kernel<DH, NW, PAD>
-#define ADDQ_K(NW) attn_packed_add_kernel<DH, NW, PAD, false>
 #define DKDV_K(NW) attn_packed_dkdv_kernel<DH, NW, PAD>
-#define ADDKV_K(NW) attn_packed_add_kernel<DH, NW, PAD, true>
   const int per = a.f.H / a.f.Hkv;
   Plan p = plan_in(a.f, DQ);
   a.f.split = p.split;
   PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, per * p.split)), DQ_K);
-  if (p.split > 1) PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, per)), ADDQ_K);
+  if (p.split > 1) {
+    const hipError_t e = launch_attn_packed_add(a, p.nw, false, false, s);
+    if (e != hipSuccess) return e;
+  }
   p = plan_in(a.f, DKDV);
   a.f.split = p.split;
   const dim3 grid(packed_grid(a.f, p.nw * WR, p.split, DH == 128));
@@ -737,20 +730,39 @@ hipError_t bwd(AttnPackedBwdArgs a, hipStream_t s) {
   } else {
     PACKED_LAUNCH(p.nw, grid, DKDV_K);
   }
-  if (p.split > 1) PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, 1, DH == 128)), ADDKV_K);
-  return hipSuccess;
+  return p.split > 1 ? launch_attn_packed_add(a, p.nw, true, DH == 128, s) : hipSuccess;
 }
 
 }  // namespace
 
+hipError_t launch_attn_packed_join(const AttnPackedArgs& args, int nw, hipStream_t s) {
+  AttnPackedArgs a = args;
+  const int ot = (width(a.dh) + 31) / 32;
+  const dim3 grid(packed_grid(a, nw * WR, a.H / a.Hkv * ((a.dh + 31) / 32)));
+  if (nw == 2) hipLaunchKernelGGL(attn_packed_join_kernel<2>, grid, dim3(128), 0, s, a, ot);
+  else hipLaunchKernelGGL(attn_packed_join_kernel<4>, grid, dim3(256), 0, s, a, ot);
+  return hipGetLastError();
+}
+
+hipError_t launch_attn_packed_add(const AttnPackedBwdArgs& args, int nw, bool kv, bool by_place, hipStream_t s) {
+  AttnPackedBwdArgs a = args;
+  const int ot = (width(a.f.dh) + 31) / 32;
+  const dim3 grid(packed_grid(a.f, nw * WR, (kv ? 2 : a.f.H / a.f.Hkv) * ((a.f.dh + 31) / 32), by_place));
+  if (kv && nw == 2) hipLaunchKernelGGL((attn_packed_add_kernel<2, true>), grid, dim3(128), 0, s, a, ot);
+  else if (kv) hipLaunchKernelGGL((attn_packed_add_kernel<4, true>), grid, dim3(256), 0, s, a, ot);
+  else if (nw == 2) hipLaunchKernelGGL((attn_packed_add_kernel<2, false>), grid, dim3(128), 0, s, a, ot);
+  else hipLaunchKernelGGL((attn_packed_add_kernel<4, false>), grid, dim3(256), 0, s, a, ot);
+  return hipGetLastError();
+}
+
 long attn_packed_ws(const AttnPackedArgs& a, bool backward) {
-  if (a.T == 0 || a.n_seq == 0 || a.dh > 128) return 0;
+  if (a.T == 0 || a.n_seq == 0) return 0;
   return backward ? std::max(plan(a, DQ).ws, plan(a, DKDV).ws) : plan(a, FWD).ws;
 }
 
 hipError_t launch_attn_packed_fwd(const AttnPackedArgs& a, hipStream_t s) {
   if (a.T == 0 || a.n_seq == 0) return hipSuccess;
-  if (a.dh > 128) return launch_attn256_packed_fwd(a, s);
+  if (a.dh > 128) return launch_attn256_packed_fwd(a, plan_in(a, FWD).split, s);
   if (a.dh == 64) return fwd<64, false>(a, s);
   if (a.dh < 64) return fwd<64, true>(a, s);
   if (a.dh == 80) return fwd<80, false>(a, s);
@@ -761,7 +773,7 @@ hipError_t launch_attn_packed_fwd(const AttnPackedArgs& a, hipStream_t s) {
 
 hipError_t launch_attn_packed_bwd(const AttnPackedBwdArgs& a, hipStream_t s) {
   if (a.f.T == 0 || a.f.n_seq == 0) return hipSuccess;
-  if (a.f.dh > 128) return launch_attn256_packed_bwd(a, s);
+  if (a.f.dh > 128) return launch_attn256_packed_bwd(a, plan_in(a.f, DQ).split, plan_in(a.f, DKDV).split, s);
   if (a.f.dh == 64) return bwd<64, false>(a, s);
   if (a.f.dh < 64) return bwd<64, true>(a, s);
   if (a.f.dh == 80) return bwd<80, false>(a, s);

@@ -377,3 +377,33 @@ def test_two_captured_graphs_at_once():
         for s, want in zip(sets, alone):
             for n in names:
                 assert torch.equal(s[n], want[n]), n
+
+
+@pytest.mark.parametrize("dh", [136, 200, 256])
+def test_few_blocks_of_wide_heads_are_split(dh):
+    """Heads of more than 128 dims: few blocks split and joined, parts without a block, and no scratch."""
+    import ctypes as C
+
+    from paper_2309_01226_amd import _lib, ops
+    for lens, H, Hkv, causal, window in (([4000], 1, 1, True, 0), ([3000, 0, 70], 4, 1, True, 0), ([2100], 2, 2, False, 0),
+                                         ([3500], 2, 1, True, 1500), ([1024, 1030], 4, 1, False, 600), ([2000, 1, 130], 1, 1, True, 0)):
+        _case(lens, H, Hkv, dh, causal, window, before=1, after=3)
+    s = _make([3000], 2, 1, dh)
+    d = _lib.sat_attn_packed_desc(n_seq=1, T=3000, H=2, Hkv=1, dh=dh, causal=1)
+    n = C.c_int64()
+    for name, least in (("fwd", 0), ("bwd", 2 * 3000)):
+        _lib.call(f"sat_op_attention_packed_{name}_ws", d, n)
+        assert n.value > least
+    _run(s, True, 0, 0.1)
+    torch.cuda.synchronize()
+    split = {x: s[x].clone() for x in ("o", "lse", "dq", "dk", "dv")}
+    p = {x: s[x].data_ptr() for x in ("q", "k", "v", "o", "lse", "cu", "dout", "dq", "dk", "dv")}
+    ld = {"ld" + x: s[x].stride(0) for x in ("q", "k", "v", "o", "dq", "dk", "dv")}
+    ws = torch.empty(6000, device="cuda")
+    d = _lib.sat_attn_packed_desc(**p, **ld, lddo=s["dout"].stride(0), n_seq=1, T=3000, H=2, Hkv=1, dh=dh, causal=1, scale=0.1)
+    _lib.call("sat_op_attention_packed_fwd", d, ops._stream())
+    d.ws, d.ws_elems = ws.data_ptr(), 6000
+    _lib.call("sat_op_attention_packed_bwd", d, ops._stream())
+    torch.cuda.synchronize()
+    _check(s, True, 0, 0.1)
+    assert any(not torch.equal(s[x], split[x]) for x in split)  # another order of sums
