@@ -399,7 +399,7 @@ class AdamWTensors:
                 raise ValueError("{}[{}] overlaps {}[{}]".format(*span[3:], *last[3:]))
             if span[1] > end:
                 end, last = span[1], span
-        self.tensors, self.device = lists, dev
+        self.tensors, self.sizes, self.device = lists, sizes, dev
         self.table = (_lib.sat_adamw_tensor * n)()
         none = [None] * n
         columns = [ptrs.get(x, none) for x in ("params", "grads", "m", "v", "m_exp", "v_exp", "shadows")]
@@ -423,12 +423,13 @@ def adamw_multi_state(tensors, m_out, v_out):
     if len(m_out) != n or len(v_out) != n:
         raise ValueError("adamw_multi_state: one output of each kind for each parameter")
     dt = torch.bfloat16 if n and m_out[0].dtype == torch.bfloat16 else torch.float32
-    want = [e.n for e in tensors.table]
+    dev = tensors.device
     for name, ts in (("m_out", m_out), ("v_out", v_out)):
-        for i, t in enumerate(ts):
-            _here(t, dt, f"{name}[{i}]", tensors.device)
-            if not t.is_contiguous() or t.numel() != want[i]:
-                raise ValueError(f"{name}[{i}]: expected {want[i]} contiguous elements, got {tuple(t.shape)}")
+        for i, (t, k) in enumerate(zip(ts, tensors.sizes)):
+            if t.dtype is not dt or t.get_device() != dev:
+                _here(t, dt, f"{name}[{i}]", dev)
+            if not t.is_contiguous() or t.numel() != k:
+                raise ValueError(f"{name}[{i}]: expected {k} contiguous elements, got {tuple(t.shape)}")
     ms, vs = ((C.c_void_p * n)(*[t.data_ptr() for t in ts]) for ts in (m_out, v_out))
     _lib.call("sat_op_adamw_multi_state", tensors.table, n, ms, vs, dt == torch.bfloat16, _stream())
 
