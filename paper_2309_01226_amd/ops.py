@@ -7,6 +7,7 @@ the stream; every element of every output is computed by the HIP kernels.
 
 import ctypes as C
 import functools
+import struct
 
 import torch
 
@@ -20,9 +21,10 @@ def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
-def _stream():
-    """The current stream's handle (without the torch.cuda.Stream object, which takes 3 us to make)."""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+def _stream(dev=None):
+    """The current stream's handle on the current device `dev` (without the torch.cuda.Stream object, which takes
+    3 us to make)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if dev is None else dev)
 
 
 def _need(t, dtype, name):
@@ -283,7 +285,12 @@ def _rows_of(t, dtype, name, rows, cols, dev):
     raise ValueError(f"{name}: expected [{rows}, >= {cols}] with contiguous rows, got {tuple(shape)} strides {t.stride()}")
 
 
-def _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev, more=()):
+# sat_attn_packed_desc's fields (packing them takes a third of the time that ctypes takes to set them)
+_PACKED = struct.Struct("3P3qPqPP7if" + "Pq3P3q" + "Pq")
+assert _PACKED.size == C.sizeof(_lib.sat_attn_packed_desc)
+
+
+def _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev, more=(0,) * 10):
     T = q.shape[0]
     bf, wq, wk = torch.bfloat16, H * dh, Hkv * dh
     _here(lse, torch.float32, "lse", dev)
@@ -295,11 +302,10 @@ def _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev, mo
         raise ValueError(f"window: {window}")
     if lse.shape != (H, T) or not lse.is_contiguous():
         raise ValueError(f"lse: expected a contiguous [{H}, {T}], got {tuple(lse.shape)}")
-    # in the order of the C struct
-    return _lib.sat_attn_packed_desc(
+    return _lib.sat_attn_packed_desc.from_buffer_copy(_PACKED.pack(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), _rows_of(q, bf, "q", T, wq, dev), _rows_of(k, bf, "k", T, wk, dev),
         _rows_of(v, bf, "v", T, wk, dev), o.data_ptr(), _rows_of(o, bf, "o", T, wq, dev), lse.data_ptr(), cu.data_ptr(),
-        n - 1, T, H, Hkv, dh, bool(causal), window, scale, *more)
+        n - 1, T, H, Hkv, dh, bool(causal), window, scale, *more))
 
 
 @functools.lru_cache(maxsize=256)
@@ -315,12 +321,13 @@ def attention_packed_fwd(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, *, wind
     """Attention inside packed sequences: rows cu[s] .. cu[s + 1] - 1 of q, o [T, >= H dh] and k, v
     [T, >= Hkv dh] (bf16, views of a wider buffer allowed) are sequence s; lse fp32 [H, T].  See
     saturn_ops.h for the masks.  Workspaces come from torch's allocator, on the current stream."""
-    d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, _device(q, "q"))
-    need = _packed_ws("fwd", d.n_seq, d.T, H, Hkv, dh, bool(causal), window)
+    dev = _device(q, "q")
+    d = _packed_desc(q, k, v, o, lse, cu, H, Hkv, dh, causal, scale, window, dev)
+    need = _packed_ws("fwd", cu.numel() - 1, q.shape[0], H, Hkv, dh, bool(causal), window)
     if need:
         ws = torch.empty(need, device=q.device, dtype=torch.float32)
         d.ws, d.ws_elems = ws.data_ptr(), need
-    _lib.call("sat_op_attention_packed_fwd", d, _stream())
+    _lib.call("sat_op_attention_packed_fwd", d, _stream(dev))
 
 
 def attention_packed_bwd(q, k, v, o, lse, cu, dout, dq, dk, dv, H, Hkv, dh, causal, scale, *, window=0):
@@ -332,7 +339,7 @@ def attention_packed_bwd(q, k, v, o, lse, cu, dout, dq, dk, dv, H, Hkv, dh, caus
         dout.data_ptr(), _rows_of(dout, bf, "dout", T, wq, dev), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
         _rows_of(dq, bf, "dq", T, wq, dev), _rows_of(dk, bf, "dk", T, wk, dev), _rows_of(dv, bf, "dv", T, wk, dev),
         ws.data_ptr(), need))
-    _lib.call("sat_op_attention_packed_bwd", d, _stream())
+    _lib.call("sat_op_attention_packed_bwd", d, _stream(dev))
 
 
 def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=True, own_freqs=False, inverse=False):
@@ -349,7 +356,7 @@ def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=Tru
     if max(pairs, default=0) > 128:  # ctypes would cut it
         raise ValueError(f"pairs: {pairs}")
     _lib.call("sat_op_rotary_axes", x.data_ptr(), ldx, y.data_ptr(), ldy, f32, pos.data_ptr(), ldp, A,
-              (C.c_int32 * A)(*pairs), T, H, dh, base, interleaved, own_freqs, inverse, _stream())
+              (C.c_int32 * A)(*pairs), T, H, dh, base, interleaved, own_freqs, inverse, _stream(dev))
     return y
 
 
