@@ -26,6 +26,7 @@
 //   4 documents in 16001 rows, 16 heads of 128 on 4 K / V heads, causal    290, 390, 650 us (forward 1.0 PFLOP/s; the
 //     backward executes 7 products for the 5 counted: 1.0 PFLOP/s executed)
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "attn_packed.h"
@@ -654,7 +655,9 @@ int width(int dh) { return dh <= 64 ? 64 : dh <= 80 ? 80 : dh <= 128 ? 128 : 256
 // products more a step) and of 256-wide dQ 2, and the parts save at least what the join's launch takes, 8 steps of a 64-wide
 // forward (8 documents in 12000 rows, 4 heads: 24 us without, 29 with).  A causal mask without a window also makes
 // the longest block of dK / dV the last to end, twice the mean for one sequence, more for several lengths: up
-// to four rounds, of 32 steps at least.  Microseconds without parts and with: 4 documents in 15992 rows, 16 heads of
+// to four rounds, of 32 steps at least.  The host does not know the lengths: sequences without a causal mask (images)
+// are taken to be alike, those with one (documents) to differ, the long ones T / n_seq^(2/3) rows.  8 documents in
+// 8000 rows, 4 heads of 64, backward 138 us by the mean, 104 so; 8 of 500 rows 29 and 31.  Microseconds without parts and with: 4 documents in 15992 rows, 16 heads of
 // 64 on 4, backward 929, 663; one of 2048 rows, 4 heads of 128, causal, forward 54, 23; 8192 rows, one head of 256,
 // forward and backward 1113, 343; two documents in 1000 rows, 8 heads of 64 on 2, backward 76, 34.
 Plan plan(const AttnPackedArgs& a, Pass pass) {
@@ -671,7 +674,8 @@ Plan plan(const AttnPackedArgs& a, Pass pass) {
                      (dh == 256 || (dh == 128 && pass == DKDV)            ? 1
                       : pass != DKDV && (dh == 64 || (dh == 80 && pass == FWD)) ? 3
                                                                            : 2);
-  const long steps = std::min(rows, 2L * a.window) / KB * (pass == DKDV ? G : 1) / (a.causal ? 2 : 1);
+  const long longer = a.causal ? (long)(a.T / cbrt((double)std::max(1, a.n_seq) * std::max(1, a.n_seq))) : rows;
+  const long steps = std::min(longer, 2L * a.window) / KB * (pass == DKDV ? G : 1) / (a.causal ? 2 : 1);
   const long least = pass == DKDV || (dh == 256 && pass == DQ) ? 2 : 4;
   const long spare = !tail ? 0 : slots == 256 ? items - 1 : items / 2;  // to the round below, above, the nearest
   p.split = (int)std::min(16L, std::max(1L, std::min((slots + spare) / items, steps / least)));
