@@ -132,8 +132,8 @@ sat_status sat_op_attention_bwd(const void* q, const void* k, const void* v, int
  *            replay; values outside [0, T] are taken as the nearer of the two.
  *   heads    H query heads, Hkv K / V heads, Hkv a divisor of H; query head h
  *            reads K / V head h / (H / Hkv).  dh: a multiple of 8 up to 256
- *            (64, 80, 128 and 256 have kernels of their width, others run in the
- *            next wider one).  Element (row t, head h, dim j) at ptr[t * ld + h * dh + j].
+ *            (32, 64, 80, 96, 128 and 256 have kernels of their width, others run
+ *            in the next wider one).  Element (row t, head h, dim j) at ptr[t * ld + h * dh + j].
  *   mask     query i and key j of one sequence: j <= i when causal, and |i - j| <
  *            window when window > 0 (0: none).  Every query sees itself.
  *   values   o = softmax(scale q k^T) v as bf16, lse [H, T] fp32 the natural-log

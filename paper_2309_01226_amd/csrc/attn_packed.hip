@@ -15,8 +15,10 @@
 // A workgroup is 2 or 4 waves of 32 rows of one sequence and head; blocks of 64 rows of the
 // other operand stream through LDS (attn_tile.h).  Only blocks that some row's mask
 // cuts are masked; blocks that no row sees are not read.  Rows of another sequence, and rows outside
-// every sequence, read as zeros and are never written.  Heads narrower than 64, 80 or 128
-// dims run in the next wider kernel with zeros behind them; 256-wide ones are in attn256.hip.
+// every sequence, read as zeros and are never written.  Heads narrower than 32, 64, 80, 96 or 128
+// dims run in the next wider kernel with zeros behind them; 256-wide ones are in attn256.hip.  (In the kernels of 64 and
+// 128 dims, 4 x 4096 rows of 16 heads take forward 268 us and backward 837 for 32 dims, 476 and 1655 for 96; in
+// their own 221 and 630, 426 and 1461.)
 //
 // Bounds and times, bf16: 64- and 80-wide heads by the vector unit (an exponential and about ten other
 // instructions a pair against 4 dh flop), 128-wide ones by the matrix cores at the clock that the power limit
@@ -40,7 +42,7 @@ namespace {
 template <int DH, int NW, bool PAD>
 __global__ __launch_bounds__(64 * NW, DH == 80 && NW == 4 ? 3 : 2) void attn_packed_fwd_kernel(AttnPackedArgs a) {
   using C = Cfg<DH>;
-  constexpr int TILE = KB * DH, WGR = NW * WR;
+  constexpr int TILE = KB * C::W, WGR = NW * WR;
   __shared__ __attribute__((aligned(1024))) bf16 smem[2 * 2 * TILE];  // 2 stages x (K, V)
   const int G = a.H / a.Hkv;
   int tile, kvh, part, s0, S, qb;
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(64 * NW, DH == 80 && NW == 4 ? 3 : 2) void attn_pac
 template <int DH, int NW, bool PAD>
 __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBwdArgs ba) {
   using C = Cfg<DH>;
-  constexpr int TILE = KB * DH, WGR = NW * WR;
+  constexpr int TILE = KB * C::W, WGR = NW * WR;
   __shared__ __attribute__((aligned(1024))) bf16 smem[2 * 2 * TILE];  // 2 stages x (K, V)
   const AttnPackedArgs& a = ba.f;
   const int G = a.H / a.Hkv;
@@ -225,12 +227,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
 }
 
 // ================================================================ dK and dV
-// dK and dV of one K / V head, 64- and 80-wide: the blocks of Q and dO of all its query heads in turn.
+// dK and dV of one K / V head, up to 80-wide: the blocks of Q and dO of all its query heads in turn.
 template <int DH, int NW, bool PAD>
 __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dkdv_kernel(AttnPackedBwdArgs ba) {
   using C = Cfg<DH>;
   constexpr int BQ = KB, WGR = NW * WR;
-  constexpr int QT = BQ * DH;
+  constexpr int QT = BQ * C::W;
   constexpr int STG = 2 * QT + 2 * 2 * BQ;  // Q, dO, lse2[64], delta[64]
   __shared__ __attribute__((aligned(1024))) bf16 smem[2 * STG];
   const AttnPackedArgs& a = ba.f;
@@ -349,7 +351,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dkdv_kernel(AttnPacked
   }
 }
 
-// 128-wide heads.  A wave owns 32 keys and takes 32 queries (a slot) at a time: S = Q K^T and dP = dO V^T with
+// 96- and 128-wide heads.  A wave owns 32 keys and takes 32 queries (a slot) at a time: S = Q K^T and dP = dO V^T with
 // queries as rows (lane = key), P = exp2(S scale log2e - lse2), dS = P (dP - delta), then dV^T += dO^T P and
 // dK^T += Q^T dS.  Its 256 registers of operands and accumulators leave room for one wave on a SIMD, which
 // has to keep the matrix cores busy alone: the products S and dP of the next slot are issued between the
@@ -362,10 +364,10 @@ struct Slot {
 
 // NEXT: the slot of rows Qn, dOn, half un of a block, with its lse2 ln and delta dn, into `nx`.  CUR: `cur`, of
 // rows Qc, dOc, half uc, into dV and dK.
-template <bool NEXT, bool CUR>
-__device__ __forceinline__ void dkdv_step(DkvState<128>& st, const TileOfs<128, KB>& to, const Slot& cur, Slot& nx, const bf16* Qn,
+template <int DH, bool NEXT, bool CUR>
+__device__ __forceinline__ void dkdv_step(DkvState<DH>& st, const TileOfs<DH, KB>& to, const Slot& cur, Slot& nx, const bf16* Qn,
                                           const float* ln, int un, const bf16* Qc, int uc, int g, float sc) {
-  constexpr int KS = Cfg<128>::KS, OT = Cfg<128>::OT, QT = KB * 128;
+  constexpr int KS = Cfg<DH>::KS, OT = Cfg<DH>::OT, QT = KB * Cfg<DH>::W;
   constexpr int PFR = 3, PFT = 3;  // k-steps, pairs of transposed fragments in flight
   bf16x8 qr[PFR + 1], dr[PFR + 1], qt[PFT + 1], dt[PFT + 1], pb[2], db[2];
   floatx16 x, y;
@@ -432,12 +434,12 @@ __device__ __forceinline__ void dkdv_step(DkvState<128>& st, const TileOfs<128, 
   }
 }
 
-template <bool PAD>
-__global__ __launch_bounds__(256, 1) void attn_packed_dkdv128_kernel(AttnPackedBwdArgs ba) {
-  constexpr int DH = 128, NW = 4;
+template <int DH, bool PAD>
+__global__ __launch_bounds__(256, 1) void attn_packed_dkdv_wide_kernel(AttnPackedBwdArgs ba) {
+  constexpr int NW = 4;
   using C = Cfg<DH>;
   constexpr int BQ = KB, WGR = NW * WR, NS = 3;  // stages: a block, the next, whose first slot is begun with it, and one on its way
-  constexpr int QT = BQ * DH;
+  constexpr int QT = BQ * C::W;
   constexpr int STG = 2 * QT + 2 * 2 * BQ;  // Q, dO, lse2[64], delta[64]
   __shared__ __attribute__((aligned(1024))) bf16 smem[NS * STG];
   const AttnPackedArgs& a = ba.f;
@@ -534,9 +536,9 @@ __global__ __launch_bounds__(256, 1) void attn_packed_dkdv128_kernel(AttnPackedB
       }
     };
     if (!decltype(whole)::value) mask(A, 0);
-    dkdv_step<true, true>(st, to, A, B, Qc, lse2(Qc), 1, Qc, 0, g, sc);
+    dkdv_step<DH, true, true>(st, to, A, B, Qc, lse2(Qc), 1, Qc, 0, g, sc);
     if (!decltype(whole)::value) mask(B, 1);
-    dkdv_step<true, true>(st, to, B, A, Qn, lse2(Qn), 0, Qc, 1, g, sc);
+    dkdv_step<DH, true, true>(st, to, B, A, Qn, lse2(Qn), 0, Qc, 1, g, sc);
     ++it;
   };
   while (it < total) {  // head by head: its blocks before this wave's, this wave's, those behind
@@ -544,7 +546,7 @@ __global__ __launch_bounds__(256, 1) void attn_packed_dkdv128_kernel(AttnPackedB
     const int end = min(total, i0 + nqb);
     const int from = min(max(it, i0 + ja), end), until = min(max(from, i0 + jb), end);
     for (; it < from; ++it) middle(it);
-    if (it < until) dkdv_step<true, false>(st, to, B, A, stage(it), lse2(stage(it)), 0, stage(it), 0, g, sc);
+    if (it < until) dkdv_step<DH, true, false>(st, to, B, A, stage(it), lse2(stage(it)), 0, stage(it), 0, g, sc);
     const int w0 = min(max(it, i0 + fa), until), w1 = min(max(w0, i0 + fb), until);
     while (it < w0) block(std::false_type{});
     while (it < w1) block(std::true_type{});
@@ -644,7 +646,7 @@ struct Plan {
 enum Pass { FWD, DQ, DKDV };
 
 // Width of the kernel that heads of dh dims run in.
-int width(int dh) { return dh <= 64 ? 64 : dh <= 80 ? 80 : dh <= 128 ? 128 : 256; }
+int width(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : dh <= 80 ? 80 : dh <= 96 ? 96 : dh <= 128 ? 128 : 256; }
 
 // Waves (of 32 rows): four share the staged blocks; two where that leaves CUs idle or where the
 // sequences are mostly too short for four (the idle waves wait).
@@ -666,21 +668,20 @@ Plan plan(const AttnPackedArgs& a, Pass pass) {
   Plan p;
   const int dh = width(a.dh);
   p.nw = (long)(a.T / 128 + 1) * a.Hkv * per < 192 || rows < (pass == FWD ? 96 : 160) ? 2 : 4;
-  if (dh == 256 || (dh == 128 && pass == DKDV)) p.nw = 4;  // 256: 128 rows, in the backward by eight waves
+  if (dh == 256 || (dh >= 96 && pass == DKDV)) p.nw = 4;  // 256: 128 rows, in the backward by eight waves
   const int R = p.nw * WR;
   const bool tail = a.causal && a.window >= a.T;
   const long items = (a.T / R + 1) * (long)a.Hkv * per;
-  const long slots = 256L * (4 / p.nw) *
-                     (dh == 256 || (dh == 128 && pass == DKDV)            ? 1
-                      : pass != DKDV && (dh == 64 || (dh == 80 && pass == FWD)) ? 3
-                                                                           : 2);
+  const int on_cu = dh == 256 || (dh >= 96 && pass == DKDV) ? 1 : dh == 32 ? (pass == DKDV ? 3 : 4)
+                    : pass != DKDV && (dh == 64 || (dh == 80 && pass == FWD)) ? 3 : 2;
+  const long slots = 256L * (4 / p.nw) * on_cu;  // workgroups that the CUs hold
   const long longer = a.causal ? (long)(a.T / cbrt((double)std::max(1, a.n_seq) * std::max(1, a.n_seq))) : rows;
   const long steps = std::min(longer, 2L * a.window) / KB * (pass == DKDV ? G : 1) / (a.causal ? 2 : 1);
   const long least = pass == DKDV || (dh == 256 && pass == DQ) ? 2 : 4;
-  const long spare = !tail ? 0 : slots == 256 ? items - 1 : items / 2;  // to the round below, above, the nearest
+  const long spare = !tail ? 0 : on_cu == 1 ? items - 1 : items / 2;  // to the round below, above, the nearest
   p.split = (int)std::min(16L, std::max(1L, std::min((slots + spare) / items, steps / least)));
   const long products = pass == FWD ? 2 : pass == DQ ? 3 : 4;  // of a step
-  if (steps * (p.split - 1) * products * dh < 1024 * p.split) p.split = 1;
+  if (steps * (p.split - 1) * products * std::max(dh, 64) < 1024 * p.split) p.split = 1;  // 32: the exponentials' time
   if (pass == DKDV && tail) p.split = (int)std::min(16L, std::max((long)p.split, std::min(4 * slots / items, steps / 32)));
   const int regs = pass == FWD ? 16 * ((dh + 31) / 32) + 4 : (pass == DKDV ? 32 : 16) * ((dh + 31) / 32);
   p.ws = p.split == 1 ? 0 : (a.T / R + a.n_seq) * (long)a.Hkv * per * p.split * p.nw * regs * 64;
@@ -726,15 +727,15 @@ hipError_t bwd(AttnPackedBwdArgs a, hipStream_t s) {
   }
   p = plan_in(a.f, DKDV);
   a.f.split = p.split;
-  const dim3 grid(packed_grid(a.f, p.nw * WR, p.split, DH == 128));
-  if constexpr (DH == 128) {
-    hipLaunchKernelGGL(attn_packed_dkdv128_kernel<PAD>, grid, dim3(256), 0, s, a);
+  const dim3 grid(packed_grid(a.f, p.nw * WR, p.split, DH >= 96));
+  if constexpr (DH >= 96) {
+    hipLaunchKernelGGL((attn_packed_dkdv_wide_kernel<DH, PAD>), grid, dim3(256), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   } else {
     PACKED_LAUNCH(p.nw, grid, DKDV_K);
   }
-  return p.split > 1 ? launch_attn_packed_add(a, p.nw, true, DH == 128, s) : hipSuccess;
+  return p.split > 1 ? launch_attn_packed_add(a, p.nw, true, DH >= 96, s) : hipSuccess;
 }
 
 }  // namespace
@@ -767,10 +768,12 @@ long attn_packed_ws(const AttnPackedArgs& a, bool backward) {
 hipError_t launch_attn_packed_fwd(const AttnPackedArgs& a, hipStream_t s) {
   if (a.T == 0 || a.n_seq == 0) return hipSuccess;
   if (a.dh > 128) return launch_attn256_packed_fwd(a, plan_in(a, FWD).split, s);
+  if (a.dh <= 32) return fwd<32, true>(a, s);
   if (a.dh == 64) return fwd<64, false>(a, s);
   if (a.dh < 64) return fwd<64, true>(a, s);
   if (a.dh == 80) return fwd<80, false>(a, s);
   if (a.dh < 80) return fwd<80, true>(a, s);
+  if (a.dh <= 96) return fwd<96, true>(a, s);
   if (a.dh == 128) return fwd<128, false>(a, s);
   return fwd<128, true>(a, s);
 }
@@ -778,10 +781,12 @@ hipError_t launch_attn_packed_fwd(const AttnPackedArgs& a, hipStream_t s) {
 hipError_t launch_attn_packed_bwd(const AttnPackedBwdArgs& a, hipStream_t s) {
   if (a.f.T == 0 || a.f.n_seq == 0) return hipSuccess;
   if (a.f.dh > 128) return launch_attn256_packed_bwd(a, plan_in(a.f, DQ).split, plan_in(a.f, DKDV).split, s);
+  if (a.f.dh <= 32) return bwd<32, true>(a, s);
   if (a.f.dh == 64) return bwd<64, false>(a, s);
   if (a.f.dh < 64) return bwd<64, true>(a, s);
   if (a.f.dh == 80) return bwd<80, false>(a, s);
   if (a.f.dh < 80) return bwd<80, true>(a, s);
+  if (a.f.dh <= 96) return bwd<96, true>(a, s);
   if (a.f.dh == 128) return bwd<128, false>(a, s);
   return bwd<128, true>(a, s);
 }

@@ -12,7 +12,8 @@
 //    [2][R] with row r of chunk t at slot r ^ 4t, after the 64-dim part.
 // Products whose output rows are head dims (O^T, dV^T, dK^T, dQ^T) use
 // 32-row MFMA tiles; for 80-wide heads the third tile's rows 80..95 read
-// dims 64..79 again and are discarded at the store.
+// dims 64..79 again and are discarded at the store.  32- and 96-wide heads (packed sequences only) are
+// staged as 64 and 128 dims, of which the products take theirs.
 #pragma once
 
 #include "common.h"
@@ -42,11 +43,12 @@ __device__ __forceinline__ lds_void* lds(const bf16* p) { return (lds_void*)(con
 
 template <int DH>
 struct Cfg {
-  static_assert(DH == 64 || DH == 80 || DH == 128, "64-, 80- or 128-wide heads");
+  static_assert(DH == 32 || DH == 64 || DH == 80 || DH == 96 || DH == 128, "32-, 64-, 80-, 96- or 128-wide heads");
   static constexpr bool TAIL = DH == 80;
-  static constexpr int PARTS = DH / 64;      // 64-dim parts of a staged tile
+  static constexpr int W = DH == 32 ? 64 : DH == 96 ? 128 : DH;  // dims of a staged row
+  static constexpr int PARTS = W / 64;       // 64-dim parts of a staged tile
   static constexpr int KS = DH / 16;         // k-steps over the head dims
-  static constexpr int RS = DH == 128 ? 4 : KS;  // k-steps whose row fragments are read together
+  static constexpr int RS = DH == 128 ? 4 : DH == 96 ? 3 : KS;  // k-steps whose row fragments are read together
   static constexpr int OT = (DH + 31) / 32;  // 32-dim output tiles
 };
 
@@ -212,7 +214,7 @@ struct FwdState {
 // the wave (always the case without MASK).  LOW: also masked are keys < low, low_rel likewise.
 // PF: 16-key steps whose V fragments are read ahead of the exponentials (80-wide
 // heads: one keeps three waves per SIMD, two make it two: 53 -> 60 us at 64 x 16 x 257).
-template <int DH, bool MASK, bool LOW = false, int PF = DH == 64 ? 4 : 1>
+template <int DH, bool MASK, bool LOW = false, int PF = DH <= 64 ? 4 : 1>
 __device__ __forceinline__ void fwd_block(FwdState<DH>& st, const TileOfs<DH, KB>& to, const bf16* Ks,
                                           const bf16* Vs, float sc, bool two, int lim_rel, int low_rel = 0) {
   using C = Cfg<DH>;
