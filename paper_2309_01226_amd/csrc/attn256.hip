@@ -912,7 +912,7 @@ hipError_t launch_attn256_fwd(const AttnArgs& a, hipStream_t s) {
 hipError_t launch_attn256_packed_fwd(const AttnPackedArgs& args, int split, hipStream_t s) {
   AttnPackedArgs a = args;
   a.split = split;
-  const dim3 grid(packed_grid(a, QPB, a.H / a.Hkv * split));
+  const dim3 grid(packed_grid(a, QPB, a.H / a.Hkv * split, false));
   if (a.dh == DH) hipLaunchKernelGGL((attn256_fwd_kernel<AttnPackedArgs, false>), grid, dim3(NT), 0, s, a);
   else hipLaunchKernelGGL((attn256_fwd_kernel<AttnPackedArgs, true>), grid, dim3(NT), 0, s, a);
   const hipError_t e = hipGetLastError();
@@ -922,17 +922,17 @@ hipError_t launch_attn256_packed_fwd(const AttnPackedArgs& args, int split, hipS
 template <bool PAD>
 static hipError_t packed_bwd(AttnPackedBwdArgs a, int qsplit, int ksplit, hipStream_t s) {
   a.f.split = qsplit;
-  const dim3 qgrid(packed_grid(a.f, QPW, a.f.H / a.f.Hkv * qsplit));
+  const dim3 qgrid(packed_grid(a.f, QPW, a.f.H / a.f.Hkv * qsplit, false));
   if (qsplit > 1) hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnPackedBwdArgs, PAD, true>), qgrid, dim3(NT8), 0, s, a);
   else hipLaunchKernelGGL((attn256_bwd_dq_kernel<AttnPackedBwdArgs, PAD, false>), qgrid, dim3(NT8), 0, s, a);
   hipError_t e = hipGetLastError();
-  if (e == hipSuccess && qsplit > 1) e = launch_attn_packed_add(a, 4, false, false, s);
+  if (e == hipSuccess && qsplit > 1) e = launch_attn_packed_add(a, 4, false, s);
   if (e != hipSuccess) return e;
   a.f.split = ksplit;
-  const dim3 kgrid(packed_grid(a.f, KPW, ksplit));
+  const dim3 kgrid(packed_grid(a.f, KPW, ksplit, true));
   hipLaunchKernelGGL((attn256_bwd_dkdv_kernel<AttnPackedBwdArgs, PAD>), kgrid, dim3(NT8), 0, s, a);
   e = hipGetLastError();
-  return e == hipSuccess && ksplit > 1 ? launch_attn_packed_add(a, 4, true, false, s) : e;
+  return e == hipSuccess && ksplit > 1 ? launch_attn_packed_add(a, 4, true, s) : e;
 }
 
 hipError_t launch_attn256_packed_bwd(const AttnPackedBwdArgs& a, int qsplit, int ksplit, hipStream_t s) {

@@ -36,11 +36,13 @@ __device__ __forceinline__ int nth_bit(uint64_t mask, int n) {
 // max(0, nb - x) of them a place of x or more.  By sequence: sum [nb > x] nb blocks are in
 // sequences of more than x, each sequence's own in a row.  A walk or a bisection over x finds the level
 // that holds the rank, bit counts the sequence on it.  Causal blocks go by place where sequences are long
-// (1024 rows on average; 256 with 64-wide heads, whose K and V are smallest), by sequence where they are short and what
-// counts is that a sequence's K and V are read once: 4 x 4096 rows, 16 heads of 64, forward 158 against 174
-// us; 24 documents in 8192 rows, 12 heads of 64, 24.3 against 26.5; 32 documents of 64 to 2048 rows, 80-wide, 155 by
-// place, 123 by sequence; dK / dV of 128-wide heads, one workgroup on a CU, always by place (50 images:
-// backward 263 against 283).  Beyond 256 sequences (four a lane) the blocks are short on average and are
+// (a mean of 256 rows with up to 64 dims, 1024 with over 128, else 2048; always dK / dV of 96 and 128 dims, one
+// workgroup on a CU, and of shared heads, whose blocks are long) and all K and V stay in the last-level cache
+// of 256 MB, since all sequences' are read over and over; else by sequence, where a sequence's are read once.
+// By place and by sequence, us: 4 x 4096 rows, 16 heads of 64, forward 158 and 174; 24 documents in 8192 rows, 12
+// heads of 64, 24.3 and 26.5; 16 x 1024, 16 heads of 80, 97 and 83; backward of 50 images of 128 dims 263 and
+// 283, of 64 x 1024, 16 heads of 80 on 4, 848 and 1022; 64 x 1024, 16 heads of 128 (537 MB), forward 612 and
+// 411, backward 1747 and 1466.  Beyond 256 sequences (four a lane) the blocks are short on average and are
 // numbered from first(i) = cu[i] / R + i instead, which leaves each sequence at least as many numbers as it
 // has blocks.  Row numbers are held to [0, T], so no row outside the buffers is touched whatever
 // cu holds.  blk counts the places in the order of causal work (a query block's own place; a key block's
@@ -209,11 +211,14 @@ __device__ __forceinline__ void store_tile(bf16* out, const floatx4 (&acc)[4], i
 
 }  // namespace
 
-// Launch shape for blocks of R rows and `per` workgroups on each block and K / V head: sets
+// Launch shape for blocks of R rows and `per` workgroups on each block and K / V head (kv: of dK / dV): sets
 // a.ntile, a.parts and a.by_place, returns the workgroups.
-inline unsigned packed_grid(AttnPackedArgs& a, int R, int per, bool always_by_place = false) {
+inline unsigned packed_grid(AttnPackedArgs& a, int R, int per, bool kv) {
   a.ntile = a.T / R + a.n_seq;
-  a.by_place = a.causal && (always_by_place || a.T >= (a.dh <= 64 ? 256L : 1024L) * a.n_seq);
+  const long bytes = 4L * a.T * a.Hkv * a.dh;  // of K and V
+  const bool always = kv && (a.H > a.Hkv || (a.dh > 80 && a.dh <= 128));
+  const long least = always ? 0 : a.dh <= 64 ? 256 : a.dh > 128 ? 1024 : 2048;
+  a.by_place = a.causal && bytes <= (1L << 28) && a.T >= least * a.n_seq;
   a.parts = a.Hkv % 8 == 0 ? 1 : a.Hkv % 4 == 0 ? 2 : a.Hkv % 2 == 0 ? 4 : 8;
   return (unsigned)((long)a.Hkv * a.parts * sat_cdiv(a.ntile, a.parts) * per);
 }

@@ -709,7 +709,7 @@ hipError_t fwd(AttnPackedArgs a, hipStream_t s) {
   const int per = a.H / a.Hkv;
   const Plan p = plan_in(a, FWD);
   a.split = p.split;
-  PACKED_LAUNCH(p.nw, dim3(packed_grid(a, p.nw * WR, per * p.split)), FWD_K);
+  PACKED_LAUNCH(p.nw, dim3(packed_grid(a, p.nw * WR, per * p.split, false)), FWD_K);
   return p.split > 1 ? launch_attn_packed_join(a, p.nw, s) : hipSuccess;
 }
 
@@ -720,14 +720,14 @@ hipError_t bwd(AttnPackedBwdArgs a, hipStream_t s) {
   const int per = a.f.H / a.f.Hkv;
   Plan p = plan_in(a.f, DQ);
   a.f.split = p.split;
-  PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, per * p.split)), DQ_K);
+  PACKED_LAUNCH(p.nw, dim3(packed_grid(a.f, p.nw * WR, per * p.split, false)), DQ_K);
   if (p.split > 1) {
-    const hipError_t e = launch_attn_packed_add(a, p.nw, false, false, s);
+    const hipError_t e = launch_attn_packed_add(a, p.nw, false, s);
     if (e != hipSuccess) return e;
   }
   p = plan_in(a.f, DKDV);
   a.f.split = p.split;
-  const dim3 grid(packed_grid(a.f, p.nw * WR, p.split, DH >= 96));
+  const dim3 grid(packed_grid(a.f, p.nw * WR, p.split, true));
   if constexpr (DH >= 96) {
     hipLaunchKernelGGL((attn_packed_dkdv_wide_kernel<DH, PAD>), grid, dim3(256), 0, s, a);
     const hipError_t e = hipGetLastError();
@@ -735,7 +735,7 @@ hipError_t bwd(AttnPackedBwdArgs a, hipStream_t s) {
   } else {
     PACKED_LAUNCH(p.nw, grid, DKDV_K);
   }
-  return p.split > 1 ? launch_attn_packed_add(a, p.nw, true, DH >= 96, s) : hipSuccess;
+  return p.split > 1 ? launch_attn_packed_add(a, p.nw, true, s) : hipSuccess;
 }
 
 }  // namespace
@@ -743,16 +743,16 @@ hipError_t bwd(AttnPackedBwdArgs a, hipStream_t s) {
 hipError_t launch_attn_packed_join(const AttnPackedArgs& args, int nw, hipStream_t s) {
   AttnPackedArgs a = args;
   const int ot = (width(a.dh) + 31) / 32;
-  const dim3 grid(packed_grid(a, nw * WR, a.H / a.Hkv * ((a.dh + 31) / 32)));
+  const dim3 grid(packed_grid(a, nw * WR, a.H / a.Hkv * ((a.dh + 31) / 32), false));
   if (nw == 2) hipLaunchKernelGGL(attn_packed_join_kernel<2>, grid, dim3(128), 0, s, a, ot);
   else hipLaunchKernelGGL(attn_packed_join_kernel<4>, grid, dim3(256), 0, s, a, ot);
   return hipGetLastError();
 }
 
-hipError_t launch_attn_packed_add(const AttnPackedBwdArgs& args, int nw, bool kv, bool by_place, hipStream_t s) {
+hipError_t launch_attn_packed_add(const AttnPackedBwdArgs& args, int nw, bool kv, hipStream_t s) {
   AttnPackedBwdArgs a = args;
   const int ot = (width(a.f.dh) + 31) / 32;
-  const dim3 grid(packed_grid(a.f, nw * WR, (kv ? 2 : a.f.H / a.f.Hkv) * ((a.f.dh + 31) / 32), by_place));
+  const dim3 grid(packed_grid(a.f, nw * WR, (kv ? 2 : a.f.H / a.f.Hkv) * ((a.f.dh + 31) / 32), kv));
   if (kv && nw == 2) hipLaunchKernelGGL((attn_packed_add_kernel<2, true>), grid, dim3(128), 0, s, a, ot);
   else if (kv) hipLaunchKernelGGL((attn_packed_add_kernel<4, true>), grid, dim3(256), 0, s, a, ot);
   else if (nw == 2) hipLaunchKernelGGL((attn_packed_add_kernel<2, false>), grid, dim3(128), 0, s, a, ot);

@@ -254,7 +254,7 @@ hipError_t launch_attn_packed_fwd(const AttnPackedArgs& a, hipStream_t s);
 hipError_t launch_attn_packed_bwd(const AttnPackedBwdArgs& a, hipStream_t s);
 // The parts of a split forward or backward (a.split of them, blocks of 32 nw rows; kv: dK and dV) made one.
 hipError_t launch_attn_packed_join(const AttnPackedArgs& a, int nw, hipStream_t s);
-hipError_t launch_attn_packed_add(const AttnPackedBwdArgs& a, int nw, bool kv, bool by_place, hipStream_t s);
+hipError_t launch_attn_packed_add(const AttnPackedBwdArgs& a, int nw, bool kv, hipStream_t s);
 // Heads of more than 128 dims, a block's work in `split` parts (dQ: qsplit, dK / dV: ksplit).
 hipError_t launch_attn256_packed_fwd(const AttnPackedArgs& a, int split, hipStream_t s);
 hipError_t launch_attn256_packed_bwd(const AttnPackedBwdArgs& a, int qsplit, int ksplit, hipStream_t s);
