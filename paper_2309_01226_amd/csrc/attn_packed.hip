@@ -650,18 +650,20 @@ int width(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : dh <= 80 ? 80 : dh <=
 
 // Waves (of 32 rows): four share the staged blocks; two where that leaves CUs idle or where the
 // sequences are mostly too short for four (the idle waves wait).
-// Parts: a block's steps (64 keys; of dK / dV, 64 queries of each head) are split among as many workgroups as
-// the CUs hold beside the other blocks': blocks of equal work (no causal mask, or a window) in one round of
-// them at most, since a second one would be as long; of the unequal ones of a causal mask, to the nearest round,
-// where a CU holds one workgroup to the next.  A part keeps at least 4 steps of an average block, of dK / dV (two
-// products more a step) and of 256-wide dQ 2, and the parts save at least what the join's launch takes, 8 steps of a 64-wide
-// forward (8 documents in 12000 rows, 4 heads: 24 us without, 29 with).  A causal mask without a window also makes
-// the longest block of dK / dV the last to end, twice the mean for one sequence, more for several lengths: up
-// to four rounds, of 32 steps at least.  The host does not know the lengths: sequences without a causal mask (images)
-// are taken to be alike, those with one (documents) to differ, the long ones T / n_seq^(2/3) rows.  8 documents in
-// 8000 rows, 4 heads of 64, backward 138 us by the mean, 104 so; 8 of 500 rows 29 and 31.  Microseconds without parts and with: 4 documents in 15992 rows, 16 heads of
-// 64 on 4, backward 929, 663; one of 2048 rows, 4 heads of 128, causal, forward 54, 23; 8192 rows, one head of 256,
-// forward and backward 1113, 343; two documents in 1000 rows, 8 heads of 64 on 2, backward 76, 34.
+// Parts of a block's steps (64 keys; of dK / dV, 64 queries of each head):
+//  * As many as let all blocks fill the CUs.  Blocks of equal work (no causal mask, or a window) in one round of
+//    workgroups at most, since a second one would be as long; a causal mask's unequal ones to the nearest round, and
+//    where a CU holds one workgroup to the next.
+//  * A part keeps at least 4 steps of a long block, of dK / dV (more products a step) and of 256-wide dQ 2, and the
+//    parts save at least what the join's launch takes, 8 steps of a 64-wide forward.
+//  * The host does not know the lengths: sequences without a causal mask (images) are taken to be alike, those with one
+//    (documents) to differ, the long ones T / n_seq^(2/3) rows.  8 documents in 8000 rows, 4 heads of 64, forward
+//    and backward 47 and 138 us by the mean, 38 and 104 so; 8 of 1500 rows each 25 and 72, 30 and 75.
+//  * A causal mask without a window makes the longest block of dK / dV the last to end, twice the mean for one
+//    sequence, more for several lengths: up to four rounds, of 32 steps at least.
+// Forward and backward without parts and with, us: 2048 rows, 4 heads of 128, 45 and 114, 24 and 63; 8192 rows, one
+// head of 256, 249 and 880, 82 and 264; documents of 700 and 300 rows, 8 heads of 64 on 2, backward 77 and 31; 4 documents
+// in 15992 rows, 16 heads of 64 on 4, backward 965 and 710.
 Plan plan(const AttnPackedArgs& a, Pass pass) {
   const int G = a.H / a.Hkv, per = pass == DKDV ? 1 : G;
   const long rows = a.T / std::max(1, a.n_seq);
