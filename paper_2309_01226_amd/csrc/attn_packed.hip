@@ -20,9 +20,10 @@
 // 128 dims, 4 x 4096 rows of 16 heads take forward 268 us and backward 837 for 32 dims, 476 and 1655 for 96; in
 // their own 221 and 630, 426 and 1461.)
 //
-// Bounds and times, bf16: 64- and 80-wide heads by the vector unit (an exponential and about ten other
-// instructions a pair against 4 dh flop), 128-wide ones by the matrix cores at the clock that the power limit
-// leaves (the large matrix product: 1.4 PFLOP/s).  Forward, dQ, dK / dV of
+// Bounds and times: 64- and 80-wide heads by a wave's chain of LDS reads, products and exponentials (an exponential and
+// about ten other instructions a pair against 4 dh flop: vector unit busy half, matrix cores a quarter to a third of the
+// cycles on these documents), 128-wide ones by the matrix cores at the clock that the power limit leaves (the
+// large matrix product: 1.4 PFLOP/s).  Forward, dQ, dK / dV of
 //   32 documents of 16 to 2048 rows in 16384, 16 heads of 64, causal       77, 100, 131 us (forward 450 TFLOP/s)
 //   64 images of 65 to 577 rows in 16448, 16 heads of 80, no mask          72, 102, 123 us
 //   4 documents in 16001 rows, 16 heads of 128 on 4 K / V heads, causal    290, 390, 650 us (forward 1.0 PFLOP/s; the
