@@ -330,7 +330,10 @@ hipError_t launch_adamw(float* p, const float* g, float* m, float* v, bf16* shad
 // tensors, entry k's chunks are workgroups first[k] .. first[k + 1] - 1.
 // vec: every array of the entry is aligned for four elements at once.
 struct AdamWEntry {
-  float* p;
+  union {
+    float* p;          // step
+    void* v_out;       // state
+  };
   const void* g;       // fp32 or bf16
   void* m;             // fp32, or uint8 codes
   void* v;
@@ -340,13 +343,12 @@ struct AdamWEntry {
     bf16* shadow;      // step; may be null
     void* m_out;       // state: fp32 or bf16
   };
-  void* v_out;
-  long n;
-  float lr_wd;
+  long n : 62;
+  unsigned long vec : 1;
+  float lr_wd;         // lr * weight decay
   uint32_t key;
-  int vec;
 };
-constexpr int kAdamWEntries = 40;  // of 88 bytes: kernel arguments below 4 KB
+constexpr int kAdamWEntries = 52;  // of 72 bytes: kernel arguments below 4 KB
 struct AdamWMulti {
   AdamWConsts c;
   int count;

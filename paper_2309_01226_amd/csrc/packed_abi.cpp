@@ -243,7 +243,6 @@ extern "C" sat_status sat_op_adamw_multi(const sat_adamw_tensor* t, int32_t coun
         const sat_adamw_tensor& e = t[k];
         o.p = e.p; o.g = e.g; o.m = e.m; o.v = e.v; o.m_exp = e.m_exp; o.v_exp = e.v_exp;
         o.shadow = (bf16*)e.shadow;
-        o.v_out = nullptr;
         o.n = e.n;
         o.lr_wd = (float)(lr * e.weight_decay);
         o.key = dither_key(seed, step, k);
