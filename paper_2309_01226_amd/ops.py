@@ -8,6 +8,7 @@ the stream; every element of every output is computed by the HIP kernels.
 import ctypes as C
 import functools
 import struct
+from array import array
 
 import torch
 
@@ -430,14 +431,17 @@ def adamw_multi_state(tensors, m_out, v_out):
     if len(m_out) != n or len(v_out) != n:
         raise ValueError("adamw_multi_state: one output of each kind for each parameter")
     dt = torch.bfloat16 if n and m_out[0].dtype == torch.bfloat16 else torch.float32
-    dev = tensors.device
+    T, dev = torch.Tensor, tensors.device
     for name, ts in (("m_out", m_out), ("v_out", v_out)):
+        # all at once first: a look at every tensor takes longer than the launches
+        if (list(map(T.numel, ts)) == tensors.sizes and all(map(T.is_contiguous, ts)) and set(map(T.get_device, ts)) <= {dev}
+                and {t.dtype for t in ts} <= {dt}):
+            continue
         for i, (t, k) in enumerate(zip(ts, tensors.sizes)):
-            if t.dtype is not dt or t.get_device() != dev:
-                _here(t, dt, f"{name}[{i}]", dev)
+            _here(t, dt, f"{name}[{i}]", dev)
             if not t.is_contiguous() or t.numel() != k:
                 raise ValueError(f"{name}[{i}]: expected {k} contiguous elements, got {tuple(t.shape)}")
-    ms, vs = ((C.c_void_p * n)(*[t.data_ptr() for t in ts]) for ts in (m_out, v_out))
+    ms, vs = ((C.c_void_p * n).from_buffer(array("Q", map(T.data_ptr, ts))) for ts in (m_out, v_out))
     _lib.call("sat_op_adamw_multi_state", tensors.table, n, ms, vs, dt == torch.bfloat16, _stream())
 
 
