@@ -138,7 +138,10 @@ sat_status sat_op_attention_bwd(const void* q, const void* k, const void* v, int
  *            window when window > 0 (0: none).  Every query sees itself.
  *   values   o = softmax(scale q k^T) v as bf16, lse [H, T] fp32 the natural-log
  *            log-sum-exp; gradients of q, k, v as bf16, dk and dv summed in fp32 over
- *            the query heads that share them.  A row of a sequence that holds NaN
+ *            the query heads that share them.  Products take p and dS rounded to
+ *            bf16.  delta = rowsum(dout o) of the backward is the fp32 sum of p dP for dk and dv
+ *            of up to 128 dims, and for dq there where a block of 64 or 128 queries sees at most 128 keys;
+ *            elsewhere it is formed from the bf16 o.  A row of a sequence that holds NaN
  *            or infinities may spoil other rows of that sequence, none of another.
  *            The same inputs give the same bits on every call.
  * q, k, v, o and dout are 16-byte aligned with leading dimensions that are
@@ -148,7 +151,8 @@ sat_status sat_op_attention_bwd(const void* q, const void* k, const void* v, int
  * forward uses it where few blocks of queries meet many keys, whose work is then split and joined,
  * and may have none (NULL); the backward needs at least H T (rounded up to 4) and
  * splits with more.  The _ws calls say how much each takes at most for the same sizes and
- * mask; results with and without differ by the order of sums only.  Calls that may overlap need a
+ * mask; results with and without differ by the order of the fp32 sums and by the running
+ * maximum under which p is rounded, and keep the same bounds.  Calls that may overlap need a
  * ws each.  The forward reads nothing else from dout on.
  * Errors: SAT_EINVAL for null pointers (T > 0), sizes, alignment, or a ws that is too small. */
 typedef struct {

@@ -123,6 +123,8 @@ __global__ __launch_bounds__(64 * NW, DH == 80 && NW == 4 ? 3 : 2) void attn_pac
 // O is as large as V.  The same sum over the keys, sum P dP, has no such error: it is formed beside dQ (a
 // multiply-add per pair) for the dK / dV kernel and, where all keys of the workgroup fit the two stages, in a pass
 // of its own before dQ.  Gradients of 24 rows: 0.27 % -> 0.24 % off, of which 0.17 % is the results' rounding.
+// A part of a split block has a part of the sum, which the join adds; blocks that fit the stages stay whole, in the
+// first part.
 template <int DH, int NW, bool PAD>
 __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBwdArgs ba) {
   using C = Cfg<DH>;
@@ -163,7 +165,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
   TileOfs<DH, KB> to;
   to.init(lane);
   int jb = key_lo(a, q0) / KB, je = (key_hi(a, q0 + WGR - 1, S) + KB - 1) / KB;  // as in the forward
-  part_of(sp, a.split, jb, je);
+  const bool brief = je - jb <= 2;
+  if (!brief) part_of(sp, a.split, jb, je);
+  else if (sp > 0) je = jb;
   const bool idle = wq0 >= S;
   const int wlo = key_lo(a, wq0), whi = idle ? 0 : key_hi(a, wq0 + WR - 1, S);
   const int lo = key_lo(a, q), hi = key_hi(a, q, S);
@@ -189,13 +193,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
   using Yes = std::true_type;
   using No = std::false_type;
   if (jb < je) copy(jb);  // a part may be empty
-  if (je - jb <= 2 && a.split == 1) {
+  if (brief) {
     if (je - jb == 2) copy(jb + 1);
     wait_vm_lgkm0<0>();
     cta_barrier();
     for (int j = jb; j < je; ++j) masked(j, Yes(), No());
-    st.dlt = halves_sum(st.pd);
-    if (g == 0 && q < S) ba.delta[hs + q] = st.dlt;
+    st.dlt = st.pd = halves_sum(st.pd);
     for (int j = jb; j < je; ++j) masked(j, No(), Yes());
   } else {
     auto step = [&](int j) {
@@ -220,11 +223,18 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_packed_dq_kernel(AttnPackedBw
       cta_barrier();
     }
     for (; j < je; ++j) step(j);
-    const float sum = halves_sum(st.pd);  // a part has a part of it only
-    if (g == 0 && q < S && sp == 0) ba.delta[hs + q] = a.split > 1 ? st.dlt : sum;
+    st.pd = halves_sum(st.pd);
   }
-  if (a.split > 1) put_acc<C::OT>(wave_share(a.ws, ((long)tile * a.H + h) * a.split + sp, NW, 16 * C::OT, wave), st.dq);
-  else if (q < S) store_rowT<DH, PAD>(ba.dq + (long)(s0 + q) * ba.lddq + (long)h * a.dh, st.dq, a.scale, g, a.dh);
+  if (a.split > 1) {
+    float* p = wave_share(a.ws, ((long)tile * a.H + h) * a.split + sp, NW, 16 * C::OT + 4, wave);
+    put_acc<C::OT>(p, st.dq);
+    p[16 * C::OT * 64] = st.pd;
+    return;
+  }
+  if (q < S) {
+    if (g == 0) ba.delta[hs + q] = st.pd;
+    store_rowT<DH, PAD>(ba.dq + (long)(s0 + q) * ba.lddq + (long)h * a.dh, st.dq, a.scale, g, a.dh);
+  }
 }
 
 // ================================================================ dK and dV
@@ -609,7 +619,8 @@ __global__ __launch_bounds__(64 * NW) void attn_packed_join_kernel(AttnPackedArg
   }
 }
 
-// dQ, or (KV) dK and dV, of split blocks: the parts' sum in their order.
+// dQ, or (KV) dK and dV, of split blocks: the parts' sum in their order.  With dQ of up to 128 dims also delta (the
+// 256-wide kernel has written it: its delta is that of the rounded O).
 template <int NW, bool KV>
 __global__ __launch_bounds__(64 * NW) void attn_packed_add_kernel(AttnPackedBwdArgs ba, int ot) {
   const AttnPackedArgs& a = ba.f;
@@ -621,10 +632,18 @@ __global__ __launch_bounds__(64 * NW) void attn_packed_add_kernel(AttnPackedBwdA
   const int t = part % nt, which = part / nt, h = KV ? kvh : kvh * G + which;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = blk * NW * WR + wave * WR + (lane & 31);
-  const int regs = (KV ? 2 : 1) * 16 * ot;
+  const bool sums = !KV && ot <= 4;
+  const int regs = (KV ? 2 : 1) * 16 * ot + (sums ? 4 : 0);
   const long step = (long)NW * regs * 64;  // from part to part
-  const float* p = wave_share(a.ws, ((long)tile * (KV ? a.Hkv : a.H) + h) * a.split, NW, regs, wave) +
-                   16 * ((KV ? which * ot : 0) + t) * 64;
+  const float* p = wave_share(a.ws, ((long)tile * (KV ? a.Hkv : a.H) + h) * a.split, NW, regs, wave);
+  if (sums && t == 0) {
+    const float* pd = p + 16 * ot * 64;
+    float sum = 0.f;
+#pragma unroll 4
+    for (int sp = 0; sp < a.split; ++sp) sum += pd[sp * step];
+    if (row < S && lane < 32) ba.delta[(long)h * a.T + s0 + row] = sum;
+  }
+  p += 16 * ((KV ? which * ot : 0) + t) * 64;
   floatx4 acc[4] = {};
 #pragma unroll 4
   for (int sp = 0; sp < a.split; ++sp)
@@ -686,7 +705,9 @@ Plan plan(const AttnPackedArgs& a, Pass pass) {
   const long products = pass == FWD ? 2 : pass == DQ ? 3 : 4;  // of a step
   if (steps * (p.split - 1) * products * std::max(dh, 64) < 1024 * p.split) p.split = 1;  // 32: the exponentials' time
   if (pass == DKDV && tail) p.split = (int)std::min(16L, std::max((long)p.split, std::min(4 * slots / items, steps / 32)));
-  const int regs = pass == FWD ? 16 * ((dh + 31) / 32) + 4 : (pass == DKDV ? 32 : 16) * ((dh + 31) / 32);
+  const int ot = (dh + 31) / 32;
+  // of a lane in the scratch: accumulators, and m and l, or (up to 128 dims) the sum of P dP
+  const int regs = pass == DKDV ? 32 * ot : 16 * ot + (pass == FWD || dh <= 128 ? 4 : 0);
   p.ws = p.split == 1 ? 0 : (a.T / R + a.n_seq) * (long)a.Hkv * per * p.split * p.nw * regs * 64;
   return p;
 }

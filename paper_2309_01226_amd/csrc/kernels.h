@@ -242,7 +242,7 @@ struct AttnPackedBwdArgs {
   AttnPackedArgs f;
   const bf16* dout;
   long lddo;
-  float* delta;      // [H, T] rowsum(dO * O)
+  float* delta;      // [H, T] rowsum(dO * O): the fp32 sum of P dP, of more than 128 dims from the bf16 O
   bf16* dq;
   bf16* dk;
   bf16* dv;
