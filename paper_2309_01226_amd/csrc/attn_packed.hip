@@ -693,7 +693,10 @@ Plan plan(const AttnPackedArgs& a, Pass pass) {
   if (dh == 256 || (dh >= 96 && pass == DKDV)) p.nw = 4;  // 256: 128 rows, in the backward by eight waves
   const int R = p.nw * WR;
   const bool tail = a.causal && a.window >= a.T;
-  const long items = (a.T / R + 1) * (long)a.Hkv * per;
+  // a sequence shorter than a block is one all the same: else parts and their scratch, which is sized for
+  // T / R + n_seq blocks, would go by far fewer blocks than there are (4096 sequences in 16384 rows, 8 heads
+  // of 128 on one: 1.1 GB and 1431 us forward and backward, so none and 1097)
+  const long items = std::max(a.T / R + 1L, (long)a.n_seq) * a.Hkv * per;
   const int on_cu = dh == 256 || (dh >= 96 && pass == DKDV) ? 1 : dh == 32 ? (pass == DKDV ? 3 : 4)
                     : pass != DKDV && (dh == 64 || (dh == 80 && pass == FWD)) ? 3 : 2;
   const long slots = 256L * (4 / p.nw) * on_cu;  // workgroups that the CUs hold

@@ -194,3 +194,21 @@ def test_rotary_division_is_exact_within_the_limits():
 
 def test_adamw_refuses_more_than_a_launch_takes():
     assert _adamw(n=(1 << 35) + 1) == _L().SAT_EINVAL
+
+
+def test_scratch_follows_the_chip_and_not_the_number_of_sequences():
+    """Parts only fill the CUs: at most four rounds of the workgroups that these hold, each with fp32 dk and dv of its rows.
+    256 CUs x 128 rows x workgroups on a CU x dims are at most 32768 x 256; rows of up to twice as many block
+    numbers as there are blocks (T / R + n_seq against the larger of the two)."""
+    L = _L()
+    n = C.c_int64()
+    for T in (64, 1000, 4096, 16384, 32768, 131072):
+        for n_seq in (1, 4, 64, 1024, 4096, 16384):
+            for H, Hkv in ((1, 1), (8, 8), (16, 4), (8, 1), (64, 1)):
+                for dh in (8, 64, 80, 128, 136, 256):
+                    for causal, window in ((1, 0), (0, 0), (1, 512)):
+                        d = L.sat_attn_packed_desc(n_seq=n_seq, T=T, H=H, Hkv=Hkv, dh=dh, causal=causal, window=window)
+                        for name, delta in (("fwd", 0), ("bwd", (H * T + 3) // 4 * 4)):
+                            f = getattr(L.lib(), f"sat_op_attention_packed_{name}_ws")
+                            assert f(C.byref(d), C.byref(n)) == 0
+                            assert 0 <= n.value - delta <= 4 * 2 * 32768 * 256 * 2, (T, n_seq, H, Hkv, dh, causal, window, name)
