@@ -364,7 +364,9 @@ def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=Tru
 class AdamWTensors:
     """The tensors of adamw_multi: parameters (fp32), gradients (all fp32 or all bf16), moments
     (all fp32, or all uint8 with m_exp and v_exp, one uint8 for each 256 elements of a tensor), bf16
-    shadows (optional) and weight decay (a number, or one per tensor).  Holds the tensors."""
+    shadows (optional) and weight decay (a number, or one per tensor).  Holds the tensors' memory as it is now:
+    a step reads and writes there even if a caller's list or tensor gets another storage later, so gradients
+    are to be written into the same tensors in every step (or the table is built again)."""
 
     def __init__(self, params, grads, m, v, *, shadows=None, weight_decay=0.0, m_exp=None, v_exp=None):
         n = len(params)
@@ -407,7 +409,9 @@ class AdamWTensors:
                 raise ValueError("{}[{}] overlaps {}[{}]".format(*span[3:], *last[3:]))
             if span[1] > end:
                 end, last = span[1], span
-        self.tensors, self.sizes, self.device = lists, sizes, dev
+        # aliases: the memory stays while the table does, whatever becomes of the caller's lists and tensors
+        self.tensors = {name: [t.detach() for t in ts] for name, ts in lists.items()}
+        self.sizes, self.device = sizes, dev
         self.table = (_lib.sat_adamw_tensor * n)()
         none = [None] * n
         columns = [ptrs.get(x, none) for x in ("params", "grads", "m", "v", "m_exp", "v_exp", "shadows")]

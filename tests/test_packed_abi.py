@@ -212,3 +212,18 @@ def test_scratch_follows_the_chip_and_not_the_number_of_sequences():
                             f = getattr(L.lib(), f"sat_op_attention_packed_{name}_ws")
                             assert f(C.byref(d), C.byref(n)) == 0
                             assert 0 <= n.value - delta <= 4 * 2 * 32768 * 256 * 2, (T, n_seq, H, Hkv, dh, causal, window, name)
+
+
+def test_adamw_table_keeps_the_memory_that_it_points_to(monkeypatch):
+    """Neither the caller's lists nor the tensors' own storage may be swapped under the pointers."""
+    from paper_2309_01226_amd import ops
+    monkeypatch.setattr(ops, "_device", lambda t, name: -1)  # of host tensors: nothing is launched here
+    lists = {k: [torch.zeros(300) for _ in range(2)] for k in ("params", "grads", "m", "v")}
+    sh = [torch.zeros(300, dtype=torch.bfloat16) for _ in range(2)]
+    t = ops.AdamWTensors(**lists, shadows=sh)
+    fields = dict(params="p", grads="g", m="m", v="v", shadows="shadow")
+    for name, ts in dict(lists, shadows=sh).items():
+        ts[0] = torch.ones(300)                   # another gradient, say
+        ts[1].data = torch.ones_like(ts[1].data)  # a parameter that moved
+        for i in range(2):
+            assert t.tensors[name][i].data_ptr() == getattr(t.table[i], fields[name]), (name, i)
