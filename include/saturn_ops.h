@@ -257,7 +257,8 @@ sat_status sat_op_adamw_multi(const sat_adamw_tensor* t, int32_t count, int32_t 
 /* The values that 8-bit moments stand for, m and v of every tensor to m_out[k] and
  * v_out[k] (host arrays of device pointers to n values), fp32 (exact) or, with out_bf16,
  * bf16 (m exact, v rounded once): to store 32-bit moments, or to look at them.  Of the
- * table, m, v, m_exp, v_exp and n are read.  Errors: SAT_EINVAL. */
+ * table, m, v, m_exp, v_exp and n are read.  No output overlaps another or what is read.
+ * Errors: SAT_EINVAL for null pointers, sizes, alignment, and outputs that overlap; SAT_ENOMEM. */
 sat_status sat_op_adamw_multi_state(const sat_adamw_tensor* t, int32_t count,
                                     void* const* m_out, void* const* v_out, int32_t out_bf16,
                                     void* stream);

@@ -1,8 +1,13 @@
 // Kernel-level C ABI (include/saturn_ops.h) of the operators on packed rows: attention inside
 // packed sequences, rotary positions with several axes, AdamW over many tensors.  Argument
-// checks, then the launches; nothing is allocated.
+// checks, then the launches; nothing is allocated on the device.
 #include <math.h>
 #include <string.h>
+
+#include <algorithm>
+#include <memory>
+#include <new>
+#include <utility>
 
 #include "../../include/saturn_ops.h"
 #include "abi_common.h"
@@ -255,6 +260,43 @@ extern "C" sat_status sat_op_adamw_multi(const sat_adamw_tensor* t, int32_t coun
   return SAT_OK;
 }
 
+// Whether outputs of adamw_multi_state, elements of `size` bytes, overlap each other or what it reads.
+static sat_status state_outputs(const sat_adamw_tensor* t, int32_t count, void* const* m_out, void* const* v_out,
+                                uintptr_t size, const char* fn) {
+  struct Span {
+    uintptr_t at, end;
+  };
+  const std::unique_ptr<Span[]> out(new (std::nothrow) Span[2 * (size_t)count + 1]);
+  if (!out) {
+    sat_set_error("%s: no host memory for %d tensors", fn, count);
+    return SAT_ENOMEM;
+  }
+  int n = 0;
+  for (void* const* list : {m_out, v_out})
+    for (int k = 0; k < count; ++k) {
+      if (t[k].n == 0) continue;
+      const uintptr_t at = reinterpret_cast<uintptr_t>(list[k]);
+      out[n++] = Span{at, at + (uintptr_t)t[k].n * size};
+    }
+  Span* const end = out.get() + n;
+  const auto before = [](const Span& a, const Span& b) { return a.at < b.at; };
+  if (!std::is_sorted(out.get(), end, before)) std::sort(out.get(), end, before);
+  for (int i = 1; i < n; ++i) SAT_CHECK_ARG(out[i].at >= out[i - 1].end, "%s: outputs overlap each other", fn);
+  for (int k = 0; k < count; ++k) {
+    if (t[k].n == 0) continue;
+    const uintptr_t blocks = (uintptr_t)(t[k].n + 255) / 256;
+    const std::pair<const void*, uintptr_t> reads[] = {
+        {t[k].m, (uintptr_t)t[k].n}, {t[k].v, (uintptr_t)t[k].n}, {t[k].m_exp, blocks}, {t[k].v_exp, blocks}};
+    for (const auto& r : reads) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(r.first);
+      // the last output that begins before the end of what is read ends before its beginning
+      const Span* o = std::lower_bound(out.get(), end, Span{at + r.second, 0}, before);
+      SAT_CHECK_ARG(o == out.get() || o[-1].end <= at, "%s: tensor %d: an output overlaps its moments", fn, k);
+    }
+  }
+  return SAT_OK;
+}
+
 extern "C" sat_status sat_op_adamw_multi_state(const sat_adamw_tensor* t, int32_t count, void* const* m_out,
                                                void* const* v_out, int32_t out_bf16, void* stream) {
   const char* fn = "adamw_multi_state";
@@ -267,6 +309,10 @@ extern "C" sat_status sat_op_adamw_multi_state(const sat_adamw_tensor* t, int32_
     SAT_CHECK_ARG(e.m && e.v && e.m_exp && e.v_exp && m_out[k] && v_out[k], "%s: tensor %d: null pointer", fn, k);
     SAT_CHECK_ARG(aligned(m_out[k], oa) && aligned(v_out[k], oa), "%s: tensor %d: outputs must be aligned to their elements",
                   fn, k);
+  }
+  if (count > 0) {
+    const sat_status st = state_outputs(t, count, m_out, v_out, oa, fn);
+    if (st != SAT_OK) return st;
   }
   AdamWConsts none;
   memset(&none, 0, sizeof none);

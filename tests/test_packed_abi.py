@@ -227,3 +227,18 @@ def test_adamw_table_keeps_the_memory_that_it_points_to(monkeypatch):
         ts[1].data = torch.ones_like(ts[1].data)  # a parameter that moved
         for i in range(2):
             assert t.tensors[name][i].data_ptr() == getattr(t.table[i], fields[name]), (name, i)
+
+
+@pytest.mark.parametrize("m_out,v_out", [
+    ((4096, 8192), (4096, 16384)), ((4096, 5292), (8192, 16384)), ((4096, 8192), (16384, 7000)),  # outputs over outputs
+    ((1 << 20, 8192), (4096, 16384)), ((4096, 8192), (12288, (1 << 21) - 1196)),                   # over codes
+    ((4096, (1 << 22) - 1196), (8192, 16384)), ((4096, 8192), (12288, (1 << 23))),                # over exponents
+])
+def test_state_refuses_outputs_that_overlap(m_out, v_out):
+    """Two tensors of 300 values, fp32 outputs of 1200 bytes."""
+    L = _L()
+    tab = (L.sat_adamw_tensor * 2)(L.sat_adamw_tensor(m=1 << 20, v=1 << 21, m_exp=1 << 22, v_exp=(1 << 22) + 64, n=300),
+                                   L.sat_adamw_tensor(m=(1 << 20) + 300, v=(1 << 21) + 300, m_exp=(1 << 23) - 1, v_exp=(1 << 23) + 1, n=300))
+    mo, vo = ((C.c_void_p * 2)(*x) for x in (m_out, v_out))
+    assert L.lib().sat_op_adamw_multi_state(tab, 2, mo, vo, 0, None) == L.SAT_EINVAL
+    assert "overlap" in L.last_error()
