@@ -347,6 +347,9 @@ def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=Tru
     """Rotary positions with len(pairs) axes on the H heads of x [T, >= H dh] (bf16 or fp32), axis a
     turning pairs[a] pairs of every head by pos[:, a] (int32 [T, axes]); in place, or into `out`.
     See saturn_ops.h.  Returns the rotated tensor."""
+    # ctypes would cut what 32 bits do not hold
+    if H < 1 or dh < 1 or min(pairs, default=0) < 0 or max(pairs, default=0) > 128:
+        raise ValueError(f"H={H}, dh={dh}, pairs: {pairs}")
     f32 = x.dtype == torch.float32
     dt = torch.float32 if f32 else torch.bfloat16
     T, A, dev = x.shape[0], len(pairs), _device(x, "x")
@@ -354,8 +357,6 @@ def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=Tru
     ldx = _rows_of(x, dt, "x", T, H * dh, dev)
     ldy = ldx if out is None else _rows_of(out, dt, "out", T, H * dh, dev)
     ldp = _rows_of(pos, torch.int32, "pos", T, A, dev)
-    if max(pairs, default=0) > 128:  # ctypes would cut it
-        raise ValueError(f"pairs: {pairs}")
     _lib.call("sat_op_rotary_axes", x.data_ptr(), ldx, y.data_ptr(), ldy, f32, pos.data_ptr(), ldp, A,
               (C.c_int32 * A)(*pairs), T, H, dh, base, interleaved, own_freqs, inverse, _stream(dev))
     return y

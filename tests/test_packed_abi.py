@@ -242,3 +242,13 @@ def test_state_refuses_outputs_that_overlap(m_out, v_out):
     mo, vo = ((C.c_void_p * 2)(*x) for x in (m_out, v_out))
     assert L.lib().sat_op_adamw_multi_state(tab, 2, mo, vo, 0, None) == L.SAT_EINVAL
     assert "overlap" in L.last_error()
+
+
+@pytest.mark.parametrize("H,dh,pairs", [
+    (1, 64, (16 - (1 << 32),)), (1, 64, ((1 << 32) + 16,)), (1, 64, (-1,)), (1, 64, (20, -4)),
+    (1 - (1 << 32), 64, (16,)), (1, 64 - (1 << 32), (16,)), (0, 64, (16,)),
+])
+def test_rotary_sizes_that_32_bits_would_cut_are_refused(H, dh, pairs):
+    from paper_2309_01226_amd import ops
+    with pytest.raises(ValueError):
+        ops.rotary_axes(torch.zeros(4, 64), torch.zeros(4, 2, dtype=torch.int32), H, dh, pairs)
