@@ -129,7 +129,9 @@ sat_status sat_op_attention_bwd(const void* q, const void* k, const void* v, int
  *            2^24.  Rows outside all sequences are
  *            not read and keep what they hold in every output.  cu is read on the
  *            device only, so a captured call takes the lengths of the
- *            replay; values outside [0, T] are taken as the nearer of the two.
+ *            replay; values outside [0, T] are taken as the nearer of the two.  A cu that decreases
+ *            touches no row outside its values either, but leaves undefined what its sequences
+ *            write.
  *   heads    H query heads, Hkv K / V heads, Hkv a divisor of H; query head h
  *            reads K / V head h / (H / Hkv).  dh: a multiple of 8 up to 256
  *            (32, 64, 80, 96, 128 and 256 have kernels of their width, others run
