@@ -237,8 +237,9 @@ sat_status sat_op_adamw(float* p, const float* g, float* m, float* v, void* shad
  *            with the mean right, by a hash of (seed, t, place in the table, element): the
  *            same call gives the same bits, and each step of a run should have its own
  *            seed or t.  A root over 0 is kept as no less than the least code, 2^-15 of its
- *            block's largest at most; an m under that is kept as 0.  A gradient that is not
- *            finite spoils p and the moments of its block.
+ *            block's largest at most; an m under that is kept as 0.  The root and the division
+ *            of the update are the hardware's approximations (1 ulp each), and a v below 2^-126
+ *            counts as 0.  A gradient that is not finite spoils p and the moments of its block.
  * Arrays are aligned to their elements (16 bytes for all is fastest).  Step t >= 1,
  * as constants: a captured call repeats the same lr and t.
  * Errors: SAT_EINVAL for null pointers, sizes, state_bits and constants. */
@@ -257,8 +258,8 @@ sat_status sat_op_adamw_multi(const sat_adamw_tensor* t, int32_t count, int32_t 
                               int32_t grad_bf16, double lr, double beta1, double beta2,
                               double eps, int64_t step, uint64_t seed, void* stream);
 /* The values that 8-bit moments stand for, m and v of every tensor to m_out[k] and
- * v_out[k] (host arrays of device pointers to n values), fp32 (exact) or, with out_bf16,
- * bf16 (m exact, v rounded once): to store 32-bit moments, or to look at them.  Of the
+ * v_out[k] (host arrays of device pointers to n values), fp32 (exact, but for a v
+ * below 2^-126) or, with out_bf16, bf16 (m exact, v rounded once): to store 32-bit moments, or to look at them.  Of the
  * table, m, v, m_exp, v_exp and n are read.  No output overlaps another or what is read.
  * Errors: SAT_EINVAL for null pointers, sizes, alignment, and outputs that overlap; SAT_ENOMEM. */
 sat_status sat_op_adamw_multi_state(const sat_adamw_tensor* t, int32_t count,

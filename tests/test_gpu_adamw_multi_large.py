@@ -104,3 +104,22 @@ def test_long_tensor_of_8_bits_against_64_bits(grad, shift):
     assert (np.abs(m8 - m) <= np.maximum(np.abs(m) * (0.125 + 1e-6), 2.25 * 2.0 ** -15 * 2.0 / 1.75 * top(np.abs(m)))).all()
     assert (np.abs(r8 - r) <= np.maximum(r * (0.0625 + 1e-6), 2.125 * 2.0 ** -15 * 2.0 / 1.9 * top(r))).all()
     assert (r8[r > 0] > 0).all()
+
+
+def test_second_moments_of_8_bits_at_the_end_of_the_range():
+    """v of 2^-125.3 is kept and decays by 0.999; below 2^-126 it counts as 0, and p moves by m / eps alone."""
+    from paper_2309_01226_amd import ops
+    n = 512
+    z8 = lambda k: torch.zeros(k, device="cuda", dtype=torch.uint8)  # noqa: E731
+    p, g, m, v, me, ve = torch.zeros(n, device="cuda"), torch.full((n,), 1.25 * 2.0 ** -58, device="cuda"), z8(n), z8(n), z8(2), z8(2)
+    g[256:] = 1.25 * 2.0 ** -59
+    t = ops.AdamWTensors([p], [g], [m], [v], m_exp=[me], v_exp=[ve])
+    ops.adamw_multi(t, LR, B1, B2, EPS, 1, seed=1)
+    out = [torch.empty(n, device="cuda") for _ in range(2)]
+    ops.adamw_multi_state(t, [out[0]], [out[1]])
+    torch.cuda.synchronize()
+    want = 0.001 * (1.25 * 2.0 ** -58) ** 2
+    assert float((out[1][:256].double().sqrt() / want ** 0.5 - 1).abs().max()) <= 1 / 16 + 1e-5 and not v[256:].any()
+    # root / (1 - b2) is 4e-18, nothing against eps
+    step = LR * _np(g) / EPS
+    assert (np.abs(_np(p) + step) <= 16 * 2.0 ** -24 * step).all()
