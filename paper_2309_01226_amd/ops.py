@@ -411,7 +411,7 @@ class AdamWTensors:
             if span[1] > end:
                 end, last = span[1], span
         # aliases: the memory stays while the table does, whatever becomes of the caller's lists and tensors
-        self.tensors = {name: [t.detach() for t in ts] for name, ts in lists.items()}
+        self.tensors = {name: list(map(torch.Tensor.detach, ts)) for name, ts in lists.items()}
         self.sizes, self.device = sizes, dev
         self.table = (_lib.sat_adamw_tensor * n)()
         none = [None] * n
