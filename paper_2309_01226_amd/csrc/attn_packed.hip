@@ -22,11 +22,11 @@
 //
 // Bounds and times: 64- and 80-wide heads by a wave's chain of LDS reads, products and exponentials (an exponential and
 // about ten other instructions a pair against 4 dh flop: vector unit busy half, matrix cores a quarter to a third of the
-// cycles on these documents), 128-wide ones by the matrix cores at the clock that the power limit leaves (the
-// large matrix product: 1.4 PFLOP/s).  Forward, dQ, dK / dV of
+// cycles on these documents), 128-wide ones by the same chain, with the matrix cores busy in 0.43 to 0.54 of the
+// cycles and the clock at 1.8 to 2.1 GHz of 2.4 meanwhile (the large matrix product: 1.4 PFLOP/s).  Forward, dQ, dK / dV of
 //   32 documents of 16 to 2048 rows in 16384, 16 heads of 64, causal       77, 100, 131 us (forward 450 TFLOP/s)
 //   64 images of 65 to 577 rows in 16448, 16 heads of 80, no mask          72, 102, 123 us
-//   4 documents in 16001 rows, 16 heads of 128 on 4 K / V heads, causal    290, 390, 650 us (forward 1.0 PFLOP/s; the
+//   4 documents in 16001 rows, 16 heads of 128 on 4 K / V heads, causal    299, 404, 663 us (forward 1.0 PFLOP/s; the
 //     backward executes 7 products for the 5 counted: 1.0 PFLOP/s executed)
 #include <algorithm>
 #include <cmath>
