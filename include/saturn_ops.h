@@ -142,8 +142,8 @@ sat_status sat_op_attention_bwd(const void* q, const void* k, const void* v, int
  *            log-sum-exp; gradients of q, k, v as bf16, dk and dv summed in fp32 over
  *            the query heads that share them.  Products take p and dS rounded to
  *            bf16.  delta = rowsum(dout o) of the backward is the fp32 sum of p dP for dk and dv
- *            of up to 128 dims, and for dq there where a block of 64 or 128 queries sees at most 128 keys;
- *            elsewhere it is formed from the bf16 o.  A row of a sequence that holds NaN
+ *            of up to 128 dims, and for dq there where a block of 64 or 128 queries sees keys of no more
+ *            than two blocks of 64; elsewhere it is formed from the bf16 o.  A row of a sequence that holds NaN
  *            or infinities may spoil other rows of that sequence, none of another.
  *            The same inputs give the same bits on every call.
  * q, k, v, o and dout are 16-byte aligned with leading dimensions that are

@@ -32,7 +32,7 @@
 // 10.5; 4 M 19.8 and 21.3; 160 M with 32-bit moments 883 us through the caches, 799 past them.  Whole aligned runs take a
 // straight-line path (8 bits: 1891 -> 1197 us), the others go element by element.
 // 160 M values with 32-bit moments: 4.80 GB in 809 us, 5.9 TB/s; 444 M with 8-bit ones: 7.1 GB in 1199 us, 5.9;
-// reading their values back as bf16, 6 bytes each: 513 us, 5.2 (another card: 744, 1102 and 471 us).  A copy of 4 GiB
+// reading their values back as bf16, 6 bytes each: 513 us, 5.2 (another card: 752, 1102 and 471 us).  A copy of 4 GiB
 // moves 4.8 TB/s, torch's product in place 5.9, its fill 6.8.
 #include "adamw_math.h"
 #include "common.h"

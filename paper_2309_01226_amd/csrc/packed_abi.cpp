@@ -271,7 +271,7 @@ static sat_status state_outputs(const sat_adamw_tensor* t, int32_t count, void* 
     sat_set_error("%s: no host memory for %d tensors", fn, count);
     return SAT_ENOMEM;
   }
-  int n = 0;
+  size_t n = 0;
   for (void* const* list : {m_out, v_out})
     for (int k = 0; k < count; ++k) {
       if (t[k].n == 0) continue;
@@ -281,7 +281,7 @@ static sat_status state_outputs(const sat_adamw_tensor* t, int32_t count, void* 
   Span* const end = out.get() + n;
   const auto before = [](const Span& a, const Span& b) { return a.at < b.at; };
   if (!std::is_sorted(out.get(), end, before)) std::sort(out.get(), end, before);
-  for (int i = 1; i < n; ++i) SAT_CHECK_ARG(out[i].at >= out[i - 1].end, "%s: outputs overlap each other", fn);
+  for (size_t i = 1; i < n; ++i) SAT_CHECK_ARG(out[i].at >= out[i - 1].end, "%s: outputs overlap each other", fn);
   for (int k = 0; k < count; ++k) {
     if (t[k].n == 0) continue;
     const uintptr_t blocks = (uintptr_t)(t[k].n + 255) / 256;

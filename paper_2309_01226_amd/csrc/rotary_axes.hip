@@ -14,7 +14,7 @@
 // cos and sin in LDS meanwhile, then rotates.  32749 rows of 20 heads of 128, bf16 in place: 335 MB
 // in 58 us, 5.8 TB/s; 5003 rows of 32 fp32 heads of 256, a quarter of the dims rotated, into another
 // buffer: 328 MB in 57 us, 5.7 TB/s (a copy of 4 GiB: 4.7).  257 rows of 32 heads of 80: 4.1 us, the launch and
-// one way to memory; a call among others takes its host side, 8.0 us.
+// one way to memory; a call among others takes its host side, 7.8 us.
 #include <algorithm>
 #include <type_traits>
 

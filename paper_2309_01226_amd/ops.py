@@ -343,12 +343,14 @@ def attention_packed_bwd(q, k, v, o, lse, cu, dout, dq, dk, dv, H, Hkv, dh, caus
     _lib.call("sat_op_attention_packed_bwd", d, _stream(dev))
 
 
+_PAIRS = frozenset(range(129))  # that one axis may turn
+
+
 def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=True, own_freqs=False, inverse=False):
     """Rotary positions with len(pairs) axes on the H heads of x [T, >= H dh] (bf16 or fp32), axis a
     turning pairs[a] pairs of every head by pos[:, a] (int32 [T, axes]); in place, or into `out`.
     See saturn_ops.h.  Returns the rotated tensor."""
-    # ctypes would cut what 32 bits do not hold
-    if H < 1 or dh < 1 or min(pairs, default=0) < 0 or max(pairs, default=0) > 128:
+    if H < 1 or dh < 1 or not _PAIRS.issuperset(pairs):  # ctypes would cut what 32 bits do not hold
         raise ValueError(f"H={H}, dh={dh}, pairs: {pairs}")
     f32 = x.dtype == torch.float32
     dt = torch.float32 if f32 else torch.bfloat16
