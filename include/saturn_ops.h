@@ -209,6 +209,79 @@ sat_status sat_op_rotary_axes(const void* x, int64_t ldx, void* y, int64_t ldy, 
                               int32_t interleaved, int32_t own_freqs, int32_t inverse,
                               void* stream);
 
+/* Dropout of x [rows, ldx] to y [rows, ldy]: y = x up where an element is kept, else 0 (also of infinities
+ * and NaN).  The generator is Philox4x32-10 with the key `seed` (low word, high word) and the counter
+ * (column / 8, row, low and high word of *step); column 8 q + e takes the low (e even) or high half of
+ * word e / 2 and is dropped when that is below t = round(65536 p); up = 65536 / (65536 - t).
+ * Nothing is stored: the backward is the same call on the gradient.  step: device int64 [1], read by
+ * the kernel, so that a captured call draws anew when the caller's own work moves it on; NULL: 0.
+ * Calls with the same seed, step and place drop the same elements: give each place in a model a seed
+ * of its own.  y == x (with ldy == ldx): in place; else y must not overlap x.  f32: x and y are fp32, else
+ * bf16.  cols up to 2^18, rows ceil(cols / 8) below 2^33; x and y aligned to their elements.  Columns
+ * behind `cols` are not touched.  Errors: SAT_EINVAL for null pointers, sizes, alignment and p outside [0, 1]. */
+sat_status sat_op_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int32_t f32,
+                          int32_t rows, int32_t cols, double p, uint64_t seed, const int64_t* step,
+                          void* stream);
+
+/* The boundary of two sublayers, over T rows of 1 <= d <= 8192 columns, forward and backward:
+ *   u = N_post(f)                     the norm of the branch's rows (f bf16), or f itself
+ *   y = alpha x + beta gate m u       the residual stream, fp32 when stream_f32, else bf16
+ *   h = N_pre(y)                      bf16, from y as it is stored: what the next sublayer reads
+ * pre, post: 0 none (pre: no h), 1 LayerNorm, 2 RMS norm (x / sqrt(mean x^2 + eps)), with gains g_*
+ * (NULL: 1) and shifts b_* (NULL: 0), fp32 [d].  gate: fp32 [d], NULL: 1.  m: dropout with the numbers of
+ * sat_op_dropout for the same p, seed, step, row and column (p 0: none); a dropped element adds
+ * nothing, whatever f holds.  stats: fp32 [4, T], mean and 1 / sqrt(var + eps) of the branch's norm, then of
+ * the next one's (a norm that is not there leaves its two rows as they are; an RMS norm's mean is 0);
+ * may be NULL without norms.  y may be x (with ldy == ldx); no other output overlaps an input.
+ * Backward, from dy (the gradient that reaches y along the stream, in its type; NULL: 0) and dh (bf16, with
+ * pre): dx = alpha t and df of t = dy + N_pre'(dh), and, where not NULL, fp32 [d] (written): dg_*, db_* and
+ * dgate, summed over the rows in fp32 in an order that depends on T and d alone.  It reads y (with pre), f (with post or
+ * dgate), stats, gains, post's shift, gate and the dropout's arguments; dx may be dy (with lddx == lddy).  ws:
+ * fp32 scratch, as much as the _ws call says (T, d and which sums are wanted are read); calls that may
+ * overlap need one each.  A row that holds NaN or infinities spoils its own rows of the outputs and the sums.
+ * Arrays are aligned to their elements (16-byte aligned rows are fastest).
+ * Errors: SAT_EINVAL for null pointers, sizes, alignment, constants, and a ws that is too small. */
+typedef struct {
+  const void* x;
+  int64_t ldx;
+  const void* f;
+  int64_t ldf;
+  void* y;
+  int64_t ldy;
+  void* h;
+  int64_t ldh;
+  float* stats;
+  const float* g_pre;
+  const float* b_pre;
+  const float* g_post;
+  const float* b_post;
+  const float* gate;
+  int32_t T, d, stream_f32, pre, post;
+  float alpha, beta, eps;
+  double p;
+  uint64_t seed;
+  const int64_t* step;
+  const void* dy;
+  int64_t lddy;
+  const void* dh;
+  int64_t lddh;
+  void* dx;
+  int64_t lddx;
+  void* df;
+  int64_t lddf;
+  float* dg_pre;
+  float* db_pre;
+  float* dg_post;
+  float* db_post;
+  float* dgate;
+  float* ws;
+  int64_t ws_elems;
+} sat_residual_norm_desc;
+sat_status sat_op_residual_norm_fwd(const sat_residual_norm_desc* d, void* stream);
+sat_status sat_op_residual_norm_bwd(const sat_residual_norm_desc* d, void* stream);
+/* fp32 elements of ws for these sizes and sums. */
+sat_status sat_op_residual_norm_bwd_ws(const sat_residual_norm_desc* d, int64_t* elems);
+
 /* Softmax cross-entropy forward + backward over fp32 logits z [N, ldz]:
  * row_loss fp32 [N] (0 for label -1), dz bf16 [N, lddz] = (softmax - onehot)
  * * inv_n (0 rows for label -1), where inv_n = 1 / (number of labels != -1). */

@@ -80,6 +80,22 @@ class sat_adamw_tensor(C.Structure):
     ]
 
 
+class sat_residual_norm_desc(C.Structure):
+    _fields_ = [
+        ("x", C.c_void_p), ("ldx", C.c_int64), ("f", C.c_void_p), ("ldf", C.c_int64),
+        ("y", C.c_void_p), ("ldy", C.c_int64), ("h", C.c_void_p), ("ldh", C.c_int64),
+        ("stats", C.c_void_p), ("g_pre", C.c_void_p), ("b_pre", C.c_void_p), ("g_post", C.c_void_p),
+        ("b_post", C.c_void_p), ("gate", C.c_void_p),
+        ("T", C.c_int32), ("d", C.c_int32), ("stream_f32", C.c_int32), ("pre", C.c_int32), ("post", C.c_int32),
+        ("alpha", C.c_float), ("beta", C.c_float), ("eps", C.c_float), ("p", C.c_double),
+        ("seed", C.c_uint64), ("step", C.c_void_p),
+        ("dy", C.c_void_p), ("lddy", C.c_int64), ("dh", C.c_void_p), ("lddh", C.c_int64),
+        ("dx", C.c_void_p), ("lddx", C.c_int64), ("df", C.c_void_p), ("lddf", C.c_int64),
+        ("dg_pre", C.c_void_p), ("db_pre", C.c_void_p), ("dg_post", C.c_void_p), ("db_post", C.c_void_p),
+        ("dgate", C.c_void_p), ("ws", C.c_void_p), ("ws_elems", C.c_int64),
+    ]
+
+
 class sat_profile_result(C.Structure):
     _fields_ = [
         ("struct_size", C.c_uint32), ("steps", C.c_int32),
@@ -137,6 +153,10 @@ SIGNATURES = {
                                      C.c_double, C.c_double, _I64, C.c_uint64, _VP]),
     "sat_op_adamw_multi_state": (C.c_int, [C.POINTER(sat_adamw_tensor), _I32, C.POINTER(_VP), C.POINTER(_VP),
                                            _I32, _VP]),
+    "sat_op_dropout": (C.c_int, [_VP, _I64, _VP, _I64, _I32, _I32, _I32, C.c_double, C.c_uint64, _VP, _VP]),
+    "sat_op_residual_norm_fwd": (C.c_int, [C.POINTER(sat_residual_norm_desc), _VP]),
+    "sat_op_residual_norm_bwd": (C.c_int, [C.POINTER(sat_residual_norm_desc), _VP]),
+    "sat_op_residual_norm_bwd_ws": (C.c_int, [C.POINTER(sat_residual_norm_desc), C.POINTER(_I64)]),
     "sat_op_rotary": (C.c_int, [_VP, _I64, _I32, _I32, _I32, _I32, _I32, _I32, _VP]),
     "sat_op_cross_entropy": (C.c_int, [_VP, _I64, _VP, _I32, _I32, _VP, _VP, _I64, _VP, _VP]),
     "sat_op_adamw": (C.c_int, [_VP, _VP, _VP, _VP, _VP, _I64, C.c_double, C.c_double, C.c_double,

@@ -10,6 +10,7 @@
 #include "common.h"
 #include "kernels.h"
 #include "adamw_math.h"
+#include "philox.h"
 
 namespace {
 
@@ -595,26 +596,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(float* __restrict__ p,
 }
 
 // ---------------------------------------------------------------- init
-// Philox4x32-10 (Salmon et al., SC'11) keyed by the seed, counter =
-// (pair index, tensor id); Box-Muller turns its outputs into two normals.
-__device__ __forceinline__ void philox_round(uint32_t& c0, uint32_t& c1, uint32_t& c2,
-                                             uint32_t& c3, uint32_t k0, uint32_t k1) {
-  const uint32_t M0 = 0xD2511F53u, M1 = 0xCD9E8D57u;
-  uint32_t hi0 = __umulhi(M0, c0), lo0 = M0 * c0;
-  uint32_t hi1 = __umulhi(M1, c2), lo1 = M1 * c2;
-  uint32_t n0 = hi1 ^ c1 ^ k0, n1 = lo1, n2 = hi0 ^ c3 ^ k1, n3 = lo0;
-  c0 = n0; c1 = n1; c2 = n2; c3 = n3;
-}
-__device__ __forceinline__ void philox4x32_10(uint32_t ctr[4], uint32_t k0, uint32_t k1) {
-  const uint32_t W0 = 0x9E3779B9u, W1 = 0xBB67AE85u;
-#pragma unroll
-  for (int r = 0; r < 10; ++r) {
-    philox_round(ctr[0], ctr[1], ctr[2], ctr[3], k0, k1);
-    k0 += W0;
-    k1 += W1;
-  }
-}
-
+// Philox4x32-10 keyed by the seed, counter = (pair index, tensor id); Box-Muller turns
+// its outputs into two normals.
 __global__ void init_normal_kernel(float* __restrict__ p, bf16* __restrict__ shadow, long n,
                                    uint32_t k0, uint32_t k1, uint32_t stream_id, float std) {
   long pair = (long)blockIdx.x * blockDim.x + threadIdx.x;

@@ -387,6 +387,53 @@ hipError_t launch_zero(void* p, long bytes, hipStream_t s);
 hipError_t launch_sum_rows_batched(const float* dh, float* out, int B, int S, int d,
                                    hipStream_t s);
 
+// ---------------------------------------------------------------- around the blocks (dropout.hip, residual_norm.hip)
+struct DropoutArgs {
+  const void* x;
+  void* y;
+  int64_t ldx, ldy;
+  int rows, cols;
+  uint64_t seed;
+  uint32_t limit;         // 65536 p: an element is dropped when its 16 bits are below it
+  float up;               // 65536 / (65536 - limit), 0 for limit = 65536
+  const uint64_t* step;   // device, NULL: 0
+  int n8;                 // set by the launch: groups of eight columns, and the inverse for dividing by it
+  uint32_t inv;
+};
+// cols <= 2^18, rows ceil(cols / 8) < 2^31 NT.
+hipError_t launch_dropout(DropoutArgs a, bool f32, hipStream_t s);
+
+enum { kNormNone = 0, kNormLayer = 1, kNormRms = 2 };
+constexpr int kResidualNormMaxD = 8192;
+struct ResidualNormArgs {
+  const void* x;
+  void* y;                // the backward reads it
+  const bf16* f;
+  bf16* h;
+  float* stats;           // [4, T]: mean and reciprocal deviation of the branch's norm, then of the next one's
+  const float *g_pre, *b_pre, *g_post, *b_post, *gate;
+  int64_t ldx, ldy, ldf, ldh;
+  int T, d, pre, post;    // kNorm*
+  float alpha, beta, eps;
+  uint64_t seed;          // dropout as in DropoutArgs; limit 0: none
+  uint32_t limit;
+  float up;
+  const uint64_t* step;
+  // backward
+  const void* dy;         // NULL: 0
+  const bf16* dh;
+  void* dx;
+  bf16* df;
+  int64_t lddy, lddh, lddx, lddf;
+  float *dg_pre, *db_pre, *dg_post, *db_post, *dgate;
+  float* ws;              // residual_norm_ws elements
+  int wpr, rows_wg, sums; // set by the launch
+};
+hipError_t launch_residual_norm_fwd(ResidualNormArgs a, bool f32, hipStream_t s);
+hipError_t launch_residual_norm_bwd(ResidualNormArgs a, bool f32, hipStream_t s);
+// fp32 elements for `sums` of the five gradients that are sums over rows.
+int64_t residual_norm_ws(int T, int d, int sums);
+
 // ---------------------------------------------------------------- ResNet (conv.hip)
 // NHWC activations ([N, H, W, C] = the matrix [N * H * W, C]).
 // col[(n Ho + i) Wo + j, (a k + b) C + c] = x[n, i s - pad + a, j s - pad + b, c]

@@ -1,0 +1,388 @@
+// The boundary of two sublayers in one pass over the rows, forward and backward:
+//
+//   u = N_post(f)                    norm of the branch's rows, or f itself
+//   y = alpha x + beta gate m u      m: dropout's 0 or 1 / (1 - p); y is rounded to the stream's type
+//   h = N_pre(y)                     the next sublayer's input, from y as it is stored
+//
+//   t  = dy + N_pre'(dh)             the gradient at y
+//   dx = alpha t                     du = beta gate m t       df = N_post'(du)
+//   dgate = sum beta m u t           dg = sum g xh, db = sum g for each norm, over the rows
+//   N'(g) = rs (a - mean(a) - xh mean(a xh)), a = gain g, xh the normalised row; RMS norms
+//   subtract no mean.
+//
+// Bound by HBM: every array is read or written once (fp32 stream, 12 bytes an element forward and 18
+// backward).  A row belongs to d / 512 waves, eight columns a thread, so that a thread's columns
+// stay the same from row to row: gains and the sums of their gradients live in its registers, and the next
+// row's loads are in flight while a row is worked on.  A mean or a variance is formed inside each
+// wave and joined by the pairwise formula of Chan, Golub and LeVeque (one barrier where a second pass
+// over the row would take two).  The sums over rows go to one row of partial sums for each
+// workgroup, added in order by a second kernel: the same bits on every call.
+#include <algorithm>
+
+#include "kernels.h"
+#include "philox.h"
+#include "rows.h"
+
+namespace {
+
+constexpr int CUS = 256;
+
+struct RowPlace {
+  int wpr;    // waves of a row
+  int rw;     // this wave's row among those of the workgroup
+  int wave;   // this wave among its row's
+  int col, n; // first column of the thread, and columns of the row from there on
+};
+
+__device__ __forceinline__ RowPlace row_place(int wpr, int d) {
+  RowPlace p;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  p.wpr = wpr;
+  p.rw = w / wpr;
+  p.wave = w - p.rw * wpr;
+  p.col = 8 * (p.wave * 64 + (threadIdx.x & 63));
+  p.n = d - p.col;
+  return p;
+}
+
+// Pairs of sums of up to 16 waves, two sets of them by turns: between a set's reads and its next
+// writes every wave passes the other set's barrier.
+struct Shared {
+  float2 part[2][16];
+};
+
+// Sums of a and b over the row.
+__device__ __forceinline__ float2 row_sums(const RowPlace& p, Shared& sh, int& turn, float a, float b) {
+  float2 s = make_float2(wave_total(a), wave_total(b));
+  if (p.wpr == 1) return s;
+  float2* part = sh.part[turn];
+  turn ^= 1;
+  if ((threadIdx.x & 63) == 0) part[p.rw * p.wpr + p.wave] = s;
+  __syncthreads();
+  s = make_float2(0.f, 0.f);
+  for (int i = 0; i < p.wpr; ++i) {
+    const float2 q = part[p.rw * p.wpr + i];
+    s.x += q.x;
+    s.y += q.y;
+  }
+  return s;
+}
+
+// Mean (0 for RMS) and reciprocal deviation of a row whose elements are v (0 behind its end).
+__device__ __forceinline__ float2 row_stats(const RowPlace& p, Shared& sh, int& turn, const float (&v)[8], int kind,
+                                            int d, float eps) {
+  float s = 0.f;
+  if (kind == kNormRms) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += v[e] * v[e];
+    return make_float2(0.f, rsqrtf(row_sums(p, sh, turn, s, 0.f).x / d + eps));
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s += v[e];
+  // columns of the row's i-th wave
+  const auto width = [&](int i) { return (float)min(512, d - 512 * i); };
+  float mean = wave_total(s) / width(p.wave), m2 = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m2 += e < p.n ? (v[e] - mean) * (v[e] - mean) : 0.f;
+  m2 = wave_total(m2);
+  if (p.wpr > 1) {
+    float2* part = sh.part[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) part[p.rw * p.wpr + p.wave] = make_float2(mean, m2);
+    __syncthreads();
+    mean = m2 = 0.f;
+    for (int i = 0; i < p.wpr; ++i) mean += part[p.rw * p.wpr + i].x * width(i);
+    mean /= d;
+    for (int i = 0; i < p.wpr; ++i) {
+      const float2 q = part[p.rw * p.wpr + i];
+      m2 += q.y + width(i) * (q.x - mean) * (q.x - mean);
+    }
+  }
+  return make_float2(mean, rsqrtf(m2 / d + eps));
+}
+
+// Columns of a vector for each channel, or `none` without one.
+__device__ __forceinline__ void channels(const float* g, const RowPlace& p, float none, float (&x)[8]) {
+  if (g != nullptr && p.n > 0) {
+    widen8(load8<false>(g + p.col, p.n), x);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = none;
+  }
+}
+
+// beta gate m of eight columns of a row; exactly 0 where dropped.
+__device__ __forceinline__ void branch_factors(const ResidualNormArgs& a, const DropConsts& c, uint64_t step, int row,
+                                               const RowPlace& p, float scale, float (&m)[8]) {
+  if (c.limit == 0) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m[e] = scale;
+    return;
+  }
+  const DropRow r = drop_bits(c, step, (uint32_t)row, (uint32_t)p.col / 8);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m[e] = drop_keeps(c, r, e) ? scale : 0.f;
+}
+
+template <class XT, int MAXT>
+__global__ __launch_bounds__(MAXT) void residual_norm_fwd_kernel(ResidualNormArgs a) {
+  __shared__ Shared sh;
+  int turn = 0;
+  const RowPlace p = row_place(a.wpr, a.d);
+  const DropConsts c = {(uint32_t)a.seed, (uint32_t)(a.seed >> 32), a.limit, a.up, a.step};
+  const uint64_t step = drop_step(c);
+  const float scale = a.beta * (c.limit ? c.up : 1.f);
+  const int rows_wg = a.rows_wg, stride = gridDim.x * rows_wg;
+  const XT* x = (const XT*)a.x;
+  XT* y = (XT*)a.y;
+  float g_pre[8], b_pre[8], g_post[8], b_post[8], gate[8];
+  Raw8<XT> nx;
+  Raw8<bf16> nf;
+  auto load = [&](int row) {
+    const int n = row < a.T ? p.n : 0;
+    nx = load8<false>(x + (int64_t)row * a.ldx + p.col, n);
+    nf = load8<false>(a.f + (int64_t)row * a.ldf + p.col, n);
+  };
+  load(blockIdx.x * rows_wg + p.rw);
+  channels(a.g_pre, p, 1.f, g_pre);
+  channels(a.b_pre, p, 0.f, b_pre);
+  channels(a.g_post, p, 1.f, g_post);
+  channels(a.b_post, p, 0.f, b_post);
+  channels(a.gate, p, 1.f, gate);
+  for (int r0 = blockIdx.x * rows_wg; r0 < a.T; r0 += stride) {
+    const int row = r0 + p.rw;
+    const int n = row < a.T ? p.n : 0;
+    float v[8], u[8];
+    widen8(nx, v);
+    widen8(nf, u);
+    load(row + stride);
+    if (a.post) {
+      const float2 st = row_stats(p, sh, turn, u, a.post, a.d, a.eps);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = (u[e] - st.x) * st.y * g_post[e] + b_post[e];
+      if (p.col == 0 && row < a.T) {
+        a.stats[row] = st.x;
+        a.stats[a.T + row] = st.y;
+      }
+    }
+    float m[8];
+    branch_factors(a, c, step, row, p, scale, m);
+    // a dropped element adds nothing, whatever the branch holds there
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = a.alpha * v[e] + (m[e] != 0.f ? m[e] * gate[e] * u[e] : 0.f);
+    store8<false>(y + (int64_t)row * a.ldy + p.col, n, v);
+    if (a.pre) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = e < n ? (float)(XT)v[e] : 0.f;
+      const float2 st = row_stats(p, sh, turn, v, a.pre, a.d, a.eps);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (v[e] - st.x) * st.y * g_pre[e] + b_pre[e];
+      store8<false>(a.h + (int64_t)row * a.ldh + p.col, n, v);
+      if (p.col == 0 && row < a.T) {
+        a.stats[2 * (int64_t)a.T + row] = st.x;
+        a.stats[3 * (int64_t)a.T + row] = st.y;
+      }
+    }
+  }
+}
+
+// The workgroup's sums for its columns, of the rows it holds at once, to its row of partial sums.
+__device__ __forceinline__ void put_sums(const ResidualNormArgs& a, const RowPlace& p, float* join, float* part,
+                                         const float (&s)[8]) {
+  if (a.rows_wg == 1) {
+    store8<false>(part + p.col, p.n, s);
+    return;
+  }
+  __syncthreads();
+  const int w = 512 * p.wpr;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) join[p.rw * w + p.col + e] = s[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.d; i += blockDim.x) {
+    float t = 0.f;
+    for (int r = 0; r < a.rows_wg; ++r) t += join[r * w + i];
+    part[i] = t;
+  }
+}
+
+template <class XT, int MAXT>
+__global__ __launch_bounds__(MAXT) void residual_norm_bwd_kernel(ResidualNormArgs a) {
+  __shared__ Shared sh;
+  __shared__ float join[MAXT <= 512 ? MAXT * 8 : 8];
+  int turn = 0;
+  const RowPlace p = row_place(a.wpr, a.d);
+  const DropConsts c = {(uint32_t)a.seed, (uint32_t)(a.seed >> 32), a.limit, a.up, a.step};
+  const uint64_t step = drop_step(c);
+  const float scale = a.beta * (c.limit ? c.up : 1.f), inv_d = 1.f / a.d;
+  const int rows_wg = a.rows_wg, stride = gridDim.x * rows_wg;
+  const bool branch = a.post || a.dgate;  // the branch's rows are needed
+  const XT* y = (const XT*)a.y;
+  const XT* dy = (const XT*)a.dy;
+  XT* dx = (XT*)a.dx;
+  float g_pre[8], g_post[8], b_post[8], gate[8];
+  Raw8<XT> ny, ndy;
+  Raw8<bf16> nf, ndh;
+  float2 nst = make_float2(0.f, 0.f), npost = make_float2(0.f, 0.f);
+  auto load = [&](int row) {
+    const int n = row < a.T ? p.n : 0;
+    const int at = min(row, a.T - 1);
+    if (a.pre) {
+      ny = load8<false>(y + (int64_t)row * a.ldy + p.col, n);
+      ndh = load8<false>(a.dh + (int64_t)row * a.lddh + p.col, n);
+      nst = make_float2(a.stats[2 * (int64_t)a.T + at], a.stats[3 * (int64_t)a.T + at]);
+    }
+    if (dy) ndy = load8<false>(dy + (int64_t)row * a.lddy + p.col, n);
+    if (branch) nf = load8<false>(a.f + (int64_t)row * a.ldf + p.col, n);
+    if (a.post) npost = make_float2(a.stats[at], a.stats[a.T + at]);
+  };
+  load(blockIdx.x * rows_wg + p.rw);
+  channels(a.g_pre, p, 1.f, g_pre);
+  channels(a.g_post, p, 1.f, g_post);
+  channels(a.b_post, p, 0.f, b_post);
+  channels(a.gate, p, 1.f, gate);
+  float s_gpre[8], s_bpre[8], s_gpost[8], s_bpost[8], s_gate[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s_gpre[e] = s_bpre[e] = s_gpost[e] = s_bpost[e] = s_gate[e] = 0.f;
+  for (int r0 = blockIdx.x * rows_wg; r0 < a.T; r0 += stride) {
+    const int row = r0 + p.rw;
+    const int n = row < a.T ? p.n : 0;
+    float t[8], yh[8], g[8], f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = yh[e] = g[e] = f[e] = 0.f;
+    if (dy) widen8(ndy, t);
+    if (a.pre) {
+      widen8(ny, yh);
+      widen8(ndh, g);
+    }
+    if (branch) widen8(nf, f);
+    const float2 st = nst, pst = npost;
+    load(row + stride);
+    if (a.pre) {
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        yh[e] = e < n ? (yh[e] - st.x) * st.y : 0.f;
+        s_gpre[e] += g[e] * yh[e];
+        s_bpre[e] += g[e];
+        g[e] *= g_pre[e];
+        s0 += g[e];
+        s1 += g[e] * yh[e];
+      }
+      const float2 s = row_sums(p, sh, turn, s0, s1);
+      const float m0 = a.pre == kNormRms ? 0.f : s.x * inv_d, m1 = s.y * inv_d;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] += st.y * (g[e] - m0 - yh[e] * m1);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) g[e] = a.alpha * t[e];
+    store8<false>(dx + (int64_t)row * a.lddx + p.col, n, g);
+    float m[8];
+    branch_factors(a, c, step, row, p, scale, m);
+    if (a.post) {
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        f[e] = e < n ? (f[e] - pst.x) * pst.y : 0.f;
+        const float tm = e < n && m[e] != 0.f ? t[e] * m[e] : 0.f;
+        if (m[e] != 0.f) s_gate[e] += tm * (f[e] * g_post[e] + b_post[e]);
+        const float du = tm * gate[e];
+        s_gpost[e] += du * f[e];
+        s_bpost[e] += du;
+        t[e] = du * g_post[e];
+        s0 += t[e];
+        s1 += t[e] * f[e];
+      }
+      const float2 s = row_sums(p, sh, turn, s0, s1);
+      const float m0 = a.post == kNormRms ? 0.f : s.x * inv_d, m1 = s.y * inv_d;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = pst.y * (t[e] - m0 - f[e] * m1);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float tm = e < n && m[e] != 0.f ? t[e] * m[e] : 0.f;
+        if (m[e] != 0.f) s_gate[e] += tm * f[e];
+        t[e] = tm * gate[e];
+      }
+    }
+    store8<false>(a.df + (int64_t)row * a.lddf + p.col, n, t);
+  }
+  float* part = a.ws + (int64_t)blockIdx.x * a.sums * a.d;
+  if (a.dg_pre) put_sums(a, p, join, part, s_gpre), part += a.d;
+  if (a.db_pre) put_sums(a, p, join, part, s_bpre), part += a.d;
+  if (a.dg_post) put_sums(a, p, join, part, s_gpost), part += a.d;
+  if (a.db_post) put_sums(a, p, join, part, s_bpost), part += a.d;
+  if (a.dgate) put_sums(a, p, join, part, s_gate);
+}
+
+// Partial sums of G workgroups, added in order: 64 columns of one sum for each workgroup, 16 slices of the
+// partial rows.
+struct SumOut {
+  float* out[5];
+};
+__global__ __launch_bounds__(1024) void residual_norm_sums_kernel(const float* __restrict__ ws, int G, int sums, int d,
+                                                                  SumOut o) {
+  __shared__ float part[16][64];
+  const int k = blockIdx.y, lane = threadIdx.x & 63, slice = threadIdx.x >> 6;
+  const int col = blockIdx.x * 64 + lane;
+  const int per = (G + 15) / 16, g1 = min(G, (slice + 1) * per);
+  float s = 0.f;
+  if (col < d) {
+#pragma unroll 8
+    for (int g = slice * per; g < g1; ++g) s += ws[((int64_t)g * sums + k) * d + col];
+  }
+  part[slice][lane] = s;
+  __syncthreads();
+  if (slice == 0 && col < d) {
+    for (int i = 1; i < 16; ++i) s += part[i][lane];
+    o.out[k][col] = s;
+  }
+}
+
+int waves_of_row(int d) { return (d + 511) / 512; }
+
+// Rows that a backward workgroup holds at once: eight waves of them (16 for rows of more than eight).
+int bwd_rows_wg(int d) { return std::max(1, 8 / waves_of_row(d)); }
+int bwd_groups(int T, int d) { return std::min(CUS, sat_cdiv(T, bwd_rows_wg(d))); }
+
+int sum_outputs(const ResidualNormArgs& a, SumOut* o) {
+  int n = 0;
+  for (float* q : {a.dg_pre, a.db_pre, a.dg_post, a.db_post, a.dgate})
+    if (q) o->out[n++] = q;
+  return n;
+}
+
+}  // namespace
+
+int64_t residual_norm_ws(int T, int d, int sums) { return (int64_t)bwd_groups(T, d) * sums * d; }
+
+hipError_t launch_residual_norm_fwd(ResidualNormArgs a, bool f32, hipStream_t s) {
+  if (a.T == 0) return hipSuccess;
+  a.wpr = waves_of_row(a.d);
+  a.rows_wg = std::max(1, 4 / a.wpr);
+  const int threads = 64 * a.wpr * a.rows_wg;
+  const dim3 grid(std::min(sat_cdiv(a.T, a.rows_wg), CUS * std::max(1, 1024 / threads)));
+  const auto kernel = threads <= 256   ? (f32 ? residual_norm_fwd_kernel<float, 256> : residual_norm_fwd_kernel<bf16, 256>)
+                      : threads <= 512 ? (f32 ? residual_norm_fwd_kernel<float, 512> : residual_norm_fwd_kernel<bf16, 512>)
+                                       : (f32 ? residual_norm_fwd_kernel<float, 1024> : residual_norm_fwd_kernel<bf16, 1024>);
+  hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_residual_norm_bwd(ResidualNormArgs a, bool f32, hipStream_t s) {
+  SumOut o;
+  a.sums = sum_outputs(a, &o);
+  a.wpr = waves_of_row(a.d);
+  a.rows_wg = bwd_rows_wg(a.d);
+  const int threads = 64 * a.wpr * a.rows_wg, G = bwd_groups(a.T, a.d);
+  if (G > 0) {
+    const auto kernel = threads <= 512 ? (f32 ? residual_norm_bwd_kernel<float, 512> : residual_norm_bwd_kernel<bf16, 512>)
+                                       : (f32 ? residual_norm_bwd_kernel<float, 1024> : residual_norm_bwd_kernel<bf16, 1024>);
+    hipLaunchKernelGGL(kernel, dim3(G), dim3(threads), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.sums)
+    hipLaunchKernelGGL(residual_norm_sums_kernel, dim3(sat_cdiv(a.d, 64), a.sums), dim3(1024), 0, s, a.ws, G, a.sums,
+                       a.d, o);
+  return hipGetLastError();
+}

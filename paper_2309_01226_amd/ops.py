@@ -455,3 +455,107 @@ def adamw_multi_state(tensors, m_out, v_out):
 def _on_device(tensors):
     if tensors.device not in (None, torch.cuda.current_device()):
         raise ValueError(f"params: on cuda:{tensors.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+# ---------------------------------------------------------------- around the blocks
+
+def _vec(t, dtype, name, n, dev):
+    """The address of a contiguous vector of n elements, or None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.get_device() != dev:
+        _here(t, dtype, name, dev)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {n} contiguous elements, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _seed(seed):
+    if not 0 <= seed < 1 << 64:  # ctypes would cut it
+        raise ValueError(f"seed: {seed} is not an unsigned number of 64 bits")
+    return seed
+
+
+def dropout(x, p, seed, *, step=None, out=None):
+    """Dropout of x [rows, cols] (bf16 or fp32, a view of a wider buffer allowed), in place or into `out`: an element is 0
+    where the generator (see saturn_ops.h) says so for (seed, *step, row, column), else x / (1 - p).  step: int64 [1] on the device.
+    The backward is the same call on the gradient.  Returns the outcome."""
+    f32 = x.dtype == torch.float32
+    dt, dev = torch.float32 if f32 else torch.bfloat16, _device(x, "x")
+    if x.dim() != 2 or (out is not None and out.shape != x.shape):
+        raise ValueError(f"dropout: expected matrices of one size, got {tuple(x.shape)}" + (f" and {tuple(out.shape)}" if out is not None else ""))
+    rows, cols = x.shape
+    y = x if out is None else out
+    ldx = _rows_of(x, dt, "x", rows, cols, dev)
+    ldy = ldx if out is None else _rows_of(out, dt, "out", rows, cols, dev)
+    _lib.call("sat_op_dropout", x.data_ptr(), ldx, y.data_ptr(), ldy, f32, rows, cols, p, _seed(seed),
+              _vec(step, torch.int64, "step", 1, dev), _stream(dev))
+    return y
+
+
+_NORMS = {None: 0, "layer": 1, "rms": 2}
+# sat_residual_norm_desc's fields
+_BOUNDARY = struct.Struct("PqPqPqPq6P5i3fdQP" + "PqPqPqPq5PPq")
+assert _BOUNDARY.size == C.sizeof(_lib.sat_residual_norm_desc)
+
+
+def _boundary_desc(rows, stats, T, d, f32, dev, back, *, pre=None, post=None, g_pre=None, b_pre=None, g_post=None,
+                   b_post=None, gate=None, alpha=1.0, beta=1.0, eps=1e-5, p=0.0, seed=0, step=None):
+    """rows: address and leading dimension of x, f, y and h; back: the fields of the backward."""
+    f = torch.float32
+    return _lib.sat_residual_norm_desc.from_buffer_copy(_BOUNDARY.pack(
+        *rows, _vec(stats, f, "stats", 4 * T, dev), _vec(g_pre, f, "g_pre", d, dev), _vec(b_pre, f, "b_pre", d, dev),
+        _vec(g_post, f, "g_post", d, dev), _vec(b_post, f, "b_post", d, dev), _vec(gate, f, "gate", d, dev),
+        T, d, f32, _norm(pre, "pre"), _norm(post, "post"), alpha, beta, eps, p, _seed(seed),
+        _vec(step, torch.int64, "step", 1, dev), *back))
+
+
+def _norm(kind, name):
+    if kind not in _NORMS:
+        raise ValueError(f"{name}: {kind!r} is not None, 'layer' or 'rms'")
+    return _NORMS[kind]
+
+
+def _matrix(t, dtype, name, T, d, dev):
+    """Address and leading dimension of a matrix that may be None."""
+    return (0, d) if t is None else (t.data_ptr(), _rows_of(t, dtype, name, T, d, dev))
+
+
+def residual_norm_fwd(x, f, y, h, stats, d, **options):
+    """The boundary of two sublayers in one pass: y = alpha x + beta gate dropout(norm(f)), h = norm(y), on rows of d columns.
+    x, y [T, >= d]: the residual stream, both fp32 or both bf16, y may be x; f [T, >= d] bf16: the branch; h [T, >= d] bf16:
+    the next sublayer's input (None without a norm for it); stats fp32 [4, T]: what the backward needs of the norms.
+    Options, the same in the backward: pre, post (None, "layer" or "rms": the norms of y for h and of f), their gains and shifts
+    g_pre, b_pre, g_post, b_post and the gate (fp32 [d] or None), alpha, beta, eps, and p, seed, step of the
+    dropout.  See saturn_ops.h."""
+    dev, f32, T = _device(x, "x"), x.dtype == torch.float32, x.shape[0]
+    xt, bf = torch.float32 if f32 else torch.bfloat16, torch.bfloat16
+    rows = (*_matrix(x, xt, "x", T, d, dev), *_matrix(f, bf, "f", T, d, dev), *_matrix(y, xt, "y", T, d, dev),
+            *_matrix(h, bf, "h", T, d, dev))
+    desc = _boundary_desc(rows, stats, T, d, f32, dev, (0, d, 0, d, 0, d, 0, d, 0, 0, 0, 0, 0, 0, 0), **options)
+    _lib.call("sat_op_residual_norm_fwd", desc, _stream(dev))
+
+
+def residual_norm_bwd(dy, dh, y, f, stats, dx, df, d, *, dg_pre=None, db_pre=None, dg_post=None, db_post=None, dgate=None, **options):
+    """Its backward from dy (the gradient of y along the stream, in its type, or None) and dh (of h, or None without that
+    norm): writes dx (may be dy), df and the sums that are given, fp32 [d].  y, f and stats are the forward's; y may be None
+    without pre, f without post and dgate.  The workspace comes from torch's allocator, on the current stream."""
+    dev, f32, T = _device(dx, "dx"), dx.dtype == torch.float32, dx.shape[0]
+    xt, bf, f4 = torch.float32 if f32 else torch.bfloat16, torch.bfloat16, torch.float32
+    sums = [_vec(t, f4, n, d, dev) for n, t in (("dg_pre", dg_pre), ("db_pre", db_pre), ("dg_post", dg_post), ("db_post", db_post),
+                                                ("dgate", dgate))]
+    need = _boundary_ws(T, d, 5 - sums.count(0))
+    ws = torch.empty(need, device=dx.device, dtype=f4) if need else None
+    back = (*_matrix(dy, xt, "dy", T, d, dev), *_matrix(dh, bf, "dh", T, d, dev), *_matrix(dx, xt, "dx", T, d, dev),
+            *_matrix(df, bf, "df", T, d, dev), *sums, 0 if ws is None else ws.data_ptr(), need)
+    rows = (0, d, *_matrix(f, bf, "f", T, d, dev), *_matrix(y, xt, "y", T, d, dev), 0, d)
+    desc = _boundary_desc(rows, stats, T, d, f32, dev, back, **options)
+    _lib.call("sat_op_residual_norm_bwd", desc, _stream(dev))
+
+
+@functools.lru_cache(maxsize=256)
+def _boundary_ws(T, d, sums):
+    desc = _lib.sat_residual_norm_desc(T=T, d=d, **dict.fromkeys(("dg_pre", "db_pre", "dg_post", "db_post", "dgate")[:sums], 1))
+    need = C.c_int64()
+    _lib.call("sat_op_residual_norm_bwd_ws", desc, need)
+    return need.value

@@ -1,0 +1,139 @@
+"""Host-side checks of the operators around a step's blocks that need no GPU: refusals of the C entry points before
+any launch, workspace sizes, the references against published numbers and differences."""
+
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+from tests import block_ref as R
+
+P = 1 << 20  # stands for a device address: no call here gets as far as reading it
+
+
+def _L():
+    from paper_2309_01226_amd import _lib
+    return _lib
+
+
+def _refused(fn, *args, word):
+    L = _L()
+    assert getattr(L.lib(), fn)(*args) == L.SAT_EINVAL
+    assert word in L.last_error()
+
+
+# ---------------------------------------------------------------- dropout
+
+@pytest.mark.parametrize("bad", [
+    dict(x=None), dict(y=None), dict(x=P + 1), dict(y=P + 2, f32=1), dict(rows=-1), dict(cols=-1), dict(cols=(1 << 18) + 1, ldx=1 << 19, ldy=1 << 19),
+    dict(rows=1 << 30, cols=72), dict(p=-0.1), dict(p=1.01), dict(p=math.nan), dict(ldx=63), dict(ldy=63), dict(ldx=1 << 40),
+    dict(y=P, ldy=72), dict(step=P + 4),
+])
+def test_dropout_refusals(bad):
+    a = dict(x=P, ldx=64, y=2 * P, ldy=64, f32=0, rows=9, cols=64, p=0.5, seed=1, step=None)
+    a.update(bad)
+    _refused("sat_op_dropout", *a.values(), None, word="dropout")
+
+
+def test_dropout_of_nothing():
+    L = _L()
+    for rows, cols in ((0, 64), (9, 0)):
+        assert L.lib().sat_op_dropout(None, 64, None, 64, 0, rows, cols, 0.5, 1, None, None) == L.SAT_OK
+
+
+def test_philox_known_answers():
+    """The published vectors of Philox4x32-10 (Random123's known answers)."""
+    for ctr, key, want in [
+            ([0] * 4, [0] * 2, [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]),
+            ([0xFFFFFFFF] * 4, [0xFFFFFFFF] * 2, [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]),
+            ([0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344], [0xA4093822, 0x299F31D0], [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1])]:
+        assert [int(x) for x in R.philox(ctr, key)] == want
+
+
+# ---------------------------------------------------------------- residual norm
+
+def _boundary(**kw):
+    d = dict(x=P, ldx=64, f=2 * P, ldf=64, y=3 * P, ldy=64, h=4 * P, ldh=64, stats=5 * P, g_pre=6 * P, b_pre=None, g_post=6 * P, b_post=None,
+             gate=7 * P, T=9, d=64, stream_f32=1, pre=1, post=2, alpha=1.0, beta=1.0, eps=1e-5, p=0.1, seed=1, step=None, dy=8 * P, lddy=64,
+             dh=9 * P, lddh=64, dx=10 * P, lddx=64, df=11 * P, lddf=64, dg_pre=12 * P, dgate=13 * P, ws=14 * P, ws_elems=1 << 40)
+    d.update(kw)
+    return _L().sat_residual_norm_desc(**d)
+
+
+SHARED = [dict(T=-1), dict(T=1 << 30), dict(d=0), dict(d=8193), dict(pre=3), dict(post=-1), dict(pre=0), dict(post=0), dict(alpha=math.inf),
+          dict(beta=math.nan), dict(eps=-1e-5), dict(eps=math.nan), dict(p=-0.5), dict(p=1.5), dict(p=math.nan), dict(stats=None),
+          dict(stats=P + 2), dict(gate=P + 1), dict(b_pre=P + 2), dict(step=P + 4)]
+
+
+@pytest.mark.parametrize("bad", SHARED + [
+    dict(x=None), dict(f=None), dict(y=None), dict(h=None), dict(x=P + 2), dict(f=P + 1), dict(h=P + 1), dict(ldx=63), dict(ldf=63),
+    dict(ldy=63), dict(ldh=1 << 40), dict(y=P, ldy=72),
+])
+def test_residual_norm_refusals(bad):
+    _refused("sat_op_residual_norm_fwd", C.byref(_boundary(**bad)), None, word="residual_norm_fwd")
+
+
+@pytest.mark.parametrize("bad", SHARED + [
+    dict(dh=None), dict(y=None), dict(f=None), dict(dx=None), dict(df=None), dict(dy=P + 2), dict(dx=P + 2), dict(df=P + 1), dict(lddx=63),
+    dict(lddf=63), dict(lddh=63), dict(lddy=63), dict(dx=8 * P, lddx=72), dict(gate=None), dict(ws=None), dict(ws_elems=9 * 2 * 64 // 8 - 1),
+    dict(dgate=P + 2), dict(db_post=P + 1), dict(post=0, g_post=None, db_post=P),
+])
+def test_residual_norm_backward_refusals(bad):
+    _refused("sat_op_residual_norm_bwd", C.byref(_boundary(**bad)), None, word="residual_norm_bwd")
+
+
+def test_residual_norm_null_and_ws():
+    L = _L()
+    n = C.c_int64()
+    _refused("sat_op_residual_norm_fwd", None, None, word="null")
+    _refused("sat_op_residual_norm_bwd", None, None, word="null")
+    _refused("sat_op_residual_norm_bwd_ws", None, C.byref(n), word="null")
+    _refused("sat_op_residual_norm_bwd_ws", C.byref(_boundary()), None, word="null")
+    _refused("sat_op_residual_norm_bwd_ws", C.byref(_boundary(d=8193)), C.byref(n), word="sizes")
+    # sizes and which sums are wanted are read; no sums, no workspace
+    for kw, least in ((dict(T=9, d=64), 0), (dict(T=9, d=64, dgate=P), 64), (dict(T=1 << 20, d=8192, dgate=P, dg_pre=P), 2 * 8192 * 256)):
+        assert L.lib().sat_op_residual_norm_bwd_ws(C.byref(L.sat_residual_norm_desc(**kw)), C.byref(n)) == 0
+        assert n.value >= least and (least or n.value == 0)
+    assert L.lib().sat_op_residual_norm_fwd(C.byref(_boundary(T=0, x=None, f=None, y=None, h=None, stats=None)), None) == L.SAT_OK
+
+
+@pytest.mark.parametrize("pre,post", [("layer", "rms"), ("rms", "layer"), ("layer", None), (None, "layer"), (None, None)])
+def test_residual_norm_gradients(pre, post):
+    """The reference's gradients are those of its own forward, by central differences of a weighted sum."""
+    rng = np.random.default_rng(3)
+    T, d = 4, 11
+    o = dict(pre=pre, post=post, g_pre=rng.normal(size=d) if pre else None, b_pre=rng.normal(size=d) if pre else None,
+             g_post=rng.normal(size=d) if post else None, b_post=rng.normal(size=d) if post else None, gate=rng.normal(size=d),
+             alpha=0.8, beta=1.3, eps=1e-3, p=0.25, seed=77, step=2)
+    x, f, dy, dh = (rng.normal(size=(T, d)) for _ in range(4))
+
+    def value(x, f, o):
+        y = R.residual_fwd(x, f, o)[0]
+        return (y * dy).sum() + ((R.residual_next(y, o)[0] * dh).sum() if pre else 0.0)
+
+    y = R.residual_fwd(x, f, o)[0]
+    st = np.zeros((4, T))
+    if post:
+        st[:2] = R.stats(f, post, o["eps"])
+    if pre:
+        st[2:] = R.stats(y, pre, o["eps"])
+    got = R.residual_bwd(dy, dh, y, f, st, o, 0)
+    e = 1e-5
+
+    def near(name, change):
+        """change(i, step): the value with element i moved; a difference is off by O(e^2) and rounding / e."""
+        g = got[name][0]
+        num = np.array([(change(i, e) - change(i, -e)) / (2 * e) for i in range(g.size)]).reshape(g.shape)
+        assert np.abs(num - g).max() < 1e-7 * max(1.0, np.abs(g).max()), name
+
+    def moved(a, i, s):
+        b = a.copy()
+        b.flat[i] += s
+        return b
+
+    near("dx", lambda i, s: value(moved(x, i, s), f, o))
+    near("df", lambda i, s: value(x, moved(f, i, s), o))
+    for name in ("gate", "g_pre", "b_pre", "g_post", "b_post"):
+        if o[name] is not None:
+            near("d" + name, lambda i, s: value(x, f, {**o, name: moved(o[name], i, s)}))
