@@ -289,6 +289,49 @@ sat_status sat_op_cross_entropy(const float* z, int64_t ldz, const int32_t* labe
                                 int32_t V, float* row_loss, void* dz, int64_t lddz, float* inv_n,
                                 void* stream);
 
+/* Softmax cross entropy of a linear head z = x w^T + bias over the whole vocabulary, and its gradients,
+ * without keeping the logits.
+ *   x [N, ldx] bf16, w [V, ldw] bf16, rows of d; bias fp32 [V] or NULL (-inf takes an entry out).  labels
+ *   int32 [N]: a row whose label is outside [0, V) (-1: ignore) takes no part and costs no product; its
+ *   loss and lse are 0, its dx is 0.
+ *   row_loss, lse fp32 [N]; inv_n fp32 [1] = 1 / (rows that take part), 1 without any.
+ *   Gradients of sum_t c_t row_loss_t, c = row_weight [N] or, when that is NULL, inv_n for every row: dx
+ *   [N, lddx] bf16, dw [V, lddw] and db [V], fp32 when grad_f32, else bf16, each NULL when not wanted.  With
+ *   accumulate (fp32 only) dw and db add to what is there.  Without any, rows are only scored.
+ * d a multiple of 8 up to 2^16, V up to 2^20.  Logits, statistics and sums are fp32; the two products of the
+ * gradients take exp(z - m) c exp(m - lse) - [v = label] c rounded to bf16, of which exp(z - m) is held as
+ * bf16 too (m: the maximum of 128 entries), the label's entry apart from that; db sums them before the last
+ * rounding.  A row whose entries are all -inf has loss 0, lse -inf and no gradient; one that holds NaN
+ * or infinities spoils its own outputs and the gradients of w and bias.  The same inputs give the same bits.
+ * x and w 16-byte aligned with leading dimensions that are multiples of 8 and below 2^21, dx and dw with
+ * 16-byte aligned rows.  Outputs overlap no input and no other output.  ws: scratch, 256-byte aligned, of as many
+ * bytes as the _ws call says (N, V, d, which gradients, grad_f32 are read): 512 MiB (1 GiB for V above 2^19)
+ * for chunks of the tokens at most, a copy of x, up to 128 MiB of partial products, with bf16 dw of
+ * several chunks its fp32 sum; calls that may overlap need one each.
+ * Errors: SAT_EINVAL for null pointers, sizes, alignment, and a ws that is too small. */
+typedef struct {
+  const void* x;
+  int64_t ldx;
+  const void* w;
+  int64_t ldw;
+  const int32_t* labels;
+  const float* bias;
+  const float* row_weight;
+  float* row_loss;
+  float* lse;
+  float* inv_n;
+  void* dx;
+  int64_t lddx;
+  void* dw;
+  int64_t lddw;
+  void* db;
+  int32_t N, V, d, grad_f32, accumulate, reserved;
+  void* ws;
+  int64_t ws_bytes;
+} sat_linear_xent_desc;
+sat_status sat_op_linear_xent(const sat_linear_xent_desc* d, void* stream);
+sat_status sat_op_linear_xent_ws(const sat_linear_xent_desc* d, int64_t* bytes);
+
 /* Fused AdamW over n fp32 values (torch semantics, decoupled decay) at step t
  * (t >= 1); refreshes the bf16 shadow when shadow != NULL. */
 sat_status sat_op_adamw(float* p, const float* g, float* m, float* v, void* shadow, int64_t n,

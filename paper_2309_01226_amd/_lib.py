@@ -96,6 +96,17 @@ class sat_residual_norm_desc(C.Structure):
     ]
 
 
+class sat_linear_xent_desc(C.Structure):
+    _fields_ = [
+        ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64),
+        ("labels", C.c_void_p), ("bias", C.c_void_p), ("row_weight", C.c_void_p),
+        ("row_loss", C.c_void_p), ("lse", C.c_void_p), ("inv_n", C.c_void_p),
+        ("dx", C.c_void_p), ("lddx", C.c_int64), ("dw", C.c_void_p), ("lddw", C.c_int64), ("db", C.c_void_p),
+        ("N", C.c_int32), ("V", C.c_int32), ("d", C.c_int32), ("grad_f32", C.c_int32), ("accumulate", C.c_int32),
+        ("reserved", C.c_int32), ("ws", C.c_void_p), ("ws_bytes", C.c_int64),
+    ]
+
+
 class sat_profile_result(C.Structure):
     _fields_ = [
         ("struct_size", C.c_uint32), ("steps", C.c_int32),
@@ -157,6 +168,8 @@ SIGNATURES = {
     "sat_op_residual_norm_fwd": (C.c_int, [C.POINTER(sat_residual_norm_desc), _VP]),
     "sat_op_residual_norm_bwd": (C.c_int, [C.POINTER(sat_residual_norm_desc), _VP]),
     "sat_op_residual_norm_bwd_ws": (C.c_int, [C.POINTER(sat_residual_norm_desc), C.POINTER(_I64)]),
+    "sat_op_linear_xent": (C.c_int, [C.POINTER(sat_linear_xent_desc), _VP]),
+    "sat_op_linear_xent_ws": (C.c_int, [C.POINTER(sat_linear_xent_desc), C.POINTER(_I64)]),
     "sat_op_rotary": (C.c_int, [_VP, _I64, _I32, _I32, _I32, _I32, _I32, _I32, _VP]),
     "sat_op_cross_entropy": (C.c_int, [_VP, _I64, _VP, _I32, _I32, _VP, _VP, _I64, _VP, _VP]),
     "sat_op_adamw": (C.c_int, [_VP, _VP, _VP, _VP, _VP, _I64, C.c_double, C.c_double, C.c_double,

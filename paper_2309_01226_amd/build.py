@@ -16,7 +16,7 @@ OUT = os.path.join(PKG, "libsaturn.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
 SOURCES = ["gemm.hip", "gemm256.hip", "norm.hip", "elementwise.hip", "attention.hip", "attn256.hip", "attn_small.hip", "attn_packed.hip", "rotary_axes.hip",
-           "adamw_multi.hip", "dropout.hip", "residual_norm.hip", "conv.hip", "ops_abi.cpp", "packed_abi.cpp", "block_abi.cpp", "model.cpp", "step.cpp",
+           "adamw_multi.hip", "dropout.hip", "residual_norm.hip", "linear_xent.hip", "conv.hip", "ops_abi.cpp", "packed_abi.cpp", "block_abi.cpp", "model.cpp", "step.cpp",
            "resnet.cpp", "abi.cpp", "profile.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -134,3 +134,59 @@ extern "C" sat_status sat_op_residual_norm_bwd(const sat_residual_norm_desc* d, 
   SAT_HIP(launch_residual_norm_bwd(a, d->stream_f32 != 0, S(stream)));
   return SAT_OK;
 }
+
+// ---------------------------------------------------------------- head with cross entropy
+
+static constexpr int64_t kMaxHeadLd = 1 << 21;  // a tile's rows stay within 32-bit buffer offsets
+
+static sat_status linear_xent_sizes(const sat_linear_xent_desc* d, LinearXentArgs* out, const char* fn) {
+  SAT_CHECK_ARG(d != nullptr, "%s: null descriptor", fn);
+  SAT_CHECK_ARG(d->N >= 0 && d->N < (1 << 30) && d->V >= 1 && d->V <= (1 << 20), "%s: bad sizes N=%d V=%d (V up to 2^20)", fn,
+                d->N, d->V);
+  SAT_CHECK_ARG(d->d >= 8 && d->d <= (1 << 16) && d->d % 8 == 0, "%s: d=%d must be a multiple of 8 up to 2^16", fn, d->d);
+  SAT_CHECK_ARG(!d->accumulate || d->grad_f32, "%s: only fp32 gradients are added to", fn);
+  SAT_CHECK_ARG(!d->db || d->bias, "%s: a gradient of a bias that is not there", fn);
+  LinearXentArgs& a = *out;
+  memset(&a, 0, sizeof a);
+  a.dx = (bf16*)d->dx; a.dw = d->dw; a.db = d->db;
+  a.N = d->N; a.V = d->V; a.d = d->d;
+  a.dw_f32 = d->grad_f32 != 0;
+  a.accumulate = d->accumulate != 0;
+  return SAT_OK;
+}
+
+extern "C" sat_status sat_op_linear_xent_ws(const sat_linear_xent_desc* d, int64_t* bytes) {
+  SAT_CHECK_ARG(bytes != nullptr, "linear_xent_ws: null pointer");
+  LinearXentArgs a;
+  const sat_status st = linear_xent_sizes(d, &a, "linear_xent_ws");
+  if (st != SAT_OK) return st;
+  *bytes = linear_xent_ws(a);
+  return SAT_OK;
+}
+
+extern "C" sat_status sat_op_linear_xent(const sat_linear_xent_desc* d, void* stream) {
+  const char* fn = "linear_xent";
+  LinearXentArgs a;
+  const sat_status st = linear_xent_sizes(d, &a, fn);
+  if (st != SAT_OK) return st;
+  SAT_CHECK_ARG(d->N == 0 || (d->x && d->labels && d->row_loss && d->lse), "%s: null pointer", fn);
+  SAT_CHECK_ARG(d->w && d->inv_n && d->ws, "%s: null pointer", fn);
+  SAT_CHECK_ARG(d->ldx >= d->d && d->ldw >= d->d && d->ldx < kMaxHeadLd && d->ldw < kMaxHeadLd && d->ldx % 8 == 0 &&
+                    d->ldw % 8 == 0 && aligned(d->x, 16) && aligned(d->w, 16),
+                "%s: x and w must be 16-byte aligned with leading dimensions %% 8 == 0, at least d and below 2^21", fn);
+  SAT_CHECK_ARG(!d->dx || (d->lddx >= d->d && d->lddx < kMaxLd && d->lddx % 8 == 0 && aligned(d->dx, 16)),
+                "%s: dx must be 16-byte aligned with lddx %% 8 == 0, at least d", fn);
+  SAT_CHECK_ARG(!d->dw || (d->lddw >= d->d && d->lddw < kMaxLd && d->lddw % (d->grad_f32 ? 4 : 8) == 0 && aligned(d->dw, 16)),
+                "%s: dw must be 16-byte aligned with 16-byte aligned rows of at least d", fn);
+  SAT_CHECK_ARG(aligned(d->labels, 4) && aligned(d->bias, 4) && aligned(d->row_weight, 4) && aligned(d->row_loss, 4) &&
+                    aligned(d->lse, 4) && aligned(d->inv_n, 4) && aligned(d->db, d->grad_f32 ? 4 : 2),
+                "%s: vectors must be aligned to their elements", fn);
+  const int64_t need = linear_xent_ws(a);
+  SAT_CHECK_ARG(d->ws_bytes >= need && aligned(d->ws, 256), "%s: ws of %ld bytes, %ld needed, 256-byte aligned", fn,
+                (long)d->ws_bytes, (long)need);
+  a.x = (const bf16*)d->x; a.w = (const bf16*)d->w; a.labels = d->labels; a.bias = d->bias; a.row_weight = d->row_weight;
+  a.row_loss = d->row_loss; a.lse = d->lse; a.inv_n = d->inv_n;
+  a.ldx = d->ldx; a.ldw = d->ldw; a.lddx = d->lddx; a.lddw = d->lddw;
+  SAT_HIP(launch_linear_xent(a, d->ws, S(stream)));
+  return SAT_OK;
+}

@@ -434,6 +434,31 @@ hipError_t launch_residual_norm_bwd(ResidualNormArgs a, bool f32, hipStream_t s)
 // fp32 elements for `sums` of the five gradients that are sums over rows.
 int64_t residual_norm_ws(int T, int d, int sums);
 
+// ---------------------------------------------------------------- head with cross entropy (linear_xent.hip)
+struct LinearXentArgs {
+  const bf16* x;          // [N, ldx], rows of d
+  const bf16* w;          // [V, ldw]
+  const int* labels;
+  const float* bias;      // [V] or NULL
+  const float* row_weight;  // [N] or NULL: 1 / rows that take part
+  float *row_loss, *lse, *inv_n;
+  bf16* dx;               // gradients, each may be NULL
+  void *dw, *db;          // fp32 when dw_f32, else bf16
+  int64_t ldx, ldw, lddx, lddw;
+  int N, V, d, dw_f32, accumulate;
+  // set by the launch: a chunk's tokens, the pitch of e, and the parts of the workspace
+  int chunk;
+  int64_t lde;
+  int *meta, *idx, *pos, *lab;  // rows that take part: [0] their number; their rows, the rows' places, their labels
+  float* zlab;            // their label's logit, then its entry of dz
+  float2* part;           // [pieces][chunk]: maximum and sum, then the factor of e
+  bf16 *xc, *e;           // compact rows of x, e [V][chunk]
+  float *dbpart, *dwsum, *partial;
+};
+// d % 8 == 0, x, w, dx, dw with 16-byte aligned rows; ws of linear_xent_ws bytes, 256-byte aligned.
+hipError_t launch_linear_xent(LinearXentArgs a, void* ws, hipStream_t s);
+int64_t linear_xent_ws(LinearXentArgs a);
+
 // ---------------------------------------------------------------- ResNet (conv.hip)
 // NHWC activations ([N, H, W, C] = the matrix [N * H * W, C]).
 // col[(n Ho + i) Wo + j, (a k + b) C + c] = x[n, i s - pad + a, j s - pad + b, c]

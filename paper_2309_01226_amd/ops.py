@@ -559,3 +559,39 @@ def _boundary_ws(T, d, sums):
     need = C.c_int64()
     _lib.call("sat_op_residual_norm_bwd_ws", desc, need)
     return need.value
+
+
+# sat_linear_xent_desc's fields
+_HEAD = struct.Struct("PqPq6P" + "PqPqP" + "6iPq")
+assert _HEAD.size == C.sizeof(_lib.sat_linear_xent_desc)
+
+
+def linear_cross_entropy(x, w, labels, row_loss, lse, inv_n, *, bias=None, row_weight=None, dx=None, dw=None, db=None,
+                         accumulate=False):
+    """Softmax cross entropy of the head x w^T + bias, x [N, >= d] and w [V, d] bf16, labels int32 [N] (outside [0, V): the row
+    takes no part), without keeping the logits: row_loss and lse fp32 [N], inv_n fp32 [1].  With dx, dw or db it
+    writes the gradients of sum row_weight row_loss (row_weight fp32 [N]; None: inv_n for every row): dx bf16 [N, >= d], dw
+    [V, >= d] and db [V] both fp32 or both bf16, fp32 ones added to what is there when accumulate.  See saturn_ops.h.  The
+    workspace comes from torch's allocator, on the current stream."""
+    if w.dim() != 2:
+        raise ValueError(f"w: expected [V, d], got {tuple(w.shape)}")
+    dev, bf, f4, (V, d), N = _device(w, "w"), torch.bfloat16, torch.float32, w.shape, labels.numel()
+    f32 = (dw if dw is not None else db).dtype == f4 if dw is not None or db is not None else False
+    gt = f4 if f32 else bf
+    need = _head_ws(N, V, d, dx is not None, dw is not None, db is not None, f32, bool(accumulate))
+    ws = torch.empty(need, device=w.device, dtype=torch.uint8)
+    desc = _lib.sat_linear_xent_desc.from_buffer_copy(_HEAD.pack(
+        *_matrix(x, bf, "x", N, d, dev), *_matrix(w, bf, "w", V, d, dev), _vec(labels, torch.int32, "labels", N, dev),
+        _vec(bias, f4, "bias", V, dev), _vec(row_weight, f4, "row_weight", N, dev), _vec(row_loss, f4, "row_loss", N, dev),
+        _vec(lse, f4, "lse", N, dev), _vec(inv_n, f4, "inv_n", 1, dev), *_matrix(dx, bf, "dx", N, d, dev),
+        *_matrix(dw, gt, "dw", V, d, dev), _vec(db, gt, "db", V, dev), N, V, d, f32, bool(accumulate), 0, ws.data_ptr(), need))
+    _lib.call("sat_op_linear_xent", desc, _stream(dev))
+
+
+@functools.lru_cache(maxsize=256)
+def _head_ws(N, V, d, dx, dw, db, f32, accumulate):
+    desc = _lib.sat_linear_xent_desc(N=N, V=V, d=d, dx=dx or None, dw=dw or None, db=db or None, bias=db or None, grad_f32=f32,
+                                     accumulate=accumulate)
+    need = C.c_int64()
+    _lib.call("sat_op_linear_xent_ws", desc, need)
+    return need.value

@@ -132,3 +132,54 @@ def residual_bwd(dy, dh, y, f, st, o, adds):
         du, odu = g, og
     out["df"] = (du, odu)
     return out
+
+
+# ---------------------------------------------------------------- head with cross entropy
+
+def head(x, w, labels, bias=None, weight=None, grads=True):
+    """{name: (value, bound)} of the linear head's cross entropy, torch tensors in 64 bits on any device (x, w, bias
+    and weight 64-bit, labels int64; rows whose label is outside the vocabulary take no part).
+
+    Bounds.  A logit is a sum of d products in fp32, at most d + 2 roundings of E each (twice that if they are not to
+    the nearest).  exp2 of a product by log2 e: 2^-22 and 4 E |z - m|; a row's sum and its joining: at most 64 + 2
+    in a lane pair, 32 + 16 pieces, the pieces' factors: 256 E in all.  The gradients' operand is rounded to bf16 twice
+    (2^-8 each), the label's once; a product's sum of n terms is off by (n + 2) 2 E of their magnitudes."""
+    import torch
+    N, (V, d) = len(labels), w.shape
+    live = (labels >= 0) & (labels < V)
+    at = torch.where(live, labels, 0)[:, None]
+    z = x @ w.T
+    oz = 2 * E * (d + 2) * (x.abs() @ w.abs().T)
+    if bias is not None:
+        z = z + bias
+        oz = oz + E * torch.where(bias.isinf(), 0.0, bias.abs()) + E * torch.where(z.isinf(), 0.0, z.abs())
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    empty = lse.isinf()
+    p = torch.where(empty, 0.0, torch.exp(z - torch.where(empty, 0.0, lse)))
+    far = torch.where(z.isinf(), 0.0, (z - z.amax(1, keepdim=True)).abs())
+    op = oz + 4 * E * far + 2.0 ** -22       # relative error of exp(z - m)
+    ol = (p * op).sum(1, keepdim=True) + 256 * E  # of lse
+    zl, ozl = z.gather(1, at), oz.gather(1, at)
+    use = live & ~empty[:, 0]
+    out = {}
+    loss = torch.where(use, (lse - zl)[:, 0], 0.0)
+    top = (z.amax(1, keepdim=True) - zl).abs()
+    out["lse"] = (torch.where(live, lse[:, 0], 0.0), (ol + 4 * E * torch.where(empty, 0.0, lse.abs()))[:, 0])
+    out["row_loss"] = (loss, torch.where(use, (ol + ozl + 4 * E * top)[:, 0], 0.0) + 4 * E * loss.abs())
+    n = int(live.sum())
+    out["inv_n"] = (torch.tensor([1 / max(n, 1)], dtype=torch.float64, device=x.device), torch.tensor([2 * E], device=x.device))
+    if not grads:
+        return out
+    c = (torch.full((N,), 1 / max(n, 1), dtype=torch.float64, device=x.device) if weight is None else weight) * use
+    hot = torch.zeros_like(p).scatter_(1, at, 1.0)
+    dz = c[:, None] * (p - hot)
+    soft = c.abs()[:, None] * p * (op + ol + 8 * E)  # of c p before roundings
+    two = torch.where(hot > 0, 2.0 ** -8 * dz.abs(), 2.0 ** -7 * 1.01 * dz.abs())
+    odz = (soft + 4 * E * (c.abs()[:, None] * hot)) * 1.01 + two
+    tiny = 2.0 ** -126
+    total = lambda a, b, oa, k: (a @ b, oa @ b.abs() + 2 * E * (k + 2) * (a.abs() @ b.abs()) + tiny)  # noqa: E731
+    out["dx"] = total(dz, w, odz, V)
+    out["dw"] = total(dz.T.contiguous(), x, odz.T.contiguous(), N)
+    odb = soft * 1.01 + 4 * E * (c.abs()[:, None] * hot) + torch.where(hot > 0, 0.0, 2.0 ** -8 * 1.01 * dz.abs())
+    out["db"] = (dz.sum(0), odb.sum(0) + E * (N + 2) * dz.abs().sum(0) + tiny)
+    return out

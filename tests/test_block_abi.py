@@ -137,3 +137,66 @@ def test_residual_norm_gradients(pre, post):
     for name in ("gate", "g_pre", "b_pre", "g_post", "b_post"):
         if o[name] is not None:
             near("d" + name, lambda i, s: value(x, f, {**o, name: moved(o[name], i, s)}))
+
+
+# ---------------------------------------------------------------- head with cross entropy
+
+def _head(**kw):
+    d = dict(x=P, ldx=64, w=2 * P, ldw=64, labels=3 * P, bias=4 * P, row_weight=None, row_loss=5 * P, lse=6 * P, inv_n=7 * P, dx=8 * P, lddx=64,
+             dw=9 * P, lddw=64, db=10 * P, N=9, V=100, d=64, grad_f32=0, accumulate=0, ws=11 * P, ws_bytes=1 << 40)
+    d.update(kw)
+    return _L().sat_linear_xent_desc(**d)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(x=None), dict(w=None), dict(labels=None), dict(row_loss=None), dict(lse=None), dict(inv_n=None), dict(ws=None), dict(ws_bytes=1000),
+    dict(ws=11 * P + 16), dict(N=-1), dict(N=1 << 30), dict(V=0), dict(V=(1 << 20) + 1), dict(d=0), dict(d=60, ldx=64), dict(d=(1 << 16) + 8),
+    dict(ldx=56), dict(ldw=56), dict(ldx=68), dict(ldw=1 << 21), dict(x=P + 8), dict(w=P + 2), dict(lddx=56), dict(lddx=68), dict(dx=P + 8),
+    dict(lddw=56), dict(lddw=68), dict(dw=P + 8), dict(grad_f32=1, lddw=66), dict(accumulate=1), dict(bias=None), dict(bias=P + 2),
+    dict(labels=P + 1), dict(row_weight=P + 2), dict(lse=P + 1), dict(db=P + 1), dict(db=P + 2, grad_f32=1), dict(inv_n=P + 3),
+])
+def test_head_refusals(bad):
+    _refused("sat_op_linear_xent", C.byref(_head(**bad)), None, word="linear_xent")
+
+
+def test_head_null_and_ws():
+    L = _L()
+    n = C.c_int64()
+    _refused("sat_op_linear_xent", None, None, word="null")
+    _refused("sat_op_linear_xent_ws", None, C.byref(n), word="null")
+    _refused("sat_op_linear_xent_ws", C.byref(_head()), None, word="null")
+
+    def ws(**kw):
+        assert L.lib().sat_op_linear_xent_ws(C.byref(L.sat_linear_xent_desc(**kw)), C.byref(n)) == 0
+        return n.value
+
+    # scoring keeps nothing of the size of the logits; the gradients what the header says
+    score = ws(N=4096, V=50400, d=4096)
+    assert score < 2 * 4096 * 4096 + (1 << 24)
+    for N in (4096, 16384, 100000):
+        x = 2 * N * 4096
+        small = 400 * 8 * 16384 + 24 * N + (N // 512 + 2) * 4 * 50400 + (1 << 20)
+        assert ws(N=N, V=50400, d=4096, dx=P, dw=P, bias=P, db=P) <= (1 << 29) + x + (1 << 27) + 4 * 50400 * 4096 + small
+        assert ws(N=N, V=50400, d=4096, dx=P, dw=P, grad_f32=1) <= (1 << 29) + x + (1 << 27) + small
+    assert ws(N=0, V=100, d=64, dw=P) > 0
+
+
+def test_head_gradients():
+    """The reference's gradients are those of its own loss, by central differences."""
+    import torch
+    g = torch.Generator().manual_seed(1)
+    r = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)  # noqa: E731
+    x, w, b, c = r(6, 5), r(9, 5), r(9), r(6)
+    labels = torch.tensor([0, 8, -1, 3, 9, 3])
+    got = R.head(x, w, labels, b, c)
+    value = lambda: (c * R.head(x, w, labels, b, c, False)["row_loss"][0]).sum().item()  # noqa: E731
+    for t, k in ((x, "dx"), (w, "dw"), (b, "db")):
+        for i in range(t.numel()):
+            old, e = t.view(-1)[i].item(), 1e-5
+            t.view(-1)[i] = old + e
+            up = value()
+            t.view(-1)[i] = old - e
+            down = value()
+            t.view(-1)[i] = old
+            assert abs((up - down) / (2 * e) - got[k][0].reshape(-1)[i].item()) < 1e-8, (k, i)
+    assert not got["dx"][0][2].any() and not got["dx"][0][4].any() and got["row_loss"][0][2] == 0
