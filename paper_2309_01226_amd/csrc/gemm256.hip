@@ -457,11 +457,11 @@ __global__ __launch_bounds__(NT, 1) void gemm256_kernel(GemmArgs p) {
   const int wm = wave >> 1, wn = wave & 1;
 
   // an operand's resource for the K-tile at k0 (K-contiguous: for all of them)
-  auto rsA = [&](int k0) {
+  auto rsA = [&](int, int k0) {
     const bf16* q = p.A + (AL == LAY_K ? (long)m0 * p.lda + kb : (long)(kb + k0) * p.lda + m0);
     return __builtin_amdgcn_make_buffer_rsrc((void*)q, (short)0, 0x7FFFFFFF, 0x00020000);
   };
-  auto rsB = [&](int k0) {
+  auto rsB = [&](int, int k0) {
     const bf16* q = p.B + (BL == LAY_K ? (long)n0 * p.ldb + kb : (long)(kb + k0) * p.ldb + n0);
     return __builtin_amdgcn_make_buffer_rsrc((void*)q, (short)0, 0x7FFFFFFF, 0x00020000);
   };
@@ -475,7 +475,16 @@ __global__ __launch_bounds__(NT, 1) void gemm256_kernel(GemmArgs p) {
   FB.init(wn * 128);
 
   floatx16 acc[4][4];
-  gemm256_loop<AL, BL>(acc, smem, la, lb, FA, FB, rsA, rsB, K, wave);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  const int nk = (K + BK - 1) / BK;
+  // k offset of tile t; tiles past the last one copy zeros (every chunk at or past K)
+  auto kof = [&](int t) { return t < nk ? t * BK : K; };
+  gemm256_loop<AL, BL>(acc, smem, la, lb, FA, FB, rsA, rsB, nk, kof, K, wave);
   if constexpr (EPI == EPI_ADAMW) {
     epilogue_adamw(p, acc, reinterpret_cast<float*>(smem), m0, n0, wave, lane);
   } else if constexpr (EPI == EPI_F32) {

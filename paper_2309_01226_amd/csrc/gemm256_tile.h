@@ -184,34 +184,25 @@ __device__ __forceinline__ void kstep_ring(floatx16 (&acc)[4][4], const bf16x8 (
   }
 }
 
-// The loop: acc = the tile's product over k in [0, K).  la, lb, FA and FB are initialised, rsA(k0) and rsB(k0)
-// give an operand's resource for the K-tile at k0 (Loader::issue).  Afterwards no copy is in flight and every
-// wave is done with smem (5 * OPE elements).
-template <int AL, int BL, class RA, class RB>
+// The loop: acc += the tile's product over nk K-tiles.  la, lb, FA and FB are initialised; K-tile t begins at
+// k = kof(t), whose operands' resources are rsA(t, k) and rsB(t, k) (Loader::issue); for t >= nk (two past the end
+// are asked for) kof gives K, the end of k.  Afterwards no copy is in flight and every wave is done with
+// smem (5 * OPE elements).
+template <int AL, int BL, class KO, class RA, class RB>
 __device__ __forceinline__ void gemm256_loop(floatx16 (&acc)[4][4], bf16* smem, const Loader<AL>& la,
                                              const Loader<BL>& lb, const Frags<AL>& FA, const Frags<BL>& FB,
-                                             RA rsA, RB rsB, int K, int wave) {
+                                             RA rsA, RB rsB, int nk, KO kof, int K, int wave) {
   constexpr int NI = Loader<LAY_K>::NI;
   static_assert(5 * OPE * 2 <= 163840 && BK == 64 && NI == 8, "LDS budget / copies");
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-
   auto sA = [&](int t) { return smem + (t % 3) * OPE; };
   auto sB = [&](int t) { return smem + (3 + (t & 1)) * OPE; };
-  const int nk = (K + BK - 1) / BK;
-  // k offset of tile t; tiles past the last one copy zeros (every chunk at or past K)
-  auto kof = [&](int t) { return t < nk ? t * BK : K; };
   // tile 0 resident; A_1 and the first half of B_1 in flight
-  la.issue(rsA(0), 0, K, sA(0), wave);
-  lb.issue(rsB(0), 0, K, sB(0), wave);
+  la.issue(rsA(0, kof(0)), kof(0), K, sA(0), wave);
+  lb.issue(rsB(0, kof(0)), kof(0), K, sB(0), wave);
   wait_vm_lgkm0<0>();
   cta_barrier();
-  la.issue(rsA(kof(1)), kof(1), K, sA(1), wave);
-  __amdgpu_buffer_rsrc_t rB1 = rsB(kof(1));  // of B_{t+1}
+  la.issue(rsA(1, kof(1)), kof(1), K, sA(1), wave);
+  __amdgpu_buffer_rsrc_t rB1 = rsB(1, kof(1));  // of B_{t+1}
   lb.template issue<0, 4>(rB1, kof(1), K, sB(1), wave);
   bf16x8 f0a[4], f0b[4], f1a[4], f1b[4];
 #pragma unroll
@@ -223,7 +214,7 @@ __device__ __forceinline__ void gemm256_loop(floatx16 (&acc)[4][4], bf16* smem, 
     bf16* a2 = sA(t + 2);
     bf16* b2 = sB(t + 2);
     const int k1 = kof(t + 1), k2 = kof(t + 2);
-    const __amdgpu_buffer_rsrc_t rA2 = rsA(k2), rB2 = rsB(k2);
+    const __amdgpu_buffer_rsrc_t rA2 = rsA(t + 2, k2), rB2 = rsB(t + 2, k2);
     __builtin_amdgcn_sched_barrier(0);
     kstep_ring(acc, f0a, f0b, f1a, f1b, FA, FB, a, b, 1, [&](int c) {
       switch (c) {
