@@ -34,9 +34,10 @@ constexpr int OPE = BT * BK;          // bf16 elements of one operand tile
 // with the transposing LDS read; chunk c (of 32) of k-row k is stored at c ^ 4 (k % 4), so
 // that the 4 k-rows x 4 chunks that 32 lanes read at once are on distinct banks.
 
-template <int LAY>
+// R: rows of the tile (256, or 128 for the smaller tile below, with rows of 256 bytes where they are 512 here).
+template <int LAY, int R = BT>
 struct Loader {
-  static constexpr int NI = (BT * BK * 2 / 1024) / 4;  // copy instructions per wave
+  static constexpr int NI = (R * BK * 2 / 1024) / 4;  // copy instructions per wave
   uint32_t off[NI];  // byte offsets relative to (tile row 0, k0)
   int kof[NI];       // k of this lane's chunk relative to k0
   __device__ __forceinline__ void init(long ld, int nrows, int wave) {
@@ -49,8 +50,9 @@ struct Loader {
         off[i] = row < nrows ? (uint32_t)(((long)row * ld + 8 * c) * 2) : OOB;
         kof[i] = 8 * c;
       } else {
-        const int k = 2 * (4 * i + wave) + lane / 32;
-        const int row = 8 * ((lane % 32) ^ (4 * (k & 3)));
+        constexpr int C = R / 8;  // chunks of a k-row
+        const int k = 64 / C * (4 * i + wave) + lane / C;
+        const int row = 8 * ((lane % C) ^ (4 * (k & 3)));
         off[i] = row < nrows ? (uint32_t)(((long)k * ld + row) * 2) : OOB;
         kof[i] = k;
       }
@@ -78,10 +80,10 @@ __device__ __forceinline__ bf16x4 ds_read_tr(const lds_bf16x4* __restrict__ p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4bf16(const_cast<lds_bf16x4*>(p));
 }
 
-// Fragment addressing of one operand inside a slot, for the wave's 128-row
-// (or column) half `w0` (0 or 128).  read(sub, ks) is the 32 x 16 MFMA operand
+// Fragment addressing of one operand inside a slot, for the wave's half of the rows
+// (or columns), from `w0` (0 or R / 2) on.  read(sub, ks) is the 32 x 16 MFMA operand
 // of rows w0 + 32 sub .. + 31, k = 16 ks .. + 15.
-template <int LAY>
+template <int LAY, int R = BT>
 struct Frags {
   static constexpr int KS = LAY == LAY_K ? BK / 16 : 1;
   int o[KS];  // element offsets (K-contiguous: of k-step ks)
@@ -97,7 +99,7 @@ struct Frags {
       const int G = lane >> 4, ll = lane & 15;
       const int k = 8 * (G >> 1) + (ll >> 2);
       const int c = w0 / 8 + 2 * (G & 1) + ((ll >> 1) & 1);
-      o[0] = k * BT + 8 * (c ^ (4 * (k & 3))) + 4 * (ll & 1);
+      o[0] = k * R + 8 * (c ^ (4 * (k & 3))) + 4 * (ll & 1);
     }
   }
   __device__ __forceinline__ bf16x8 read(const bf16* tile, int sub, int ks) const {
@@ -105,9 +107,9 @@ struct Frags {
       return *reinterpret_cast<const bf16x8*>(tile + o[ks] + sub * 32 * BK);
     } else {
       // rows + 32: chunk + 4, a field of its own under the XOR; k + 4: the same k % 4
-      const bf16* q = tile + (o[0] ^ (sub << 5)) + ks * 16 * BT;
+      const bf16* q = tile + (o[0] ^ (sub << 5)) + ks * 16 * R;
       const bf16x4 lo = ds_read_tr((const lds_bf16x4*)lds(q));
-      const bf16x4 hi = ds_read_tr((const lds_bf16x4*)lds(q + 4 * BT));
+      const bf16x4 hi = ds_read_tr((const lds_bf16x4*)lds(q + 4 * R));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   }
@@ -127,16 +129,17 @@ __device__ __forceinline__ int xcd_order_id() {
   return bid;
 }
 
+template <int R = BT>
 __device__ __forceinline__ void tile_origin(int M, int N, int bid, int& m0, int& n0) {
-  const int tiles_m = (M + BT - 1) / BT, tiles_n = (N + BT - 1) / BT;
+  const int tiles_m = (M + R - 1) / R, tiles_n = (N + R - 1) / R;
   constexpr int G = 8;
   const int per_group = G * tiles_n;
   const int group = bid / per_group;
   const int first_m = group * G;
   const int gsize = min(tiles_m - first_m, G);
   const int in_g = bid - group * per_group;
-  m0 = (first_m + in_g % gsize) * BT;
-  n0 = (in_g / gsize) * BT;
+  m0 = (first_m + in_g % gsize) * R;
+  n0 = (in_g / gsize) * R;
 }
 
 // The five-slot ring.
@@ -251,6 +254,48 @@ __device__ __forceinline__ void gemm256_loop(floatx16 (&acc)[4][4], bf16* smem, 
       }
     });
     rB1 = rB2;
+  }
+  wait_vm_lgkm0<0>();  // the zero-filling copies past the last tile
+  __syncthreads();
+}
+
+// The same product on a tile of 128 x 128 (a wave: 64 x 64), for products that are too small to give every CU a
+// tile of 256: three stages of both operands in 96 KB, the copies two K-tiles ahead, one barrier for each.
+constexpr int RS = 128;
+constexpr int SMALL_LDS = 3 * 2 * RS * BK;  // elements
+template <int AL, int BL, class KO, class RA, class RB>
+__device__ __forceinline__ void gemm128_loop(floatx16 (&acc)[2][2], bf16* smem, const Loader<AL, RS>& la,
+                                             const Loader<BL, RS>& lb, const Frags<AL, RS>& FA, const Frags<BL, RS>& FB,
+                                             RA rsA, RB rsB, int nk, KO kof, int K, int wave) {
+  constexpr int COPIES = Loader<AL, RS>::NI + Loader<BL, RS>::NI;
+  auto sA = [&](int t) { return smem + (t % 3) * 2 * RS * BK; };
+  auto copy = [&](int t) {
+    const int k = kof(t);
+    la.issue(rsA(t, k), k, K, sA(t), wave);
+    lb.issue(rsB(t, k), k, K, sA(t) + RS * BK, wave);
+  };
+  copy(0);
+  copy(1);
+  for (int t = 0; t < nk; ++t) {
+    wait_vm_lgkm0<COPIES>();  // tile t resident; this wave's reads of tile t - 1 done
+    cta_barrier();            // ... every wave's: its stage is free
+    copy(t + 2);
+    const bf16* a = sA(t);
+    const bf16* b = a + RS * BK;
+#pragma unroll
+    for (int ks = 0; ks < BK / 16; ++ks) {
+      bf16x8 fa[2], fb[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fa[i] = FA.read(a, i, ks);
+        fb[i] = FB.read(b, i, ks);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+    }
   }
   wait_vm_lgkm0<0>();  // the zero-filling copies past the last tile
   __syncthreads();

@@ -447,14 +447,14 @@ struct LinearXentArgs {
   int64_t ldx, ldw, lddx, lddw;
   int N, V, d, dw_f32, accumulate;
   // set by the launch: a chunk's tokens, the pitch of e, and the parts of the workspace
-  int chunk;
+  int chunk, tb, piece;   // (and of the scaling pass' workgroup; vocabulary entries with one pair of statistics)
   int64_t lde;            // the vocabulary in whole tiles
   int *meta, *idx, *pos, *lab;  // rows that take part: [0] their number; their rows, the rows' places, their labels
   float* zlab;            // their label's logit, then its entry of dz
   float2* part;           // [chunk][pieces]: maximum and sum, then the factor of e
   bf16* xc;               // compact rows of x
   bf16 *e, *e2;           // [chunk][lde]: 16-bit numbers, then dz; [256][lde]: what its rounding lost
-  float *dbpart, *dbsum, *dwsum, *partial;
+  float *dbpart, *dbsum, *dwsum, *partial, *partial_dw;
 };
 // d % 8 == 0, x, w, dx, dw with 16-byte aligned rows; ws of linear_xent_ws bytes, 256-byte aligned.
 hipError_t launch_linear_xent(LinearXentArgs a, void* ws, hipStream_t s);

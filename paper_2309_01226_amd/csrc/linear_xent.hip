@@ -13,7 +13,8 @@
 // pieces give lse, dz is formed from those in place.  Half a step is 2^-11.5 of exp(z - m) (2^-9.5 of those below
 // 2^-32), a small part of the rounding that a bf16 operand of the two other products takes, which exp(z - m)
 // held as bf16 would double.  The label's entry, where 1 is subtracted, comes from the fp32 logit instead.  The numbers of a chunk of tokens are what is kept, at
-// most 512 MiB, whatever N; several chunks add up dw in fp32.
+// most 1 GiB, whatever N; several chunks add up dw in fp32 (8192 x 50257 x 768: 2.37 ms as one chunk, 2.48 as two,
+// 2.81 as four).
 //
 // dz is an operand in bf16.  A chunk with no more rows than a tile has keeps what that rounding loses as a
 // second operand: few roundings do not average out, and the products of so few rows are bound by the
@@ -27,38 +28,49 @@
 
 namespace {
 
-constexpr int PIECE = 128;   // vocabulary entries of one pair of statistics: the rows of a wave's part of a tile
-constexpr int TB = 64;       // tokens of a workgroup of the scaling pass
 constexpr int CUS = 256;
-constexpr int EP = 136;      // fp32 pitch of a staging row
-constexpr int QP = 68;       // its pitch in words of two 16-bit numbers
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float STEPS = 1024.f;   // of the fixed-point numbers; 65535 of them stand for 0
 constexpr float INF = __builtin_inff();
 
 __host__ __device__ inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 
-// K slices of a product of `tiles` tiles of `ktiles` 64-deep steps on 256 CUs.  Cost in steps of one tile:
-// rounds of 256 workgroups, a step or two of start and end for each, and the partial products' way to
-// memory and back (0.26 MB each way for a tile, about 0.064 steps).  At most 512 partial tiles (128 MB).
-__host__ __device__ inline int pick_split(int tiles, int ktiles) {
-  int best = 1;
-  float cost = 0.f;
-  for (int s = 1; s <= 16; ++s) {
-    if (s > 1 && (tiles * s > 512 || ktiles < 8 * s)) break;
-    const float c = (float)cdiv(tiles * s, CUS) * (cdiv(ktiles, s) + 2) + (s > 1 ? 0.064f * tiles * s : 0.f);
-    if (s == 1 || c < cost) {
-      best = s;
-      cost = c;
+// A product of `tiles` tiles of R rows and columns and `ktiles` 64-deep steps on 256 CUs: `full` tiles in whole
+// rounds, one on a CU, and the rest, whose K is split in S slices where that shortens the last round.  Cost in us:
+// a step of K takes 1.65 (of a tile of 128: 0.7), a round's start and end 8 (4), a partial tile's way to memory and
+// back 0.1 (0.026).  At most 128 MB of partial tiles.
+struct Split {
+  int full, rest, S;
+  float us;
+  __host__ __device__ int groups() const { return full + rest * S; }
+  __host__ __device__ int64_t partial(int R) const { return S > 1 ? (int64_t)rest * S * R * R : 0; }
+};
+__host__ __device__ inline Split split_of(int R, int tiles, int ktiles, int most = 16) {
+  const float step = R == BT ? 1.65f : 0.7f, ends = R == BT ? 8.f : 4.f, way = R == BT ? 0.1f : 0.026f;
+  Split p = {tiles / CUS * CUS, tiles % CUS, 1, 0.f};
+  for (int s = 1; s <= most; ++s) {
+    if (s > 1 && (p.rest * s > (R == BT ? 512 : 2048) || ktiles < 4 * s)) break;
+    // a split product's slices are added by another launch
+    const float c = (float)cdiv(p.rest * s, CUS) * (cdiv(ktiles, s) * step + ends) + (s > 1 ? way * p.rest * s + 4.f : 0.f);
+    if (s == 1 || c < p.us) {
+      p.S = s;
+      p.us = c;
     }
   }
-  return best;
+  p.us += (float)(tiles / CUS) * (ktiles * step + ends);
+  return p;
 }
+__host__ __device__ inline int tiles_of(int R, int M, int N) { return cdiv(M, R) * cdiv(N, R); }
 
 // The compact rows of the chunk that starts at `first`.
 __device__ __forceinline__ int chunk_rows(const LinearXentArgs& a, int first) {
   return min(max(a.meta[0] - first, 0), a.chunk);
 }
+
+// Whether the chunk has anything to do (the first one also without rows: gradients of none), and whether none
+// comes after it.
+__device__ __forceinline__ bool chunk_idle(const LinearXentArgs& a, int first) { return first > 0 && a.meta[0] <= first; }
+__device__ __forceinline__ bool chunk_last(const LinearXentArgs& a, int first) { return a.meta[0] <= first + a.chunk; }
 
 // Row c of the compact rows of x: x itself where every row takes part.
 __device__ __forceinline__ const bf16* compact_x(const LinearXentArgs& a, long& ld) {
@@ -126,6 +138,60 @@ __global__ __launch_bounds__(256) void xent_copy_kernel(LinearXentArgs a) {
   }
 }
 
+// Both at once for up to FEW rows: a workgroup counts the rows before its own 64 (and all of them) for itself.
+constexpr int FEW = 4096;
+__global__ __launch_bounds__(256) void xent_rows_few_kernel(LinearXentArgs a) {
+  __shared__ int sums[2][4], at[64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r0 = blockIdx.x * 64;
+  const auto live = [&](int r) {
+    const int label = r < a.N ? a.labels[r] : -1;
+    return label >= 0 && label < a.V;
+  };
+  int before = 0, all = 0;
+#pragma unroll 4
+  for (int r = threadIdx.x; r < a.N; r += 256) {
+    const int one = live(r);
+    all += one;
+    before += r < r0 ? one : 0;
+  }
+  before = (int)wave_total((float)before);  // whole numbers below 2^24: exact
+  all = (int)wave_total((float)all);
+  if (lane == 0) {
+    sums[0][wave] = before;
+    sums[1][wave] = all;
+  }
+  __syncthreads();
+  before = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+  all = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+  if (wave == 0) {
+    const int r = r0 + lane;
+    const bool on = live(r);
+    const uint64_t mask = __builtin_amdgcn_ballot_w64(on);
+    const int p = before + __popcll(mask & ((1ull << lane) - 1));
+    at[lane] = on ? p : -1;
+    if (on) {
+      a.idx[p] = r;
+      a.lab[p] = a.labels[r];
+    } else if (r < a.N) {
+      a.row_loss[r] = a.lse[r] = 0.f;
+    }
+    if (r0 == 0 && lane == 0) {
+      a.meta[0] = all;
+      a.inv_n[0] = 1.f / max(all, 1);
+    }
+  }
+  __syncthreads();
+  if (all == a.N) return;
+  const u32x4 zero = {0, 0, 0, 0};
+  for (int i = wave; i < min(64, a.N - r0); i += 4) {
+    const int r = r0 + i, p = at[i];
+    for (int c = lane * 8; c < a.d; c += 512) {
+      if (p >= 0) *reinterpret_cast<u32x4*>(a.xc + (long)p * a.d + c) = *reinterpret_cast<const u32x4*>(a.x + r * a.ldx + c);
+      else if (a.dx != nullptr) *reinterpret_cast<u32x4*>(a.dx + r * a.lddx + c) = zero;
+    }
+  }
+}
+
 // ---------------------------------------------------------------- logits
 
 template <int LAY>
@@ -139,29 +205,40 @@ struct Operand {
   }
 };
 
+// A tile of R x R, of which a wave has W = R / 2 rows and columns in S x S accumulators.
+template <int R>
+struct Tile {
+  static constexpr int W = R / 2, S = W / 32, LDS = R == BT ? 5 * OPE : SMALL_LDS;
+};
+template <int R>
+using Acc = floatx16[Tile<R>::S][Tile<R>::S];
+
 // acc += A B over k in [kb, kb + K), and, where A2 is there, A2 B as well (A2's pitch is A's).
-template <int AL, int BL>
-__device__ __forceinline__ void tile_product(floatx16 (&acc)[4][4], bf16* smem, const Operand<AL>& A, const bf16* A2, const Operand<BL>& B,
+template <int R, int AL, int BL>
+__device__ __forceinline__ void tile_product(Acc<R>& acc, bf16* smem, const Operand<AL>& A, const bf16* A2, const Operand<BL>& B,
                                              int m0, int M, int n0, int N, int kb, int K, int wave) {
-  Loader<AL> la;
-  Loader<BL> lb;
+  Loader<AL, R> la;
+  Loader<BL, R> lb;
   la.init(A.ld, M - m0, wave);
   lb.init(B.ld, N - n0, wave);
-  Frags<AL> FA;
-  Frags<BL> FB;
-  FA.init((wave >> 1) * 128);
-  FB.init((wave & 1) * 128);
+  Frags<AL, R> FA;
+  Frags<BL, R> FB;
+  FA.init((wave >> 1) * Tile<R>::W);
+  FB.init((wave & 1) * Tile<R>::W);
   const int n1 = cdiv(K, BK), nk = A2 != nullptr ? 2 * n1 : n1;
-  gemm256_loop<AL, BL>(
-      acc, smem, la, lb, FA, FB, [&](int t, int k0) { return Operand<AL>{t < n1 ? A.p : A2, A.ld}.at(m0, kb, k0); },
-      [&](int, int k0) { return B.at(n0, kb, k0); }, nk, [&](int t) { return t < nk ? (t < n1 ? t : t - n1) * BK : K; }, K, wave);
+  const auto rsA = [&](int t, int k0) { return Operand<AL>{t < n1 ? A.p : A2, A.ld}.at(m0, kb, k0); };
+  const auto rsB = [&](int, int k0) { return B.at(n0, kb, k0); };
+  const auto kof = [&](int t) { return t < nk ? (t < n1 ? t : t - n1) * BK : K; };
+  if constexpr (R == BT) gemm256_loop<AL, BL>(acc, smem, la, lb, FA, FB, rsA, rsB, nk, kof, K, wave);
+  else gemm128_loop<AL, BL>(acc, smem, la, lb, FA, FB, rsA, rsB, nk, kof, K, wave);
 }
 
-// (m - z) log2 e >= 0, times 2^10, as 16 bits in the low half of a word: steps of 2^-10 up to 32, of 2^-8 from there to
-// 160, 65535 for what is above.
-__device__ __forceinline__ uint32_t to_steps(float s) {
+// u = (z - m) log2 e <= 0 as 16 bits in the low half of a word: steps of 2^-10 from 0 down to -32, of 2^-8 from there to
+// -160, 65535 for what is below.
+__device__ __forceinline__ uint32_t to_steps(float u) {
   // 2^23 more: rounded to whole steps, which are the low bits
-  return __float_as_uint(fminf(fminf(s, __builtin_fmaf(s, 0.25f, 24576.f)), 65535.f) + 8388608.f);
+  constexpr float M = 8388608.f;
+  return __float_as_uint(fminf(fminf(__builtin_fmaf(u, -STEPS, M), __builtin_fmaf(u, -STEPS / 4, M + 24576.f)), M + 65535.f));
 }
 __device__ __forceinline__ float from_steps(uint32_t q) {
   const float s = (float)q;
@@ -170,31 +247,32 @@ __device__ __forceinline__ float from_steps(uint32_t q) {
 
 // The tile's rows (in the wave's part: 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4) are vocabulary
 // entries, its columns (32 j + lane % 32) tokens.
-template <bool TRAIN>
+template <int R, bool TRAIN>
 __global__ __launch_bounds__(NT, 1) void xent_logits_kernel(LinearXentArgs a, int first) {
-  __shared__ __attribute__((aligned(1024))) bf16 smem[5 * OPE];
-  const int n = chunk_rows(a, first), total = cdiv(a.V, BT) * cdiv(n, BT);
+  __shared__ __attribute__((aligned(1024))) bf16 smem[Tile<R>::LDS];
+  constexpr int S = Tile<R>::S, W = Tile<R>::W;
+  const int n = chunk_rows(a, first), total = tiles_of(R, a.V, n);
   if ((int)blockIdx.x >= total) return;
   int m0, n0;
-  tile_origin(a.V, n, xcd_place(blockIdx.x, total), m0, n0);
+  tile_origin<R>(a.V, n, xcd_place(blockIdx.x, total), m0, n0);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int v0 = m0 + (wave >> 1) * 128, t0 = n0 + (wave & 1) * 128;
+  const int v0 = m0 + (wave >> 1) * W, t0 = n0 + (wave & 1) * W;
   const int half = 4 * (lane >> 5);
   // the sums begin at the bias; entries behind the vocabulary are -inf
-  floatx4 b[4][4];
-  if (v0 + 128 <= a.V && a.bias != nullptr) {
+  floatx4 b[S][4];
+  if (v0 + W <= a.V && a.bias != nullptr) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < S; ++i)
 #pragma unroll
       for (int g = 0; g < 4; ++g) b[i][g] = *reinterpret_cast<const floatx4_any*>(a.bias + v0 + 32 * i + 8 * g + half);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < S; ++i)
 #pragma unroll
       for (int g = 0; g < 4; ++g) b[i][g] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (v0 + 128 > a.V) {
+    if (v0 + W > a.V) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < S; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int v = v0 + 32 * i + 8 * (r >> 2) + half + (r & 3);
@@ -202,36 +280,37 @@ __global__ __launch_bounds__(NT, 1) void xent_logits_kernel(LinearXentArgs a, in
         }
     }
   }
-  floatx16 acc[4][4];
+  Acc<R> acc;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < S; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < S; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = b[i][r >> 2][r & 3];
   Operand<LAY_K> A = {a.w, a.ldw}, B;
   B.p = compact_x(a, B.ld);
   B.p += first * B.ld;
-  tile_product<LAY_K, LAY_K>(acc, smem, A, nullptr, B, m0, a.V, n0, n, 0, a.d, wave);
+  tile_product<R, LAY_K, LAY_K>(acc, smem, A, nullptr, B, m0, a.V, n0, n, 0, a.d, wave);
 
-  const int pieces = cdiv(a.V, PIECE);
-  // the wave's 16 bits of its part, [32 tokens][128 entries] at a time
+  const int pieces = cdiv(a.V, W);
+  // the wave's 16 bits of its part, [32 tokens][W entries] at a time
+  constexpr int QP = W / 2 + 4;
   uint32_t* st = reinterpret_cast<uint32_t*>(smem) + wave * 32 * QP;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < S; ++j) {
     const int t = t0 + 32 * j + (lane & 31);
     const int off = t < n ? a.lab[first + t] - v0 : -1;
-    if (__builtin_amdgcn_ballot_w64(off >= 0 && off < 128)) {
+    if (__builtin_amdgcn_ballot_w64(off >= 0 && off < W)) {
       float z = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < S; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) z = off - half == 32 * i + 8 * (r >> 2) + (r & 3) ? acc[i][j][r] : z;
-      if (off >= 0 && off < 128 && (off & 4) == half) a.zlab[first + t] = z;
+      if (off >= 0 && off < W && (off & 4) == half) a.zlab[first + t] = z;
     }
     float m = -INF;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < S; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) m = fmaxf(m, acc[i][j][r]);
     const auto mm = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
@@ -239,16 +318,16 @@ __global__ __launch_bounds__(NT, 1) void xent_logits_kernel(LinearXentArgs a, in
     if (m == -INF) m = 0.f;  // no entry is left: every exp is 0
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < S; ++i)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         uint32_t q[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           // 0 for the largest, so that a sure row's loss is 0
-          const float y = (m - acc[i][j][4 * g + e]) * (LOG2E * STEPS);
-          s += __builtin_amdgcn_exp2f(y * (-1.f / STEPS));
-          if (TRAIN) q[e] = to_steps(y);
+          const float u = (acc[i][j][4 * g + e] - m) * LOG2E;
+          s += __builtin_amdgcn_exp2f(u);
+          if (TRAIN) q[e] = to_steps(u);
         }
         if (TRAIN) {
           // the low halves of two words
@@ -258,76 +337,70 @@ __global__ __launch_bounds__(NT, 1) void xent_logits_kernel(LinearXentArgs a, in
       }
     const auto ss = __builtin_amdgcn_permlane32_swap(__float_as_uint(s), __float_as_uint(s), false, false);
     s = __uint_as_float(ss[0]) + __uint_as_float(ss[1]);
-    if (lane < 32 && t < n && v0 < a.V) a.part[(long)t * pieces + v0 / PIECE] = make_float2(m, s);
+    if (lane < 32 && t < n && v0 < a.V) a.part[(long)t * pieces + v0 / W] = make_float2(m, s);
     if constexpr (TRAIN) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int row = 4 * k + (lane >> 4);
-        const u32x4 w = *reinterpret_cast<const u32x4*>(st + row * QP + 4 * (lane & 15));
-        *reinterpret_cast<u32x4*>(a.e + (long)(t0 + 32 * j + row) * a.lde + v0 + 8 * (lane & 15)) = w;
+      for (int k = 0; k < W / 16; ++k) {
+        const int row = 512 / W * k + lane / (W / 8), c = lane % (W / 8);
+        const u32x4 w = *reinterpret_cast<const u32x4*>(st + row * QP + 4 * c);
+        *reinterpret_cast<u32x4*>(a.e + (long)(t0 + 32 * j + row) * a.lde + v0 + 8 * c) = w;
       }
     }
   }
 }
 
-// 16 tokens x 16 slices of the pieces: lse and loss, and, for the gradients, every piece's factor c exp(m - lse).
+// A wave a token: lse and loss from its pieces' statistics, and, for the gradients, every piece's factor
+// c exp(m - lse).
 template <bool TRAIN>
 __global__ __launch_bounds__(256) void xent_join_kernel(LinearXentArgs a, int first) {
-  __shared__ float2 sh[16][17];
-  const int n = chunk_rows(a, first), tl = threadIdx.x >> 4, sl = threadIdx.x & 15;
-  const int t0 = blockIdx.x * 16, t = t0 + tl;
-  if (t0 >= n) return;
-  const int pieces = cdiv(a.V, PIECE);
-  float2* part = a.part + (long)min(t, n - 1) * pieces;
-  float m = -INF, s = 0.f;
-#pragma unroll 4
-  for (int p = sl; p < pieces; p += 16) {
-    const float2 q = part[p];
-    if (q.y == 0.f) continue;  // no entry is left there
-    const float top = fmaxf(m, q.x);
-    s = s * __builtin_amdgcn_exp2f((m - top) * LOG2E) + q.y * __builtin_amdgcn_exp2f((q.x - top) * LOG2E);
-    m = top;
-  }
-  sh[sl][tl] = make_float2(m, s);
-  __syncthreads();
-  m = -INF;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) m = fmaxf(m, sh[i][tl].x);
-  s = 0.f;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float2 q = sh[i][tl];
-    if (q.y != 0.f) s += q.y * __builtin_amdgcn_exp2f((q.x - m) * LOG2E);
-  }
+  const int n = chunk_rows(a, first), lane = threadIdx.x & 63;
+  const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (t >= n) return;
+  const int pieces = cdiv(a.V, a.piece);
+  float2* part = a.part + (long)t * pieces;
+  float top = -INF;
+#pragma unroll 4
+  for (int p = lane; p < pieces; p += 64) {
+    const float2 q = part[p];
+    if (q.y != 0.f) top = fmaxf(top, q.x);  // an entry is left there
+  }
+  const float m = wave_max(top);
+  float sum = 0.f;
+#pragma unroll 4
+  for (int p = lane; p < pieces; p += 64) {
+    const float2 q = part[p];
+    if (q.y != 0.f) sum += q.y * __builtin_amdgcn_exp2f((q.x - m) * LOG2E);
+  }
+  const float s = wave_total(sum);
   const bool none = s == 0.f;  // every entry is -inf
   const float log_s = none ? 0.f : logf(s), z = a.zlab[first + t] - m;
   const int row = a.idx[first + t];
-  if (sl == 0) {
+  if (lane == 0) {
     a.lse[row] = none ? -INF : m + log_s;
     a.row_loss[row] = none ? 0.f : log_s - z;
   }
   if constexpr (TRAIN) {
     const float c = none ? 0.f : a.row_weight != nullptr ? a.row_weight[row] : a.inv_n[0];
     const float up = none ? 0.f : c / s;
-    for (int p = sl; p < pieces; p += 16) {
-      float2& q = part[p];
-      q.x = none || q.y == 0.f ? 0.f : up * __builtin_amdgcn_exp2f((q.x - m) * LOG2E);
+#pragma unroll 4
+    for (int p = lane; p < pieces; p += 64) {
+      const float2 q = part[p];
+      part[p].x = none || q.y == 0.f ? 0.f : up * __builtin_amdgcn_exp2f((q.x - m) * LOG2E);
     }
     // the label's entry of dz
-    if (sl == 0) a.zlab[first + t] = none ? 0.f : up * __builtin_amdgcn_exp2f(z * LOG2E) - c;
+    if (lane == 0) a.zlab[first + t] = none ? 0.f : up * __builtin_amdgcn_exp2f(z * LOG2E) - c;
   }
 }
 
-// dz from the 16-bit numbers in place, for TB tokens and 2048 entries of the vocabulary: a thread has eight
+// dz from the 16-bit numbers in place, for a.tb tokens and 2048 entries of the vocabulary: a thread has eight
 // entries, of one piece, and goes from token to token.
 template <bool DB>
 __global__ __launch_bounds__(256) void xent_scale_kernel(LinearXentArgs a, int first) {
-  const int n = chunk_rows(a, first), pieces = cdiv(a.V, PIECE), blocks = cdiv(a.V, 2048);
+  const int n = chunk_rows(a, first), pieces = cdiv(a.V, a.piece), blocks = cdiv(a.V, 2048);
   const int tb = blockIdx.x / blocks, v = (blockIdx.x - tb * blocks) * 2048 + 8 * threadIdx.x;
-  const int r0 = tb * TB, r1 = min(n, r0 + TB);
+  const int r0 = tb * a.tb, r1 = min(n, r0 + a.tb);
   if (r0 >= n || v >= a.V) return;
-  const float2* part = a.part + v / PIECE;
+  const float2* part = a.part + v / a.piece;
   float db[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) db[e] = 0.f;
@@ -362,15 +435,16 @@ __global__ __launch_bounds__(256) void xent_scale_kernel(LinearXentArgs a, int f
 }
 
 // db of a chunk from its blocks of tokens, in order, added to the chunks before it.
-__global__ __launch_bounds__(256) void xent_db_kernel(LinearXentArgs a, int first, int last) {
-  const int v = blockIdx.x * 256 + threadIdx.x, blocks = cdiv(chunk_rows(a, first), TB);
+__global__ __launch_bounds__(256) void xent_db_kernel(LinearXentArgs a, int first) {
+  if (chunk_idle(a, first)) return;
+  const int v = blockIdx.x * 256 + threadIdx.x, blocks = cdiv(chunk_rows(a, first), a.tb);
   if (v >= a.V) return;
   float* f32 = reinterpret_cast<float*>(a.db);
   float* sum = a.dw_f32 ? f32 : a.dbsum;
   float s = (a.dw_f32 ? a.accumulate : 0) || first > 0 ? sum[v] : 0.f;
 #pragma unroll 8
   for (int b = 0; b < blocks; ++b) s += a.dbpart[(long)b * a.V + v];
-  if (a.dw_f32 || !last) sum[v] = s;
+  if (a.dw_f32 || !chunk_last(a, first)) sum[v] = s;
   else reinterpret_cast<bf16*>(a.db)[v] = f2bf(s);
 }
 
@@ -397,45 +471,55 @@ struct RowsOut {
   }
 };
 
-// C[m, c] = sum_k (A + A2)(m, k) B(c, k) of a tile (A2 may be absent), K split in S slices of kc: to `o`, or, with slices, to partial
-// products [S][rows of whole tiles][N] in `partial`.
-template <int AL>
+// C[m, c] = sum_k (A + A2)(m, k) B(c, k) of a tile (A2 may be absent): to `o`, or, where the tile's K is split, to
+// its slice's partial product [R][R] in `partial`.
+template <int R, int AL>
 __device__ __forceinline__ void product(bf16* smem, const Operand<AL>& A, const bf16* A2, const Operand<LAY_MN>& B, int M, int N,
-                                         int K, int S, float* partial, const RowsOut& o) {
-  const int tiles = cdiv(M, BT) * cdiv(N, BT), kc = cdiv(cdiv(K, BK), S) * BK;
-  if ((int)blockIdx.x >= tiles * S) return;
-  const int bid = xcd_place(blockIdx.x, tiles * S), slice = bid / tiles;
+                                        int K, const Split& sp, int bid, float* partial, const RowsOut& o) {
+  if (bid >= sp.groups()) return;
+  int tile, kb = 0, kc = K;
+  float* part = nullptr;
+  if (bid < sp.full) {
+    tile = xcd_place(bid, sp.full);
+  } else {
+    const int i = xcd_place(bid - sp.full, sp.rest * sp.S), slice = i / sp.rest;
+    tile = sp.full + i - slice * sp.rest;
+    if (sp.S > 1) {
+      kc = cdiv(cdiv(K, BK), sp.S) * BK;
+      kb = slice * kc;
+      kc = max(0, min(kc, K - kb));
+      part = partial + (long)i * R * R;
+    }
+  }
   int m0, n0;
-  tile_origin(M, N, bid - slice * tiles, m0, n0);
+  tile_origin<R>(M, N, tile, m0, n0);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kb = slice * kc;
-  floatx16 acc[4][4];
+  constexpr int S = Tile<R>::S, W = Tile<R>::W, EP = W + 8;
+  Acc<R> acc;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < S; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < S; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  tile_product<AL, LAY_MN>(acc, smem, A, A2, B, m0, M, n0, N, kb, max(0, min(kc, K - kb)), wave);
+  tile_product<R, AL, LAY_MN>(acc, smem, A, A2, B, m0, M, n0, N, kb, kc, wave);
   float* st = reinterpret_cast<float*>(smem) + wave * 32 * EP;
-  const int cl = 8 * (lane & 15), col = n0 + (wave & 1) * 128 + cl;
-  RowsOut q = o;
-  if (S > 1) q = RowsOut{partial + (long)slice * cdiv(M, BT) * BT * N, N, true, nullptr, 0, nullptr};
+  const int cl = 8 * (lane % (W / 8)), cw = (wave & 1) * W + cl;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < S; ++i) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < S; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         st[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * EP + 32 * j + (lane & 31)] = acc[i][j][r];
 #pragma unroll 2
-    for (int s = 0; s < 8; ++s) {
-      const int rl = 4 * s + (lane >> 4), m = m0 + (wave >> 1) * 128 + 32 * i + rl;
-      if (m >= M || col >= N) continue;
+    for (int s = 0; s < W / 16; ++s) {
+      const int rl = 512 / W * s + lane / (W / 8), rw = (wave >> 1) * W + 32 * i + rl;
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = st[rl * EP + cl + e];
-      q.put(m, col, x);
+      if (part != nullptr) store8<false>(part + rw * R + cw, 8, x);
+      else if (m0 + rw < M && n0 + cw < N) o.put(m0 + rw, n0 + cw, x);
     }
   }
 }
@@ -443,74 +527,113 @@ __device__ __forceinline__ void product(bf16* smem, const Operand<AL>& A, const 
 __device__ __forceinline__ RowsOut dx_out(const LinearXentArgs& a, int first) {
   return RowsOut{a.dx, a.lddx, false, nullptr, 0, a.idx + first};
 }
-__device__ __forceinline__ int dx_split(const LinearXentArgs& a, int n) {
-  return pick_split(cdiv(n, BT) * cdiv(a.d, BT), cdiv(a.V, BK));
+__host__ __device__ inline Split dx_split(int R, const LinearXentArgs& a, int n) {
+  return split_of(R, tiles_of(R, n, a.d), cdiv(a.V, BK));
 }
 // dw of one of several chunks goes to an fp32 sum; the last one's outcome to dw.
-__device__ __forceinline__ RowsOut dw_out(const LinearXentArgs& a, int first, bool last) {
+__device__ __forceinline__ RowsOut dw_out(const LinearXentArgs& a, int first) {
   const bool sum = a.dwsum != nullptr;
   RowsOut o = {a.dw, a.lddw, a.dw_f32 != 0, nullptr, 0, nullptr};
   if (sum) {
     if (first > 0) o.add = a.dwsum, o.ldadd = a.d;
-    if (!last) o.out = a.dwsum, o.ld = a.d, o.f32 = true;
+    if (!chunk_last(a, first)) o.out = a.dwsum, o.ld = a.d, o.f32 = true;
   } else if (first > 0 || a.accumulate) {
     o.add = reinterpret_cast<const float*>(a.dw);
     o.ldadd = a.lddw;
   }
   return o;
 }
-__device__ __forceinline__ int dw_split(const LinearXentArgs& a, int n) {
-  return pick_split(cdiv(a.V, BT) * cdiv(a.d, BT), cdiv(n, BK));
+__host__ __device__ inline Split dw_split(int R, const LinearXentArgs& a, int n) {
+  return split_of(R, tiles_of(R, a.V, a.d), cdiv(n, BK));
 }
 
-__global__ __launch_bounds__(NT, 1) void xent_dx_kernel(LinearXentArgs a, int first) {
-  __shared__ __attribute__((aligned(1024))) bf16 smem[5 * OPE];
+template <int R>
+__device__ __forceinline__ void dx_tile(const LinearXentArgs& a, int first, bf16* smem, int bid) {
   const int n = chunk_rows(a, first);
   const Operand<LAY_K> A = {a.e, a.lde};
   const Operand<LAY_MN> B = {a.w, a.ldw};
-  product<LAY_K>(smem, A, n <= BT ? a.e2 : nullptr, B, n, a.d, a.V, dx_split(a, n), a.partial, dx_out(a, first));
+  product<R, LAY_K>(smem, A, n <= BT ? a.e2 : nullptr, B, n, a.d, a.V, dx_split(R, a, n), bid, a.partial, dx_out(a, first));
 }
-
-__global__ __launch_bounds__(NT, 1) void xent_dw_kernel(LinearXentArgs a, int first, int last) {
-  __shared__ __attribute__((aligned(1024))) bf16 smem[5 * OPE];
+template <int R>
+__device__ __forceinline__ void dw_tile(const LinearXentArgs& a, int first, bf16* smem, int bid) {
+  if (chunk_idle(a, first)) return;
   const int n = chunk_rows(a, first);
   const Operand<LAY_MN> A = {a.e, a.lde};
   Operand<LAY_MN> B;
   B.p = compact_x(a, B.ld);
   B.p += first * B.ld;
-  product<LAY_MN>(smem, A, n <= BT ? a.e2 : nullptr, B, a.V, a.d, n, dw_split(a, n), a.partial, dw_out(a, first, last));
+  product<R, LAY_MN>(smem, A, n <= BT ? a.e2 : nullptr, B, a.V, a.d, n, dw_split(R, a, n), bid, a.partial_dw, dw_out(a, first));
 }
 
-// The slices of a product's tiles added in order; none where it was not split.
+template <int R>
+__global__ __launch_bounds__(NT, 1) void xent_dx_kernel(LinearXentArgs a, int first) {
+  __shared__ __attribute__((aligned(1024))) bf16 smem[Tile<R>::LDS];
+  dx_tile<R>(a, first, smem, blockIdx.x);
+}
+template <int R>
+__global__ __launch_bounds__(NT, 1) void xent_dw_kernel(LinearXentArgs a, int first) {
+  __shared__ __attribute__((aligned(1024))) bf16 smem[Tile<R>::LDS];
+  dw_tile<R>(a, first, smem, blockIdx.x);
+}
+// Both products at once, where each is small: the first `groups` workgroups dx, the others dw.
+__global__ __launch_bounds__(NT, 1) void xent_both_kernel(LinearXentArgs a, int first, int groups) {
+  __shared__ __attribute__((aligned(1024))) bf16 smem[SMALL_LDS];
+  if ((int)blockIdx.x < groups) dx_tile<RS>(a, first, smem, blockIdx.x);
+  else dw_tile<RS>(a, first, smem, blockIdx.x - groups);
+}
+
+// The slices of a product's split tiles added in order, 2048 elements of a tile at a time by each of `groups` workgroups.
 template <bool DW>
-__global__ __launch_bounds__(256) void xent_slices_kernel(LinearXentArgs a, int first, int last) {
-  const int n = chunk_rows(a, first), M = DW ? a.V : n, S = DW ? dw_split(a, n) : dx_split(a, n);
-  if (S == 1) return;
-  const RowsOut o = DW ? dw_out(a, first, last) : dx_out(a, first);
-  const int n8 = a.d / 8;
-  const long stride = (long)cdiv(M, BT) * BT * a.d, total = (long)M * n8;
-  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long)gridDim.x * 256) {
-    const int m = (int)(i / n8), col = (int)(i - (long)m * n8) * 8;
-    const float* p = a.partial + (long)m * a.d + col;
+__device__ __forceinline__ void add_slices(const LinearXentArgs& a, int first, int R, int bid, int groups) {
+  const int n = chunk_rows(a, first), M = DW ? a.V : n, per = R * R / 2048;
+  const Split sp = DW ? dw_split(R, a, n) : dx_split(R, a, n);
+  if (sp.S == 1 || chunk_idle(a, first)) return;
+  const RowsOut o = DW ? dw_out(a, first) : dx_out(a, first);
+  for (int j = bid; j < per * sp.rest; j += groups) {
+    const int i = j / per, e = (j % per) * 2048 + 8 * threadIdx.x;
+    int m0, n0;
+    if (R == BT) tile_origin<BT>(M, a.d, sp.full + i, m0, n0);
+    else tile_origin<RS>(M, a.d, sp.full + i, m0, n0);
+    const int m = m0 + e / R, col = n0 + e % R;
+    if (m >= M || col >= a.d) continue;
+    const float* p = (DW ? a.partial_dw : a.partial) + (long)i * R * R + e;
     float x[8], b[8];
     widen8(load8<false>(p, 8), x);
-    for (int s = 1; s < S; ++s) {
-      widen8(load8<false>(p + s * stride, 8), b);
+#pragma unroll 4
+    for (int s = 1; s < sp.S; ++s) {
+      widen8(load8<false>(p + (long)s * sp.rest * R * R, 8), b);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] += b[e];
+      for (int k = 0; k < 8; ++k) x[k] += b[k];
     }
     o.put(m, col, x);
   }
 }
+// The first gx workgroups dx, the others dw.
+__global__ __launch_bounds__(256) void xent_slices_kernel(LinearXentArgs a, int first, int rx, int gx, int rw) {
+  if ((int)blockIdx.x < gx) add_slices<false>(a, first, rx, blockIdx.x, gx);
+  else add_slices<true>(a, first, rw, blockIdx.x - gx, gridDim.x - gx);
+}
 
-constexpr int64_t kMaxE = 1LL << 28;   // numbers of a chunk
+constexpr int64_t kMaxE = 1LL << 29;   // numbers of a chunk
 constexpr int kMaxChunk = 16384;       // tokens of a chunk
+
+struct Launch {
+  int R = BT, groups = 1, split = 0;  // tile; workgroups of a product; tiles whose K is split
+  int64_t partial = 0;
+  void join(const Split& p) {
+    groups = std::max(groups, p.groups());
+    if (p.S > 1) split = std::max(split, p.rest);
+    partial = std::max(partial, p.partial(R));
+  }
+  int slices() const { return split ? std::min(R * R / 2048 * split, 8 * CUS) : 0; }
+};
 
 // The workspace: 256-byte aligned parts, whose places go into `a` when it has a workspace.
 struct Layout {
   int64_t bytes = 0;
   char* base;
-  bool dx_split, dw_split;  // whether any number of rows has the product split
+  Launch logits, dx, dw;
+  bool both;
   template <class T>
   void part(T*& p, int64_t n) {
     p = n > 0 ? reinterpret_cast<T*>(base + bytes) : nullptr;
@@ -526,31 +649,35 @@ void plan(LinearXentArgs& a, Layout& l) {
   const int chunks = std::max(1, (int)((a.N + cap - 1) / cap));
   a.chunk = std::max(1, cdiv(cdiv(a.N, chunks), BT)) * BT;
   a.lde = vp;
+  // tokens of a workgroup of the scaling pass: fewer where there would be few workgroups
+  a.tb = 64;
+  while (a.tb > 4 && (int64_t)cdiv(a.V, 2048) * cdiv(std::min(a.N, a.chunk), a.tb) < 4 * CUS) a.tb /= 2;
+  // tiles of 128 where those of 256 would leave most CUs without one, by the estimated time
+  const int n = std::min(a.N, a.chunk);
+  const auto small = [&](auto split) { return split(RS).us < split(BT).us ? RS : BT; };
+  l.logits.R = small([&](int R) { return split_of(R, tiles_of(R, a.V, n), cdiv(a.d, BK), 1); });
+  l.dx.R = small([&](int R) { return dx_split(R, a, n); });
+  l.dw.R = small([&](int R) { return dw_split(R, a, n); });
+  a.piece = l.logits.R / 2;
   l.part(a.meta, 64);
   l.part(a.idx, a.N);
   l.part(a.pos, a.N);
   l.part(a.lab, a.N);
   l.part(a.zlab, a.N);
-  l.part(a.part, (int64_t)cdiv(a.V, PIECE) * a.chunk);
+  l.part(a.part, (int64_t)cdiv(a.V, a.piece) * a.chunk);
   l.part(a.xc, (int64_t)a.N * a.d);
   l.part(a.e, train ? (int64_t)a.chunk * a.lde : 0);
   l.part(a.e2, train ? (int64_t)BT * a.lde : 0);
-  l.part(a.dbpart, a.db ? (int64_t)cdiv(a.chunk, TB) * a.V : 0);
+  l.part(a.dbpart, a.db ? (int64_t)cdiv(a.chunk, a.tb) * a.V : 0);
   l.part(a.dbsum, a.db && !a.dw_f32 && a.N > a.chunk ? a.V : 0);
   l.part(a.dwsum, a.dw && !a.dw_f32 && a.N > a.chunk ? (int64_t)a.V * a.d : 0);
-  const int tn = cdiv(a.d, BT), tv = cdiv(a.V, BT);
-  int64_t dx = 0, dw = 0;
-  for (int n = BT; a.dx && n <= a.chunk; n += BT) {
-    const int S = pick_split(n / BT * tn, cdiv(a.V, BK));
-    if (S > 1) dx = std::max(dx, (int64_t)S * n * a.d);
-  }
-  for (int n = BK; a.dw && n <= a.chunk; n += BK) {
-    const int S = pick_split(tv * tn, n / BK);
-    if (S > 1) dw = std::max(dw, (int64_t)S * vp * a.d);
-  }
-  l.part(a.partial, std::max(dx, dw));
-  l.dx_split = dx > 0;
-  l.dw_split = dw > 0;
+  // the most that any number of rows that take part asks for
+  for (int i = 0; a.dx && i <= a.chunk; i += l.dx.R) l.dx.join(dx_split(l.dx.R, a, i));
+  for (int i = 0; a.dw && i <= a.chunk; i += BK) l.dw.join(dw_split(l.dw.R, a, i));
+  l.both = a.dx && a.dw && l.dx.R == RS && l.dw.R == RS;
+  l.part(a.partial, l.both ? l.dx.partial : std::max(l.dx.partial, l.dw.partial));
+  if (l.both) l.part(a.partial_dw, l.dw.partial);
+  else a.partial_dw = a.partial;
 }
 
 }  // namespace
@@ -567,26 +694,39 @@ hipError_t launch_linear_xent(LinearXentArgs a, void* ws, hipStream_t s) {
   l.base = (char*)ws;
   plan(a, l);
   const bool train = a.dx || a.dw || a.db;
-  const int tn = cdiv(a.d, BT), tv = cdiv(a.V, BT), tt = cdiv(a.chunk, BT);
-  hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, a);
-  if (a.N > 0) hipLaunchKernelGGL(xent_copy_kernel, dim3(cdiv(a.N, 4)), dim3(256), 0, s, a);
+  const int RL = l.logits.R, RX = l.dx.R, RW = l.dw.R;
+  const auto logits = RL == BT ? (train ? xent_logits_kernel<BT, true> : xent_logits_kernel<BT, false>)
+                               : (train ? xent_logits_kernel<RS, true> : xent_logits_kernel<RS, false>);
+  if (a.N <= FEW) {
+    hipLaunchKernelGGL(xent_rows_few_kernel, dim3(std::max(1, cdiv(a.N, 64))), dim3(256), 0, s, a);
+  } else {
+    hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL(xent_copy_kernel, dim3(cdiv(a.N, 4)), dim3(256), 0, s, a);
+  }
   // without rows, too: dw and db of none
   for (int first = 0; first < std::max(a.N, 1); first += a.chunk) {
-    const int last = first + a.chunk >= a.N;
-    const auto logits = train ? xent_logits_kernel<true> : xent_logits_kernel<false>;
-    hipLaunchKernelGGL(logits, dim3(tv * tt), dim3(NT), 0, s, a, first);
-    hipLaunchKernelGGL(train ? xent_join_kernel<true> : xent_join_kernel<false>, dim3(cdiv(a.chunk, 16)), dim3(256), 0, s, a, first);
+    hipLaunchKernelGGL(logits, dim3(tiles_of(RL, a.V, a.chunk)), dim3(NT), 0, s, a, first);
+    hipLaunchKernelGGL(train ? xent_join_kernel<true> : xent_join_kernel<false>, dim3(cdiv(a.chunk, 4)), dim3(256), 0, s, a, first);
     if (!train) continue;
-    hipLaunchKernelGGL(a.db ? xent_scale_kernel<true> : xent_scale_kernel<false>, dim3(cdiv(a.V, 2048) * cdiv(a.chunk, TB)), dim3(256), 0, s, a,
+    hipLaunchKernelGGL(a.db ? xent_scale_kernel<true> : xent_scale_kernel<false>, dim3(cdiv(a.V, 2048) * cdiv(a.chunk, a.tb)), dim3(256), 0, s, a,
                        first);
-    if (a.db) hipLaunchKernelGGL(xent_db_kernel, dim3(cdiv(a.V, 256)), dim3(256), 0, s, a, first, last);
+    if (a.db) hipLaunchKernelGGL(xent_db_kernel, dim3(cdiv(a.V, 256)), dim3(256), 0, s, a, first);
+    const int gx = a.dx ? l.dx.slices() : 0, gw = a.dw ? l.dw.slices() : 0;
+    const auto slices = [&](int x, int w) {
+      if (x + w) hipLaunchKernelGGL(xent_slices_kernel, dim3(x + w), dim3(256), 0, s, a, first, RX, x, RW);
+    };
+    if (l.both) {
+      hipLaunchKernelGGL(xent_both_kernel, dim3(l.dx.groups + l.dw.groups), dim3(NT), 0, s, a, first, l.dx.groups);
+      slices(gx, gw);
+      continue;
+    }
     if (a.dx) {
-      hipLaunchKernelGGL(xent_dx_kernel, dim3(std::max(tt * tn, 512)), dim3(NT), 0, s, a, first);
-      if (l.dx_split) hipLaunchKernelGGL(xent_slices_kernel<false>, dim3(2048), dim3(256), 0, s, a, first, last);
+      hipLaunchKernelGGL(RX == BT ? xent_dx_kernel<BT> : xent_dx_kernel<RS>, dim3(l.dx.groups), dim3(NT), 0, s, a, first);
+      slices(gx, 0);
     }
     if (a.dw) {
-      hipLaunchKernelGGL(xent_dw_kernel, dim3(std::max(tv * tn, 512)), dim3(NT), 0, s, a, first, last);
-      if (l.dw_split) hipLaunchKernelGGL(xent_slices_kernel<true>, dim3(2048), dim3(256), 0, s, a, first, last);
+      hipLaunchKernelGGL(RW == BT ? xent_dw_kernel<BT> : xent_dw_kernel<RS>, dim3(l.dw.groups), dim3(NT), 0, s, a, first);
+      slices(0, gw);
     }
   }
   return hipGetLastError();

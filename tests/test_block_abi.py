@@ -176,8 +176,8 @@ def test_head_null_and_ws():
     for N in (4096, 16384, 100000):
         x = 2 * N * 4096
         small = 400 * 8 * 16384 + 24 * N + (N // 512 + 2) * 4 * 50400 + (1 << 20)
-        assert ws(N=N, V=50400, d=4096, dx=P, dw=P, bias=P, db=P) <= (1 << 29) + x + (1 << 27) + 4 * 50400 * 4096 + small
-        assert ws(N=N, V=50400, d=4096, dx=P, dw=P, grad_f32=1) <= (1 << 29) + x + (1 << 27) + small
+        assert ws(N=N, V=50400, d=4096, dx=P, dw=P, bias=P, db=P) <= (1 << 30) + x + (1 << 27) + 4 * 50400 * 4096 + small
+        assert ws(N=N, V=50400, d=4096, dx=P, dw=P, grad_f32=1) <= (1 << 30) + x + (1 << 27) + small
     assert ws(N=0, V=100, d=64, dw=P) > 0
 
 
