@@ -235,9 +235,9 @@ sat_status sat_op_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int3
  * may be NULL without norms.  y may be x (with ldy == ldx); no other output overlaps an input.
  * Backward, from dy (the gradient that reaches y along the stream, in its type; NULL: 0) and dh (bf16, with
  * pre): dx = alpha t and df of t = dy + N_pre'(dh), and, where not NULL, fp32 [d] (written): dg_*, db_* and
- * dgate, summed over the rows in fp32 in an order that depends on T and d alone.  It reads y (with pre), f (with post or
+ * dgate, summed over the rows in fp32 in an order that depends on T, d and whether there is a post alone.  It reads y (with pre), f (with post or
  * dgate), stats, gains, post's shift, gate and the dropout's arguments; dx may be dy (with lddx == lddy).  ws:
- * fp32 scratch, as much as the _ws call says (T, d and which sums are wanted are read); calls that may
+ * fp32 scratch, as much as the _ws call says (T, d, post and which sums are wanted are read); calls that may
  * overlap need one each.  A row that holds NaN or infinities spoils its own rows of the outputs and the sums.
  * Arrays are aligned to their elements (16-byte aligned rows are fastest).
  * Errors: SAT_EINVAL for null pointers, sizes, alignment, constants, and a ws that is too small. */

@@ -188,7 +188,7 @@ __device__ __forceinline__ void kstep_ring(floatx16 (&acc)[4][4], const bf16x8 (
 }
 
 // The loop: acc += the tile's product over nk K-tiles.  la, lb, FA and FB are initialised; K-tile t begins at
-// k = kof(t), whose operands' resources are rsA(t, k) and rsB(t, k) (Loader::issue); for t >= nk (two past the end
+// k = kof(t), whose operands' resources are rsA(t, k) and rsB(t, k) (Loader::issue); for t >= nk (a few past the end
 // are asked for) kof gives K, the end of k.  Afterwards no copy is in flight and every wave is done with
 // smem (5 * OPE elements).
 template <int AL, int BL, class KO, class RA, class RB>
@@ -260,26 +260,27 @@ __device__ __forceinline__ void gemm256_loop(floatx16 (&acc)[4][4], bf16* smem, 
 }
 
 // The same product on a tile of 128 x 128 (a wave: 64 x 64), for products that are too small to give every CU a
-// tile of 256: three stages of both operands in 96 KB, the copies two K-tiles ahead, one barrier for each.
+// tile of 256: four stages of both operands in 128 KB, the copies three K-tiles ahead, one barrier for each.
 constexpr int RS = 128;
-constexpr int SMALL_LDS = 3 * 2 * RS * BK;  // elements
+constexpr int STAGES = 4;
+constexpr int SMALL_LDS = STAGES * 2 * RS * BK;  // elements
 template <int AL, int BL, class KO, class RA, class RB>
 __device__ __forceinline__ void gemm128_loop(floatx16 (&acc)[2][2], bf16* smem, const Loader<AL, RS>& la,
                                              const Loader<BL, RS>& lb, const Frags<AL, RS>& FA, const Frags<BL, RS>& FB,
                                              RA rsA, RB rsB, int nk, KO kof, int K, int wave) {
   constexpr int COPIES = Loader<AL, RS>::NI + Loader<BL, RS>::NI;
-  auto sA = [&](int t) { return smem + (t % 3) * 2 * RS * BK; };
+  auto sA = [&](int t) { return smem + (t % STAGES) * 2 * RS * BK; };
   auto copy = [&](int t) {
     const int k = kof(t);
     la.issue(rsA(t, k), k, K, sA(t), wave);
     lb.issue(rsB(t, k), k, K, sA(t) + RS * BK, wave);
   };
-  copy(0);
-  copy(1);
+#pragma unroll
+  for (int t = 0; t < STAGES - 1; ++t) copy(t);
   for (int t = 0; t < nk; ++t) {
-    wait_vm_lgkm0<COPIES>();  // tile t resident; this wave's reads of tile t - 1 done
+    wait_vm_lgkm0<(STAGES - 2) * COPIES>();  // tile t resident; this wave's reads of tile t - 1 done
     cta_barrier();            // ... every wave's: its stage is free
-    copy(t + 2);
+    copy(t + STAGES - 1);
     const bf16* a = sA(t);
     const bf16* b = a + RS * BK;
 #pragma unroll

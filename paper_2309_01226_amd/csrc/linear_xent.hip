@@ -349,46 +349,97 @@ __global__ __launch_bounds__(NT, 1) void xent_logits_kernel(LinearXentArgs a, in
   }
 }
 
-// A wave a token: lse and loss from its pieces' statistics, and, for the gradients, every piece's factor
-// c exp(m - lse).
-template <bool TRAIN>
-__global__ __launch_bounds__(256) void xent_join_kernel(LinearXentArgs a, int first) {
-  const int n = chunk_rows(a, first), lane = threadIdx.x & 63;
-  const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (t >= n) return;
-  const int pieces = cdiv(a.V, a.piece);
-  float2* part = a.part + (long)t * pieces;
-  float top = -INF;
-#pragma unroll 4
-  for (int p = lane; p < pieces; p += 64) {
-    const float2 q = part[p];
-    if (q.y != 0.f) top = fmaxf(top, q.x);  // an entry is left there
-  }
+// A token's row on one wave: its pieces' statistics, up to 64 J of them in registers, joined to lse and loss.
+struct Joined {
+  float m, up, dlabel;  // what is common to all pieces, c / (sum of exp(z - m)), and the label's entry of dz
+};
+// f(p, q) for the lane's pieces.
+template <int J, class F>
+__device__ __forceinline__ void over_pieces(const float2 (&q)[J], const float2* part, int pieces, F f) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+    if (lane + 64 * j < pieces) f(lane + 64 * j, q[j]);
+  for (int p = lane + 64 * J; p < pieces; p += 64) f(p, part[p]);
+}
+template <int J>
+__device__ __forceinline__ Joined join_row(const LinearXentArgs& a, int first, int t, int pieces, const float2* part, float2 (&q)[J]) {
+  const int lane = threadIdx.x & 63;
+  // (sum 0: no entry is left there)
+#pragma unroll
+  for (int j = 0; j < J; ++j) q[j] = lane + 64 * j < pieces ? part[lane + 64 * j] : make_float2(0.f, 0.f);
+  const float zlab = a.zlab[first + t];
+  const int row = a.idx[first + t];
+  float top = -INF, sum = 0.f;
+  over_pieces(q, part, pieces, [&](int, float2 x) { top = x.y != 0.f ? fmaxf(top, x.x) : top; });
   const float m = wave_max(top);
-  float sum = 0.f;
-#pragma unroll 4
-  for (int p = lane; p < pieces; p += 64) {
-    const float2 q = part[p];
-    if (q.y != 0.f) sum += q.y * __builtin_amdgcn_exp2f((q.x - m) * LOG2E);
-  }
+  over_pieces(q, part, pieces, [&](int, float2 x) { sum += x.y != 0.f ? x.y * __builtin_amdgcn_exp2f((x.x - m) * LOG2E) : 0.f; });
   const float s = wave_total(sum);
   const bool none = s == 0.f;  // every entry is -inf
-  const float log_s = none ? 0.f : logf(s), z = a.zlab[first + t] - m;
-  const int row = a.idx[first + t];
+  const float log_s = none ? 0.f : logf(s), z = zlab - m;
   if (lane == 0) {
     a.lse[row] = none ? -INF : m + log_s;
     a.row_loss[row] = none ? 0.f : log_s - z;
   }
+  if (none) return Joined{m, 0.f, 0.f};
+  const float c = a.row_weight != nullptr ? a.row_weight[row] : a.inv_n[0], up = c / s;
+  return Joined{m, up, up * __builtin_amdgcn_exp2f(z * LOG2E) - c};
+}
+// What a piece's exp(z - its own maximum) is multiplied by to give c softmax.
+__device__ __forceinline__ float piece_factor(const Joined& r, float2 q) {
+  return r.up == 0.f || q.y == 0.f ? 0.f : r.up * __builtin_amdgcn_exp2f((q.x - r.m) * LOG2E);
+}
+
+// A wave a token: lse and loss, and, for the gradients, the pieces' factors and the label's entry.
+template <bool TRAIN>
+__global__ __launch_bounds__(256) void xent_join_kernel(LinearXentArgs a, int first) {
+  const int n = chunk_rows(a, first);
+  const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (t >= n) return;
+  const int pieces = cdiv(a.V, a.piece);
+  float2* part = a.part + (long)t * pieces;
+  float2 q[16];
+  const Joined r = join_row(a, first, t, pieces, part, q);
   if constexpr (TRAIN) {
-    const float c = none ? 0.f : a.row_weight != nullptr ? a.row_weight[row] : a.inv_n[0];
-    const float up = none ? 0.f : c / s;
-#pragma unroll 4
-    for (int p = lane; p < pieces; p += 64) {
-      const float2 q = part[p];
-      part[p].x = none || q.y == 0.f ? 0.f : up * __builtin_amdgcn_exp2f((q.x - m) * LOG2E);
-    }
-    // the label's entry of dz
-    if (lane == 0) a.zlab[first + t] = none ? 0.f : up * __builtin_amdgcn_exp2f(z * LOG2E) - c;
+    over_pieces(q, part, pieces, [&](int p, float2 x) { part[p].x = piece_factor(r, x); });
+    if ((threadIdx.x & 63) == 0) a.zlab[first + t] = r.dlabel;
+  }
+}
+
+// dz of a token's eight entries from their 16-bit numbers, in place; in two parts where the chunk has few rows.
+__device__ __forceinline__ void scale8(const LinearXentArgs& a, int r, int n, int v, u32x4 w, float f, int off, float dlabel, float (&x)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    x[e] = from_steps(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu) * f;
+    x[e] = off == e ? dlabel : x[e];
+  }
+  bf16x8 y;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = f2bf(x[e]);
+  *reinterpret_cast<bf16x8*>(a.e + (long)r * a.lde + v) = y;
+  if (n <= BT) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = f2bf(x[e] - bf2f(y[e]));
+    *reinterpret_cast<bf16x8*>(a.e2 + (long)r * a.lde + v) = y;
+  }
+}
+
+// Both for a vocabulary of up to 64 pieces: a wave joins its token and scales its whole row.
+__global__ __launch_bounds__(256) void xent_join_scale_kernel(LinearXentArgs a, int first) {
+  const int n = chunk_rows(a, first), lane = threadIdx.x & 63;
+  const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (t >= n) return;
+  const int pieces = cdiv(a.V, a.piece), label = a.lab[first + t];
+  float2 q[1];
+  const Joined r = join_row(a, first, t, pieces, a.part + (long)t * pieces, q);
+  const float f = piece_factor(r, q[0]);
+  const bf16* e = a.e + (long)t * a.lde;
+  for (int v0 = 0; v0 < a.V; v0 += 512) {
+    const int v = v0 + 8 * lane;
+    const float mine = __shfl(f, min(v, a.V - 1) / a.piece, SAT_WAVE);
+    if (v >= a.V) continue;
+    float x[8];
+    scale8(a, t, n, v, *reinterpret_cast<const u32x4*>(e + v), mine, label - v, r.dlabel, x);
   }
 }
 
@@ -406,30 +457,12 @@ __global__ __launch_bounds__(256) void xent_scale_kernel(LinearXentArgs a, int f
   for (int e = 0; e < 8; ++e) db[e] = 0.f;
 #pragma unroll 4
   for (int r = r0; r < r1; ++r) {
-    u32x4* q = reinterpret_cast<u32x4*>(a.e + (long)r * a.lde + v);
-    const u32x4 w = *q;
-    const float f = part[(long)r * pieces].x;
-    const int off = a.lab[first + r] - v;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(a.e + (long)r * a.lde + v);
     float x[8];
+    scale8(a, r, n, v, w, part[(long)r * pieces].x, a.lab[first + r] - v, a.zlab[first + r], x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = from_steps(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu) * f;
-    if (off >= 0 && off < 8) {
-      const float dl = a.zlab[first + r];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = off == e ? dl : x[e];
-    }
-    bf16x8 y;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < 8; ++e)
       if (DB) db[e] += x[e];
-      y[e] = f2bf(x[e]);
-    }
-    *reinterpret_cast<bf16x8*>(q) = y;
-    if (n <= BT) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = f2bf(x[e] - bf2f(y[e]));
-      *reinterpret_cast<bf16x8*>(a.e2 + (long)r * a.lde + v) = y;
-    }
   }
   if (DB) store8<false>(a.dbpart + (long)tb * a.V + v, a.V - v, db);
 }
@@ -706,10 +739,17 @@ hipError_t launch_linear_xent(LinearXentArgs a, void* ws, hipStream_t s) {
   // without rows, too: dw and db of none
   for (int first = 0; first < std::max(a.N, 1); first += a.chunk) {
     hipLaunchKernelGGL(logits, dim3(tiles_of(RL, a.V, a.chunk)), dim3(NT), 0, s, a, first);
-    hipLaunchKernelGGL(train ? xent_join_kernel<true> : xent_join_kernel<false>, dim3(cdiv(a.chunk, 4)), dim3(256), 0, s, a, first);
-    if (!train) continue;
-    hipLaunchKernelGGL(a.db ? xent_scale_kernel<true> : xent_scale_kernel<false>, dim3(cdiv(a.V, 2048) * cdiv(a.chunk, a.tb)), dim3(256), 0, s, a,
-                       first);
+    const dim3 tokens(cdiv(a.chunk, 4)), scaling(cdiv(a.V, 2048) * cdiv(a.chunk, a.tb));
+    if (!train) {
+      hipLaunchKernelGGL(xent_join_kernel<false>, tokens, dim3(256), 0, s, a, first);
+      continue;
+    }
+    if (!a.db && cdiv(a.V, a.piece) <= 64) {
+      hipLaunchKernelGGL(xent_join_scale_kernel, tokens, dim3(256), 0, s, a, first);
+    } else {
+      hipLaunchKernelGGL(xent_join_kernel<true>, tokens, dim3(256), 0, s, a, first);
+      hipLaunchKernelGGL(a.db ? xent_scale_kernel<true> : xent_scale_kernel<false>, scaling, dim3(256), 0, s, a, first);
+    }
     if (a.db) hipLaunchKernelGGL(xent_db_kernel, dim3(cdiv(a.V, 256)), dim3(256), 0, s, a, first);
     const int gx = a.dx ? l.dx.slices() : 0, gw = a.dw ? l.dw.slices() : 0;
     const auto slices = [&](int x, int w) {

@@ -11,8 +11,8 @@
 //   subtract no mean.
 //
 // Bound by HBM: every array is read or written once (fp32 stream, 12 bytes an element forward and 18
-// backward).  A row belongs to d / 512 waves, eight columns a thread, so that a thread's columns
-// stay the same from row to row: gains and the sums of their gradients live in its registers, and the next
+// backward).  A row belongs to d / 512 waves, or to 8, 16 or 32 lanes of one, eight columns a thread, so that a thread's
+// columns stay the same from row to row: gains and the sums of their gradients live in its registers, and the next
 // row's loads are in flight while a row is worked on.  A mean or a variance is formed inside each
 // wave and joined by the pairwise formula of Chan, Golub and LeVeque (one barrier where a second pass
 // over the row would take two).  The sums over rows go to one row of partial sums for each
@@ -27,23 +27,27 @@ namespace {
 
 constexpr int CUS = 256;
 
+// NARROW: rows of up to 256 columns, on 8, 16 or 32 lanes; else a row's place is the same for a whole wave.
+template <bool NARROW>
 struct RowPlace {
   int wpr;    // waves of a row
-  int rw;     // this wave's row among those of the workgroup
+  int L;      // lanes of a row in each of them
+  int rw;     // this thread's row among those of the workgroup
+  int at;     // this wave's pair in the row's part of Shared
   int wave;   // this wave among its row's
   int col, n; // first column of the thread, and columns of the row from there on
+  __device__ __forceinline__ RowPlace(int waves, int lanes, int d) {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    wpr = NARROW ? 1 : waves;
+    L = NARROW ? lanes : 64;
+    const int q = w / wpr;
+    wave = w - q * wpr;
+    at = q * wpr;
+    rw = NARROW ? q * (64 / L) + lane / L : q;
+    col = 8 * (wave * 64 + lane % L);
+    n = d - col;
+  }
 };
-
-__device__ __forceinline__ RowPlace row_place(int wpr, int d) {
-  RowPlace p;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  p.wpr = wpr;
-  p.rw = w / wpr;
-  p.wave = w - p.rw * wpr;
-  p.col = 8 * (p.wave * 64 + (threadIdx.x & 63));
-  p.n = d - p.col;
-  return p;
-}
 
 // Pairs of sums of up to 16 waves, two sets of them by turns: between a set's reads and its next
 // writes every wave passes the other set's barrier.
@@ -52,16 +56,17 @@ struct Shared {
 };
 
 // Sums of a and b over the row.
-__device__ __forceinline__ float2 row_sums(const RowPlace& p, Shared& sh, int& turn, float a, float b) {
-  float2 s = make_float2(wave_total(a), wave_total(b));
+template <bool NARROW>
+__device__ __forceinline__ float2 row_sums(const RowPlace<NARROW>& p, Shared& sh, int& turn, float a, float b) {
+  float2 s = make_float2(group_total(a, p.L), group_total(b, p.L));
   if (p.wpr == 1) return s;
   float2* part = sh.part[turn];
   turn ^= 1;
-  if ((threadIdx.x & 63) == 0) part[p.rw * p.wpr + p.wave] = s;
+  if ((threadIdx.x & 63) == 0) part[p.at + p.wave] = s;
   __syncthreads();
   s = make_float2(0.f, 0.f);
   for (int i = 0; i < p.wpr; ++i) {
-    const float2 q = part[p.rw * p.wpr + i];
+    const float2 q = part[p.at + i];
     s.x += q.x;
     s.y += q.y;
   }
@@ -69,7 +74,8 @@ __device__ __forceinline__ float2 row_sums(const RowPlace& p, Shared& sh, int& t
 }
 
 // Mean (0 for RMS) and reciprocal deviation of a row whose elements are v (0 behind its end).
-__device__ __forceinline__ float2 row_stats(const RowPlace& p, Shared& sh, int& turn, const float (&v)[8], int kind,
+template <bool NARROW>
+__device__ __forceinline__ float2 row_stats(const RowPlace<NARROW>& p, Shared& sh, int& turn, const float (&v)[8], int kind,
                                             int d, float eps) {
   float s = 0.f;
   if (kind == kNormRms) {
@@ -81,20 +87,20 @@ __device__ __forceinline__ float2 row_stats(const RowPlace& p, Shared& sh, int& 
   for (int e = 0; e < 8; ++e) s += v[e];
   // columns of the row's i-th wave
   const auto width = [&](int i) { return (float)min(512, d - 512 * i); };
-  float mean = wave_total(s) / width(p.wave), m2 = 0.f;
+  float mean = group_total(s, p.L) / width(p.wave), m2 = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) m2 += e < p.n ? (v[e] - mean) * (v[e] - mean) : 0.f;
-  m2 = wave_total(m2);
+  m2 = group_total(m2, p.L);
   if (p.wpr > 1) {
     float2* part = sh.part[turn];
     turn ^= 1;
-    if ((threadIdx.x & 63) == 0) part[p.rw * p.wpr + p.wave] = make_float2(mean, m2);
+    if ((threadIdx.x & 63) == 0) part[p.at + p.wave] = make_float2(mean, m2);
     __syncthreads();
     mean = m2 = 0.f;
-    for (int i = 0; i < p.wpr; ++i) mean += part[p.rw * p.wpr + i].x * width(i);
+    for (int i = 0; i < p.wpr; ++i) mean += part[p.at + i].x * width(i);
     mean /= d;
     for (int i = 0; i < p.wpr; ++i) {
-      const float2 q = part[p.rw * p.wpr + i];
+      const float2 q = part[p.at + i];
       m2 += q.y + width(i) * (q.x - mean) * (q.x - mean);
     }
   }
@@ -102,7 +108,8 @@ __device__ __forceinline__ float2 row_stats(const RowPlace& p, Shared& sh, int& 
 }
 
 // Columns of a vector for each channel, or `none` without one.
-__device__ __forceinline__ void channels(const float* g, const RowPlace& p, float none, float (&x)[8]) {
+template <class P>
+__device__ __forceinline__ void channels(const float* g, const P& p, float none, float (&x)[8]) {
   if (g != nullptr && p.n > 0) {
     widen8(load8<false>(g + p.col, p.n), x);
   } else {
@@ -112,8 +119,9 @@ __device__ __forceinline__ void channels(const float* g, const RowPlace& p, floa
 }
 
 // beta gate m of eight columns of a row; exactly 0 where dropped.
+template <class P>
 __device__ __forceinline__ void branch_factors(const ResidualNormArgs& a, const DropConsts& c, uint64_t step, int row,
-                                               const RowPlace& p, float scale, float (&m)[8]) {
+                                               const P& p, float scale, float (&m)[8]) {
   if (c.limit == 0) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) m[e] = scale;
@@ -124,11 +132,11 @@ __device__ __forceinline__ void branch_factors(const ResidualNormArgs& a, const 
   for (int e = 0; e < 8; ++e) m[e] = drop_keeps(c, r, e) ? scale : 0.f;
 }
 
-template <class XT, int MAXT>
+template <class XT, int MAXT, bool NARROW = false>
 __global__ __launch_bounds__(MAXT) void residual_norm_fwd_kernel(ResidualNormArgs a) {
   __shared__ Shared sh;
   int turn = 0;
-  const RowPlace p = row_place(a.wpr, a.d);
+  const RowPlace<NARROW> p(a.wpr, a.L, a.d);
   const DropConsts c = {(uint32_t)a.seed, (uint32_t)(a.seed >> 32), a.limit, a.up, a.step};
   const uint64_t step = drop_step(c);
   const float scale = a.beta * (c.limit ? c.up : 1.f);
@@ -187,14 +195,15 @@ __global__ __launch_bounds__(MAXT) void residual_norm_fwd_kernel(ResidualNormArg
 }
 
 // The workgroup's sums for its columns, of the rows it holds at once, to its row of partial sums.
-__device__ __forceinline__ void put_sums(const ResidualNormArgs& a, const RowPlace& p, float* join, float* part,
+template <class P>
+__device__ __forceinline__ void put_sums(const ResidualNormArgs& a, const P& p, float* join, float* part,
                                          const float (&s)[8]) {
   if (a.rows_wg == 1) {
     store8<false>(part + p.col, p.n, s);
     return;
   }
   __syncthreads();
-  const int w = 512 * p.wpr;
+  const int w = 8 * p.L * p.wpr;
 #pragma unroll
   for (int e = 0; e < 8; ++e) join[p.rw * w + p.col + e] = s[e];
   __syncthreads();
@@ -205,17 +214,21 @@ __device__ __forceinline__ void put_sums(const ResidualNormArgs& a, const RowPla
   }
 }
 
-template <class XT, int MAXT>
-__global__ __launch_bounds__(MAXT) void residual_norm_bwd_kernel(ResidualNormArgs a) {
+// POST: with a norm of the branch.  Without one its sums' registers are free, and four waves fit a SIMD; with
+// one, two.  The widest rows take all 16 waves of a workgroup: there nothing is loaded ahead and gains are read again for
+// each row (KEEP false).
+template <class XT, int MAXT, bool POST, bool NARROW = false>
+__global__ __launch_bounds__(MAXT, POST && MAXT <= 512 ? 2 : 4) void residual_norm_bwd_kernel(ResidualNormArgs a) {
   __shared__ Shared sh;
   __shared__ float join[MAXT <= 512 ? MAXT * 8 : 8];
   int turn = 0;
-  const RowPlace p = row_place(a.wpr, a.d);
+  const RowPlace<NARROW> p(a.wpr, a.L, a.d);
   const DropConsts c = {(uint32_t)a.seed, (uint32_t)(a.seed >> 32), a.limit, a.up, a.step};
   const uint64_t step = drop_step(c);
   const float scale = a.beta * (c.limit ? c.up : 1.f), inv_d = 1.f / a.d;
   const int rows_wg = a.rows_wg, stride = gridDim.x * rows_wg;
-  const bool branch = a.post || a.dgate;  // the branch's rows are needed
+  constexpr bool KEEP = MAXT <= 512;
+  const bool branch = POST || a.dgate;  // the branch's rows are needed
   const XT* y = (const XT*)a.y;
   const XT* dy = (const XT*)a.dy;
   XT* dx = (XT*)a.dx;
@@ -233,19 +246,27 @@ __global__ __launch_bounds__(MAXT) void residual_norm_bwd_kernel(ResidualNormArg
     }
     if (dy) ndy = load8<false>(dy + (int64_t)row * a.lddy + p.col, n);
     if (branch) nf = load8<false>(a.f + (int64_t)row * a.ldf + p.col, n);
-    if (a.post) npost = make_float2(a.stats[at], a.stats[a.T + at]);
+    if (POST) npost = make_float2(a.stats[at], a.stats[a.T + at]);
   };
-  load(blockIdx.x * rows_wg + p.rw);
-  channels(a.g_pre, p, 1.f, g_pre);
-  channels(a.g_post, p, 1.f, g_post);
-  channels(a.b_post, p, 0.f, b_post);
-  channels(a.gate, p, 1.f, gate);
+  if (KEEP) load(blockIdx.x * rows_wg + p.rw);
+  const auto vectors = [&]() {
+    if (POST) {
+      channels(a.g_post, p, 1.f, g_post);
+      channels(a.b_post, p, 0.f, b_post);
+    }
+    channels(a.gate, p, 1.f, gate);
+  };
+  if (KEEP) {
+    channels(a.g_pre, p, 1.f, g_pre);
+    vectors();
+  }
   float s_gpre[8], s_bpre[8], s_gpost[8], s_bpost[8], s_gate[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) s_gpre[e] = s_bpre[e] = s_gpost[e] = s_bpost[e] = s_gate[e] = 0.f;
   for (int r0 = blockIdx.x * rows_wg; r0 < a.T; r0 += stride) {
     const int row = r0 + p.rw;
     const int n = row < a.T ? p.n : 0;
+    if (!KEEP) load(row);
     float t[8], yh[8], g[8], f[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) t[e] = yh[e] = g[e] = f[e] = 0.f;
@@ -256,8 +277,9 @@ __global__ __launch_bounds__(MAXT) void residual_norm_bwd_kernel(ResidualNormArg
     }
     if (branch) widen8(nf, f);
     const float2 st = nst, pst = npost;
-    load(row + stride);
+    if (KEEP) load(row + stride);
     if (a.pre) {
+      if (!KEEP) channels(a.g_pre, p, 1.f, g_pre);
       float s0 = 0.f, s1 = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -278,7 +300,8 @@ __global__ __launch_bounds__(MAXT) void residual_norm_bwd_kernel(ResidualNormArg
     store8<false>(dx + (int64_t)row * a.lddx + p.col, n, g);
     float m[8];
     branch_factors(a, c, step, row, p, scale, m);
-    if (a.post) {
+    if (POST) {
+      if (!KEEP) vectors();
       float s0 = 0.f, s1 = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -297,6 +320,7 @@ __global__ __launch_bounds__(MAXT) void residual_norm_bwd_kernel(ResidualNormArg
 #pragma unroll
       for (int e = 0; e < 8; ++e) t[e] = pst.y * (t[e] - m0 - f[e] * m1);
     } else {
+      if (!KEEP) vectors();
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float tm = e < n && m[e] != 0.f ? t[e] * m[e] : 0.f;
@@ -309,8 +333,8 @@ __global__ __launch_bounds__(MAXT) void residual_norm_bwd_kernel(ResidualNormArg
   float* part = a.ws + (int64_t)blockIdx.x * a.sums * a.d;
   if (a.dg_pre) put_sums(a, p, join, part, s_gpre), part += a.d;
   if (a.db_pre) put_sums(a, p, join, part, s_bpre), part += a.d;
-  if (a.dg_post) put_sums(a, p, join, part, s_gpost), part += a.d;
-  if (a.db_post) put_sums(a, p, join, part, s_bpost), part += a.d;
+  if (POST && a.dg_post) put_sums(a, p, join, part, s_gpost), part += a.d;
+  if (POST && a.db_post) put_sums(a, p, join, part, s_bpost), part += a.d;
   if (a.dgate) put_sums(a, p, join, part, s_gate);
 }
 
@@ -339,10 +363,14 @@ __global__ __launch_bounds__(1024) void residual_norm_sums_kernel(const float* _
 }
 
 int waves_of_row(int d) { return (d + 511) / 512; }
+int lanes_of_row(int d) { return d > 256 ? 64 : d > 128 ? 32 : d > 64 ? 16 : 8; }
 
-// Rows that a backward workgroup holds at once: eight waves of them (16 for rows of more than eight).
-int bwd_rows_wg(int d) { return std::max(1, 8 / waves_of_row(d)); }
-int bwd_groups(int T, int d) { return std::min(CUS, sat_cdiv(T, bwd_rows_wg(d))); }
+// Rows that a backward workgroup holds at once, of eight waves (16 for rows of more than eight), and workgroups:
+// as many as the registers leave room for.
+int bwd_rows_wg(int d) { return std::max(1, 8 / waves_of_row(d)) * (64 / lanes_of_row(d)); }
+int bwd_groups(int T, int d, bool post) {
+  return std::min(CUS * (post || waves_of_row(d) > 8 ? 1 : 2), sat_cdiv(T, bwd_rows_wg(d)));
+}
 
 int sum_outputs(const ResidualNormArgs& a, SumOut* o) {
   int n = 0;
@@ -353,17 +381,23 @@ int sum_outputs(const ResidualNormArgs& a, SumOut* o) {
 
 }  // namespace
 
-int64_t residual_norm_ws(int T, int d, int sums) { return (int64_t)bwd_groups(T, d) * sums * d; }
+int64_t residual_norm_ws(int T, int d, bool post, int sums) { return (int64_t)bwd_groups(T, d, post) * sums * d; }
 
 hipError_t launch_residual_norm_fwd(ResidualNormArgs a, bool f32, hipStream_t s) {
   if (a.T == 0) return hipSuccess;
   a.wpr = waves_of_row(a.d);
-  a.rows_wg = std::max(1, 4 / a.wpr);
-  const int threads = 64 * a.wpr * a.rows_wg;
+  a.L = lanes_of_row(a.d);
+  const int lines = std::max(1, 4 / a.wpr);  // of waves
+  a.rows_wg = lines * (64 / a.L);
+  const int threads = 64 * a.wpr * lines;
   const dim3 grid(std::min(sat_cdiv(a.T, a.rows_wg), CUS * std::max(1, 1024 / threads)));
-  const auto kernel = threads <= 256   ? (f32 ? residual_norm_fwd_kernel<float, 256> : residual_norm_fwd_kernel<bf16, 256>)
-                      : threads <= 512 ? (f32 ? residual_norm_fwd_kernel<float, 512> : residual_norm_fwd_kernel<bf16, 512>)
-                                       : (f32 ? residual_norm_fwd_kernel<float, 1024> : residual_norm_fwd_kernel<bf16, 1024>);
+  const auto pick = [&](auto narrow, auto small, auto middle, auto wide) {
+    return a.L < 64 ? narrow : threads <= 256 ? small : threads <= 512 ? middle : wide;
+  };
+  const auto kernel = f32 ? pick(residual_norm_fwd_kernel<float, 256, true>, residual_norm_fwd_kernel<float, 256>,
+                                 residual_norm_fwd_kernel<float, 512>, residual_norm_fwd_kernel<float, 1024>)
+                          : pick(residual_norm_fwd_kernel<bf16, 256, true>, residual_norm_fwd_kernel<bf16, 256>,
+                                 residual_norm_fwd_kernel<bf16, 512>, residual_norm_fwd_kernel<bf16, 1024>);
   hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
   return hipGetLastError();
 }
@@ -372,11 +406,20 @@ hipError_t launch_residual_norm_bwd(ResidualNormArgs a, bool f32, hipStream_t s)
   SumOut o;
   a.sums = sum_outputs(a, &o);
   a.wpr = waves_of_row(a.d);
+  a.L = lanes_of_row(a.d);
   a.rows_wg = bwd_rows_wg(a.d);
-  const int threads = 64 * a.wpr * a.rows_wg, G = bwd_groups(a.T, a.d);
+  const int threads = a.wpr * a.L * a.rows_wg, G = bwd_groups(a.T, a.d, a.post);
   if (G > 0) {
-    const auto kernel = threads <= 512 ? (f32 ? residual_norm_bwd_kernel<float, 512> : residual_norm_bwd_kernel<bf16, 512>)
-                                       : (f32 ? residual_norm_bwd_kernel<float, 1024> : residual_norm_bwd_kernel<bf16, 1024>);
+    const auto pick = [&](auto narrow, auto middle, auto wide) { return a.L < 64 ? narrow : threads <= 512 ? middle : wide; };
+    const auto kernel =
+        a.post ? (f32 ? pick(residual_norm_bwd_kernel<float, 512, true, true>, residual_norm_bwd_kernel<float, 512, true>,
+                             residual_norm_bwd_kernel<float, 1024, true>)
+                      : pick(residual_norm_bwd_kernel<bf16, 512, true, true>, residual_norm_bwd_kernel<bf16, 512, true>,
+                             residual_norm_bwd_kernel<bf16, 1024, true>))
+               : (f32 ? pick(residual_norm_bwd_kernel<float, 512, false, true>, residual_norm_bwd_kernel<float, 512, false>,
+                             residual_norm_bwd_kernel<float, 1024, false>)
+                      : pick(residual_norm_bwd_kernel<bf16, 512, false, true>, residual_norm_bwd_kernel<bf16, 512, false>,
+                             residual_norm_bwd_kernel<bf16, 1024, false>));
     hipLaunchKernelGGL(kernel, dim3(G), dim3(threads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -97,17 +97,21 @@ __device__ __forceinline__ void store8(float* p, int n, const float (&x)[8]) {
     if (e < n) p[e] = x[e];
 }
 
-// Sum over the wave on the vector unit, in every lane: lanes 1 and 2 away, 4 and 8 around the row of 16,
-// then the rows and the halves.
-__device__ __forceinline__ float wave_total(float v) {
-  auto step = [&](int o) { return __int_as_float(o); };
-  const auto i = [](float x) { return __float_as_int(x); };
-  v += step(__builtin_amdgcn_update_dpp(0, i(v), 0xB1, 15, 15, true));
-  v += step(__builtin_amdgcn_update_dpp(0, i(v), 0x4E, 15, 15, true));
-  v += step(__builtin_amdgcn_update_dpp(0, i(v), 0x124, 15, 15, true));
-  v += step(__builtin_amdgcn_update_dpp(0, i(v), 0x128, 15, 15, true));
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(h[0]) + __uint_as_float(h[1]);
+// Sum over each group of L lanes (8, 16, 32 or 64) on the vector unit, in every lane: lanes 1 and 2 away, the mirror images
+// in 8 and 16, then the rows of 16 and the halves.
+__device__ __forceinline__ float group_total(float v, int L) {
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 15, 15, true));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 15, 15, true));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 15, 15, true));
+  if (L >= 16) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 15, 15, true));
+  if (L >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if (L >= 64) {
+    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+  }
+  return v;
 }
+__device__ __forceinline__ float wave_total(float v) { return group_total(v, 64); }

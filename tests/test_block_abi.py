@@ -76,7 +76,7 @@ def test_residual_norm_refusals(bad):
 
 @pytest.mark.parametrize("bad", SHARED + [
     dict(dh=None), dict(y=None), dict(f=None), dict(dx=None), dict(df=None), dict(dy=P + 2), dict(dx=P + 2), dict(df=P + 1), dict(lddx=63),
-    dict(lddf=63), dict(lddh=63), dict(lddy=63), dict(dx=8 * P, lddx=72), dict(gate=None), dict(ws=None), dict(ws_elems=9 * 2 * 64 // 8 - 1),
+    dict(lddf=63), dict(lddh=63), dict(lddy=63), dict(dx=8 * P, lddx=72), dict(gate=None), dict(ws=None), dict(ws_elems=127),  # one workgroup's two sums of 64
     dict(dgate=P + 2), dict(db_post=P + 1), dict(post=0, g_post=None, db_post=P),
 ])
 def test_residual_norm_backward_refusals(bad):
