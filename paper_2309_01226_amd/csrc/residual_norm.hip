@@ -55,6 +55,12 @@ struct Shared {
   float2 part[2][16];
 };
 
+// What a wave wrote to LDS is there for all; the next row's loads stay in flight.
+__device__ __forceinline__ void share() {
+  wait_lgkm0();
+  cta_barrier();
+}
+
 // Sums of a and b over the row.
 template <bool NARROW>
 __device__ __forceinline__ float2 row_sums(const RowPlace<NARROW>& p, Shared& sh, int& turn, float a, float b) {
@@ -63,7 +69,7 @@ __device__ __forceinline__ float2 row_sums(const RowPlace<NARROW>& p, Shared& sh
   float2* part = sh.part[turn];
   turn ^= 1;
   if ((threadIdx.x & 63) == 0) part[p.at + p.wave] = s;
-  __syncthreads();
+  share();
   s = make_float2(0.f, 0.f);
   for (int i = 0; i < p.wpr; ++i) {
     const float2 q = part[p.at + i];
@@ -95,7 +101,7 @@ __device__ __forceinline__ float2 row_stats(const RowPlace<NARROW>& p, Shared& s
     float2* part = sh.part[turn];
     turn ^= 1;
     if ((threadIdx.x & 63) == 0) part[p.at + p.wave] = make_float2(mean, m2);
-    __syncthreads();
+    share();
     mean = m2 = 0.f;
     for (int i = 0; i < p.wpr; ++i) mean += part[p.at + i].x * width(i);
     mean /= d;
@@ -105,6 +111,78 @@ __device__ __forceinline__ float2 row_stats(const RowPlace<NARROW>& p, Shared& s
     }
   }
   return make_float2(mean, rsqrtf(m2 / d + eps));
+}
+
+// Rows of a matrix that begin at row r0 for the workgroup, this thread's eight columns of its row; nothing where `on` is
+// false or the row is not there.  FAST: rows are whole 16-byte pieces, and an access that is not wanted has an
+// offset past the end of the buffer, for which the hardware reads zeros and writes nothing.  So no access
+// stands behind a branch and the compiler's waits count exactly: the next row's loads stay in flight over the
+// whole row (with branches it has to wait for them at once: 16384 rows of 4096, backward, 280 us instead of 229).
+constexpr uint32_t NOWHERE = 0x80000000u;
+template <class T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const T* p) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)p, (short)0, 0x7FFFFFFF, 0x00020000);
+}
+template <bool NARROW, class T>
+__device__ __forceinline__ uint32_t place(const RowPlace<NARROW>& p, int64_t ld, int n) {
+  return n > 0 ? (uint32_t)(((NARROW ? p.rw * (int)ld : 0) + p.col) * (int)sizeof(T)) : NOWHERE;
+}
+template <bool FAST, bool NARROW, class T>
+__device__ __forceinline__ Raw8<T> get(const RowPlace<NARROW>& p, const T* m, int64_t ld, int r0, int rows, bool on) {
+  const int row = r0 + p.rw, n = on && row < rows ? p.n : 0;
+  if constexpr (!FAST) return load8<false>(m + (int64_t)row * ld + p.col, n);
+  const __amdgpu_buffer_rsrc_t b = buffer(m + (int64_t)(NARROW ? r0 : row) * ld);
+  const uint32_t o = place<NARROW, T>(p, ld, n);
+  Raw8<T> r;
+  if constexpr (sizeof(T) == 2) {
+    r.w = __builtin_amdgcn_raw_buffer_load_b128(b, o, 0, 0);
+  } else {
+    r.w[0] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(b, o, 0, 0));
+    r.w[1] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(b, o, 16, 0));
+  }
+  return r;
+}
+template <bool FAST, bool NARROW, class T>
+__device__ __forceinline__ void put(const RowPlace<NARROW>& p, T* m, int64_t ld, int r0, int rows, bool on, const float (&x)[8]) {
+  const int row = r0 + p.rw, n = on && row < rows ? p.n : 0;
+  if constexpr (!FAST) {
+    store8<false>(m + (int64_t)row * ld + p.col, n, x);
+    return;
+  }
+  const __amdgpu_buffer_rsrc_t b = buffer(m + (int64_t)(NARROW ? r0 : row) * ld);
+  const uint32_t o = place<NARROW, T>(p, ld, n);
+  if constexpr (sizeof(T) == 2) {
+    bf16x8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = f2bf(x[e]);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, y), b, o, 0, 0);
+  } else {
+    const floatx4 lo = {x[0], x[1], x[2], x[3]}, hi = {x[4], x[5], x[6], x[7]};
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), b, o, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), b, o, 16, 0);
+  }
+}
+// The row's pair of statistics, 0 for the branch's norm and 2 for the next one's.
+template <bool FAST, bool NARROW>
+__device__ __forceinline__ float2 get_stats(const RowPlace<NARROW>& p, const float* stats, int which, int r0, int rows, bool on) {
+  const int row = r0 + p.rw;
+  const float* s = stats + (int64_t)which * rows + r0;
+  if constexpr (!FAST) return on && row < rows ? make_float2(s[p.rw], s[rows + p.rw]) : make_float2(0.f, 0.f);
+  const uint32_t o = on && row < rows ? (uint32_t)p.rw * 4 : NOWHERE;
+  return make_float2(__uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer(s), o, 0, 0)),
+                     __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer(s + rows), o, 0, 0)));
+}
+template <bool FAST, bool NARROW>
+__device__ __forceinline__ void put_stats(const RowPlace<NARROW>& p, float* stats, int which, int r0, int rows, bool on, float2 v) {
+  const bool me = on && p.col == 0 && r0 + p.rw < rows;
+  float* s = stats + (int64_t)which * rows + r0;
+  if constexpr (!FAST) {
+    if (me) s[p.rw] = v.x, s[rows + p.rw] = v.y;
+    return;
+  }
+  const uint32_t o = me ? (uint32_t)p.rw * 4 : NOWHERE;
+  __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v.x), buffer(s), o, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v.y), buffer(s + rows), o, 0, 0);
 }
 
 // Columns of a vector for each channel, or `none` without one.
@@ -132,7 +210,7 @@ __device__ __forceinline__ void branch_factors(const ResidualNormArgs& a, const 
   for (int e = 0; e < 8; ++e) m[e] = drop_keeps(c, r, e) ? scale : 0.f;
 }
 
-template <class XT, int MAXT, bool NARROW = false>
+template <class XT, int MAXT, bool FAST, bool NARROW = false>
 __global__ __launch_bounds__(MAXT) void residual_norm_fwd_kernel(ResidualNormArgs a) {
   __shared__ Shared sh;
   int turn = 0;
@@ -140,57 +218,61 @@ __global__ __launch_bounds__(MAXT) void residual_norm_fwd_kernel(ResidualNormArg
   const DropConsts c = {(uint32_t)a.seed, (uint32_t)(a.seed >> 32), a.limit, a.up, a.step};
   const uint64_t step = drop_step(c);
   const float scale = a.beta * (c.limit ? c.up : 1.f);
-  const int rows_wg = a.rows_wg, stride = gridDim.x * rows_wg;
+  const int rows_wg = a.rows_wg, stride = gridDim.x * rows_wg, T = a.T;
   const XT* x = (const XT*)a.x;
   XT* y = (XT*)a.y;
+  const bool pre = a.pre != 0, post = a.post != 0;
   float g_pre[8], b_pre[8], g_post[8], b_post[8], gate[8];
-  Raw8<XT> nx;
-  Raw8<bf16> nf;
-  auto load = [&](int row) {
-    const int n = row < a.T ? p.n : 0;
-    nx = load8<false>(x + (int64_t)row * a.ldx + p.col, n);
-    nf = load8<false>(a.f + (int64_t)row * a.ldf + p.col, n);
-  };
-  load(blockIdx.x * rows_wg + p.rw);
   channels(a.g_pre, p, 1.f, g_pre);
   channels(a.b_pre, p, 0.f, b_pre);
   channels(a.g_post, p, 1.f, g_post);
   channels(a.b_post, p, 0.f, b_post);
   channels(a.gate, p, 1.f, gate);
-  for (int r0 = blockIdx.x * rows_wg; r0 < a.T; r0 += stride) {
+  Raw8<XT> nx;
+  Raw8<bf16> nf;
+  auto load = [&](int r0) {
+    nx = get<FAST>(p, x, a.ldx, r0, T, true);
+    nf = get<FAST>(p, a.f, a.ldf, r0, T, true);
+  };
+  // a row's outputs, in the order of the loop below; before the loop for no row, so that as many accesses follow
+  // the first loads as the others
+  const float none[8] = {};
+  load(blockIdx.x * rows_wg);
+  if (FAST) {
+    put_stats<FAST>(p, a.stats, 0, 0, 0, false, make_float2(0.f, 0.f));
+    put<FAST>(p, y, a.ldy, 0, 0, false, none);
+    put<FAST>(p, a.h, a.ldh, 0, 0, false, none);
+    put_stats<FAST>(p, a.stats, 2, 0, 0, false, make_float2(0.f, 0.f));
+  }
+  for (int r0 = blockIdx.x * rows_wg; r0 < T; r0 += stride) {
     const int row = r0 + p.rw;
-    const int n = row < a.T ? p.n : 0;
+    const int n = row < T ? p.n : 0;
     float v[8], u[8];
     widen8(nx, v);
     widen8(nf, u);
-    load(row + stride);
-    if (a.post) {
-      const float2 st = row_stats(p, sh, turn, u, a.post, a.d, a.eps);
+    load(r0 + stride);
+    float2 st = make_float2(0.f, 0.f);
+    if (post) {
+      st = row_stats(p, sh, turn, u, a.post, a.d, a.eps);
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[e] = (u[e] - st.x) * st.y * g_post[e] + b_post[e];
-      if (p.col == 0 && row < a.T) {
-        a.stats[row] = st.x;
-        a.stats[a.T + row] = st.y;
-      }
     }
+    put_stats<FAST>(p, a.stats, 0, r0, T, post, st);
     float m[8];
     branch_factors(a, c, step, row, p, scale, m);
     // a dropped element adds nothing, whatever the branch holds there
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = a.alpha * v[e] + (m[e] != 0.f ? m[e] * gate[e] * u[e] : 0.f);
-    store8<false>(y + (int64_t)row * a.ldy + p.col, n, v);
-    if (a.pre) {
+    put<FAST>(p, y, a.ldy, r0, T, true, v);
+    if (pre) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = e < n ? (float)(XT)v[e] : 0.f;
-      const float2 st = row_stats(p, sh, turn, v, a.pre, a.d, a.eps);
+      st = row_stats(p, sh, turn, v, a.pre, a.d, a.eps);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = (v[e] - st.x) * st.y * g_pre[e] + b_pre[e];
-      store8<false>(a.h + (int64_t)row * a.ldh + p.col, n, v);
-      if (p.col == 0 && row < a.T) {
-        a.stats[2 * (int64_t)a.T + row] = st.x;
-        a.stats[3 * (int64_t)a.T + row] = st.y;
-      }
     }
+    put<FAST>(p, a.h, a.ldh, r0, T, pre, v);
+    put_stats<FAST>(p, a.stats, 2, r0, T, pre, st);
   }
 }
 
@@ -215,40 +297,24 @@ __device__ __forceinline__ void put_sums(const ResidualNormArgs& a, const P& p, 
 }
 
 // POST: with a norm of the branch.  Without one its sums' registers are free, and four waves fit a SIMD; with
-// one, two.  The widest rows take all 16 waves of a workgroup: there nothing is loaded ahead and gains are read again for
-// each row (KEEP false).
-template <class XT, int MAXT, bool POST, bool NARROW = false>
-__global__ __launch_bounds__(MAXT, POST && MAXT <= 512 ? 2 : 4) void residual_norm_bwd_kernel(ResidualNormArgs a) {
+// one, three, or two of rows of eight waves.  The widest rows take all 16 waves of a workgroup: there nothing is loaded
+// ahead and gains are read again for each row (KEEP false).
+template <class XT, int MAXT, bool POST, bool FAST, bool NARROW = false>
+__global__ __launch_bounds__(MAXT, !POST || MAXT > 768 ? 4 : MAXT > 512 ? 3 : 2) void residual_norm_bwd_kernel(ResidualNormArgs a) {
   __shared__ Shared sh;
-  __shared__ float join[MAXT <= 512 ? MAXT * 8 : 8];
+  __shared__ float join[MAXT * 8];
+  constexpr bool KEEP = FAST && MAXT <= 768;
   int turn = 0;
   const RowPlace<NARROW> p(a.wpr, a.L, a.d);
   const DropConsts c = {(uint32_t)a.seed, (uint32_t)(a.seed >> 32), a.limit, a.up, a.step};
   const uint64_t step = drop_step(c);
   const float scale = a.beta * (c.limit ? c.up : 1.f), inv_d = 1.f / a.d;
-  const int rows_wg = a.rows_wg, stride = gridDim.x * rows_wg;
-  constexpr bool KEEP = MAXT <= 512;
-  const bool branch = POST || a.dgate;  // the branch's rows are needed
+  const int rows_wg = a.rows_wg, stride = gridDim.x * rows_wg, T = a.T;
+  const bool pre = a.pre != 0, branch = POST || a.dgate;  // whether the branch's rows are needed
   const XT* y = (const XT*)a.y;
   const XT* dy = (const XT*)a.dy;
   XT* dx = (XT*)a.dx;
   float g_pre[8], g_post[8], b_post[8], gate[8];
-  Raw8<XT> ny, ndy;
-  Raw8<bf16> nf, ndh;
-  float2 nst = make_float2(0.f, 0.f), npost = make_float2(0.f, 0.f);
-  auto load = [&](int row) {
-    const int n = row < a.T ? p.n : 0;
-    const int at = min(row, a.T - 1);
-    if (a.pre) {
-      ny = load8<false>(y + (int64_t)row * a.ldy + p.col, n);
-      ndh = load8<false>(a.dh + (int64_t)row * a.lddh + p.col, n);
-      nst = make_float2(a.stats[2 * (int64_t)a.T + at], a.stats[3 * (int64_t)a.T + at]);
-    }
-    if (dy) ndy = load8<false>(dy + (int64_t)row * a.lddy + p.col, n);
-    if (branch) nf = load8<false>(a.f + (int64_t)row * a.ldf + p.col, n);
-    if (POST) npost = make_float2(a.stats[at], a.stats[a.T + at]);
-  };
-  if (KEEP) load(blockIdx.x * rows_wg + p.rw);
   const auto vectors = [&]() {
     if (POST) {
       channels(a.g_post, p, 1.f, g_post);
@@ -260,25 +326,39 @@ __global__ __launch_bounds__(MAXT, POST && MAXT <= 512 ? 2 : 4) void residual_no
     channels(a.g_pre, p, 1.f, g_pre);
     vectors();
   }
+  Raw8<XT> ny, ndy;
+  Raw8<bf16> nf, ndh;
+  float2 nst, npost;
+  auto load = [&](int r0) {
+    ny = get<FAST>(p, y, a.ldy, r0, T, pre);
+    ndh = get<FAST>(p, a.dh, a.lddh, r0, T, pre);
+    nst = get_stats<FAST>(p, a.stats, 2, r0, T, pre);
+    ndy = get<FAST>(p, dy, a.lddy, r0, T, dy != nullptr);
+    nf = get<FAST>(p, a.f, a.ldf, r0, T, branch);
+    npost = get_stats<FAST>(p, a.stats, 0, r0, T, POST);
+  };
+  if (KEEP) {
+    load(blockIdx.x * rows_wg);
+    // as many accesses after the first loads as after the others
+    const float none[8] = {};
+    put<FAST>(p, dx, a.lddx, 0, 0, false, none);
+    put<FAST>(p, a.df, a.lddf, 0, 0, false, none);
+  }
   float s_gpre[8], s_bpre[8], s_gpost[8], s_bpost[8], s_gate[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) s_gpre[e] = s_bpre[e] = s_gpost[e] = s_bpost[e] = s_gate[e] = 0.f;
-  for (int r0 = blockIdx.x * rows_wg; r0 < a.T; r0 += stride) {
+  for (int r0 = blockIdx.x * rows_wg; r0 < T; r0 += stride) {
     const int row = r0 + p.rw;
-    const int n = row < a.T ? p.n : 0;
-    if (!KEEP) load(row);
+    const int n = row < T ? p.n : 0;
+    if (!KEEP) load(r0);
     float t[8], yh[8], g[8], f[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = yh[e] = g[e] = f[e] = 0.f;
-    if (dy) widen8(ndy, t);
-    if (a.pre) {
-      widen8(ny, yh);
-      widen8(ndh, g);
-    }
-    if (branch) widen8(nf, f);
+    widen8(ndy, t);
+    widen8(ny, yh);
+    widen8(ndh, g);
+    widen8(nf, f);
     const float2 st = nst, pst = npost;
-    if (KEEP) load(row + stride);
-    if (a.pre) {
+    if (KEEP) load(r0 + stride);
+    if (pre) {
       if (!KEEP) channels(a.g_pre, p, 1.f, g_pre);
       float s0 = 0.f, s1 = 0.f;
 #pragma unroll
@@ -297,7 +377,7 @@ __global__ __launch_bounds__(MAXT, POST && MAXT <= 512 ? 2 : 4) void residual_no
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) g[e] = a.alpha * t[e];
-    store8<false>(dx + (int64_t)row * a.lddx + p.col, n, g);
+    put<FAST>(p, dx, a.lddx, r0, T, true, g);
     float m[8];
     branch_factors(a, c, step, row, p, scale, m);
     if (POST) {
@@ -328,7 +408,7 @@ __global__ __launch_bounds__(MAXT, POST && MAXT <= 512 ? 2 : 4) void residual_no
         t[e] = tm * gate[e];
       }
     }
-    store8<false>(a.df + (int64_t)row * a.lddf + p.col, n, t);
+    put<FAST>(p, a.df, a.lddf, r0, T, true, t);
   }
   float* part = a.ws + (int64_t)blockIdx.x * a.sums * a.d;
   if (a.dg_pre) put_sums(a, p, join, part, s_gpre), part += a.d;
@@ -365,11 +445,39 @@ __global__ __launch_bounds__(1024) void residual_norm_sums_kernel(const float* _
 int waves_of_row(int d) { return (d + 511) / 512; }
 int lanes_of_row(int d) { return d > 256 ? 64 : d > 128 ? 32 : d > 64 ? 16 : 8; }
 
-// Rows that a backward workgroup holds at once, of eight waves (16 for rows of more than eight), and workgroups:
-// as many as the registers leave room for.
-int bwd_rows_wg(int d) { return std::max(1, 8 / waves_of_row(d)) * (64 / lanes_of_row(d)); }
-int bwd_groups(int T, int d, bool post) {
-  return std::min(CUS * (post || waves_of_row(d) > 8 ? 1 : 2), sat_cdiv(T, bwd_rows_wg(d)));
+// A backward workgroup: its most threads by the kernel's registers, rows of waves in it, and workgroups on a CU.
+struct BwdShape {
+  int most, lines, per_cu;
+};
+BwdShape bwd_shape(int d, bool post, bool fast) {
+  const int w = waves_of_row(d);
+  if (d <= 256) return post ? BwdShape{768, 12, 1} : BwdShape{512, 8, 2};
+  if (!fast || w > 12) return {1024, std::max(1, 16 / w), 1};
+  if (!post) return w > 8 || 8 % w ? BwdShape{1024, std::max(1, 16 / w), 1} : BwdShape{512, 8 / w, 2};
+  return w == 7 || w == 8 ? BwdShape{512, 1, 1} : BwdShape{768, 12 / w, 1};
+}
+int bwd_rows_wg(int d, const BwdShape& b) { return b.lines * (64 / lanes_of_row(d)); }
+int bwd_groups(int T, int d, const BwdShape& b) { return std::min(CUS * b.per_cu, sat_cdiv(T, bwd_rows_wg(d, b))); }
+
+using Kernel = void (*)(ResidualNormArgs);
+template <class XT, bool FAST>
+Kernel fwd_kernel(int L, int threads) {
+  if (L < 64) return residual_norm_fwd_kernel<XT, 256, FAST, true>;
+  if constexpr (FAST) {
+    if (threads <= 256) return residual_norm_fwd_kernel<XT, 256, true>;
+    if (threads <= 512) return residual_norm_fwd_kernel<XT, 512, true>;
+  }
+  return residual_norm_fwd_kernel<XT, 1024, FAST>;
+}
+template <class XT, bool POST, bool FAST>
+Kernel bwd_kernel(int L, int most) {
+  if (L < 64) return residual_norm_bwd_kernel<XT, POST ? 768 : 512, POST, FAST, true>;
+  if constexpr (FAST) {
+    if (most == 512) return residual_norm_bwd_kernel<XT, 512, POST, true>;
+    if constexpr (POST)
+      if (most == 768) return residual_norm_bwd_kernel<XT, 768, true, true>;
+  }
+  return residual_norm_bwd_kernel<XT, 1024, POST, FAST>;
 }
 
 int sum_outputs(const ResidualNormArgs& a, SumOut* o) {
@@ -381,7 +489,31 @@ int sum_outputs(const ResidualNormArgs& a, SumOut* o) {
 
 }  // namespace
 
-int64_t residual_norm_ws(int T, int d, bool post, int sums) { return (int64_t)bwd_groups(T, d, post) * sums * d; }
+// (the same for either way of access, so that alignment does not matter to the caller)
+int64_t residual_norm_ws(int T, int d, bool post, int sums) {
+  return (int64_t)std::max(bwd_groups(T, d, bwd_shape(d, post, true)), bwd_groups(T, d, bwd_shape(d, post, false))) * sums * d;
+}
+
+// Whether rows are whole 16-byte pieces, of every array that is there.
+static bool fast_rows(const ResidualNormArgs& a, bool f32, bool back) {
+  bool ok = a.d % 8 == 0;
+  const auto rows = [&](const void* p, int64_t ld, int size) {
+    if (p != nullptr) ok = ok && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0 && ld < (1 << 21);
+  };
+  const int size = f32 ? 4 : 2;
+  rows(a.y, a.ldy, size);
+  rows(a.f, a.ldf, 2);
+  if (back) {
+    rows(a.dy, a.lddy, size);
+    rows(a.dx, a.lddx, size);
+    rows(a.dh, a.lddh, 2);
+    rows(a.df, a.lddf, 2);
+  } else {
+    rows(a.x, a.ldx, size);
+    rows(a.h, a.ldh, 2);
+  }
+  return ok;
+}
 
 hipError_t launch_residual_norm_fwd(ResidualNormArgs a, bool f32, hipStream_t s) {
   if (a.T == 0) return hipSuccess;
@@ -391,13 +523,8 @@ hipError_t launch_residual_norm_fwd(ResidualNormArgs a, bool f32, hipStream_t s)
   a.rows_wg = lines * (64 / a.L);
   const int threads = 64 * a.wpr * lines;
   const dim3 grid(std::min(sat_cdiv(a.T, a.rows_wg), CUS * std::max(1, 1024 / threads)));
-  const auto pick = [&](auto narrow, auto small, auto middle, auto wide) {
-    return a.L < 64 ? narrow : threads <= 256 ? small : threads <= 512 ? middle : wide;
-  };
-  const auto kernel = f32 ? pick(residual_norm_fwd_kernel<float, 256, true>, residual_norm_fwd_kernel<float, 256>,
-                                 residual_norm_fwd_kernel<float, 512>, residual_norm_fwd_kernel<float, 1024>)
-                          : pick(residual_norm_fwd_kernel<bf16, 256, true>, residual_norm_fwd_kernel<bf16, 256>,
-                                 residual_norm_fwd_kernel<bf16, 512>, residual_norm_fwd_kernel<bf16, 1024>);
+  const auto kernel = fast_rows(a, f32, false) ? (f32 ? fwd_kernel<float, true>(a.L, threads) : fwd_kernel<bf16, true>(a.L, threads))
+                                               : (f32 ? fwd_kernel<float, false>(a.L, threads) : fwd_kernel<bf16, false>(a.L, threads));
   hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
   return hipGetLastError();
 }
@@ -407,19 +534,15 @@ hipError_t launch_residual_norm_bwd(ResidualNormArgs a, bool f32, hipStream_t s)
   a.sums = sum_outputs(a, &o);
   a.wpr = waves_of_row(a.d);
   a.L = lanes_of_row(a.d);
-  a.rows_wg = bwd_rows_wg(a.d);
-  const int threads = a.wpr * a.L * a.rows_wg, G = bwd_groups(a.T, a.d, a.post);
+  const bool fast = fast_rows(a, f32, true);
+  const BwdShape shape = bwd_shape(a.d, a.post, fast);
+  a.rows_wg = bwd_rows_wg(a.d, shape);
+  const int threads = 64 * a.wpr * shape.lines, G = bwd_groups(a.T, a.d, shape);
   if (G > 0) {
-    const auto pick = [&](auto narrow, auto middle, auto wide) { return a.L < 64 ? narrow : threads <= 512 ? middle : wide; };
-    const auto kernel =
-        a.post ? (f32 ? pick(residual_norm_bwd_kernel<float, 512, true, true>, residual_norm_bwd_kernel<float, 512, true>,
-                             residual_norm_bwd_kernel<float, 1024, true>)
-                      : pick(residual_norm_bwd_kernel<bf16, 512, true, true>, residual_norm_bwd_kernel<bf16, 512, true>,
-                             residual_norm_bwd_kernel<bf16, 1024, true>))
-               : (f32 ? pick(residual_norm_bwd_kernel<float, 512, false, true>, residual_norm_bwd_kernel<float, 512, false>,
-                             residual_norm_bwd_kernel<float, 1024, false>)
-                      : pick(residual_norm_bwd_kernel<bf16, 512, false, true>, residual_norm_bwd_kernel<bf16, 512, false>,
-                             residual_norm_bwd_kernel<bf16, 1024, false>));
+    const auto kernel = a.post ? (fast ? (f32 ? bwd_kernel<float, true, true>(a.L, shape.most) : bwd_kernel<bf16, true, true>(a.L, shape.most))
+                                       : (f32 ? bwd_kernel<float, true, false>(a.L, shape.most) : bwd_kernel<bf16, true, false>(a.L, shape.most)))
+                               : (fast ? (f32 ? bwd_kernel<float, false, true>(a.L, shape.most) : bwd_kernel<bf16, false, true>(a.L, shape.most))
+                                       : (f32 ? bwd_kernel<float, false, false>(a.L, shape.most) : bwd_kernel<bf16, false, false>(a.L, shape.most)));
     hipLaunchKernelGGL(kernel, dim3(G), dim3(threads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

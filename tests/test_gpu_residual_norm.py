@@ -52,11 +52,10 @@ def _wide(o):
 
 
 def _adds(T, d):
-    """Additions between a row's term and its sum over the rows: rows of a workgroup, those that it holds at once, 16 slices of workgroups."""
-    wpr = -(-d // 512)
-    rw = max(1, 8 // wpr)
-    G = min(256, -(-T // rw))
-    return -(-T // (G * rw)) + rw + -(-G // 16) + 16
+    """Additions between a row's term and its sum over the rows: at least 256 workgroups share the rows where there are more
+    than a workgroup holds at once, so a thread adds T / 256 + 1 of them at most; then the rows that a workgroup holds at
+    once (12 waves of 8 rows at most), a sixteenth of at most 512 workgroups, and the 16 slices of those."""
+    return T // 256 + 1 + 96 + 512 // 16 + 16
 
 
 def _case(T, d, dt, pre, post, gain=True, shift=True, gate=True, alpha=1.0, beta=1.0, p=0.1, width=0, inplace=False, nody=False):
