@@ -300,7 +300,7 @@ __device__ __forceinline__ void put_sums(const ResidualNormArgs& a, const P& p, 
 // one, three, or two of rows of eight waves.  The widest rows take all 16 waves of a workgroup: there nothing is loaded
 // ahead and gains are read again for each row (KEEP false).
 template <class XT, int MAXT, bool POST, bool FAST, bool NARROW = false>
-__global__ __launch_bounds__(MAXT, !POST || MAXT > 768 ? 4 : MAXT > 512 ? 3 : 2) void residual_norm_bwd_kernel(ResidualNormArgs a) {
+__global__ __launch_bounds__(MAXT, MAXT > 768 ? 4 : MAXT > 512 ? 3 : 2) void residual_norm_bwd_kernel(ResidualNormArgs a) {
   __shared__ Shared sh;
   __shared__ float join[MAXT * 8];
   constexpr bool KEEP = FAST && MAXT <= 768;
@@ -449,11 +449,10 @@ int lanes_of_row(int d) { return d > 256 ? 64 : d > 128 ? 32 : d > 64 ? 16 : 8; 
 struct BwdShape {
   int most, lines, per_cu;
 };
-BwdShape bwd_shape(int d, bool post, bool fast) {
+BwdShape bwd_shape(int d, bool fast) {
   const int w = waves_of_row(d);
-  if (d <= 256) return post ? BwdShape{768, 12, 1} : BwdShape{512, 8, 2};
+  if (d <= 256) return {768, 12, 1};
   if (!fast || w > 12) return {1024, std::max(1, 16 / w), 1};
-  if (!post) return w > 8 || 8 % w ? BwdShape{1024, std::max(1, 16 / w), 1} : BwdShape{512, 8 / w, 2};
   return w == 7 || w == 8 ? BwdShape{512, 1, 1} : BwdShape{768, 12 / w, 1};
 }
 int bwd_rows_wg(int d, const BwdShape& b) { return b.lines * (64 / lanes_of_row(d)); }
@@ -471,11 +470,10 @@ Kernel fwd_kernel(int L, int threads) {
 }
 template <class XT, bool POST, bool FAST>
 Kernel bwd_kernel(int L, int most) {
-  if (L < 64) return residual_norm_bwd_kernel<XT, POST ? 768 : 512, POST, FAST, true>;
+  if (L < 64) return residual_norm_bwd_kernel<XT, 768, POST, FAST, true>;
   if constexpr (FAST) {
     if (most == 512) return residual_norm_bwd_kernel<XT, 512, POST, true>;
-    if constexpr (POST)
-      if (most == 768) return residual_norm_bwd_kernel<XT, 768, true, true>;
+    if (most == 768) return residual_norm_bwd_kernel<XT, 768, POST, true>;
   }
   return residual_norm_bwd_kernel<XT, 1024, POST, FAST>;
 }
@@ -491,7 +489,7 @@ int sum_outputs(const ResidualNormArgs& a, SumOut* o) {
 
 // (the same for either way of access, so that alignment does not matter to the caller)
 int64_t residual_norm_ws(int T, int d, bool post, int sums) {
-  return (int64_t)std::max(bwd_groups(T, d, bwd_shape(d, post, true)), bwd_groups(T, d, bwd_shape(d, post, false))) * sums * d;
+  return (int64_t)std::max(bwd_groups(T, d, bwd_shape(d, true)), bwd_groups(T, d, bwd_shape(d, false))) * sums * d;
 }
 
 // Whether rows are whole 16-byte pieces, of every array that is there.
@@ -535,7 +533,7 @@ hipError_t launch_residual_norm_bwd(ResidualNormArgs a, bool f32, hipStream_t s)
   a.wpr = waves_of_row(a.d);
   a.L = lanes_of_row(a.d);
   const bool fast = fast_rows(a, f32, true);
-  const BwdShape shape = bwd_shape(a.d, a.post, fast);
+  const BwdShape shape = bwd_shape(a.d, fast);
   a.rows_wg = bwd_rows_wg(a.d, shape);
   const int threads = 64 * a.wpr * shape.lines, G = bwd_groups(a.T, a.d, shape);
   if (G > 0) {
