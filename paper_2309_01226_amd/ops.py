@@ -499,17 +499,6 @@ _BOUNDARY = struct.Struct("PqPqPqPq6P5i3fdQP" + "PqPqPqPq5PPq")
 assert _BOUNDARY.size == C.sizeof(_lib.sat_residual_norm_desc)
 
 
-def _boundary_desc(rows, stats, T, d, f32, dev, back, *, pre=None, post=None, g_pre=None, b_pre=None, g_post=None,
-                   b_post=None, gate=None, alpha=1.0, beta=1.0, eps=1e-5, p=0.0, seed=0, step=None):
-    """rows: address and leading dimension of x, f, y and h; back: the fields of the backward."""
-    f = torch.float32
-    return _lib.sat_residual_norm_desc.from_buffer_copy(_BOUNDARY.pack(
-        *rows, _vec(stats, f, "stats", 4 * T, dev), _vec(g_pre, f, "g_pre", d, dev), _vec(b_pre, f, "b_pre", d, dev),
-        _vec(g_post, f, "g_post", d, dev), _vec(b_post, f, "b_post", d, dev), _vec(gate, f, "gate", d, dev),
-        T, d, f32, _norm(pre, "pre"), _norm(post, "post"), alpha, beta, eps, p, _seed(seed),
-        _vec(step, torch.int64, "step", 1, dev), *back))
-
-
 def _norm(kind, name):
     if kind not in _NORMS:
         raise ValueError(f"{name}: {kind!r} is not None, 'layer' or 'rms'")
@@ -521,22 +510,39 @@ def _matrix(t, dtype, name, T, d, dev):
     return (0, d) if t is None else (t.data_ptr(), _rows_of(t, dtype, name, T, d, dev))
 
 
-def residual_norm_fwd(x, f, y, h, stats, d, **options):
+def _options(stats, T, d, f32, dev, pre, post, g_pre, b_pre, g_post, b_post, gate, alpha, beta, eps, p, seed, step):
+    """The fields of both directions' options (a None costs no call: a single row's launch is shorter than its host side)."""
+    f = torch.float32
+    return (0 if stats is None else _vec(stats, f, "stats", 4 * T, dev), 0 if g_pre is None else _vec(g_pre, f, "g_pre", d, dev),
+            0 if b_pre is None else _vec(b_pre, f, "b_pre", d, dev), 0 if g_post is None else _vec(g_post, f, "g_post", d, dev),
+            0 if b_post is None else _vec(b_post, f, "b_post", d, dev), 0 if gate is None else _vec(gate, f, "gate", d, dev),
+            T, d, f32, _norm(pre, "pre"), _norm(post, "post"), alpha, beta, eps, p, _seed(seed),
+            0 if step is None else _vec(step, torch.int64, "step", 1, dev))
+
+
+def residual_norm_fwd(x, f, y, h, stats, d, *, pre=None, post=None, g_pre=None, b_pre=None, g_post=None, b_post=None, gate=None,
+                      alpha=1.0, beta=1.0, eps=1e-5, p=0.0, seed=0, step=None):
     """The boundary of two sublayers in one pass: y = alpha x + beta gate dropout(norm(f)), h = norm(y), on rows of d columns.
     x, y [T, >= d]: the residual stream, both fp32 or both bf16, y may be x; f [T, >= d] bf16: the branch; h [T, >= d] bf16:
     the next sublayer's input (None without a norm for it); stats fp32 [4, T]: what the backward needs of the norms.
     Options, the same in the backward: pre, post (None, "layer" or "rms": the norms of y for h and of f), their gains and shifts
     g_pre, b_pre, g_post, b_post and the gate (fp32 [d] or None), alpha, beta, eps, and p, seed, step of the
     dropout.  See saturn_ops.h."""
-    dev, f32, T = _device(x, "x"), x.dtype == torch.float32, x.shape[0]
-    xt, bf = torch.float32 if f32 else torch.bfloat16, torch.bfloat16
-    rows = (*_matrix(x, xt, "x", T, d, dev), *_matrix(f, bf, "f", T, d, dev), *_matrix(y, xt, "y", T, d, dev),
-            *_matrix(h, bf, "h", T, d, dev))
-    desc = _boundary_desc(rows, stats, T, d, f32, dev, (0, d, 0, d, 0, d, 0, d, 0, 0, 0, 0, 0, 0, 0), **options)
+    dev, xt, bf, T = _device(x, "x"), x.dtype, torch.bfloat16, x.shape[0]
+    f32 = xt is torch.float32
+    if not f32:
+        xt = bf
+    desc = _lib.sat_residual_norm_desc.from_buffer_copy(_BOUNDARY.pack(
+        x.data_ptr(), _rows_of(x, xt, "x", T, d, dev), f.data_ptr(), _rows_of(f, bf, "f", T, d, dev),
+        y.data_ptr(), _rows_of(y, xt, "y", T, d, dev), *_matrix(h, bf, "h", T, d, dev),
+        *_options(stats, T, d, f32, dev, pre, post, g_pre, b_pre, g_post, b_post, gate, alpha, beta, eps, p, seed, step),
+        0, d, 0, d, 0, d, 0, d, 0, 0, 0, 0, 0, 0, 0))
     _lib.call("sat_op_residual_norm_fwd", desc, _stream(dev))
 
 
-def residual_norm_bwd(dy, dh, y, f, stats, dx, df, d, *, dg_pre=None, db_pre=None, dg_post=None, db_post=None, dgate=None, **options):
+def residual_norm_bwd(dy, dh, y, f, stats, dx, df, d, *, dg_pre=None, db_pre=None, dg_post=None, db_post=None, dgate=None,
+                      pre=None, post=None, g_pre=None, b_pre=None, g_post=None, b_post=None, gate=None, alpha=1.0, beta=1.0,
+                      eps=1e-5, p=0.0, seed=0, step=None):
     """Its backward from dy (the gradient of y along the stream, in its type, or None) and dh (of h, or None without that
     norm): writes dx (may be dy), df and the sums that are given, fp32 [d].  y, f and stats are the forward's; y may be None
     without pre, f without post and dgate.  The workspace comes from torch's allocator, on the current stream."""
@@ -544,12 +550,13 @@ def residual_norm_bwd(dy, dh, y, f, stats, dx, df, d, *, dg_pre=None, db_pre=Non
     xt, bf, f4 = torch.float32 if f32 else torch.bfloat16, torch.bfloat16, torch.float32
     sums = [_vec(t, f4, n, d, dev) for n, t in (("dg_pre", dg_pre), ("db_pre", db_pre), ("dg_post", dg_post), ("db_post", db_post),
                                                 ("dgate", dgate))]
-    need = _boundary_ws(T, d, options.get("post") is not None, 5 - sums.count(0))
+    need = _boundary_ws(T, d, post is not None, 5 - sums.count(0))
     ws = torch.empty(need, device=dx.device, dtype=f4) if need else None
-    back = (*_matrix(dy, xt, "dy", T, d, dev), *_matrix(dh, bf, "dh", T, d, dev), *_matrix(dx, xt, "dx", T, d, dev),
-            *_matrix(df, bf, "df", T, d, dev), *sums, 0 if ws is None else ws.data_ptr(), need)
-    rows = (0, d, *_matrix(f, bf, "f", T, d, dev), *_matrix(y, xt, "y", T, d, dev), 0, d)
-    desc = _boundary_desc(rows, stats, T, d, f32, dev, back, **options)
+    desc = _lib.sat_residual_norm_desc.from_buffer_copy(_BOUNDARY.pack(
+        0, d, *_matrix(f, bf, "f", T, d, dev), *_matrix(y, xt, "y", T, d, dev), 0, d,
+        *_options(stats, T, d, f32, dev, pre, post, g_pre, b_pre, g_post, b_post, gate, alpha, beta, eps, p, seed, step),
+        *_matrix(dy, xt, "dy", T, d, dev), *_matrix(dh, bf, "dh", T, d, dev), *_matrix(dx, xt, "dx", T, d, dev),
+        *_matrix(df, bf, "df", T, d, dev), *sums, 0 if ws is None else ws.data_ptr(), need))
     _lib.call("sat_op_residual_norm_bwd", desc, _stream(dev))
 
 
