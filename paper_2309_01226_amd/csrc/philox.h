@@ -5,15 +5,9 @@
 
 #include "common.h"
 
-// a m, 64 bits, in one instruction (the compiler takes one for each half).
-__device__ __forceinline__ uint64_t mul_wide(uint32_t a, uint32_t m) {
-  uint64_t r;
-  asm("v_mad_u64_u32 %0, vcc, %1, %2, 0" : "=v"(r) : "v"(a), "s"(m) : "vcc");
-  return r;
-}
 __device__ __forceinline__ void philox_round(uint32_t& c0, uint32_t& c1, uint32_t& c2,
                                              uint32_t& c3, uint32_t k0, uint32_t k1) {
-  const uint64_t p = mul_wide(c0, 0xD2511F53u), q = mul_wide(c2, 0xCD9E8D57u);
+  const uint64_t p = (uint64_t)c0 * 0xD2511F53u, q = (uint64_t)c2 * 0xCD9E8D57u;
   const uint32_t n0 = (uint32_t)(q >> 32) ^ c1 ^ k0, n2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
   c0 = n0; c1 = (uint32_t)q; c2 = n2; c3 = (uint32_t)p;
 }
