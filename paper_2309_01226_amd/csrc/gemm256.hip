@@ -436,6 +436,8 @@ __device__ __forceinline__ void epilogue_adamw(const GemmArgs& p, floatx16 (&acc
 
 template <int AL, int BL, int EPI, int GE>
 __global__ __launch_bounds__(NT, 1) void gemm256_kernel(GemmArgs p) {
+  constexpr int NI = Loader<LAY_K>::NI;
+  static_assert(5 * OPE * 2 <= 163840 && BK == 64 && NI == 8, "LDS budget / copies");
   __shared__ __attribute__((aligned(1024))) bf16 smem[5 * OPE];
 
   const int M = p.M, N = p.N;
@@ -457,11 +459,11 @@ __global__ __launch_bounds__(NT, 1) void gemm256_kernel(GemmArgs p) {
   const int wm = wave >> 1, wn = wave & 1;
 
   // an operand's resource for the K-tile at k0 (K-contiguous: for all of them)
-  auto rsA = [&](int, int k0) {
+  auto rsA = [&](int k0) {
     const bf16* q = p.A + (AL == LAY_K ? (long)m0 * p.lda + kb : (long)(kb + k0) * p.lda + m0);
     return __builtin_amdgcn_make_buffer_rsrc((void*)q, (short)0, 0x7FFFFFFF, 0x00020000);
   };
-  auto rsB = [&](int, int k0) {
+  auto rsB = [&](int k0) {
     const bf16* q = p.B + (BL == LAY_K ? (long)n0 * p.ldb + kb : (long)(kb + k0) * p.ldb + n0);
     return __builtin_amdgcn_make_buffer_rsrc((void*)q, (short)0, 0x7FFFFFFF, 0x00020000);
   };
@@ -481,10 +483,70 @@ __global__ __launch_bounds__(NT, 1) void gemm256_kernel(GemmArgs p) {
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+  auto sA = [&](int t) { return smem + (t % 3) * OPE; };
+  auto sB = [&](int t) { return smem + (3 + (t & 1)) * OPE; };
   const int nk = (K + BK - 1) / BK;
   // k offset of tile t; tiles past the last one copy zeros (every chunk at or past K)
   auto kof = [&](int t) { return t < nk ? t * BK : K; };
-  gemm256_loop<AL, BL>(acc, smem, la, lb, FA, FB, rsA, rsB, nk, kof, K, wave);
+  // tile 0 resident; A_1 and the first half of B_1 in flight
+  la.issue(rsA(0), 0, K, sA(0), wave);
+  lb.issue(rsB(0), 0, K, sB(0), wave);
+  wait_vm_lgkm0<0>();
+  cta_barrier();
+  la.issue(rsA(kof(1)), kof(1), K, sA(1), wave);
+  __amdgpu_buffer_rsrc_t rB1 = rsB(kof(1));  // of B_{t+1}
+  lb.template issue<0, 4>(rB1, kof(1), K, sB(1), wave);
+  bf16x8 f0a[4], f0b[4], f1a[4], f1b[4];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) read_q(f0a, f0b, FA, FB, sA(0), sB(0), 0, q);
+  for (int t = 0; t < nk; ++t) {
+    const bf16* a = sA(t);
+    const bf16* b = sB(t);
+    bf16* b1 = sB(t + 1);
+    bf16* a2 = sA(t + 2);
+    bf16* b2 = sB(t + 2);
+    const int k1 = kof(t + 1), k2 = kof(t + 2);
+    const __amdgpu_buffer_rsrc_t rA2 = rsA(k2), rB2 = rsB(k2);
+    __builtin_amdgcn_sched_barrier(0);
+    kstep_ring(acc, f0a, f0b, f1a, f1b, FA, FB, a, b, 1, [&](int c) {
+      switch (c) {
+        case 0: lb.template issue<4, 5>(rB1, k1, K, b1, wave); break;
+        case 1: lb.template issue<5, 6>(rB1, k1, K, b1, wave); break;
+        case 2: lb.template issue<6, 7>(rB1, k1, K, b1, wave); break;
+        default: lb.template issue<7, 8>(rB1, k1, K, b1, wave); break;
+      }
+    });
+    kstep_ring(acc, f1a, f1b, f0a, f0b, FA, FB, a, b, 2, [&](int c) {
+      switch (c) {
+        case 0: la.template issue<0, 1>(rA2, k2, K, a2, wave); break;
+        case 1: la.template issue<1, 2>(rA2, k2, K, a2, wave); break;
+        case 2: la.template issue<2, 3>(rA2, k2, K, a2, wave); break;
+        default: la.template issue<3, 4>(rA2, k2, K, a2, wave); break;
+      }
+    });
+    kstep_ring(acc, f0a, f0b, f1a, f1b, FA, FB, a, b, 3, [&](int c) {
+      switch (c) {
+        case 0: la.template issue<4, 5>(rA2, k2, K, a2, wave); break;
+        case 1: la.template issue<5, 6>(rA2, k2, K, a2, wave); break;
+        case 2: la.template issue<6, 7>(rA2, k2, K, a2, wave); break;
+        default: la.template issue<7, 8>(rA2, k2, K, a2, wave); break;
+      }
+    });
+    wait_vm_lgkm0<NI>();  // A_{t+1}, B_{t+1} resident; reads of tile t done
+    cta_barrier();                // ... in every wave: A_t's and B_t's slots are free
+    kstep_ring(acc, f1a, f1b, f0a, f0b, FA, FB, sA(t + 1), b1, 0, [&](int c) {
+      switch (c) {
+        case 0: lb.template issue<0, 1>(rB2, k2, K, b2, wave); break;
+        case 1: lb.template issue<1, 2>(rB2, k2, K, b2, wave); break;
+        case 2: lb.template issue<2, 3>(rB2, k2, K, b2, wave); break;
+        default: lb.template issue<3, 4>(rB2, k2, K, b2, wave); break;
+      }
+    });
+    rB1 = rB2;
+  }
+  wait_vm_lgkm0<0>();  // the zero-filling copies past the last tile
+  __syncthreads();
   if constexpr (EPI == EPI_ADAMW) {
     epilogue_adamw(p, acc, reinterpret_cast<float*>(smem), m0, n0, wave, lane);
   } else if constexpr (EPI == EPI_F32) {
