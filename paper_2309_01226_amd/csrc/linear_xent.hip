@@ -259,34 +259,34 @@ __global__ __launch_bounds__(NT, 1) void xent_logits_kernel(LinearXentArgs a, in
   const int v0 = m0 + (wave >> 1) * W, t0 = n0 + (wave & 1) * W;
   const int half = 4 * (lane >> 5);
   // the sums begin at the bias; entries behind the vocabulary are -inf
-  floatx4 b[S][4];
-  if (v0 + W <= a.V && a.bias != nullptr) {
-#pragma unroll
-    for (int i = 0; i < S; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) b[i][g] = *reinterpret_cast<const floatx4_any*>(a.bias + v0 + 32 * i + 8 * g + half);
-  } else {
-#pragma unroll
-    for (int i = 0; i < S; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) b[i][g] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (v0 + W > a.V) {
-#pragma unroll
-      for (int i = 0; i < S; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int v = v0 + 32 * i + 8 * (r >> 2) + half + (r & 3);
-          b[i][r >> 2][r & 3] = v >= a.V ? -INF : a.bias != nullptr ? a.bias[v] : 0.f;
-        }
-    }
-  }
   Acc<R> acc;
+  const auto begin = [&](auto four) {
 #pragma unroll
-  for (int i = 0; i < S; ++i)
+    for (int i = 0; i < S; ++i)
 #pragma unroll
-    for (int j = 0; j < S; ++j)
+      for (int g = 0; g < 4; ++g) {
+        const floatx4 b = four(v0 + 32 * i + 8 * g + half);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = b[i][r >> 2][r & 3];
+        for (int j = 0; j < S; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] = b[e];
+      }
+  };
+  if (v0 + W > a.V) {
+    begin([&](int v) {
+      floatx4 b;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = a.bias != nullptr ? a.bias[min(v + e, a.V - 1)] : 0.f;
+        b[e] = v + e < a.V ? x : -INF;
+      }
+      return b;
+    });
+  } else if (a.bias != nullptr) {
+    begin([&](int v) { return *reinterpret_cast<const floatx4_any*>(a.bias + v); });
+  } else {
+    begin([](int) { return floatx4{0.f, 0.f, 0.f, 0.f}; });
+  }
   Operand<LAY_K> A = {a.w, a.ldw}, B;
   B.p = compact_x(a, B.ld);
   B.p += first * B.ld;
