@@ -299,9 +299,10 @@ sat_status sat_op_cross_entropy(const float* z, int64_t ldz, const int32_t* labe
  *   [N, lddx] bf16, dw [V, lddw] and db [V], fp32 when grad_f32, else bf16, each NULL when not wanted.  With
  *   accumulate (fp32 only) dw and db add to what is there.  Without any, rows are only scored.
  * d a multiple of 8 up to 2^16, V up to 2^20.  Logits, statistics and sums are fp32; the two products of the
- * gradients take dz = c (softmax - onehot) rounded to bf16 (where a chunk of the tokens has at most 256 rows, in
- * two parts), of which the softmax comes from z - m (m: the maximum of 128 entries) rounded to
- * 2^-11.5 of its exponential, 2^-9.5 where that is below 2^-32; the label's entry is apart from that.  db sums dz before its
+ * gradients take dz = row_weight (softmax - onehot) rounded to bf16 (where a chunk of the tokens has at most 256 rows,
+ * in two parts) and are multiplied by inv_n afterwards where there is no row_weight.  The softmax in dz comes from z - m
+ * (m: the maximum of up to 128 entries) rounded to 2^-11.5 of its exponential, 2^-9.5 where that is below 2^-32; the
+ * label's entry is apart from that.  db sums dz before its
  * rounding.  A row whose entries are all -inf has loss 0, lse -inf and no gradient; one that holds NaN
  * or infinities spoils its own outputs and the gradients of w and bias.  The same inputs give the same bits.
  * x and w 16-byte aligned with leading dimensions that are multiples of 8 and below 2^21, dx and dw with

@@ -72,6 +72,11 @@ __device__ __forceinline__ int chunk_rows(const LinearXentArgs& a, int first) {
 __device__ __forceinline__ bool chunk_idle(const LinearXentArgs& a, int first) { return first > 0 && a.meta[0] <= first; }
 __device__ __forceinline__ bool chunk_last(const LinearXentArgs& a, int first) { return a.meta[0] <= first + a.chunk; }
 
+// What the sums of all rows' dz are multiplied by: dz holds a row's own weight, but without weights the common 1 / n
+// stays out of it.  Labels' entries near -1 round best just below a power of two, those near -1 / n wherever that
+// happens to lie (7232 rows, 66 entries, d 96: dx is off by 0.21% instead of 0.26%, of which its own rounding is 0.17%).
+__device__ __forceinline__ float common_factor(const LinearXentArgs& a) { return a.row_weight != nullptr ? 1.f : a.inv_n[0]; }
+
 // Row c of the compact rows of x: x itself where every row takes part.
 __device__ __forceinline__ const bf16* compact_x(const LinearXentArgs& a, long& ld) {
   const bool all = a.meta[0] == a.N;
@@ -382,7 +387,7 @@ __device__ __forceinline__ Joined join_row(const LinearXentArgs& a, int first, i
     a.row_loss[row] = none ? 0.f : log_s - z;
   }
   if (none) return Joined{m, 0.f, 0.f};
-  const float c = a.row_weight != nullptr ? a.row_weight[row] : a.inv_n[0], up = c / s;
+  const float c = a.row_weight != nullptr ? a.row_weight[row] : 1.f, up = c / s;
   return Joined{m, up, up * __builtin_amdgcn_exp2f(z * LOG2E) - c};
 }
 // What a piece's exp(z - its own maximum) is multiplied by to give c softmax.
@@ -474,16 +479,18 @@ __global__ __launch_bounds__(256) void xent_db_kernel(LinearXentArgs a, int firs
   if (v >= a.V) return;
   float* f32 = reinterpret_cast<float*>(a.db);
   float* sum = a.dw_f32 ? f32 : a.dbsum;
-  float s = (a.dw_f32 ? a.accumulate : 0) || first > 0 ? sum[v] : 0.f;
+  const float old = (a.dw_f32 ? a.accumulate : 0) || first > 0 ? sum[v] : 0.f;
+  float s = 0.f;
 #pragma unroll 8
   for (int b = 0; b < blocks; ++b) s += a.dbpart[(long)b * a.V + v];
+  s = old + s * common_factor(a);
   if (a.dw_f32 || !chunk_last(a, first)) sum[v] = s;
   else reinterpret_cast<bf16*>(a.db)[v] = f2bf(s);
 }
 
 // ---------------------------------------------------------------- the other products
 
-// Where a row's eight columns go: fp32 or bf16, plus an fp32 addend.
+// Where a row's eight columns go: fp32 or bf16, times a factor, plus an fp32 addend.
 struct RowsOut {
   void* out;
   long ld;
@@ -491,7 +498,10 @@ struct RowsOut {
   const float* add;  // may be out
   long ldadd;
   const int* map;    // row m is row map[m] of out
+  float c;           // what the columns are multiplied by, before the addition
   __device__ __forceinline__ void put(int m, int col, float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= c;
     if (add != nullptr) {
       float b[8];
       widen8(load8<false>(add + (long)m * ldadd + col, 8), b);
@@ -558,7 +568,7 @@ __device__ __forceinline__ void product(bf16* smem, const Operand<AL>& A, const 
 }
 
 __device__ __forceinline__ RowsOut dx_out(const LinearXentArgs& a, int first) {
-  return RowsOut{a.dx, a.lddx, false, nullptr, 0, a.idx + first};
+  return RowsOut{a.dx, a.lddx, false, nullptr, 0, a.idx + first, common_factor(a)};
 }
 __host__ __device__ inline Split dx_split(int R, const LinearXentArgs& a, int n) {
   return split_of(R, tiles_of(R, n, a.d), cdiv(a.V, BK));
@@ -566,7 +576,7 @@ __host__ __device__ inline Split dx_split(int R, const LinearXentArgs& a, int n)
 // dw of one of several chunks goes to an fp32 sum; the last one's outcome to dw.
 __device__ __forceinline__ RowsOut dw_out(const LinearXentArgs& a, int first) {
   const bool sum = a.dwsum != nullptr;
-  RowsOut o = {a.dw, a.lddw, a.dw_f32 != 0, nullptr, 0, nullptr};
+  RowsOut o = {a.dw, a.lddw, a.dw_f32 != 0, nullptr, 0, nullptr, common_factor(a)};
   if (sum) {
     if (first > 0) o.add = a.dwsum, o.ldadd = a.d;
     if (!chunk_last(a, first)) o.out = a.dwsum, o.ld = a.d, o.f32 = true;
