@@ -26,6 +26,7 @@
 namespace {
 
 constexpr int CUS = 256;
+constexpr int64_t kStream = 450000000;  // bytes of a call
 
 // NARROW: rows of up to 256 columns, on 8, 16 or 32 lanes; else a row's place is the same for a whole wave.
 template <bool NARROW>
@@ -118,7 +119,9 @@ __device__ __forceinline__ float2 row_stats(const RowPlace<NARROW>& p, Shared& s
 // offset past the end of the buffer, for which the hardware reads zeros and writes nothing.  So no access
 // stands behind a branch and the compiler's waits count exactly: the next row's loads stay in flight over the
 // whole row (with branches it has to wait for them at once: 16384 rows of 4096, backward, 280 us instead of 229).
+// FAST 2: past the caches, but for fp32 stores, whose lanes write halves of lines apart.
 constexpr uint32_t NOWHERE = 0x80000000u;
+constexpr int NONTEMPORAL = 2;
 template <class T>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const T* p) {
   return __builtin_amdgcn_make_buffer_rsrc((void*)p, (short)0, 0x7FFFFFFF, 0x00020000);
@@ -127,22 +130,23 @@ template <bool NARROW, class T>
 __device__ __forceinline__ uint32_t place(const RowPlace<NARROW>& p, int64_t ld, int n) {
   return n > 0 ? (uint32_t)(((NARROW ? p.rw * (int)ld : 0) + p.col) * (int)sizeof(T)) : NOWHERE;
 }
-template <bool FAST, bool NARROW, class T>
+template <int FAST, bool NARROW, class T>
 __device__ __forceinline__ Raw8<T> get(const RowPlace<NARROW>& p, const T* m, int64_t ld, int r0, int rows, bool on) {
   const int row = r0 + p.rw, n = on && row < rows ? p.n : 0;
   if constexpr (!FAST) return load8<false>(m + (int64_t)row * ld + p.col, n);
   const __amdgpu_buffer_rsrc_t b = buffer(m + (int64_t)(NARROW ? r0 : row) * ld);
   const uint32_t o = place<NARROW, T>(p, ld, n);
+  constexpr int AUX = FAST == 2 ? NONTEMPORAL : 0;
   Raw8<T> r;
   if constexpr (sizeof(T) == 2) {
-    r.w = __builtin_amdgcn_raw_buffer_load_b128(b, o, 0, 0);
+    r.w = __builtin_amdgcn_raw_buffer_load_b128(b, o, 0, AUX);
   } else {
-    r.w[0] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(b, o, 0, 0));
-    r.w[1] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(b, o, 16, 0));
+    r.w[0] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(b, o, 0, AUX));
+    r.w[1] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(b, o, 16, AUX));
   }
   return r;
 }
-template <bool FAST, bool NARROW, class T>
+template <int FAST, bool NARROW, class T>
 __device__ __forceinline__ void put(const RowPlace<NARROW>& p, T* m, int64_t ld, int r0, int rows, bool on, const float (&x)[8]) {
   const int row = r0 + p.rw, n = on && row < rows ? p.n : 0;
   if constexpr (!FAST) {
@@ -151,11 +155,12 @@ __device__ __forceinline__ void put(const RowPlace<NARROW>& p, T* m, int64_t ld,
   }
   const __amdgpu_buffer_rsrc_t b = buffer(m + (int64_t)(NARROW ? r0 : row) * ld);
   const uint32_t o = place<NARROW, T>(p, ld, n);
+  constexpr int AUX = FAST == 2 ? NONTEMPORAL : 0;
   if constexpr (sizeof(T) == 2) {
     bf16x8 y;
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = f2bf(x[e]);
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, y), b, o, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, y), b, o, 0, AUX);
   } else {
     const floatx4 lo = {x[0], x[1], x[2], x[3]}, hi = {x[4], x[5], x[6], x[7]};
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), b, o, 0, 0);
@@ -163,7 +168,7 @@ __device__ __forceinline__ void put(const RowPlace<NARROW>& p, T* m, int64_t ld,
   }
 }
 // The row's pair of statistics, 0 for the branch's norm and 2 for the next one's.
-template <bool FAST, bool NARROW>
+template <int FAST, bool NARROW>
 __device__ __forceinline__ float2 get_stats(const RowPlace<NARROW>& p, const float* stats, int which, int r0, int rows, bool on) {
   const int row = r0 + p.rw;
   const float* s = stats + (int64_t)which * rows + r0;
@@ -172,7 +177,7 @@ __device__ __forceinline__ float2 get_stats(const RowPlace<NARROW>& p, const flo
   return make_float2(__uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer(s), o, 0, 0)),
                      __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer(s + rows), o, 0, 0)));
 }
-template <bool FAST, bool NARROW>
+template <int FAST, bool NARROW>
 __device__ __forceinline__ void put_stats(const RowPlace<NARROW>& p, float* stats, int which, int r0, int rows, bool on, float2 v) {
   const bool me = on && p.col == 0 && r0 + p.rw < rows;
   float* s = stats + (int64_t)which * rows + r0;
@@ -210,7 +215,7 @@ __device__ __forceinline__ void branch_factors(const ResidualNormArgs& a, const 
   for (int e = 0; e < 8; ++e) m[e] = drop_keeps(c, r, e) ? scale : 0.f;
 }
 
-template <class XT, int MAXT, bool FAST, bool NARROW = false>
+template <class XT, int MAXT, int FAST, bool NARROW = false>
 __global__ __launch_bounds__(MAXT) void residual_norm_fwd_kernel(ResidualNormArgs a) {
   __shared__ Shared sh;
   int turn = 0;
@@ -299,7 +304,7 @@ __device__ __forceinline__ void put_sums(const ResidualNormArgs& a, const P& p, 
 // POST: with a norm of the branch.  Without one its sums' registers are free, and four waves fit a SIMD; with
 // one, three, or two of rows of eight waves.  The widest rows take all 16 waves of a workgroup: there nothing is loaded
 // ahead and gains are read again for each row (KEEP false).
-template <class XT, int MAXT, bool POST, bool FAST, bool NARROW = false>
+template <class XT, int MAXT, bool POST, int FAST, bool NARROW = false>
 __global__ __launch_bounds__(MAXT, MAXT > 768 ? 4 : MAXT > 512 ? 3 : 2) void residual_norm_bwd_kernel(ResidualNormArgs a) {
   __shared__ Shared sh;
   __shared__ float join[MAXT * 8];
@@ -459,23 +464,31 @@ int bwd_rows_wg(int d, const BwdShape& b) { return b.lines * (64 / lanes_of_row(
 int bwd_groups(int T, int d, const BwdShape& b) { return std::min(CUS * b.per_cu, sat_cdiv(T, bwd_rows_wg(d, b))); }
 
 using Kernel = void (*)(ResidualNormArgs);
-template <class XT, bool FAST>
-Kernel fwd_kernel(int L, int threads) {
-  if (L < 64) return residual_norm_fwd_kernel<XT, 256, FAST, true>;
-  if constexpr (FAST) {
-    if (threads <= 256) return residual_norm_fwd_kernel<XT, 256, true>;
-    if (threads <= 512) return residual_norm_fwd_kernel<XT, 512, true>;
-  }
-  return residual_norm_fwd_kernel<XT, 1024, FAST>;
+template <class XT>
+Kernel fwd_kernel(int L, int threads, int fast) {
+  if (L < 64) return fast ? residual_norm_fwd_kernel<XT, 256, 1, true> : residual_norm_fwd_kernel<XT, 256, 0, true>;
+  if (!fast) return residual_norm_fwd_kernel<XT, 1024, 0>;
+  if (fast == 2)
+    return threads <= 256   ? residual_norm_fwd_kernel<XT, 256, 2>
+           : threads <= 512 ? residual_norm_fwd_kernel<XT, 512, 2>
+                            : residual_norm_fwd_kernel<XT, 1024, 2>;
+  return threads <= 256   ? residual_norm_fwd_kernel<XT, 256, 1>
+         : threads <= 512 ? residual_norm_fwd_kernel<XT, 512, 1>
+                          : residual_norm_fwd_kernel<XT, 1024, 1>;
 }
-template <class XT, bool POST, bool FAST>
-Kernel bwd_kernel(int L, int most) {
-  if (L < 64) return residual_norm_bwd_kernel<XT, 768, POST, FAST, true>;
-  if constexpr (FAST) {
-    if (most == 512) return residual_norm_bwd_kernel<XT, 512, POST, true>;
-    if (most == 768) return residual_norm_bwd_kernel<XT, 768, POST, true>;
+template <class XT, bool POST>
+Kernel bwd_kernel(int L, int most, int fast) {
+  if (L < 64) return fast ? residual_norm_bwd_kernel<XT, 768, POST, 1, true> : residual_norm_bwd_kernel<XT, 768, POST, 0, true>;
+  if (!fast) return residual_norm_bwd_kernel<XT, 1024, POST, 0>;
+  if constexpr (!POST || sizeof(XT) == 2) {
+    if (fast == 2)
+      return most == 512   ? residual_norm_bwd_kernel<XT, 512, POST, 2>
+             : most == 768 ? residual_norm_bwd_kernel<XT, 768, POST, 2>
+                           : residual_norm_bwd_kernel<XT, 1024, POST, 2>;
   }
-  return residual_norm_bwd_kernel<XT, 1024, POST, FAST>;
+  return most == 512   ? residual_norm_bwd_kernel<XT, 512, POST, 1>
+         : most == 768 ? residual_norm_bwd_kernel<XT, 768, POST, 1>
+                       : residual_norm_bwd_kernel<XT, 1024, POST, 1>;
 }
 
 int sum_outputs(const ResidualNormArgs& a, SumOut* o) {
@@ -492,8 +505,12 @@ int64_t residual_norm_ws(int T, int d, bool post, int sums) {
   return (int64_t)std::max(bwd_groups(T, d, bwd_shape(d, true)), bwd_groups(T, d, bwd_shape(d, false))) * sums * d;
 }
 
-// Whether rows are whole 16-byte pieces, of every array that is there.
-static bool fast_rows(const ResidualNormArgs& a, bool f32, bool back) {
+// How rows are accessed: 1 where they are whole 16-byte pieces, of every array that is there; 2 also past the caches, where
+// all of them together exceed the last-level one (256 MB) well (us with and without: 16384 x 4096, fp32, both norms
+// forward 130 and 147, bf16 109 and 113; backward without a norm of the branch 209 and 225; 32768 x 200 18 and 14); not
+// with an fp32 stream for that backward (236 and 217) and for the forward of rows of more than 8 waves (10922 x 6144:
+// 153 and 148).
+static int fast_rows(const ResidualNormArgs& a, bool f32, bool back) {
   bool ok = a.d % 8 == 0;
   const auto rows = [&](const void* p, int64_t ld, int size) {
     if (p != nullptr) ok = ok && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0 && ld < (1 << 21);
@@ -510,7 +527,9 @@ static bool fast_rows(const ResidualNormArgs& a, bool f32, bool back) {
     rows(a.x, a.ldx, size);
     rows(a.h, a.ldh, 2);
   }
-  return ok;
+  if (!ok) return 0;
+  const int64_t bytes = (int64_t)a.T * a.d * (back ? (2 + !!a.pre) * size + 2 * (1 + !!a.pre + (a.post || a.dgate)) : 2 * size + 2 * (1 + !!a.pre));
+  return bytes >= kStream && !(f32 && (back ? a.post != 0 : waves_of_row(a.d) > 8)) ? 2 : 1;
 }
 
 hipError_t launch_residual_norm_fwd(ResidualNormArgs a, bool f32, hipStream_t s) {
@@ -521,8 +540,8 @@ hipError_t launch_residual_norm_fwd(ResidualNormArgs a, bool f32, hipStream_t s)
   a.rows_wg = lines * (64 / a.L);
   const int threads = 64 * a.wpr * lines;
   const dim3 grid(std::min(sat_cdiv(a.T, a.rows_wg), CUS * std::max(1, 1024 / threads)));
-  const auto kernel = fast_rows(a, f32, false) ? (f32 ? fwd_kernel<float, true>(a.L, threads) : fwd_kernel<bf16, true>(a.L, threads))
-                                               : (f32 ? fwd_kernel<float, false>(a.L, threads) : fwd_kernel<bf16, false>(a.L, threads));
+  const int fast = fast_rows(a, f32, false);
+  const Kernel kernel = f32 ? fwd_kernel<float>(a.L, threads, fast) : fwd_kernel<bf16>(a.L, threads, fast);
   hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
   return hipGetLastError();
 }
@@ -532,15 +551,13 @@ hipError_t launch_residual_norm_bwd(ResidualNormArgs a, bool f32, hipStream_t s)
   a.sums = sum_outputs(a, &o);
   a.wpr = waves_of_row(a.d);
   a.L = lanes_of_row(a.d);
-  const bool fast = fast_rows(a, f32, true);
+  const int fast = fast_rows(a, f32, true);
   const BwdShape shape = bwd_shape(a.d, fast);
   a.rows_wg = bwd_rows_wg(a.d, shape);
   const int threads = 64 * a.wpr * shape.lines, G = bwd_groups(a.T, a.d, shape);
   if (G > 0) {
-    const auto kernel = a.post ? (fast ? (f32 ? bwd_kernel<float, true, true>(a.L, shape.most) : bwd_kernel<bf16, true, true>(a.L, shape.most))
-                                       : (f32 ? bwd_kernel<float, true, false>(a.L, shape.most) : bwd_kernel<bf16, true, false>(a.L, shape.most)))
-                               : (fast ? (f32 ? bwd_kernel<float, false, true>(a.L, shape.most) : bwd_kernel<bf16, false, true>(a.L, shape.most))
-                                       : (f32 ? bwd_kernel<float, false, false>(a.L, shape.most) : bwd_kernel<bf16, false, false>(a.L, shape.most)));
+    const Kernel kernel = a.post ? (f32 ? bwd_kernel<float, true>(a.L, shape.most, fast) : bwd_kernel<bf16, true>(a.L, shape.most, fast))
+                                 : (f32 ? bwd_kernel<float, false>(a.L, shape.most, fast) : bwd_kernel<bf16, false>(a.L, shape.most, fast));
     hipLaunchKernelGGL(kernel, dim3(G), dim3(threads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

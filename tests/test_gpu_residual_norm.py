@@ -260,3 +260,31 @@ def test_streams_and_graph():
         go(eager)
         torch.cuda.synchronize()
         assert all(same(b, eager) for _, b in graphs)
+
+
+@pytest.mark.parametrize("dt,post,T,d", [(F4, "rms", 20011, 4096), (BF, "rms", 20011, 4096), (F4, None, 60001, 1280), (BF, None, 9000, 8192),
+                                         (F4, "layer", 6000, 8192), (BF, "layer", 300007, 264), (F4, "layer", 300007, 256)])
+def test_large_calls(dt, post, T, d):
+    """Calls past the size where rows go past the caches: their first and last rows are those of small calls, bit for bit."""
+    from paper_2309_01226_amd import ops
+    flush("large", dt, post, T, d)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    r = lambda rows, t: torch.randn(rows, d, device="cuda", generator=g, dtype=torch.float32).to(t)  # noqa: E731
+    x, f, dy, dh = r(T, dt), r(T, BF), r(T, dt), r(T, BF)
+    kw = dict(pre="layer", post=post, gate=torch.randn(d, device="cuda", generator=g), alpha=0.5)
+
+    def go(at, p):
+        a = [t[at] for t in (x, f, dy, dh)]
+        y, h, st = torch.empty_like(a[0]), torch.empty_like(a[1]), torch.empty(4, len(a[0]), device="cuda")
+        dx, df, dgate = torch.empty_like(a[2]), torch.empty_like(a[1]), torch.empty(d, device="cuda")
+        ops.residual_norm_fwd(a[0], a[1], y, h, st, d, p=p, seed=3, **kw)
+        ops.residual_norm_bwd(a[2], a[3], y, a[1], st, dx, df, d, dgate=dgate, p=p, seed=3, **kw)
+        assert torch.isfinite(dgate).all()
+        return y, h, dx, df
+
+    for at, p in ((slice(0, 130), 0.25), (slice(T - 130, T), 0.0)):
+        whole, part = go(slice(0, T), p), go(at, p)
+        for name, a, b in zip(("y", "h", "dx", "df"), whole, part):
+            assert torch.equal(a[at], b), (name, p)
+        del whole
