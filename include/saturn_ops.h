@@ -217,7 +217,7 @@ sat_status sat_op_rotary_axes(const void* x, int64_t ldx, void* y, int64_t ldy, 
  * the kernel, so that a captured call draws anew when the caller's own work moves it on; NULL: 0.
  * Calls with the same seed, step and place drop the same elements: give each place in a model a seed
  * of its own.  y == x (with ldy == ldx): in place; else y must not overlap x.  f32: x and y are fp32, else
- * bf16.  cols up to 2^18, rows ceil(cols / 8) below 2^33; x and y aligned to their elements.  Columns
+ * bf16.  cols up to 2^18, rows ceil(cols / 8) below 2^31; x and y aligned to their elements.  Columns
  * behind `cols` are not touched.  Errors: SAT_EINVAL for null pointers, sizes, alignment and p outside [0, 1]. */
 sat_status sat_op_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int32_t f32,
                           int32_t rows, int32_t cols, double p, uint64_t seed, const int64_t* step,
@@ -298,7 +298,7 @@ sat_status sat_op_cross_entropy(const float* z, int64_t ldz, const int32_t* labe
  *   Gradients of sum_t c_t row_loss_t, c = row_weight [N] or, when that is NULL, inv_n for every row: dx
  *   [N, lddx] bf16, dw [V, lddw] and db [V], fp32 when grad_f32, else bf16, each NULL when not wanted.  With
  *   accumulate (fp32 only) dw and db add to what is there.  Without any, rows are only scored.
- * d a multiple of 8 up to 2^16, V up to 2^20.  Logits, statistics and sums are fp32; the two products of the
+ * N up to 2^25, d a multiple of 8 up to 2^16, V up to 2^20.  Logits, statistics and sums are fp32; the two products of the
  * gradients take dz = row_weight (softmax - onehot) rounded to bf16 (where a chunk of the tokens has at most 256 rows,
  * in two parts) and are multiplied by inv_n afterwards where there is no row_weight.  The softmax in dz comes from z - m
  * (m: the maximum of up to 128 entries) rounded to 2^-11.5 of its exponential, 2^-9.5 where that is below 2^-32; the

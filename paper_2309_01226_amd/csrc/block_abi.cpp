@@ -28,7 +28,7 @@ extern "C" sat_status sat_op_dropout(const void* x, int64_t ldx, void* y, int64_
                                      int32_t cols, double p, uint64_t seed, const int64_t* step, void* stream) {
   const char* fn = "dropout";
   SAT_CHECK_ARG(rows >= 0 && cols >= 0 && cols <= (1 << 18), "%s: bad sizes rows=%d cols=%d (up to 2^18)", fn, rows, cols);
-  SAT_CHECK_ARG((int64_t)rows * ((cols + 7) / 8) < (1LL << 33), "%s: %d rows of %d columns are too many", fn, rows, cols);
+  SAT_CHECK_ARG((int64_t)rows * ((cols + 7) / 8) < (1LL << 31), "%s: %d rows of %d columns are too many", fn, rows, cols);
   SAT_CHECK_ARG(rows == 0 || cols == 0 || (x && y), "%s: null pointer", fn);
   SAT_CHECK_ARG(p >= 0 && p <= 1, "%s: p=%g must be in [0, 1]", fn, p);
   SAT_CHECK_ARG(ldx >= cols && ldy >= cols && ldx < kMaxLd && ldy < kMaxLd, "%s: leading dimensions must cover the columns", fn);
@@ -141,8 +141,8 @@ static constexpr int64_t kMaxHeadLd = 1 << 21;  // a tile's rows stay within 32-
 
 static sat_status linear_xent_sizes(const sat_linear_xent_desc* d, LinearXentArgs* out, const char* fn) {
   SAT_CHECK_ARG(d != nullptr, "%s: null descriptor", fn);
-  SAT_CHECK_ARG(d->N >= 0 && d->N < (1 << 30) && d->V >= 1 && d->V <= (1 << 20), "%s: bad sizes N=%d V=%d (V up to 2^20)", fn,
-                d->N, d->V);
+  SAT_CHECK_ARG(d->N >= 0 && d->N <= (1 << 25) && d->V >= 1 && d->V <= (1 << 20),
+                "%s: bad sizes N=%d V=%d (up to 2^25 and 2^20)", fn, d->N, d->V);
   SAT_CHECK_ARG(d->d >= 8 && d->d <= (1 << 16) && d->d % 8 == 0, "%s: d=%d must be a multiple of 8 up to 2^16", fn, d->d);
   SAT_CHECK_ARG(!d->accumulate || d->grad_f32, "%s: only fp32 gradients are added to", fn);
   SAT_CHECK_ARG(!d->db || d->bias, "%s: a gradient of a bias that is not there", fn);
@@ -178,6 +178,7 @@ extern "C" sat_status sat_op_linear_xent(const sat_linear_xent_desc* d, void* st
                 "%s: dx must be 16-byte aligned with lddx %% 8 == 0, at least d", fn);
   SAT_CHECK_ARG(!d->dw || (d->lddw >= d->d && d->lddw < kMaxLd && d->lddw % (d->grad_f32 ? 4 : 8) == 0 && aligned(d->dw, 16)),
                 "%s: dw must be 16-byte aligned with 16-byte aligned rows of at least d", fn);
+  SAT_CHECK_ARG((!d->dx || d->dx != d->x) && (!d->dw || d->dw != d->w), "%s: gradients are not written over x or w", fn);
   SAT_CHECK_ARG(aligned(d->labels, 4) && aligned(d->bias, 4) && aligned(d->row_weight, 4) && aligned(d->row_loss, 4) &&
                     aligned(d->lse, 4) && aligned(d->inv_n, 4) && aligned(d->db, d->grad_f32 ? 4 : 2),
                 "%s: vectors must be aligned to their elements", fn);

@@ -400,7 +400,7 @@ struct DropoutArgs {
   int n8;                 // set by the launch: groups of eight columns, and the inverse for dividing by it
   uint32_t inv;
 };
-// cols <= 2^18, rows ceil(cols / 8) < 2^31 NT.
+// cols <= 2^18, rows ceil(cols / 8) < 2^31.
 hipError_t launch_dropout(DropoutArgs a, bool f32, hipStream_t s);
 
 enum { kNormNone = 0, kNormLayer = 1, kNormRms = 2 };
@@ -448,8 +448,9 @@ struct LinearXentArgs {
   int N, V, d, dw_f32, accumulate;
   // set by the launch: a chunk's tokens, the pitch of e, and the parts of the workspace
   int chunk, tb, piece;   // (and of the scaling pass' workgroup; vocabulary entries with one pair of statistics)
+  int rx, rw, s_dx, s_dw; // tiles of dx and dw, and slices of their products for a full chunk
   int64_t lde;            // the vocabulary in whole tiles
-  int *meta, *idx, *pos, *lab;  // rows that take part: [0] their number; their rows, the rows' places, their labels
+  int *meta, *idx, *pos, *lab;  // rows that take part: [0] their number, [1] and [2] slices of the last chunk; their rows, the rows' places, their labels
   float* zlab;            // their label's logit, then its entry of dz
   float2* part;           // [chunk][pieces]: maximum and sum, then the factor of e
   bf16* xc;               // compact rows of x

@@ -36,31 +36,47 @@ constexpr float INF = __builtin_inff();
 __host__ __device__ inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 
 // A product of `tiles` tiles of R rows and columns and `ktiles` 64-deep steps on 256 CUs: `full` tiles in whole
-// rounds, one on a CU, and the rest, whose K is split in S slices where that shortens the last round.  Cost in us:
-// a step of K takes 1.65 (of a tile of 128: 0.7), a round's start and end 8 (4), a partial tile's way to memory and
-// back 0.1 (0.026).  At most 128 MB of partial tiles.
+// rounds, one on a CU, and the rest, whose K is split in S slices where that shortens the last round.  Cost in ns: a
+// step of K takes 1650 (of a tile of 128: 700), a round's start and end 8000 (4000), a partial tile's way to memory and
+// back 100 (26), the launch that adds the slices 4000.  At most 128 MB of partial tiles.  Whole numbers: the host plans the
+// workspace and the launch by what the rows' kernel then chooses on the device (by the number of rows that take part), so
+// both have to choose alike.
+constexpr int SLICES = 64;
 struct Split {
   int full, rest, S;
-  float us;
   __host__ __device__ int groups() const { return full + rest * S; }
   __host__ __device__ int64_t partial(int R) const { return S > 1 ? (int64_t)rest * S * R * R : 0; }
 };
-__host__ __device__ inline Split split_of(int R, int tiles, int ktiles, int most = 16) {
-  const float step = R == BT ? 1.65f : 0.7f, ends = R == BT ? 8.f : 4.f, way = R == BT ? 0.1f : 0.026f;
-  Split p = {tiles / CUS * CUS, tiles % CUS, 1, 0.f};
-  for (int s = 1; s <= most; ++s) {
-    if (s > 1 && (p.rest * s > (R == BT ? 512 : 2048) || ktiles < 4 * s)) break;
-    // a split product's slices are added by another launch
-    const float c = (float)cdiv(p.rest * s, CUS) * (cdiv(ktiles, s) * step + ends) + (s > 1 ? way * p.rest * s + 4.f : 0.f);
-    if (s == 1 || c < p.us) {
-      p.S = s;
-      p.us = c;
-    }
-  }
-  p.us += (float)(tiles / CUS) * (ktiles * step + ends);
-  return p;
+__host__ __device__ inline bool slices_fit(int R, int tiles, int ktiles, int s) {
+  return s == 1 || (tiles % CUS * s <= (R == BT ? 512 : 2048) && ktiles >= 4 * s);
+}
+// Cost of the rest in s slices; the least number wins, of equal ones the fewest slices (the low bits).
+__host__ __device__ inline int64_t slices_key(int R, int tiles, int ktiles, int s) {
+  const int rest = tiles % CUS, step = R == BT ? 1650 : 700, ends = R == BT ? 8000 : 4000, way = R == BT ? 100 : 26;
+  if (!slices_fit(R, tiles, ktiles, s)) return INT64_MAX;
+  const int64_t ns = (int64_t)cdiv(rest * s, CUS) * ((int64_t)cdiv(ktiles, s) * step + ends) + (s > 1 ? way * rest * s + 4000 : 0);
+  return ns * 128 + s;
+}
+// The best number of slices, by one wave.
+__device__ __forceinline__ int wave_slices(int R, int tiles, int ktiles) {
+  int64_t key = slices_key(R, tiles, ktiles, 1 + (threadIdx.x & 63));
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) key = min(key, (int64_t)__shfl_xor((long long)key, o, SAT_WAVE));
+  return (int)(key & 127);
+}
+inline Split split_of(int R, int tiles, int ktiles, int64_t* ns = nullptr, int most = SLICES) {
+  int64_t key = INT64_MAX;
+  for (int s = 1; s <= most && slices_fit(R, tiles, ktiles, s); ++s) key = std::min(key, slices_key(R, tiles, ktiles, s));
+  if (ns) *ns = key / 128 + (int64_t)(tiles / CUS) * ((int64_t)ktiles * (R == BT ? 1650 : 700) + (R == BT ? 8000 : 4000));
+  return Split{tiles / CUS * CUS, tiles % CUS, (int)(key & 127)};
 }
 __host__ __device__ inline int tiles_of(int R, int M, int N) { return cdiv(M, R) * cdiv(N, R); }
+
+// Tiles and K steps of dx = dz w and of dw = dz^T x for n rows.
+__host__ __device__ inline int dx_tiles(int R, const LinearXentArgs& a, int n) { return tiles_of(R, n, a.d); }
+__host__ __device__ inline int dx_steps(const LinearXentArgs& a) { return cdiv(a.V, BK); }
+__host__ __device__ inline int dw_tiles(int R, const LinearXentArgs& a) { return tiles_of(R, a.V, a.d); }
+__host__ __device__ inline int dw_steps(int n) { return cdiv(n, BK); }
 
 // The compact rows of the chunk that starts at `first`.
 __device__ __forceinline__ int chunk_rows(const LinearXentArgs& a, int first) {
@@ -88,6 +104,13 @@ __device__ __forceinline__ const bf16* compact_x(const LinearXentArgs& a, long& 
 __device__ __forceinline__ int xcd_place(int bid, int total) {
   const int x = bid & 7, q = total >> 3, r = total & 7;
   return x * q + min(x, r) + (bid >> 3);
+}
+
+// How the products of the chunk that is not full are split, by one wave each: meta[1] dx, meta[2] dw.
+__device__ __forceinline__ void choose_slices(const LinearXentArgs& a, int rows, int which) {
+  const int n = rows % a.chunk;
+  const int S = which == 1 ? wave_slices(a.rx, dx_tiles(a.rx, a, n), dx_steps(a)) : wave_slices(a.rw, dw_tiles(a.rw, a), dw_steps(n));
+  if ((threadIdx.x & 63) == 0) a.meta[which] = S;
 }
 
 // ---------------------------------------------------------------- rows
@@ -126,6 +149,7 @@ __global__ __launch_bounds__(1024) void xent_rows_kernel(LinearXentArgs a) {
     a.meta[0] = base;
     a.inv_n[0] = 1.f / max(base, 1);
   }
+  if (wave == 1 || wave == 2) choose_slices(a, base, wave);
 }
 
 // One wave a row: x of rows that take part, to their compact place unless all do; zeros to dx of the others.
@@ -185,6 +209,7 @@ __global__ __launch_bounds__(256) void xent_rows_few_kernel(LinearXentArgs a) {
       a.inv_n[0] = 1.f / max(all, 1);
     }
   }
+  if (r0 == 0 && (wave == 1 || wave == 2)) choose_slices(a, all, wave);
   __syncthreads();
   if (all == a.N) return;
   const u32x4 zero = {0, 0, 0, 0};
@@ -570,8 +595,9 @@ __device__ __forceinline__ void product(bf16* smem, const Operand<AL>& A, const 
 __device__ __forceinline__ RowsOut dx_out(const LinearXentArgs& a, int first) {
   return RowsOut{a.dx, a.lddx, false, nullptr, 0, a.idx + first, common_factor(a)};
 }
-__host__ __device__ inline Split dx_split(int R, const LinearXentArgs& a, int n) {
-  return split_of(R, tiles_of(R, n, a.d), cdiv(a.V, BK));
+__device__ __forceinline__ Split dx_split(int R, const LinearXentArgs& a, int n) {
+  const int tiles = dx_tiles(R, a, n);
+  return Split{tiles / CUS * CUS, tiles % CUS, n == a.chunk ? a.s_dx : a.meta[1]};
 }
 // dw of one of several chunks goes to an fp32 sum; the last one's outcome to dw.
 __device__ __forceinline__ RowsOut dw_out(const LinearXentArgs& a, int first) {
@@ -586,8 +612,9 @@ __device__ __forceinline__ RowsOut dw_out(const LinearXentArgs& a, int first) {
   }
   return o;
 }
-__host__ __device__ inline Split dw_split(int R, const LinearXentArgs& a, int n) {
-  return split_of(R, tiles_of(R, a.V, a.d), cdiv(n, BK));
+__device__ __forceinline__ Split dw_split(int R, const LinearXentArgs& a, int n) {
+  const int tiles = dw_tiles(R, a);
+  return Split{tiles / CUS * CUS, tiles % CUS, n == a.chunk ? a.s_dw : a.meta[2]};
 }
 
 template <int R>
@@ -697,10 +724,15 @@ void plan(LinearXentArgs& a, Layout& l) {
   while (a.tb > 4 && (int64_t)cdiv(a.V, 2048) * cdiv(std::min(a.N, a.chunk), a.tb) < 4 * CUS) a.tb /= 2;
   // tiles of 128 where those of 256 would leave most CUs without one, by the estimated time
   const int n = std::min(a.N, a.chunk);
-  const auto small = [&](auto split) { return split(RS).us < split(BT).us ? RS : BT; };
-  l.logits.R = small([&](int R) { return split_of(R, tiles_of(R, a.V, n), cdiv(a.d, BK), 1); });
-  l.dx.R = small([&](int R) { return dx_split(R, a, n); });
-  l.dw.R = small([&](int R) { return dw_split(R, a, n); });
+  const auto pick = [&](int large, int small, int steps, int most) {
+    int64_t at_large, at_small;
+    split_of(BT, large, steps, &at_large, most);
+    split_of(RS, small, steps, &at_small, most);
+    return at_small < at_large ? RS : BT;
+  };
+  l.logits.R = pick(tiles_of(BT, a.V, n), tiles_of(RS, a.V, n), cdiv(a.d, BK), 1);
+  l.dx.R = a.rx = pick(dx_tiles(BT, a, n), dx_tiles(RS, a, n), dx_steps(a), SLICES);
+  l.dw.R = a.rw = pick(dw_tiles(BT, a), dw_tiles(RS, a), dw_steps(n), SLICES);
   a.piece = l.logits.R / 2;
   l.part(a.meta, 64);
   l.part(a.idx, a.N);
@@ -715,8 +747,12 @@ void plan(LinearXentArgs& a, Layout& l) {
   l.part(a.dbsum, a.db && !a.dw_f32 && a.N > a.chunk ? a.V : 0);
   l.part(a.dwsum, a.dw && !a.dw_f32 && a.N > a.chunk ? (int64_t)a.V * a.d : 0);
   // the most that any number of rows that take part asks for
-  for (int i = 0; a.dx && i <= a.chunk; i += l.dx.R) l.dx.join(dx_split(l.dx.R, a, i));
-  for (int i = 0; a.dw && i <= a.chunk; i += BK) l.dw.join(dw_split(l.dw.R, a, i));
+  const auto dx = [&](int rows) { return split_of(a.rx, dx_tiles(a.rx, a, rows), dx_steps(a)); };
+  const auto dw = [&](int rows) { return split_of(a.rw, dw_tiles(a.rw, a), dw_steps(rows)); };
+  for (int i = 0; a.dx && i <= a.chunk; i += a.rx) l.dx.join(dx(i));
+  for (int i = 0; a.dw && i <= a.chunk; i += BK) l.dw.join(dw(i));
+  a.s_dx = dx(a.chunk).S;
+  a.s_dw = dw(a.chunk).S;
   l.both = a.dx && a.dw && l.dx.R == RS && l.dw.R == RS;
   l.part(a.partial, l.both ? l.dx.partial : std::max(l.dx.partial, l.dw.partial));
   if (l.both) l.part(a.partial_dw, l.dw.partial);

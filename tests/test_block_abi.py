@@ -29,6 +29,7 @@ def _refused(fn, *args, word):
     dict(x=None), dict(y=None), dict(x=P + 1), dict(y=P + 2, f32=1), dict(rows=-1), dict(cols=-1), dict(cols=(1 << 18) + 1, ldx=1 << 19, ldy=1 << 19),
     dict(rows=1 << 30, cols=72), dict(p=-0.1), dict(p=1.01), dict(p=math.nan), dict(ldx=63), dict(ldy=63), dict(ldx=1 << 40),
     dict(y=P, ldy=72), dict(step=P + 4),
+    dict(rows=1 << 28, cols=64), dict(rows=1 << 16, cols=1 << 18, ldx=1 << 18, ldy=1 << 18),
 ])
 def test_dropout_refusals(bad):
     a = dict(x=P, ldx=64, y=2 * P, ldy=64, f32=0, rows=9, cols=64, p=0.5, seed=1, step=None)
@@ -154,6 +155,7 @@ def _head(**kw):
     dict(ldx=56), dict(ldw=56), dict(ldx=68), dict(ldw=1 << 21), dict(x=P + 8), dict(w=P + 2), dict(lddx=56), dict(lddx=68), dict(dx=P + 8),
     dict(lddw=56), dict(lddw=68), dict(dw=P + 8), dict(grad_f32=1, lddw=66), dict(accumulate=1), dict(bias=None), dict(bias=P + 2),
     dict(labels=P + 1), dict(row_weight=P + 2), dict(lse=P + 1), dict(db=P + 1), dict(db=P + 2, grad_f32=1), dict(inv_n=P + 3),
+    dict(N=(1 << 25) + 1), dict(dx=P), dict(dw=2 * P),
 ])
 def test_head_refusals(bad):
     _refused("sat_op_linear_xent", C.byref(_head(**bad)), None, word="linear_xent")
