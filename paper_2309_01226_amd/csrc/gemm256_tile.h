@@ -261,11 +261,11 @@ __device__ __forceinline__ void gemm256_loop(floatx16 (&acc)[4][4], bf16* smem, 
 }
 
 // The same product on a tile of 128 x 128 (a wave: 64 x 64), for products that are too small to give every CU a
-// tile of 256: four stages of both operands in 128 KB, the copies three K-tiles ahead, one barrier for each.
+// tile of 256: STAGES stages of both operands (32 KB each), the copies STAGES - 1 K-tiles ahead, one barrier for each.
+// Four stages where no CU has more than one such tile, two (and two workgroups on a CU) where there are more.
 constexpr int RS = 128;
-constexpr int STAGES = 4;
-constexpr int SMALL_LDS = STAGES * 2 * RS * BK;  // elements
-template <int AL, int BL, class KO, class RA, class RB>
+constexpr int small_lds(int stages) { return stages * 2 * RS * BK; }  // elements
+template <int STAGES, int AL, int BL, class KO, class RA, class RB>
 __device__ __forceinline__ void gemm128_loop(floatx16 (&acc)[2][2], bf16* smem, const Loader<AL, RS>& la,
                                              const Loader<BL, RS>& lb, const Frags<AL, RS>& FA, const Frags<BL, RS>& FB,
                                              RA rsA, RB rsB, int nk, KO kof, int K, int wave) {

@@ -12,9 +12,9 @@
 // gradients, (m - z) log2 e as a number of 16 bits, in steps of 2^-10 up to 32 and of 2^-8 up to 160.  Once all
 // pieces give lse, dz is formed from those in place.  Half a step is 2^-11.5 of exp(z - m) (2^-9.5 of those below
 // 2^-32), a small part of the rounding that a bf16 operand of the two other products takes, which exp(z - m)
-// held as bf16 would double.  The label's entry, where 1 is subtracted, comes from the fp32 logit instead.  The numbers of a chunk of tokens are what is kept, at
-// most 1 GiB, whatever N; several chunks add up dw in fp32 (8192 x 50257 x 768: 2.37 ms as one chunk, 2.48 as two,
-// 2.81 as four).
+// held as bf16 would double.  The label's entry, where 1 is subtracted, comes from the fp32 logit instead.  The
+// numbers of a chunk of tokens are what is kept, at most 1 GiB, whatever N; several chunks add up dw in fp32
+// (8192 x 50257 x 768: 2.37 ms as one chunk, 2.48 as two, 2.81 as four, before the last steps).
 //
 // dz is an operand in bf16.  A chunk with no more rows than a tile has keeps what that rounding loses as a
 // second operand: few roundings do not average out, and the products of so few rows are bound by the
@@ -167,21 +167,22 @@ __global__ __launch_bounds__(256) void xent_copy_kernel(LinearXentArgs a) {
   }
 }
 
-// Both at once for up to FEW rows: a workgroup counts the rows before its own 64 (and all of them) for itself.
+// Both at once for up to FEW rows: a workgroup, which has four rows, counts the rows before them (and all of them) for
+// itself.  (1019 x 739 x 2576, 30% without a label: 6 us; with 64 rows for a workgroup, 33.)
 constexpr int FEW = 4096;
 __global__ __launch_bounds__(256) void xent_rows_few_kernel(LinearXentArgs a) {
-  __shared__ int sums[2][4], at[64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r0 = blockIdx.x * 64;
-  const auto live = [&](int r) {
-    const int label = r < a.N ? a.labels[r] : -1;
+  __shared__ int sums[2][4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r0 = blockIdx.x * 4, r = r0 + wave;
+  const auto live = [&](int i) {
+    const int label = i < a.N ? a.labels[i] : -1;
     return label >= 0 && label < a.V;
   };
   int before = 0, all = 0;
 #pragma unroll 4
-  for (int r = threadIdx.x; r < a.N; r += 256) {
-    const int one = live(r);
+  for (int i = threadIdx.x; i < a.N; i += 256) {
+    const int one = live(i);
     all += one;
-    before += r < r0 ? one : 0;
+    before += i < r0 ? one : 0;
   }
   before = (int)wave_total((float)before);  // whole numbers below 2^24: exact
   all = (int)wave_total((float)all);
@@ -190,35 +191,35 @@ __global__ __launch_bounds__(256) void xent_rows_few_kernel(LinearXentArgs a) {
     sums[1][wave] = all;
   }
   __syncthreads();
-  before = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
   all = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
-  if (wave == 0) {
-    const int r = r0 + lane;
-    const bool on = live(r);
-    const uint64_t mask = __builtin_amdgcn_ballot_w64(on);
-    const int p = before + __popcll(mask & ((1ull << lane) - 1));
-    at[lane] = on ? p : -1;
-    if (on) {
-      a.idx[p] = r;
-      a.lab[p] = a.labels[r];
-    } else if (r < a.N) {
-      a.row_loss[r] = a.lse[r] = 0.f;
-    }
-    if (r0 == 0 && lane == 0) {
+  if (r0 == 0) {
+    if (threadIdx.x == 0) {
       a.meta[0] = all;
       a.inv_n[0] = 1.f / max(all, 1);
     }
+    if (wave == 1 || wave == 2) choose_slices(a, all, wave);
   }
-  if (r0 == 0 && (wave == 1 || wave == 2)) choose_slices(a, all, wave);
-  __syncthreads();
-  if (all == a.N) return;
-  const u32x4 zero = {0, 0, 0, 0};
-  for (int i = wave; i < min(64, a.N - r0); i += 4) {
-    const int r = r0 + i, p = at[i];
-    for (int c = lane * 8; c < a.d; c += 512) {
-      if (p >= 0) *reinterpret_cast<u32x4*>(a.xc + (long)p * a.d + c) = *reinterpret_cast<const u32x4*>(a.x + r * a.ldx + c);
-      else if (a.dx != nullptr) *reinterpret_cast<u32x4*>(a.dx + r * a.lddx + c) = zero;
+  if (r >= a.N) return;
+  const int label = a.labels[r];
+  const bool on = label >= 0 && label < a.V;
+  int p = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+  for (int i = r0; i < r; ++i) p += live(i);
+  if (lane == 0) {
+    if (on) {
+      a.idx[p] = r;
+      a.lab[p] = label;
+    } else {
+      a.row_loss[r] = a.lse[r] = 0.f;
     }
+  }
+  if (all == a.N || (!on && a.dx == nullptr)) return;
+  const bf16* from = a.x + r * a.ldx;
+  bf16* to = on ? a.xc + (long)p * a.d : a.dx + r * a.lddx;
+#pragma unroll 4
+  for (int c = lane * 8; c < a.d; c += 512) {
+    u32x4 v = {0, 0, 0, 0};
+    if (on) v = *reinterpret_cast<const u32x4*>(from + c);
+    *reinterpret_cast<u32x4*>(to + c) = v;
   }
 }
 
@@ -235,16 +236,17 @@ struct Operand {
   }
 };
 
-// A tile of R x R, of which a wave has W = R / 2 rows and columns in S x S accumulators.
+// A tile of R x R, of which a wave has W = R / 2 rows and columns in S x S accumulators; elements of LDS with ST stages.
 template <int R>
 struct Tile {
-  static constexpr int W = R / 2, S = W / 32, LDS = R == BT ? 5 * OPE : SMALL_LDS;
+  static constexpr int W = R / 2, S = W / 32;
 };
+constexpr int lds_of(int R, int ST) { return R == BT ? 5 * OPE : small_lds(ST); }
 template <int R>
 using Acc = floatx16[Tile<R>::S][Tile<R>::S];
 
 // acc += A B over k in [kb, kb + K), and, where A2 is there, A2 B as well (A2's pitch is A's).
-template <int R, int AL, int BL>
+template <int R, int ST, int AL, int BL>
 __device__ __forceinline__ void tile_product(Acc<R>& acc, bf16* smem, const Operand<AL>& A, const bf16* A2, const Operand<BL>& B,
                                              int m0, int M, int n0, int N, int kb, int K, int wave) {
   Loader<AL, R> la;
@@ -260,7 +262,7 @@ __device__ __forceinline__ void tile_product(Acc<R>& acc, bf16* smem, const Oper
   const auto rsB = [&](int, int k0) { return B.at(n0, kb, k0); };
   const auto kof = [&](int t) { return t < nk ? (t < n1 ? t : t - n1) * BK : K; };
   if constexpr (R == BT) gemm256_loop<AL, BL>(acc, smem, la, lb, FA, FB, rsA, rsB, nk, kof, K, wave);
-  else gemm128_loop<AL, BL>(acc, smem, la, lb, FA, FB, rsA, rsB, nk, kof, K, wave);
+  else gemm128_loop<ST, AL, BL>(acc, smem, la, lb, FA, FB, rsA, rsB, nk, kof, K, wave);
 }
 
 // u = (z - m) log2 e <= 0 as 16 bits in the low half of a word: steps of 2^-10 from 0 down to -32, of 2^-8 from there to
@@ -277,9 +279,9 @@ __device__ __forceinline__ float from_steps(uint32_t q) {
 
 // The tile's rows (in the wave's part: 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4) are vocabulary
 // entries, its columns (32 j + lane % 32) tokens.
-template <int R, bool TRAIN>
-__global__ __launch_bounds__(NT, 1) void xent_logits_kernel(LinearXentArgs a, int first) {
-  __shared__ __attribute__((aligned(1024))) bf16 smem[Tile<R>::LDS];
+template <int R, int ST, bool TRAIN>
+__global__ __launch_bounds__(NT, ST == 2 ? 2 : 1) void xent_logits_kernel(LinearXentArgs a, int first) {
+  __shared__ __attribute__((aligned(1024))) bf16 smem[lds_of(R, ST)];
   constexpr int S = Tile<R>::S, W = Tile<R>::W;
   const int n = chunk_rows(a, first), total = tiles_of(R, a.V, n);
   if ((int)blockIdx.x >= total) return;
@@ -320,7 +322,7 @@ __global__ __launch_bounds__(NT, 1) void xent_logits_kernel(LinearXentArgs a, in
   Operand<LAY_K> A = {a.w, a.ldw}, B;
   B.p = compact_x(a, B.ld);
   B.p += first * B.ld;
-  tile_product<R, LAY_K, LAY_K>(acc, smem, A, nullptr, B, m0, a.V, n0, n, 0, a.d, wave);
+  tile_product<R, ST, LAY_K, LAY_K>(acc, smem, A, nullptr, B, m0, a.V, n0, n, 0, a.d, wave);
 
   const int pieces = cdiv(a.V, W);
   // the wave's 16 bits of its part, [32 tokens][W entries] at a time
@@ -541,7 +543,7 @@ struct RowsOut {
 
 // C[m, c] = sum_k (A + A2)(m, k) B(c, k) of a tile (A2 may be absent): to `o`, or, where the tile's K is split, to
 // its slice's partial product [R][R] in `partial`.
-template <int R, int AL>
+template <int R, int ST, int AL>
 __device__ __forceinline__ void product(bf16* smem, const Operand<AL>& A, const bf16* A2, const Operand<LAY_MN>& B, int M, int N,
                                         int K, const Split& sp, int bid, float* partial, const RowsOut& o) {
   if (bid >= sp.groups()) return;
@@ -570,7 +572,7 @@ __device__ __forceinline__ void product(bf16* smem, const Operand<AL>& A, const 
     for (int j = 0; j < S; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  tile_product<R, AL, LAY_MN>(acc, smem, A, A2, B, m0, M, n0, N, kb, kc, wave);
+  tile_product<R, ST, AL, LAY_MN>(acc, smem, A, A2, B, m0, M, n0, N, kb, kc, wave);
   float* st = reinterpret_cast<float*>(smem) + wave * 32 * EP;
   const int cl = 8 * (lane % (W / 8)), cw = (wave & 1) * W + cl;
 #pragma unroll
@@ -617,14 +619,14 @@ __device__ __forceinline__ Split dw_split(int R, const LinearXentArgs& a, int n)
   return Split{tiles / CUS * CUS, tiles % CUS, n == a.chunk ? a.s_dw : a.meta[2]};
 }
 
-template <int R>
+template <int R, int ST>
 __device__ __forceinline__ void dx_tile(const LinearXentArgs& a, int first, bf16* smem, int bid) {
   const int n = chunk_rows(a, first);
   const Operand<LAY_K> A = {a.e, a.lde};
   const Operand<LAY_MN> B = {a.w, a.ldw};
-  product<R, LAY_K>(smem, A, n <= BT ? a.e2 : nullptr, B, n, a.d, a.V, dx_split(R, a, n), bid, a.partial, dx_out(a, first));
+  product<R, ST, LAY_K>(smem, A, n <= BT ? a.e2 : nullptr, B, n, a.d, a.V, dx_split(R, a, n), bid, a.partial, dx_out(a, first));
 }
-template <int R>
+template <int R, int ST>
 __device__ __forceinline__ void dw_tile(const LinearXentArgs& a, int first, bf16* smem, int bid) {
   if (chunk_idle(a, first)) return;
   const int n = chunk_rows(a, first);
@@ -632,24 +634,25 @@ __device__ __forceinline__ void dw_tile(const LinearXentArgs& a, int first, bf16
   Operand<LAY_MN> B;
   B.p = compact_x(a, B.ld);
   B.p += first * B.ld;
-  product<R, LAY_MN>(smem, A, n <= BT ? a.e2 : nullptr, B, a.V, a.d, n, dw_split(R, a, n), bid, a.partial_dw, dw_out(a, first));
+  product<R, ST, LAY_MN>(smem, A, n <= BT ? a.e2 : nullptr, B, a.V, a.d, n, dw_split(R, a, n), bid, a.partial_dw, dw_out(a, first));
 }
 
-template <int R>
-__global__ __launch_bounds__(NT, 1) void xent_dx_kernel(LinearXentArgs a, int first) {
-  __shared__ __attribute__((aligned(1024))) bf16 smem[Tile<R>::LDS];
-  dx_tile<R>(a, first, smem, blockIdx.x);
+template <int R, int ST>
+__global__ __launch_bounds__(NT, ST == 2 ? 2 : 1) void xent_dx_kernel(LinearXentArgs a, int first) {
+  __shared__ __attribute__((aligned(1024))) bf16 smem[lds_of(R, ST)];
+  dx_tile<R, ST>(a, first, smem, blockIdx.x);
 }
-template <int R>
-__global__ __launch_bounds__(NT, 1) void xent_dw_kernel(LinearXentArgs a, int first) {
-  __shared__ __attribute__((aligned(1024))) bf16 smem[Tile<R>::LDS];
-  dw_tile<R>(a, first, smem, blockIdx.x);
+template <int R, int ST>
+__global__ __launch_bounds__(NT, ST == 2 ? 2 : 1) void xent_dw_kernel(LinearXentArgs a, int first) {
+  __shared__ __attribute__((aligned(1024))) bf16 smem[lds_of(R, ST)];
+  dw_tile<R, ST>(a, first, smem, blockIdx.x);
 }
 // Both products at once, where each is small: the first `groups` workgroups dx, the others dw.
-__global__ __launch_bounds__(NT, 1) void xent_both_kernel(LinearXentArgs a, int first, int groups) {
-  __shared__ __attribute__((aligned(1024))) bf16 smem[SMALL_LDS];
-  if ((int)blockIdx.x < groups) dx_tile<RS>(a, first, smem, blockIdx.x);
-  else dw_tile<RS>(a, first, smem, blockIdx.x - groups);
+template <int ST>
+__global__ __launch_bounds__(NT, ST == 2 ? 2 : 1) void xent_both_kernel(LinearXentArgs a, int first, int groups) {
+  __shared__ __attribute__((aligned(1024))) bf16 smem[lds_of(RS, ST)];
+  if ((int)blockIdx.x < groups) dx_tile<RS, ST>(a, first, smem, blockIdx.x);
+  else dw_tile<RS, ST>(a, first, smem, blockIdx.x - groups);
 }
 
 // The slices of a product's split tiles added in order, 2048 elements of a tile at a time by each of `groups` workgroups.
@@ -774,17 +777,29 @@ hipError_t launch_linear_xent(LinearXentArgs a, void* ws, hipStream_t s) {
   plan(a, l);
   const bool train = a.dx || a.dw || a.db;
   const int RL = l.logits.R, RX = l.dx.R, RW = l.dw.R;
-  const auto logits = RL == BT ? (train ? xent_logits_kernel<BT, true> : xent_logits_kernel<BT, false>)
-                               : (train ? xent_logits_kernel<RS, true> : xent_logits_kernel<RS, false>);
+  const int tiles = tiles_of(RL, a.V, a.chunk), live = tiles_of(RL, a.V, std::min(a.N, a.chunk));
+  // tiles of 128: four stages where no CU has more than one (64 x 50400 x 4096: 142 us for the logits), else two and two
+  // workgroups on a CU (131)
+  const auto pick = [](int R, int groups, auto large, auto four, auto two) {
+    return R == BT ? large : groups <= CUS ? four : two;
+  };
+  const auto logits = train ? pick(RL, live, xent_logits_kernel<BT, 4, true>, xent_logits_kernel<RS, 4, true>,
+                                   xent_logits_kernel<RS, 2, true>)
+                            : pick(RL, live, xent_logits_kernel<BT, 4, false>, xent_logits_kernel<RS, 4, false>,
+                                   xent_logits_kernel<RS, 2, false>);
+  const auto dx = pick(RX, l.dx.groups, xent_dx_kernel<BT, 4>, xent_dx_kernel<RS, 4>, xent_dx_kernel<RS, 2>);
+  const auto dw = pick(RW, l.dw.groups, xent_dw_kernel<BT, 4>, xent_dw_kernel<RS, 4>, xent_dw_kernel<RS, 2>);
+  const int groups = l.dx.groups + l.dw.groups;
+  const auto both = groups <= CUS ? xent_both_kernel<4> : xent_both_kernel<2>;
   if (a.N <= FEW) {
-    hipLaunchKernelGGL(xent_rows_few_kernel, dim3(std::max(1, cdiv(a.N, 64))), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(xent_rows_few_kernel, dim3(std::max(1, cdiv(a.N, 4))), dim3(256), 0, s, a);
   } else {
     hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, a);
     hipLaunchKernelGGL(xent_copy_kernel, dim3(cdiv(a.N, 4)), dim3(256), 0, s, a);
   }
   // without rows, too: dw and db of none
   for (int first = 0; first < std::max(a.N, 1); first += a.chunk) {
-    hipLaunchKernelGGL(logits, dim3(tiles_of(RL, a.V, a.chunk)), dim3(NT), 0, s, a, first);
+    hipLaunchKernelGGL(logits, dim3(tiles), dim3(NT), 0, s, a, first);
     const dim3 tokens(cdiv(a.chunk, 4)), scaling(cdiv(a.V, 2048) * cdiv(a.chunk, a.tb));
     if (!train) {
       hipLaunchKernelGGL(xent_join_kernel<false>, tokens, dim3(256), 0, s, a, first);
@@ -802,16 +817,16 @@ hipError_t launch_linear_xent(LinearXentArgs a, void* ws, hipStream_t s) {
       if (x + w) hipLaunchKernelGGL(xent_slices_kernel, dim3(x + w), dim3(256), 0, s, a, first, RX, x, RW);
     };
     if (l.both) {
-      hipLaunchKernelGGL(xent_both_kernel, dim3(l.dx.groups + l.dw.groups), dim3(NT), 0, s, a, first, l.dx.groups);
+      hipLaunchKernelGGL(both, dim3(groups), dim3(NT), 0, s, a, first, l.dx.groups);
       slices(gx, gw);
       continue;
     }
     if (a.dx) {
-      hipLaunchKernelGGL(RX == BT ? xent_dx_kernel<BT> : xent_dx_kernel<RS>, dim3(l.dx.groups), dim3(NT), 0, s, a, first);
+      hipLaunchKernelGGL(dx, dim3(l.dx.groups), dim3(NT), 0, s, a, first);
       slices(gx, 0);
     }
     if (a.dw) {
-      hipLaunchKernelGGL(RW == BT ? xent_dw_kernel<BT> : xent_dw_kernel<RS>, dim3(l.dw.groups), dim3(NT), 0, s, a, first);
+      hipLaunchKernelGGL(dw, dim3(l.dw.groups), dim3(NT), 0, s, a, first);
       slices(0, gw);
     }
   }
