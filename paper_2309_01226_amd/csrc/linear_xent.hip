@@ -36,11 +36,11 @@ constexpr float INF = __builtin_inff();
 __host__ __device__ inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 
 // A product of `tiles` tiles of R rows and columns and `ktiles` 64-deep steps on 256 CUs: `full` tiles in whole
-// rounds, one on a CU, and the rest, whose K is split in S slices where that shortens the last round.  Cost in ns: a
-// step of K takes 1650 (of a tile of 128: 700), a round's start and end 8000 (4000), a partial tile's way to memory and
-// back 100 (26), the launch that adds the slices 4000.  At most 128 MB of partial tiles.  Whole numbers: the host plans the
-// workspace and the launch by what the rows' kernel then chooses on the device (by the number of rows that take part), so
-// both have to choose alike.
+// rounds, one for each CU, and the rest, whose K is split in S slices where that shortens the last round.  Cost in ns:
+// a round takes 1650 for each step and 11000 for its start and end, of tiles of 128 700 and 4000, but in whole rounds,
+// with two on a CU, 580 and 1000; a partial tile's way to memory and back 100 (26), the launch that adds the slices
+// 4000.  At most 128 MB of partial tiles.  Whole numbers: the host plans the workspace and the launch by what the
+// rows' kernel then chooses on the device (by the number of rows that take part), so both have to choose alike.
 constexpr int SLICES = 64;
 struct Split {
   int full, rest, S;
@@ -50,11 +50,14 @@ struct Split {
 __host__ __device__ inline bool slices_fit(int R, int tiles, int ktiles, int s) {
   return s == 1 || (tiles % CUS * s <= (R == BT ? 512 : 2048) && ktiles >= 4 * s);
 }
+__host__ __device__ inline int64_t round_ns(int R, int steps) {
+  return R == BT ? (int64_t)steps * 1650 + 11000 : (int64_t)steps * 700 + 4000;
+}
 // Cost of the rest in s slices; the least number wins, of equal ones the fewest slices (the low bits).
 __host__ __device__ inline int64_t slices_key(int R, int tiles, int ktiles, int s) {
-  const int rest = tiles % CUS, step = R == BT ? 1650 : 700, ends = R == BT ? 8000 : 4000, way = R == BT ? 100 : 26;
+  const int rest = tiles % CUS, way = R == BT ? 100 : 26;
   if (!slices_fit(R, tiles, ktiles, s)) return INT64_MAX;
-  const int64_t ns = (int64_t)cdiv(rest * s, CUS) * ((int64_t)cdiv(ktiles, s) * step + ends) + (s > 1 ? way * rest * s + 4000 : 0);
+  const int64_t ns = cdiv(rest * s, CUS) * round_ns(R, cdiv(ktiles, s)) + (s > 1 ? way * rest * s + 4000 : 0);
   return ns * 128 + s;
 }
 // The best number of slices, by one wave.
@@ -67,7 +70,7 @@ __device__ __forceinline__ int wave_slices(int R, int tiles, int ktiles) {
 inline Split split_of(int R, int tiles, int ktiles, int64_t* ns = nullptr, int most = SLICES) {
   int64_t key = INT64_MAX;
   for (int s = 1; s <= most && slices_fit(R, tiles, ktiles, s); ++s) key = std::min(key, slices_key(R, tiles, ktiles, s));
-  if (ns) *ns = key / 128 + (int64_t)(tiles / CUS) * ((int64_t)ktiles * (R == BT ? 1650 : 700) + (R == BT ? 8000 : 4000));
+  if (ns) *ns = key / 128 + tiles / CUS * (R == BT ? round_ns(R, ktiles) : (int64_t)ktiles * 580 + 1000);
   return Split{tiles / CUS * CUS, tiles % CUS, (int)(key & 127)};
 }
 __host__ __device__ inline int tiles_of(int R, int M, int N) { return cdiv(M, R) * cdiv(N, R); }
@@ -725,17 +728,26 @@ void plan(LinearXentArgs& a, Layout& l) {
   // tokens of a workgroup of the scaling pass: fewer where there would be few workgroups
   a.tb = 64;
   while (a.tb > 4 && (int64_t)cdiv(a.V, 2048) * cdiv(std::min(a.N, a.chunk), a.tb) < 4 * CUS) a.tb /= 2;
-  // tiles of 128 where those of 256 would leave most CUs without one, by the estimated time
+  // tiles of 128 or 256 by the estimated time; a launch saved where both gradients take those of 128.  256 has the
+  // larger rate (8192 x 50257 x 768: 2.26 ms, with tiles of 128 2.49), 128 the shorter ends and more tiles to share out
+  // (64 x 50400 x 4096: 416 us against 522, 1024 x 1024 x 1024: 41 against 100)
   const int n = std::min(a.N, a.chunk);
-  const auto pick = [&](int large, int small, int steps, int most) {
-    int64_t at_large, at_small;
-    split_of(BT, large, steps, &at_large, most);
-    split_of(RS, small, steps, &at_small, most);
-    return at_small < at_large ? RS : BT;
+  const auto cost = [](int R, int tiles, int steps, int most = SLICES) {
+    int64_t ns;
+    split_of(R, tiles, steps, &ns, most);
+    return ns;
   };
-  l.logits.R = pick(tiles_of(BT, a.V, n), tiles_of(RS, a.V, n), cdiv(a.d, BK), 1);
-  l.dx.R = a.rx = pick(dx_tiles(BT, a, n), dx_tiles(RS, a, n), dx_steps(a), SLICES);
-  l.dw.R = a.rw = pick(dw_tiles(BT, a), dw_tiles(RS, a), dw_steps(n), SLICES);
+  const auto logits = [&](int R) {  // with the exponentials, which tiles of 256 have within their 11000
+    const int tiles = tiles_of(R, a.V, n);
+    return cost(R, tiles, cdiv(a.d, BK), 1) + (R == RS ? tiles / CUS * 1000 : 0);
+  };
+  const auto dx = [&](int R) { return cost(R, dx_tiles(R, a, n), dx_steps(a)); };
+  const auto dw = [&](int R) { return cost(R, dw_tiles(R, a), dw_steps(n)); };
+  const int64_t x = dx(RS) - dx(BT), w = dw(RS) - dw(BT);
+  const bool together = a.dx && a.dw && x + w - 8000 < std::min<int64_t>(x, 0) + std::min<int64_t>(w, 0);
+  l.logits.R = logits(RS) < logits(BT) ? RS : BT;
+  l.dx.R = a.rx = together || x < 0 ? RS : BT;
+  l.dw.R = a.rw = together || w < 0 ? RS : BT;
   a.piece = l.logits.R / 2;
   l.part(a.meta, 64);
   l.part(a.idx, a.N);
@@ -750,12 +762,12 @@ void plan(LinearXentArgs& a, Layout& l) {
   l.part(a.dbsum, a.db && !a.dw_f32 && a.N > a.chunk ? a.V : 0);
   l.part(a.dwsum, a.dw && !a.dw_f32 && a.N > a.chunk ? (int64_t)a.V * a.d : 0);
   // the most that any number of rows that take part asks for
-  const auto dx = [&](int rows) { return split_of(a.rx, dx_tiles(a.rx, a, rows), dx_steps(a)); };
-  const auto dw = [&](int rows) { return split_of(a.rw, dw_tiles(a.rw, a), dw_steps(rows)); };
-  for (int i = 0; a.dx && i <= a.chunk; i += a.rx) l.dx.join(dx(i));
-  for (int i = 0; a.dw && i <= a.chunk; i += BK) l.dw.join(dw(i));
-  a.s_dx = dx(a.chunk).S;
-  a.s_dw = dw(a.chunk).S;
+  const auto split_dx = [&](int rows) { return split_of(a.rx, dx_tiles(a.rx, a, rows), dx_steps(a)); };
+  const auto split_dw = [&](int rows) { return split_of(a.rw, dw_tiles(a.rw, a), dw_steps(rows)); };
+  for (int i = 0; a.dx && i <= a.chunk; i += a.rx) l.dx.join(split_dx(i));
+  for (int i = 0; a.dw && i <= a.chunk; i += BK) l.dw.join(split_dw(i));
+  a.s_dx = split_dx(a.chunk).S;
+  a.s_dw = split_dw(a.chunk).S;
   l.both = a.dx && a.dw && l.dx.R == RS && l.dw.R == RS;
   l.part(a.partial, l.both ? l.dx.partial : std::max(l.dx.partial, l.dw.partial));
   if (l.both) l.part(a.partial_dw, l.dw.partial);
