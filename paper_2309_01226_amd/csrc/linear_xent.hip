@@ -248,7 +248,8 @@ constexpr int lds_of(int R, int ST) { return R == BT ? 5 * OPE : small_lds(ST); 
 template <int R>
 using Acc = floatx16[Tile<R>::S][Tile<R>::S];
 
-// acc += A B over k in [kb, kb + K), and, where A2 is there, A2 B as well (A2's pitch is A's).
+// acc += A B over k in [kb, kb + K), and, where A2 is there, A2 B as well (A2's pitch is A's): each K-tile of B is
+// asked for twice in a row, and comes from memory once.
 template <int R, int ST, int AL, int BL>
 __device__ __forceinline__ void tile_product(Acc<R>& acc, bf16* smem, const Operand<AL>& A, const bf16* A2, const Operand<BL>& B,
                                              int m0, int M, int n0, int N, int kb, int K, int wave) {
@@ -260,10 +261,10 @@ __device__ __forceinline__ void tile_product(Acc<R>& acc, bf16* smem, const Oper
   Frags<BL, R> FB;
   FA.init((wave >> 1) * Tile<R>::W);
   FB.init((wave & 1) * Tile<R>::W);
-  const int n1 = cdiv(K, BK), nk = A2 != nullptr ? 2 * n1 : n1;
-  const auto rsA = [&](int t, int k0) { return Operand<AL>{t < n1 ? A.p : A2, A.ld}.at(m0, kb, k0); };
+  const int parts = A2 != nullptr ? 2 : 1, nk = parts * cdiv(K, BK);
+  const auto rsA = [&](int t, int k0) { return Operand<AL>{t & (parts - 1) ? A2 : A.p, A.ld}.at(m0, kb, k0); };
   const auto rsB = [&](int, int k0) { return B.at(n0, kb, k0); };
-  const auto kof = [&](int t) { return t < nk ? (t < n1 ? t : t - n1) * BK : K; };
+  const auto kof = [&](int t) { return t < nk ? (t >> (parts - 1)) * BK : K; };
   if constexpr (R == BT) gemm256_loop<AL, BL>(acc, smem, la, lb, FA, FB, rsA, rsB, nk, kof, K, wave);
   else gemm128_loop<ST, AL, BL>(acc, smem, la, lb, FA, FB, rsA, rsB, nk, kof, K, wave);
 }
