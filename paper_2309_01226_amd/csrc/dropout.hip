@@ -16,10 +16,10 @@ namespace {
 
 constexpr int NT = 256;
 constexpr int U = 1;  // items of a thread (8192 x 16384: 91.5 us; two 101.5, four 103.6, cached stores)
-// Elements from which on bf16 results go past the caches: what is read and written then exceeds the last-level one
-// (8192 x 16384: 91.5 -> 85 us; 20000 x 4096: 54 -> 49; 16384 x 4096: 41.0 and 42.4).  Not fp32, whose lanes store
-// two 16-byte halves of lines apart (32768 x 4096: 185 -> 197 us).
-constexpr int64_t kStream = 75000000;
+// Elements from which on bf16 results go past the caches: what is read and written then nearly fills the last-level one
+// of 256 MB (8192 x 16384: 91.5 -> 85 us; in turn with other operands, 16384 x 4096: 46.7 -> 45.2).  Not fp32, whose
+// lanes store two 16-byte halves of lines apart (32768 x 4096: 185 -> 197 us).
+constexpr int64_t kStream = 60000000;
 
 // x / n for inv = 2^32 / n + 1 (0 for n = 1): exact while x n < 2^32.
 __device__ __forceinline__ int div_by(int x, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)x, inv) : x; }

@@ -11,8 +11,8 @@
 //   subtract no mean.
 //
 // Bound by HBM: every array is read or written once (fp32 stream, 12 bytes an element forward and 18
-// backward).  16384 x 4096, fp32, both norms: forward 130 us, 6.2 TB/s, backward 219 us, 5.5 TB/s (a copy of 1 GiB:
-// 5.0); 16448 x 1280, bf16, backward 50 us, 5.1 TB/s; one row of 4096 9 us, the call's host side.
+// backward).  16384 x 4096, fp32, both norms: forward 146 us, 5.5 TB/s, backward 213 us, 5.7 TB/s (a copy of 1 GiB:
+// 5.0); 16448 x 1280, bf16, backward 50 us, 5.0 TB/s; one row of 4096 9 us, the call's host side.
 //
 // A row belongs to d / 512 waves, or to 8, 16 or 32 lanes of one, eight columns a thread, so that a thread's
 // columns stay the same from row to row: gains and the sums of their gradients live in its registers, and the next
@@ -29,7 +29,7 @@
 namespace {
 
 constexpr int CUS = 256;
-constexpr int64_t kStream = 450000000;  // bytes of a call
+constexpr int64_t kStream = 240000000;  // bytes of a call
 
 // NARROW: rows of up to 256 columns, on 8, 16 or 32 lanes; else a row's place is the same for a whole wave.
 template <bool NARROW>
@@ -122,7 +122,8 @@ __device__ __forceinline__ float2 row_stats(const RowPlace<NARROW>& p, Shared& s
 // offset past the end of the buffer, for which the hardware reads zeros and writes nothing.  So no access
 // stands behind a branch and the compiler's waits count exactly: the next row's loads stay in flight over the
 // whole row (with branches it has to wait for them at once: 16384 rows of 4096, backward, 280 us instead of 229).
-// FAST 2: past the caches, but for fp32 stores, whose lanes write halves of lines apart.
+// FAST 2: bf16 past the caches.  Not fp32, whose lanes take halves of lines apart (16384 x 4096, backward with both
+// norms: 219 us with the fp32 loads past them too, 214 without).
 constexpr uint32_t NOWHERE = 0x80000000u;
 constexpr int NONTEMPORAL = 2;
 template <class T>
@@ -144,8 +145,8 @@ __device__ __forceinline__ Raw8<T> get(const RowPlace<NARROW>& p, const T* m, in
   if constexpr (sizeof(T) == 2) {
     r.w = __builtin_amdgcn_raw_buffer_load_b128(b, o, 0, AUX);
   } else {
-    r.w[0] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(b, o, 0, AUX));
-    r.w[1] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(b, o, 16, AUX));
+    r.w[0] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(b, o, 0, 0));
+    r.w[1] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(b, o, 16, 0));
   }
   return r;
 }
@@ -483,12 +484,10 @@ template <class XT, bool POST>
 Kernel bwd_kernel(int L, int most, int fast) {
   if (L < 64) return fast ? residual_norm_bwd_kernel<XT, 768, POST, 1, true> : residual_norm_bwd_kernel<XT, 768, POST, 0, true>;
   if (!fast) return residual_norm_bwd_kernel<XT, 1024, POST, 0>;
-  if constexpr (!POST || sizeof(XT) == 2) {
-    if (fast == 2)
-      return most == 512   ? residual_norm_bwd_kernel<XT, 512, POST, 2>
-             : most == 768 ? residual_norm_bwd_kernel<XT, 768, POST, 2>
-                           : residual_norm_bwd_kernel<XT, 1024, POST, 2>;
-  }
+  if (fast == 2)
+    return most == 512   ? residual_norm_bwd_kernel<XT, 512, POST, 2>
+           : most == 768 ? residual_norm_bwd_kernel<XT, 768, POST, 2>
+                         : residual_norm_bwd_kernel<XT, 1024, POST, 2>;
   return most == 512   ? residual_norm_bwd_kernel<XT, 512, POST, 1>
          : most == 768 ? residual_norm_bwd_kernel<XT, 768, POST, 1>
                        : residual_norm_bwd_kernel<XT, 1024, POST, 1>;
@@ -508,11 +507,11 @@ int64_t residual_norm_ws(int T, int d, bool post, int sums) {
   return (int64_t)std::max(bwd_groups(T, d, bwd_shape(d, true)), bwd_groups(T, d, bwd_shape(d, false))) * sums * d;
 }
 
-// How rows are accessed: 1 where they are whole 16-byte pieces, of every array that is there; 2 also past the caches, where
-// all of them together exceed the last-level one (256 MB) well (us with and without: 16384 x 4096, fp32, both norms
-// forward 130 and 147, bf16 109 and 113; backward without a norm of the branch 209 and 225; 32768 x 200 18 and 14); not
-// with an fp32 stream for that backward (236 and 217) and for the forward of rows of more than 8 waves (10922 x 6144:
-// 153 and 148).
+// How rows are accessed: 1 where they are whole 16-byte pieces, of every array that is there; 2 with bf16 past the caches
+// as well, where all arrays together nearly fill the last-level one (256 MB), so that the next kernel would not find the
+// results there.  us with and without, operands in turn, rows of 4096: a backward of 300 MB, bf16, 57 and 63; of
+// 1.2 GB, fp32, both norms 213 and 219; a forward of 0.8 GB, fp32, both norms 146 and 152.  A bf16 forward and a copy of h:
+// 200 MB in all 57 and 56, 250 MB 70 and 73, 300 MB 83 and 91.
 static int fast_rows(const ResidualNormArgs& a, bool f32, bool back) {
   bool ok = a.d % 8 == 0;
   const auto rows = [&](const void* p, int64_t ld, int size) {
@@ -531,8 +530,9 @@ static int fast_rows(const ResidualNormArgs& a, bool f32, bool back) {
     rows(a.h, a.ldh, 2);
   }
   if (!ok) return 0;
-  const int64_t bytes = (int64_t)a.T * a.d * (back ? (2 + !!a.pre) * size + 2 * (1 + !!a.pre + (a.post || a.dgate)) : 2 * size + 2 * (1 + !!a.pre));
-  return bytes >= kStream && !(f32 && (back ? a.post != 0 : waves_of_row(a.d) > 8)) ? 2 : 1;
+  const int wide = back ? 2 + !!a.pre : 2, narrow = back ? 1 + !!a.pre + (a.post || a.dgate) : 1 + !!a.pre;  // arrays
+  const int64_t bytes = (int64_t)a.T * a.d * (wide * size + narrow * 2);
+  return bytes >= kStream ? 2 : 1;
 }
 
 hipError_t launch_residual_norm_fwd(ResidualNormArgs a, bool f32, hipStream_t s) {
