@@ -174,8 +174,9 @@ __global__ __launch_bounds__(256) void xent_copy_kernel(LinearXentArgs a) {
 }
 
 // Both at once for up to FEW rows: a workgroup, which has four rows, counts the rows before them (and all of them) for
-// itself.  (1019 x 739 x 2576, 30% without a label: 6 us; with 64 rows for a workgroup, 33.)
-constexpr int FEW = 4096;
+// itself.  (1019 x 739 x 2576, 30% without a label: 6 us; with 64 rows for a workgroup, 33.  The whole of 8192 x 66 x 96, half
+// without: 32 us, with the two kernels above 36; of 16384 rows 50 and 50, of 24000 74 and 67.)
+constexpr int FEW = 12000;
 __global__ __launch_bounds__(256) void xent_rows_few_kernel(LinearXentArgs a) {
   __shared__ int sums[2][4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r0 = blockIdx.x * 4, r = r0 + wave;

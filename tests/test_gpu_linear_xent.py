@@ -119,9 +119,11 @@ def test_few_rows(rows):
     _check(o, _want(i, False))
 
 
-@pytest.mark.parametrize("N,V,d,ignored,dt", [(17000, 300, 64, 0.0, BF), (17000, 300, 64, 0.45, F4), (6000, 50257, 64, 0.0, BF), (40000, 70, 32, 0.7, BF)])
+@pytest.mark.parametrize("N,V,d,ignored,dt", [
+    (17000, 300, 64, 0.0, BF), (17000, 300, 64, 0.45, F4), (6000, 50257, 64, 0.0, BF), (40000, 70, 32, 0.7, BF),
+    (12000, 66, 96, 0.3, BF), (12001, 66, 96, 0.3, F4)])
 def test_chunks(N, V, d, ignored, dt):
-    """More rows than a chunk holds; with many ignored, the last chunks are empty."""
+    """More rows than a chunk holds (with many ignored, the last chunks are empty), or than one kernel numbers."""
     flush("chunks", N, V, d, ignored, dt)
     i = _inputs(N, V, d, ignored, "plain", True)
     o = _outputs(i, dt)
