@@ -23,7 +23,7 @@
 // Bound by the matrix products (6 N V d operations), whose loop is the one of gemm256.hip.  8192 x 50257 x 768: 2.22 ms
 // or 0.85 PFLOP/s, of which the logits take 0.73, dx 0.54, dw 0.58 and the pass that forms dz 0.36 (1.65 GB, 4.6
 // TB/s); 4096 x 50400 x 4096: 4.30 ms, 1.18 PFLOP/s, 1.40, 1.28, 1.52 and 0.16.  8 x 50257 x 1024 without gradients: 25 us,
-// w once at 4.2 TB/s.  64 x 512 x 64: 28 us, the latency of four launches.
+// w once at 4.2 TB/s.  64 x 512 x 64: 27 us, the latency of four launches.
 #include <algorithm>
 
 #include "gemm256_tile.h"
@@ -63,9 +63,10 @@ __host__ __device__ inline int64_t slices_key(int R, int tiles, int ktiles, int 
   const int64_t ns = cdiv(rest * s, CUS) * round_ns(R, cdiv(ktiles, s)) + (s > 1 ? way * rest * s + 4000 : 0);
   return ns * 128 + s;
 }
-// The best number of slices, by one wave.
-__device__ __forceinline__ int wave_slices(int R, int tiles, int ktiles) {
-  int64_t key = slices_key(R, tiles, ktiles, 1 + (threadIdx.x & 63));
+// The best number of slices up to `most`, by one wave.
+__device__ __forceinline__ int wave_slices(int R, int tiles, int ktiles, int most) {
+  const int s = 1 + (threadIdx.x & 63);
+  int64_t key = s <= most ? slices_key(R, tiles, ktiles, s) : INT64_MAX;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) key = min(key, (int64_t)__shfl_xor((long long)key, o, SAT_WAVE));
   return (int)(key & 127);
@@ -112,10 +113,12 @@ __device__ __forceinline__ int xcd_place(int bid, int total) {
   return x * q + min(x, r) + (bid >> 3);
 }
 
-// How the products of the chunk that is not full are split, by one wave each: meta[1] dx, meta[2] dw.
+// How the products of the chunk that is not full are split, by one wave each: meta[1] dx, meta[2] dw (whose K is the
+// chunk's rows: no more slices than a full one's).
 __device__ __forceinline__ void choose_slices(const LinearXentArgs& a, int rows, int which) {
   const int n = rows % a.chunk;
-  const int S = which == 1 ? wave_slices(a.rx, dx_tiles(a.rx, a, n), dx_steps(a)) : wave_slices(a.rw, dw_tiles(a.rw, a), dw_steps(n));
+  const int S = which == 1 ? wave_slices(a.rx, dx_tiles(a.rx, a, n), dx_steps(a), SLICES)
+                           : wave_slices(a.rw, dw_tiles(a.rw, a), dw_steps(n), a.s_dw);
   if ((threadIdx.x & 63) == 0) a.meta[which] = S;
 }
 
@@ -769,11 +772,11 @@ void plan(LinearXentArgs& a, Layout& l) {
   l.part(a.dwsum, a.dw && !a.dw_f32 && a.N > a.chunk ? (int64_t)a.V * a.d : 0);
   // the most that any number of rows that take part asks for
   const auto split_dx = [&](int rows) { return split_of(a.rx, dx_tiles(a.rx, a, rows), dx_steps(a)); };
-  const auto split_dw = [&](int rows) { return split_of(a.rw, dw_tiles(a.rw, a), dw_steps(rows)); };
+  const Split split_dw = split_of(a.rw, dw_tiles(a.rw, a), dw_steps(a.chunk));
   for (int i = 0; a.dx && i <= a.chunk; i += a.rx) l.dx.join(split_dx(i));
-  for (int i = 0; a.dw && i <= a.chunk; i += BK) l.dw.join(split_dw(i));
+  if (a.dw) l.dw.join(split_dw);
   a.s_dx = split_dx(a.chunk).S;
-  a.s_dw = split_dw(a.chunk).S;
+  a.s_dw = split_dw.S;
   l.both = a.dx && a.dw && l.dx.R == RS && l.dw.R == RS;
   l.part(a.partial, l.both ? l.dx.partial : std::max(l.dx.partial, l.dw.partial));
   if (l.both) l.part(a.partial_dw, l.dw.partial);
