@@ -235,10 +235,10 @@ sat_status sat_op_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int3
  * may be NULL without norms.  y may be x (with ldy == ldx); no other output overlaps an input.
  * Backward, from dy (the gradient that reaches y along the stream, in its type; NULL: 0) and dh (bf16, with
  * pre): dx = alpha t and df of t = dy + N_pre'(dh), and, where not NULL, fp32 [d] (written): dg_*, db_* and
- * dgate, summed over the rows in fp32 in an order that depends on T, d and whether there is a post alone.  It reads y (with pre), f (with post or
- * dgate), stats, gains, post's shift, gate and the dropout's arguments; dx may be dy (with lddx == lddy).  ws:
- * fp32 scratch, as much as the _ws call says (T, d, post and which sums are wanted are read); calls that may
- * overlap need one each.  A row that holds NaN or infinities spoils its own rows of the outputs and the sums.
+ * dgate, summed over the rows in fp32 in an order that depends on T, d and whether all rows are 16-byte aligned
+ * alone.  It reads y (with pre), f (with post or dgate), stats, gains, post's shift, gate and the dropout's arguments;
+ * dx may be dy (with lddx == lddy).  ws: fp32 scratch, as much as the _ws call says (T, d and which sums are wanted are
+ * read); calls that may overlap need one each.  A row that holds NaN or infinities spoils its own rows of the outputs and the sums.
  * Arrays are aligned to their elements (16-byte aligned rows are fastest).
  * Errors: SAT_EINVAL for null pointers, sizes, alignment, constants, and a ws that is too small. */
 typedef struct {
@@ -307,8 +307,9 @@ sat_status sat_op_cross_entropy(const float* z, int64_t ldz, const int32_t* labe
  * or infinities spoils its own outputs and the gradients of w and bias.  The same inputs give the same bits.
  * x and w 16-byte aligned with leading dimensions that are multiples of 8 and below 2^21, dx and dw with
  * 16-byte aligned rows.  Outputs overlap no input and no other output.  ws: scratch, 256-byte aligned, of as many
- * bytes as the _ws call says (N, V, d, which gradients, grad_f32 are read): at most 1 GiB for a chunk of the tokens, a
- * copy of x, 128 MiB of partial products, 512 V bytes, and, with bf16 gradients of several chunks, their fp32 sums;
+ * bytes as the _ws call says (N, V, d, which gradients, grad_f32 are read): at most 1 GiB for a chunk of the tokens and a
+ * tenth of that for its statistics, a copy of x, 128 MiB of partial products (256 where dx and dw are small and formed
+ * together), 512 V bytes, and, with bf16 gradients of several chunks, their fp32 sums;
  * calls that may overlap need one each.
  * Errors: SAT_EINVAL for null pointers, sizes, alignment, and a ws that is too small. */
 typedef struct {

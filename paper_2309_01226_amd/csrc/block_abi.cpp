@@ -101,7 +101,7 @@ extern "C" sat_status sat_op_residual_norm_bwd_ws(const sat_residual_norm_desc* 
   SAT_CHECK_ARG(d && elems, "residual_norm_bwd_ws: null pointer");
   SAT_CHECK_ARG(d->T >= 0 && d->T < (1 << 30) && d->d >= 1 && d->d <= kResidualNormMaxD,
                 "residual_norm_bwd_ws: bad sizes T=%d d=%d", d->T, d->d);
-  *elems = residual_norm_ws(d->T, d->d, d->post != 0, sums_of(d));
+  *elems = residual_norm_ws(d->T, d->d, sums_of(d));
   return SAT_OK;
 }
 
@@ -124,7 +124,7 @@ extern "C" sat_status sat_op_residual_norm_bwd(const sat_residual_norm_desc* d, 
   SAT_CHECK_ARG(aligned(d->dg_pre, 4) && aligned(d->db_pre, 4) && aligned(d->dg_post, 4) && aligned(d->db_post, 4) &&
                     aligned(d->dgate, 4) && aligned(d->ws, 4),
                 "%s: vectors must be aligned to their elements", fn);
-  const int64_t need = residual_norm_ws(d->T, d->d, d->post != 0, sums_of(d));
+  const int64_t need = residual_norm_ws(d->T, d->d, sums_of(d));
   SAT_CHECK_ARG(need == 0 || (d->ws && d->ws_elems >= need), "%s: ws of %ld elements, %ld needed", fn, (long)d->ws_elems,
                 (long)need);
   a.dy = d->dy; a.dh = (const bf16*)d->dh; a.dx = d->dx; a.df = (bf16*)d->df;

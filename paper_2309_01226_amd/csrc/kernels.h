@@ -431,8 +431,8 @@ struct ResidualNormArgs {
 };
 hipError_t launch_residual_norm_fwd(ResidualNormArgs a, bool f32, hipStream_t s);
 hipError_t launch_residual_norm_bwd(ResidualNormArgs a, bool f32, hipStream_t s);
-// fp32 elements for `sums` of the five gradients that are sums over rows; post: with a norm of the branch.
-int64_t residual_norm_ws(int T, int d, bool post, int sums);
+// fp32 elements for `sums` of the five gradients that are sums over rows.
+int64_t residual_norm_ws(int T, int d, int sums);
 
 // ---------------------------------------------------------------- head with cross entropy (linear_xent.hip)
 struct LinearXentArgs {

@@ -42,7 +42,7 @@ __host__ __device__ inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 // rounds, one for each CU, and the rest, whose K is split in S slices where that shortens the last round.  Cost in ns:
 // a round takes 1650 for each step and 11000 for its start and end, of tiles of 128 700 and 4000, but in whole rounds,
 // with two on a CU, 580 and 1000; a partial tile's way to memory and back 100 (26), the launch that adds the slices
-// 4000.  At most 128 MB of partial tiles.  Whole numbers: the host plans the workspace and the launch by what the
+// 4000.  At most 128 MB of partial tiles a product.  Whole numbers: the host plans the workspace and the launch by what the
 // rows' kernel then chooses on the device (by the number of rows that take part), so both have to choose alike.
 constexpr int SLICES = 64;
 struct Split {
@@ -177,12 +177,13 @@ __global__ __launch_bounds__(256) void xent_copy_kernel(LinearXentArgs a) {
 }
 
 // Both at once for up to FEW rows: a workgroup, which has four rows, counts the rows before them (and all of them) for
-// itself.  (1019 x 739 x 2576, 30% without a label: 6 us; with 64 rows for a workgroup, 33.  The whole of 8192 x 66 x 96, half
-// without: 32 us, with the two kernels above 36; of 16384 rows 50 and 50, of 24000 74 and 67.)
+// itself.  (1019 x 739 x 2576, 30% without a label: 6 us; with 64 rows for a workgroup, 33.  The whole of 8192 x 66 x
+// 96, half without: 32 us, with the two kernels above 36; of 16384 rows 50 and 50, of 24000 74 and 67.)
 constexpr int FEW = 12000;
 __global__ __launch_bounds__(256) void xent_rows_few_kernel(LinearXentArgs a) {
   __shared__ int sums[2][4];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r0 = blockIdx.x * 4, r = r0 + wave;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r0 = blockIdx.x * 4, r = r0 + wave;
   const auto live = [&](int i) {
     const int label = i < a.N ? a.labels[i] : -1;
     return label >= 0 && label < a.V;

@@ -503,7 +503,7 @@ int sum_outputs(const ResidualNormArgs& a, SumOut* o) {
 }  // namespace
 
 // (the same for either way of access, so that alignment does not matter to the caller)
-int64_t residual_norm_ws(int T, int d, bool post, int sums) {
+int64_t residual_norm_ws(int T, int d, int sums) {
   return (int64_t)std::max(bwd_groups(T, d, bwd_shape(d, true)), bwd_groups(T, d, bwd_shape(d, false))) * sums * d;
 }
 
@@ -559,8 +559,9 @@ hipError_t launch_residual_norm_bwd(ResidualNormArgs a, bool f32, hipStream_t s)
   a.rows_wg = bwd_rows_wg(a.d, shape);
   const int threads = 64 * a.wpr * shape.lines, G = bwd_groups(a.T, a.d, shape);
   if (G > 0) {
-    const Kernel kernel = a.post ? (f32 ? bwd_kernel<float, true>(a.L, shape.most, fast) : bwd_kernel<bf16, true>(a.L, shape.most, fast))
-                                 : (f32 ? bwd_kernel<float, false>(a.L, shape.most, fast) : bwd_kernel<bf16, false>(a.L, shape.most, fast));
+    const auto pick = f32 ? (a.post ? bwd_kernel<float, true> : bwd_kernel<float, false>)
+                          : (a.post ? bwd_kernel<bf16, true> : bwd_kernel<bf16, false>);
+    const Kernel kernel = pick(a.L, shape.most, fast);
     hipLaunchKernelGGL(kernel, dim3(G), dim3(threads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -550,7 +550,7 @@ def residual_norm_bwd(dy, dh, y, f, stats, dx, df, d, *, dg_pre=None, db_pre=Non
     xt, bf, f4 = torch.float32 if f32 else torch.bfloat16, torch.bfloat16, torch.float32
     sums = [_vec(t, f4, n, d, dev) for n, t in (("dg_pre", dg_pre), ("db_pre", db_pre), ("dg_post", dg_post), ("db_post", db_post),
                                                 ("dgate", dgate))]
-    need = _boundary_ws(T, d, post is not None, 5 - sums.count(0))
+    need = _boundary_ws(T, d, 5 - sums.count(0))
     ws = torch.empty(need, device=dx.device, dtype=f4) if need else None
     desc = _lib.sat_residual_norm_desc.from_buffer_copy(_BOUNDARY.pack(
         0, d, *_matrix(f, bf, "f", T, d, dev), *_matrix(y, xt, "y", T, d, dev), 0, d,
@@ -561,8 +561,8 @@ def residual_norm_bwd(dy, dh, y, f, stats, dx, df, d, *, dg_pre=None, db_pre=Non
 
 
 @functools.lru_cache(maxsize=256)
-def _boundary_ws(T, d, post, sums):
-    desc = _lib.sat_residual_norm_desc(T=T, d=d, post=post, **dict.fromkeys(("dg_pre", "db_pre", "dg_post", "db_post", "dgate")[:sums], 1))
+def _boundary_ws(T, d, sums):
+    desc = _lib.sat_residual_norm_desc(T=T, d=d, **dict.fromkeys(("dg_pre", "db_pre", "dg_post", "db_post", "dgate")[:sums], 1))
     need = C.c_int64()
     _lib.call("sat_op_residual_norm_bwd_ws", desc, need)
     return need.value
