@@ -143,6 +143,19 @@ def test_split_products(N, V, d):
     _check(o, _want(i))
 
 
+@pytest.mark.parametrize("N,V,d,dt", [(33, 40000, 200, BF), (300, 34001, 520, F4), (1, 50001, 1024, BF), (2000, 8000, 800, F4)])
+def test_many_tiles(N, V, d, dt):
+    """Products of more small tiles than there are compute units, with and without gradients, the same on each call."""
+    flush("many tiles", N, V, d, dt)
+    i = _inputs(N, V, d, 0.2 if N > 1 else 0.0, "masked", True, spare=8)
+    o, again, scored = _outputs(i, dt, spare=16), _outputs(i, dt), _outputs(i, grads="")
+    for each in (o, again, scored):
+        _call(i, each)
+    torch.cuda.synchronize()
+    _check(o, _want(i))
+    assert all(torch.equal(again[k], o[k]) for k in o) and all(torch.equal(scored[k], o[k]) for k in scored)
+
+
 def test_accumulate():
     for N, V in ((200, 700), (17000, 64)):  # one chunk and two
         i = _inputs(N, V, 128, 0.3, "plain")
