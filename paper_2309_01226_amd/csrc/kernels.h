@@ -449,6 +449,7 @@ struct LinearXentArgs {
   // set by the launch: a chunk's tokens, the pitch of e, and the parts of the workspace
   int chunk, tb, piece;   // (and of the scaling pass' workgroup; vocabulary entries with one pair of statistics)
   int rx, rw, s_dx, s_dw; // tiles of dx and dw, and slices of their products for a full chunk
+  int direct;             // rows are not numbered first: all are compact ones, lab is labels
   int64_t lde;            // the vocabulary in whole tiles
   int *meta, *idx, *pos, *lab;  // rows that take part: [0] their number, [1] and [2] slices of the last chunk; their rows, the rows' places, their labels
   float* zlab;            // their label's logit, then its entry of dz

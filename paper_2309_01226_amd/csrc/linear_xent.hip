@@ -22,8 +22,8 @@
 //
 // Bound by the matrix products (6 N V d operations), whose loop is the one of gemm256.hip.  8192 x 50257 x 768: 2.22 ms
 // or 0.85 PFLOP/s, of which the logits take 0.73, dx 0.54, dw 0.58 and the pass that forms dz 0.36 (1.65 GB, 4.6
-// TB/s); 4096 x 50400 x 4096: 4.30 ms, 1.18 PFLOP/s, 1.40, 1.28, 1.52 and 0.16.  8 x 50257 x 1024 without gradients: 25 us,
-// w once at 4.2 TB/s.  64 x 512 x 64: 27 us, the latency of four launches.
+// TB/s); 4096 x 50400 x 4096: 4.30 ms, 1.18 PFLOP/s, 1.40, 1.28, 1.52 and 0.16.  8 x 50257 x 1024 without gradients: 26 us,
+// w once at 4.0 TB/s.  64 x 512 x 64: 26 us, the latency of four launches.
 #include <algorithm>
 
 #include "gemm256_tile.h"
@@ -85,9 +85,10 @@ __host__ __device__ inline int dx_steps(const LinearXentArgs& a) { return cdiv(a
 __host__ __device__ inline int dw_tiles(int R, const LinearXentArgs& a) { return tiles_of(R, a.V, a.d); }
 __host__ __device__ inline int dw_steps(int n) { return cdiv(n, BK); }
 
-// The compact rows of the chunk that starts at `first`.
+// The compact rows, and those of the chunk that starts at `first`.
+__device__ __forceinline__ int compact_rows(const LinearXentArgs& a) { return a.direct ? a.N : a.meta[0]; }
 __device__ __forceinline__ int chunk_rows(const LinearXentArgs& a, int first) {
-  return min(max(a.meta[0] - first, 0), a.chunk);
+  return min(max(compact_rows(a) - first, 0), a.chunk);
 }
 
 // Whether the chunk has anything to do (the first one also without rows: gradients of none), and whether none
@@ -102,7 +103,7 @@ __device__ __forceinline__ float common_factor(const LinearXentArgs& a) { return
 
 // Row c of the compact rows of x: x itself where every row takes part.
 __device__ __forceinline__ const bf16* compact_x(const LinearXentArgs& a, long& ld) {
-  const bool all = a.meta[0] == a.N;
+  const bool all = compact_rows(a) == a.N;
   ld = all ? a.ldx : a.d;
   return all ? a.x : a.xc;
 }
@@ -343,7 +344,7 @@ __global__ __launch_bounds__(NT, ST == 2 ? 2 : 1) void xent_logits_kernel(Linear
 #pragma unroll
   for (int j = 0; j < S; ++j) {
     const int t = t0 + 32 * j + (lane & 31);
-    const int off = t < n ? a.lab[first + t] - v0 : -1;
+    const int off = t < n ? (int)((uint32_t)a.lab[first + t] - (uint32_t)v0) : -1;  // (any label where rows are not numbered)
     if (__builtin_amdgcn_ballot_w64(off >= 0 && off < W)) {
       float z = 0.f;
 #pragma unroll
@@ -413,7 +414,7 @@ __device__ __forceinline__ Joined join_row(const LinearXentArgs& a, int first, i
 #pragma unroll
   for (int j = 0; j < J; ++j) q[j] = lane + 64 * j < pieces ? part[lane + 64 * j] : make_float2(0.f, 0.f);
   const float zlab = a.zlab[first + t];
-  const int row = a.idx[first + t];
+  const int row = a.direct ? t : a.idx[first + t];
   float top = -INF, sum = 0.f;
   over_pieces(q, part, pieces, [&](int, float2 x) { top = x.y != 0.f ? fmaxf(top, x.x) : top; });
   const float m = wave_max(top);
@@ -434,11 +435,25 @@ __device__ __forceinline__ float piece_factor(const Joined& r, float2 q) {
   return r.up == 0.f || q.y == 0.f ? 0.f : r.up * __builtin_amdgcn_exp2f((q.x - r.m) * LOG2E);
 }
 
-// A wave a token: lse and loss, and, for the gradients, the pieces' factors and the label's entry.
+// A wave a token: lse and loss, and, for the gradients, the pieces' factors and the label's entry.  Where rows are not
+// numbered first, those that take no part end here.
 template <bool TRAIN>
 __global__ __launch_bounds__(256) void xent_join_kernel(LinearXentArgs a, int first) {
-  const int n = chunk_rows(a, first);
+  const int n = chunk_rows(a, first), lane = threadIdx.x & 63;
   const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (!TRAIN && a.direct) {
+    const auto live = [&](int i) { return a.labels[i] >= 0 && a.labels[i] < a.V; };
+    if (t == 0) {
+      int all = 0;
+      for (int i = lane; i < a.N; i += 64) all += live(i);
+      all = (int)wave_total((float)all);
+      if (lane == 0) a.inv_n[0] = 1.f / max(all, 1);
+    }
+    if (t < n && !live(t)) {
+      if (lane == 0) a.row_loss[t] = a.lse[t] = 0.f;
+      return;
+    }
+  }
   if (t >= n) return;
   const int pieces = cdiv(a.V, a.piece);
   float2* part = a.part + (long)t * pieces;
@@ -446,7 +461,7 @@ __global__ __launch_bounds__(256) void xent_join_kernel(LinearXentArgs a, int fi
   const Joined r = join_row(a, first, t, pieces, part, q);
   if constexpr (TRAIN) {
     over_pieces(q, part, pieces, [&](int p, float2 x) { part[p].x = piece_factor(r, x); });
-    if ((threadIdx.x & 63) == 0) a.zlab[first + t] = r.dlabel;
+    if (lane == 0) a.zlab[first + t] = r.dlabel;
   }
 }
 
@@ -822,7 +837,12 @@ hipError_t launch_linear_xent(LinearXentArgs a, void* ws, hipStream_t s) {
   const auto dw = pick(RW, l.dw.groups, xent_dw_kernel<BT, 4>, xent_dw_kernel<RS, 4>, xent_dw_kernel<RS, 2>);
   const int groups = l.dx.groups + l.dw.groups;
   const auto both = groups <= CUS ? xent_both_kernel<4> : xent_both_kernel<2>;
-  if (a.N <= FEW) {
+  // rows of one tile that are only scored are not numbered first: each has a place in it (8 x 50257
+  // x 1024, operands in turn: 30 -> 27 us)
+  a.direct = !train && a.N <= RS;
+  if (a.direct) {
+    a.lab = const_cast<int*>(a.labels);
+  } else if (a.N <= FEW) {
     hipLaunchKernelGGL(xent_rows_few_kernel, dim3(std::max(1, cdiv(a.N, 4))), dim3(256), 0, s, a);
   } else {
     hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, s, a);

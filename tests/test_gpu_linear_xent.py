@@ -119,6 +119,21 @@ def test_few_rows(rows):
     _check(o, _want(i, False))
 
 
+@pytest.mark.parametrize("rows,V,ignored", [(1, 300, 1.0), (7, 50, 0.5), (128, 700, 0.3), (129, 700, 0.3), (90, 1000, 1.0)])
+def test_few_rows_without_labels(rows, V, ignored):
+    """Few rows scored, some or all of which take no part, whatever they hold."""
+    flush("few rows without labels", rows, V, ignored)
+    i = _inputs(rows, V, 136, ignored, "plain", spare=8)
+    out = (i["labels"] < 0) | (i["labels"] >= V)
+    i["x"][out] = math.nan
+    o = _outputs(i, grads="")
+    _call(i, o)
+    torch.cuda.synchronize()
+    assert not o["row_loss"][out].any() and not o["lse"][out].any()
+    i["x"][out] = 0.0
+    _check(o, _want(i, False))
+
+
 @pytest.mark.parametrize("N,V,d,ignored,dt", [
     (17000, 300, 64, 0.0, BF), (17000, 300, 64, 0.45, F4), (6000, 50257, 64, 0.0, BF), (40000, 70, 32, 0.7, BF),
     (12000, 66, 96, 0.3, BF), (12001, 66, 96, 0.3, F4)])
