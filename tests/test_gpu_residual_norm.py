@@ -263,7 +263,8 @@ def test_streams_and_graph():
 
 
 @pytest.mark.parametrize("dt,post,T,d", [(F4, "rms", 20011, 4096), (BF, "rms", 20011, 4096), (F4, None, 60001, 1280), (BF, None, 9000, 8192),
-                                         (F4, "layer", 6000, 8192), (BF, "layer", 300007, 264), (F4, "layer", 300007, 256)])
+                                         (F4, "layer", 6000, 8192), (BF, "layer", 300007, 264), (F4, "layer", 300007, 256),
+                                         (F4, "layer", 30001, 1280), (BF, None, 20011, 1280)])
 def test_large_calls(dt, post, T, d):
     """Calls past the size where rows go past the caches: their first and last rows are those of small calls, bit for bit."""
     from paper_2309_01226_amd import ops
