@@ -32,7 +32,7 @@ extern "C" sat_status sat_op_dropout(const void* x, int64_t ldx, void* y, int64_
   SAT_CHECK_ARG(rows == 0 || cols == 0 || (x && y), "%s: null pointer", fn);
   SAT_CHECK_ARG(p >= 0 && p <= 1, "%s: p=%g must be in [0, 1]", fn, p);
   SAT_CHECK_ARG(ldx >= cols && ldy >= cols && ldx < kMaxLd && ldy < kMaxLd, "%s: leading dimensions must cover the columns", fn);
-  SAT_CHECK_ARG(x != y || ldx == ldy, "%s: in place, ldx and ldy must agree", fn);
+  SAT_CHECK_ARG(x != y || !x || ldx == ldy, "%s: in place, ldx and ldy must agree", fn);
   const uintptr_t size = f32 ? 4 : 2;
   SAT_CHECK_ARG(aligned(x, size) && aligned(y, size) && aligned(step, 8), "%s: x, y and step must be aligned to their elements", fn);
   const DropRate r = drop_rate(p);
@@ -88,7 +88,7 @@ extern "C" sat_status sat_op_residual_norm_fwd(const sat_residual_norm_desc* d, 
   SAT_CHECK_ARG(rows_ok(d->x, d->ldx, size, d) && rows_ok(d->y, d->ldy, size, d) && rows_ok(d->f, d->ldf, 2, d) &&
                     (!d->pre || rows_ok(d->h, d->ldh, 2, d)),
                 "%s: x, f, y and, with a norm, h: null, not aligned to their elements, or rows shorter than d", fn);
-  SAT_CHECK_ARG(d->x != d->y || d->ldx == d->ldy, "%s: in place, ldx and ldy must agree", fn);
+  SAT_CHECK_ARG(d->x != d->y || !d->x || d->ldx == d->ldy, "%s: in place, ldx and ldy must agree", fn);
   SAT_HIP(launch_residual_norm_fwd(a, d->stream_f32 != 0, S(stream)));
   return SAT_OK;
 }
@@ -118,7 +118,7 @@ extern "C" sat_status sat_op_residual_norm_bwd(const sat_residual_norm_desc* d, 
                 "%s: dx, df and what the norms and the gate need of dy, dh, y and f: null, not aligned to their elements, "
                 "or rows shorter than d",
                 fn);
-  SAT_CHECK_ARG(d->dx != d->dy || d->lddx == d->lddy, "%s: in place, lddx and lddy must agree", fn);
+  SAT_CHECK_ARG(d->dx != d->dy || !d->dx || d->lddx == d->lddy, "%s: in place, lddx and lddy must agree", fn);
   SAT_CHECK_ARG((d->pre || (!d->dg_pre && !d->db_pre)) && (d->post || (!d->dg_post && !d->db_post)) && (d->gate || !d->dgate),
                 "%s: a gradient of something that is not there", fn);
   SAT_CHECK_ARG(aligned(d->dg_pre, 4) && aligned(d->db_pre, 4) && aligned(d->dg_post, 4) && aligned(d->db_post, 4) &&

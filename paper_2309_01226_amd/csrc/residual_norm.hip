@@ -566,8 +566,7 @@ hipError_t launch_residual_norm_bwd(ResidualNormArgs a, bool f32, hipStream_t s)
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.sums)
-    hipLaunchKernelGGL(residual_norm_sums_kernel, dim3(sat_cdiv(a.d, 64), a.sums), dim3(1024), 0, s, a.ws, G, a.sums,
-                       a.d, o);
+  if (a.sums == 0) return hipSuccess;
+  hipLaunchKernelGGL(residual_norm_sums_kernel, dim3(sat_cdiv(a.d, 64), a.sums), dim3(1024), 0, s, a.ws, G, a.sums, a.d, o);
   return hipGetLastError();
 }
