@@ -151,7 +151,7 @@ extern "C" sat_status sat_op_rotary_axes(const void* x, int64_t ldx, void* y, in
                 half, dh);
   SAT_CHECK_ARG(ldx >= (int64_t)H * dh && ldy >= (int64_t)H * dh && ldp >= n_axes,
                 "%s: leading dimensions must cover the heads and the axes", fn);
-  SAT_CHECK_ARG(x != y || ldx == ldy, "%s: in place, ldx and ldy must agree", fn);
+  SAT_CHECK_ARG(x != y || !x || ldx == ldy, "%s: in place, ldx and ldy must agree", fn);
   SAT_CHECK_ARG(aligned(x, f32 ? 4 : 2) && aligned(y, f32 ? 4 : 2) && aligned(pos, 4),
                 "%s: x, y and pos must be aligned to their elements", fn);
   SAT_CHECK_ARG(base > 0 && isfinite(base), "%s: base must be positive and finite", fn);

@@ -31,6 +31,12 @@ def test_boundary_backward_of_nothing():
     assert L.lib().sat_op_residual_norm_bwd(C.byref(d), None) == L.SAT_OK, L.last_error()
 
 
+def test_rotary_of_nothing():
+    L = _L()
+    assert L.lib().sat_op_rotary_axes(None, 64, None, 72, 0, None, 1, 1, (C.c_int32 * 1)(8), 0, 4, 16, 10000.0, 1, 0, 0, None) == L.SAT_OK, \
+        L.last_error()
+
+
 @pytest.mark.gpu
 def test_empty_views():
     """As a program makes them: rows of a wider buffer, none of which is there."""
@@ -42,4 +48,5 @@ def test_empty_views():
     st, s = torch.empty(4, 0, device="cuda"), torch.full((64,), 7.0, device="cuda")
     ops.residual_norm_fwd(wide(f4), flat(bf), flat(f4), flat(bf), st, 64, pre="rms", post="layer")
     ops.residual_norm_bwd(wide(f4), flat(bf), flat(f4), flat(bf), st, flat(f4), flat(bf), 64, pre="rms", post="layer", dg_pre=s)
+    ops.rotary_axes(wide(bf), torch.empty(0, 1, dtype=torch.int32, device="cuda"), 4, 16, [8], out=flat(bf))
     assert not s.any()
