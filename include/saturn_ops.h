@@ -307,10 +307,11 @@ sat_status sat_op_cross_entropy(const float* z, int64_t ldz, const int32_t* labe
  * or infinities spoils its own outputs and the gradients of w and bias.  The same inputs give the same bits.
  * x and w 16-byte aligned with leading dimensions that are multiples of 8 and below 2^21, dx and dw with
  * 16-byte aligned rows.  Outputs overlap no input and no other output.  ws: scratch, 256-byte aligned, of as many
- * bytes as the _ws call says (N, V, d, which gradients, grad_f32 are read): at most 1 GiB for a chunk of the tokens and a
- * tenth of that for its statistics, a copy of x, 128 MiB of partial products (256 where dx and dw are small and formed
- * together), 512 V bytes, and, with bf16 gradients of several chunks, their fp32 sums;
- * calls that may overlap need one each.
+ * bytes as the _ws call says (N, V, d, which gradients, grad_f32 are read): a copy of x and 16 bytes a row; for gradients
+ * at most 1 GiB for a chunk of the tokens and a tenth of that for its statistics, 128 MiB of partial products (256 where
+ * dx and dw are small and formed together), 512 V bytes, and, with bf16 gradients of several chunks, their fp32 sums; for
+ * rows that are only scored a chunk's statistics, 8 bytes for 64 entries of a row, at most 1 GiB.  Calls that may
+ * overlap need one each.
  * Errors: SAT_EINVAL for null pointers, sizes, alignment, and a ws that is too small. */
 typedef struct {
   const void* x;

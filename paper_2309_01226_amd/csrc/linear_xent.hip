@@ -726,6 +726,7 @@ __global__ __launch_bounds__(256) void xent_slices_kernel(LinearXentArgs a, int 
 
 constexpr int64_t kMaxE = 1LL << 29;   // numbers of a chunk
 constexpr int kMaxChunk = 16384;       // tokens of a chunk
+constexpr int64_t kMaxStats = 1LL << 30;  // bytes of a chunk's statistics, where they are all that is kept
 
 struct Launch {
   int R = BT, groups = 1, split = 0;  // tile; workgroups of a product; tiles whose K is split
@@ -754,7 +755,9 @@ struct Layout {
 void plan(LinearXentArgs& a, Layout& l) {
   const bool train = a.dx || a.dw || a.db;
   const int vp = cdiv(a.V, BT) * BT;
-  int64_t cap = kMaxChunk;
+  // Statistics are of pieces of 64 entries at least; where gradients are wanted, the numbers are the closer limit.  (A tenth
+  // of it would give 16384 x 151936 x 1024, scored, three chunks of one: 4.47 -> 4.66 ms, and 4096 x 2^20 x 256 six: 3.27 -> 4.37.)
+  int64_t cap = std::min<int64_t>(kMaxChunk, std::max<int64_t>(BT, kMaxStats / (8 * cdiv(a.V, RS / 2)) / BT * BT));
   if (train) cap = std::min<int64_t>(cap, std::max<int64_t>(BT, kMaxE / vp / BT * BT));
   const int chunks = std::max(1, (int)((a.N + cap - 1) / cap));
   a.chunk = std::max(1, cdiv(cdiv(a.N, chunks), BT)) * BT;
