@@ -4,8 +4,9 @@ import pytest
 import torch
 
 from tests import test_gpu_linear_xent as T
+from tests import test_head_operand as O
 from tests.gpu_util import flush
-from tests.test_head_workspace import LOOSE, _ws
+from tests.test_head_workspace import LOOSE, P, _ws
 
 pytestmark = pytest.mark.gpu
 BF, F4 = torch.bfloat16, torch.float32
@@ -27,3 +28,56 @@ def test_scores_in_chunks():
         rows = {k: i[k][at] for k in ("x", "labels")}
         want = T._want({**i, **rows}, False)
         T._check({k: o[k][at] for k in ("row_loss", "lse")}, want)
+
+
+def _several(N, V, d):
+    """Several chunks: then bf16 gradients have fp32 sums beside them."""
+    a = dict(N=N, V=V, d=d, dx=P, dw=P, db=P, bias=P)
+    return _ws(**a) - _ws(**a, grad_f32=1) >= 4 * V * d
+
+
+@pytest.mark.parametrize("dt", [BF, F4])
+def test_chunks_of_a_wide_vocabulary(dt):
+    """More rows than there are 16-bit numbers for in 1 GiB: dw and db summed over two chunks."""
+    N, V, d = 11000, 50257, 64
+    flush("chunks of a wide vocabulary", N, V, d, dt)
+    assert _several(N, V, d) and not _several(10496, V, d)
+    i = T._inputs(N, V, d, 0.05, "plain", True)
+    o = T._outputs(i, dt)
+    T._call(i, o)
+    torch.cuda.synchronize()
+    T._check(o, T._want(i))
+
+
+@pytest.mark.parametrize("dt,accumulate", [(BF, False), (F4, False), (F4, True)])
+@pytest.mark.parametrize("more", [1, 100, 256, 257])
+def test_last_chunk_of_few_rows(more, dt, accumulate):
+    """A full chunk of rows that take part and a few: those have dz in two parts, and slices chosen on the device."""
+    N, V, d, full = 17000, 300, 64, 8704  # two chunks, of 8500 in whole tiles
+    flush("last chunk of few rows", more, dt, accumulate)
+    assert _several(N, V, d)
+    g = torch.Generator().manual_seed(more)
+    r = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    labels = torch.full((N,), -1, dtype=torch.int32)
+    rows = torch.randperm(N, generator=g)[:full + more].sort().values
+    labels[rows] = torch.randint(0, V, (full + more,), generator=g, dtype=torch.int32)
+    # few entries for the last rows, which then are all that these entries' dw has (but for other rows' softmax, which
+    # the bias keeps small)
+    labels[rows[:full]] %= V - 20
+    labels[rows[full:]] = labels[rows[full:]] % 20 + V - 20
+    bias = r(V)
+    bias[-20:] -= 14
+    i = O.on_device(dict(x=(1.5 * r(N, d)).to(BF), w=(r(V, d) / 8).to(BF), labels=labels, bias=bias, weight=torch.rand(N, generator=g) + 0.1))
+    few = torch.zeros(N, dtype=torch.bool)
+    few[rows[full:]] = more <= O.FEW
+    want = O.gradients(i, few.cuda())
+    o = T._outputs(i, dt)
+    add = {}
+    if accumulate:
+        for k in ("dw", "db"):
+            add[k] = r(*o[k].shape).cuda() * 1e-3
+            o[k].copy_(add[k])
+    T._call(i, o, accumulate=accumulate)
+    torch.cuda.synchronize()
+    T._check({k: o[k] for k in want}, want, {k: t.double() for k, t in add.items()})
+    T._check({k: o[k] for k in ("row_loss", "lse", "inv_n")}, T._want(i, False))
