@@ -81,3 +81,28 @@ def test_last_chunk_of_few_rows(more, dt, accumulate):
     torch.cuda.synchronize()
     T._check({k: o[k] for k in want}, want, {k: t.double() for k, t in add.items()})
     T._check({k: o[k] for k in ("row_loss", "lse", "inv_n")}, T._want(i, False))
+
+
+@pytest.mark.parametrize("N,V,d,ignored", [(1, 2, 8, 0.0), (33, 257, 1024, 0.3), (333, 1501, 256, 0.3), (300, 9001, 768, 0.1), (700, 2050, 320, 0.5),
+                                           (17000, 300, 64, 0.45), (2000, 20011, 256, 0.9)])
+def test_workspace_contents(N, V, d, ignored):
+    """What a workspace holds before a call (zeros, NaN) reaches no output, nor do outputs' own earlier values."""
+    from paper_2309_01226_amd import _lib as L
+    flush("workspace contents", N, V, d, ignored)
+    i = T._inputs(N, V, d, ignored, "plain", True)
+    for dt, grads in ((BF, "dx dw db"), (F4, "dx dw db"), (BF, "dx"), (F4, "dw"), (BF, "db"), (BF, "")):
+        seen = []
+        for fill in (0, 255):
+            o = T._outputs(i, dt, grads=grads)
+            for t in o.values():
+                t.view(torch.uint8).fill_(fill)
+            at = lambda k: o[k].data_ptr() if k in o else None  # noqa: E731
+            sizes = dict(N=N, V=V, d=d, dx=at("dx"), dw=at("dw"), db=at("db"), bias=i["bias"].data_ptr(), grad_f32=dt == F4)
+            ws = torch.full((_ws(**sizes),), fill, dtype=torch.uint8, device="cuda")
+            L.call("sat_op_linear_xent", L.sat_linear_xent_desc(
+                x=i["x"].data_ptr(), ldx=d, w=i["w"].data_ptr(), ldw=d, labels=i["labels"].data_ptr(), row_weight=i["weight"].data_ptr(),
+                row_loss=at("row_loss"), lse=at("lse"), inv_n=at("inv_n"), lddx=d, lddw=d, ws=ws.data_ptr(), ws_bytes=ws.numel(), **sizes),
+                torch.cuda.current_stream().cuda_stream)
+            torch.cuda.synchronize()
+            seen.append(o)
+        assert all(torch.equal(seen[0][k], seen[1][k]) for k in o), (dt, grads)
