@@ -454,18 +454,18 @@ __global__ __launch_bounds__(1024) void residual_norm_sums_kernel(const float* _
 int waves_of_row(int d) { return (d + 511) / 512; }
 int lanes_of_row(int d) { return d > 256 ? 64 : d > 128 ? 32 : d > 64 ? 16 : 8; }
 
-// A backward workgroup: its most threads by the kernel's registers, rows of waves in it, and workgroups on a CU.
+// A backward workgroup, one on a CU: its most threads by the kernel's registers, and rows of waves in it.
 struct BwdShape {
-  int most, lines, per_cu;
+  int most, lines;
 };
 BwdShape bwd_shape(int d, bool fast) {
   const int w = waves_of_row(d);
-  if (d <= 256) return {768, 12, 1};
-  if (!fast || w > 12) return {1024, std::max(1, 16 / w), 1};
-  return w == 7 || w == 8 ? BwdShape{512, 1, 1} : BwdShape{768, 12 / w, 1};
+  if (d <= 256) return {768, 12};
+  if (!fast || w > 12) return {1024, std::max(1, 16 / w)};
+  return w == 7 || w == 8 ? BwdShape{512, 1} : BwdShape{768, 12 / w};
 }
 int bwd_rows_wg(int d, const BwdShape& b) { return b.lines * (64 / lanes_of_row(d)); }
-int bwd_groups(int T, int d, const BwdShape& b) { return std::min(CUS * b.per_cu, sat_cdiv(T, bwd_rows_wg(d, b))); }
+int bwd_groups(int T, int d, const BwdShape& b) { return std::min(CUS, sat_cdiv(T, bwd_rows_wg(d, b))); }
 
 using Kernel = void (*)(ResidualNormArgs);
 template <class XT>
