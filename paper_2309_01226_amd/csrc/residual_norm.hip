@@ -512,6 +512,9 @@ int64_t residual_norm_ws(int T, int d, int sums) {
 // results there.  us with and without, operands in turn, rows of 4096: a backward of 300 MB, bf16, 57 and 63; of
 // 1.2 GB, fp32, both norms 213 and 219; a forward of 0.8 GB, fp32, both norms 146 and 152.  A bf16 forward and a copy of h:
 // 200 MB in all 57 and 56, 250 MB 70 and 73, 300 MB 83 and 91.
+// 0, by elements, where they are not: dearest backward, where nothing is loaded ahead and the kernel with a norm of the branch
+// spills.  Both norms, gate, all sums, fp32: 16384 x 4095 forward 204 us, backward 401 (4096: 178 and 229), 16448 x 1283
+// 82 and 150 (1280: 72 and 90).
 static int fast_rows(const ResidualNormArgs& a, bool f32, bool back) {
   bool ok = a.d % 8 == 0;
   const auto rows = [&](const void* p, int64_t ld, int size) {
