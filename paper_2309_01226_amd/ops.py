@@ -485,6 +485,8 @@ def dropout(x, p, seed, *, step=None, out=None):
     if x.dim() != 2 or (out is not None and out.shape != x.shape):
         raise ValueError(f"dropout: expected matrices of one size, got {tuple(x.shape)}" + (f" and {tuple(out.shape)}" if out is not None else ""))
     rows, cols = x.shape
+    if (rows | cols) >> 31:  # ctypes would cut it
+        raise ValueError(f"dropout: {rows} rows of {cols} columns are too many")
     y = x if out is None else out
     ldx = _rows_of(x, dt, "x", rows, cols, dev)
     ldy = ldx if out is None else _rows_of(out, dt, "out", rows, cols, dev)

@@ -102,3 +102,15 @@ def test_head():
     assert ((dw[entries].double() - want).abs() <= (2.0 ** -8 * 1.1 + 2.0 ** -11.5 + bound * 2) * size + 2.0 ** -8 * want.abs()
             + 2 * O.E * (N + 2) * size).all()
     assert not (dw == 7).any()
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 32) + 5, 1), (1 << 31, 1)])
+def test_too_many_rows(rows, cols):
+    """More rows than 32 bits hold are refused, not cut to what they hold."""
+    from paper_2309_01226_amd import _lib, ops
+    flush("too many rows", rows)
+    x = torch.empty(rows, cols, dtype=BF, device="cuda")
+    x[:8] = 1
+    with pytest.raises((ValueError, _lib.SatError)):
+        ops.dropout(x, 0.5, 1)
+    assert (x[:8] == 1).all()
