@@ -114,3 +114,14 @@ def test_too_many_rows(rows, cols):
     with pytest.raises((ValueError, _lib.SatError)):
         ops.dropout(x, 0.5, 1)
     assert (x[:8] == 1).all()
+
+
+def test_too_many_rows_to_turn():
+    from paper_2309_01226_amd import ops
+    flush("too many rows to turn")
+    rows = (1 << 32) + 3
+    x, pos = torch.empty(rows, 2, dtype=BF, device="cuda"), torch.empty(rows, 1, dtype=torch.int32, device="cuda")
+    x[:8], pos[:8] = 1, 1
+    with pytest.raises(ValueError):
+        ops.rotary_axes(x, pos, 1, 2, [1])
+    assert (x[:8] == 1).all()
