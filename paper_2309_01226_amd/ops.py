@@ -350,11 +350,11 @@ def rotary_axes(x, pos, H, dh, pairs, *, out=None, base=10000.0, interleaved=Tru
     """Rotary positions with len(pairs) axes on the H heads of x [T, >= H dh] (bf16 or fp32), axis a
     turning pairs[a] pairs of every head by pos[:, a] (int32 [T, axes]); in place, or into `out`.
     See saturn_ops.h.  Returns the rotated tensor."""
-    T, A, dev = x.shape[0], len(pairs), _device(x, "x")
+    T, A = x.shape[0], len(pairs)
     if H < 1 or dh < 1 or (T | H | dh) >> 31 or not _PAIRS.issuperset(pairs):  # ctypes would cut what 32 bits do not hold
         raise ValueError(f"T={T}, H={H}, dh={dh}, pairs: {pairs}")
     f32 = x.dtype == torch.float32
-    dt = torch.float32 if f32 else torch.bfloat16
+    dt, dev = torch.float32 if f32 else torch.bfloat16, _device(x, "x")
     y = x if out is None else out
     ldx = _rows_of(x, dt, "x", T, H * dh, dev)
     ldy = ldx if out is None else _rows_of(out, dt, "out", T, H * dh, dev)
